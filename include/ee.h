@@ -50,8 +50,8 @@ typedef enum {
 } ee_status_t;
 
 typedef enum { EE_F32 = 0, EE_BF16 = 1 } ee_dtype_t;
-typedef enum { EE_OP_CONV = 0, EE_OP_DWCONV = 1, EE_OP_MAXPOOL = 2 } ee_op_t;
-typedef enum { EE_ACT_NONE = 0, EE_ACT_RELU = 1, EE_ACT_RELU6 = 2 } ee_act_t;
+typedef enum { EE_OP_CONV = 0, EE_OP_DWCONV = 1, EE_OP_MAXPOOL = 2, EE_OP_GROUPNORM = 3 } ee_op_t;
+typedef enum { EE_ACT_NONE = 0, EE_ACT_RELU = 1, EE_ACT_RELU6 = 2, EE_ACT_SILU = 3 /* group norm only */ } ee_act_t;
 
 /* Sources for ee_layer_desc_t.input_from / residual_from. */
 #define EE_FROM_PREV (-1)         /* input_from: output of the previous layer (stage input for layer 0) */
@@ -62,7 +62,9 @@ typedef enum { EE_ACT_NONE = 0, EE_ACT_RELU = 1, EE_ACT_RELU6 = 2 } ee_act_t;
 /* One layer of a stage.  y = act(scale[c] * conv(x, weight) + bias[c] (+ residual)), stored in
  * the model dtype with one round-to-nearest-even.  BN is folded into scale/bias by the caller.
  * EE_OP_DWCONV is a depthwise convolution (groups = cin = cout, weight [C][kh][kw][1]).
- * EE_OP_MAXPOOL takes the window maximum over in-range taps; weight/scale/bias are ignored. */
+ * EE_OP_MAXPOOL takes the window maximum over in-range taps; weight/scale/bias are ignored.
+ * EE_OP_GROUPNORM is ee_group_norm on the layer's input (cin = cout, kh = kw = stride = 1, pad = 0, weight ignored): gamma =
+ * scale, beta = bias, norm_groups, norm_eps, act, and the residual operand where there is one. */
 typedef struct {
   int op;             /* ee_op_t */
   int cin, cout, kh, kw, stride, pad;
@@ -75,6 +77,8 @@ typedef struct {
   int pad_w;          /* padding of the columns; EE_PAD_W_SAME (-1): `pad` pads rows and columns alike, otherwise `pad`
                          pads the rows only (filters that are not square, such as 1 x 7 and 7 x 1, pad along their own
                          axis); dense convolutions only */
+  int norm_groups;    /* EE_OP_GROUPNORM: groups that the channels fall into (a divisor of cin); ignored elsewhere */
+  float norm_eps;     /* EE_OP_GROUPNORM: added to the variance, >= 0 */
 } ee_layer_desc_t;
 
 /* One stage = a subnet followed by its exit head (global average pool, one FC layer, softmax;
@@ -375,6 +379,63 @@ ee_status_t ee_wait_count(const int32_t* n_surv_host, int32_t sentinel, double t
 /* Synchronises the stream and reports device-side faults the kernels recorded instead of hanging:
  * EE_ERR_TIMEOUT when a bounded wait on a barrier ran out.  The flag is cleared by the call. */
 ee_status_t ee_model_check(ee_model_t* model, void* cuda_stream);
+
+/* ---- Operators that need no model ------------------------------------------------------------------------------------
+ * The parts of an exit branch that many requests share, as calls of their own.  The current device must be the one the
+ * buffers live on; all pointers DEVICE, contiguous, aligned to their elements (16-byte alignment is faster).  They allocate
+ * nothing and keep nothing from call to call.  A row's (sample's, sequence's) result depends on its own inputs alone; except
+ * where stated its bits do not depend on what else is in the call either.  Make the first call on a device outside any stream
+ * capture; later ones may be captured.  On an error nothing has been launched. */
+
+/* Group norm with an activation on a channels-last map: over the hw pixels of a sample and the c / groups channels of a group,
+ *   y = act(gamma[c] * (x - mean) / sqrt(var + eps) + beta[c] (+ residual)),   var biased (divided by the count),
+ * statistics and sums in fp32, one rounding to the model dtype.  x, residual (or NULL), y: [batch][hw][c]; gamma (NULL = 1)
+ * and beta (NULL = 0): [c] fp32.  Unlike a folded batch norm it takes its statistics from the sample itself, so it suits a batch
+ * that shrinks and is refilled: the bits of a sample do not depend on the batch.  y may be x or residual (in place); other
+ * overlaps are refused.  act: ee_act_t.  Errors: INVALID_ARG, CAPACITY (a grid beyond 2^31 - 1 blocks), CUDA. */
+ee_status_t ee_group_norm(int dtype, const void* x, const void* residual, int batch, int hw, int c, int groups, const float* gamma,
+                          const float* beta, float eps, int act, void* y, void* cuda_stream);
+
+/* A projection shared by all rows with a low-rank adapter of each row's own beside it (requests of many tenants in one batch):
+ *   y[t] = weight x[t] + bias + scale[i] * b[i] (a[i] x[t]),   i = adapter[t];
+ * a row whose adapter[t] is negative or >= n_adapters has none.  x: [rows][c], weight: [n][c], a: [n_adapters][rank][c],
+ * b: [n_adapters][n][rank], y: [rows][n], all of dtype; bias: [n] fp32 (NULL = 0), scale: [n_adapters] fp32 (NULL = 1),
+ * adapter: [rows].  Rows need not be sorted by adapter (rows of one adapter beside one another cost least).  Sums: bf16 products
+ * in fp32 (a x enters the second product as two bf16 parts, 2^-17 of it), fp32 products in fp64; one rounding to dtype.
+ * rank: 1 to 128.  n_adapters = 0 is the plain projection (a, b, adapter and workspace may be NULL).  `workspace` (256-byte
+ * aligned): at least ee_adapted_linear_workspace_bytes(rows, rank) bytes, undefined afterwards; calls that may overlap (two
+ * streams, or two captured graphs) need one each.  y must not overlap x or the workspace.  How the sums are grouped depends
+ * on the number of rows, so a row's last bit may.  Errors: INVALID_ARG, CAPACITY (workspace too small, more than 2^22 rows), CUDA. */
+ee_status_t ee_adapted_linear(int dtype, const void* x, int rows, int c, const void* weight, int n, const float* bias, const void* a,
+                              const void* b, int rank, int n_adapters, const float* scale, const int32_t* adapter, void* y,
+                              void* workspace, size_t workspace_bytes, void* cuda_stream);
+size_t ee_adapted_linear_workspace_bytes(int rows, int rank);
+
+/* Probabilities of rows of logits: probs[v] = exp((logits[v] - max) / t) / sum, t = temperature[row] (NULL = 1).  logits: [rows][n]
+ * of dtype, probs: [rows][n] fp32.  A logit of -inf is masked: its probability is 0; a row with nothing else is all 0.
+ * A temperature that is not above 0 puts 1 on the largest logit (the lowest index on ties).  A row that holds NaN or +inf is NaN
+ * throughout.  probs may be logits (fp32); other overlaps are refused.  n up to 409600 (fp32) or 819200 (bf16).
+ * Errors: INVALID_ARG, CAPACITY (n or the grid too large), CUDA. */
+ee_status_t ee_softmax(int dtype, const void* logits, int rows, int n, const float* temperature, float* probs, void* cuda_stream);
+
+/* Verification of drafts.  An early exit has answered k positions of each of `batch` sequences (tokens, or classes of n), a later
+ * one gives their probabilities: the answers that may stand stay, and the first that may not is drawn anew, so that what comes
+ * out is distributed as the later exit's own answers.  p: [batch][k + 1][n] fp32, the later exit's probabilities of every drafted
+ * position and of the one behind; q: [batch][k][n], the early one's (NULL: its answers were certain); drafts: [batch][k];
+ * u: [batch][k] and r: [batch], random numbers in [0, 1); n_draft: [batch], how many drafts a sequence has, at most k (NULL:
+ * k; larger counts as k; negative: an empty place of a padded batch, whose outputs are left as they are).
+ *   Draft i is accepted while u[i] * q[i][x_i] < p[i][x_i] (the product is exact; q = 1 where NULL); one outside [0, n) never is.
+ *   At the first that is not, a token is drawn from max(p[i] - q[i], 0) (q NULL: from p[i] without x_i), from p[i] itself where that
+ *   leaves nothing; where all are, from p[n_draft], the row behind them.  The draw is the first v whose running sum (fp64)
+ *   exceeds r times the total; values that are not positive and finite weigh nothing; -1 where nothing weighs anything.
+ * tokens: [batch][k + 1]: the accepted drafts, the drawn token, then -1.  n_accepted: [batch].  p may hold anything in rows behind
+ * the one drawn from, and q too.  k = 0 draws from p (q, drafts and u may be NULL).  Errors: INVALID_ARG, CAPACITY, CUDA. */
+ee_status_t ee_verify_drafts(const float* p, const float* q, const int32_t* drafts, const float* u, const float* r, const int32_t* n_draft,
+                             int batch, int k, int n, int32_t* tokens, int32_t* n_accepted, void* cuda_stream);
+
+/* Synchronises the stream and reports what ee_model_check reports, for the operators above on the current device:
+ * EE_ERR_TIMEOUT when a bounded wait of one of their kernels ran out since the last call. */
+ee_status_t ee_operators_check(void* cuda_stream);
 
 const char* ee_status_string(ee_status_t s);
 const char* ee_last_cuda_error(void); /* text of the last CUDA error seen by this thread, "" if none */

@@ -22,7 +22,8 @@ STATUS_NAMES = ["EE_OK", "EE_ERR_INVALID_ARG", "EE_ERR_SHAPE", "EE_ERR_CAPACITY"
 EXPORTS = ["ee_model_create", "ee_model_destroy", "ee_model_query", "ee_stage_run", "ee_layer_run", "ee_batch_refill", "ee_exit_head",
            "ee_exit_head_scratch_bytes", "ee_exit_head_static", "ee_gather_survivors", "ee_model_set_graphs", "ee_model_set_branches", "ee_model_set_fused_head", "ee_model_set_proj_fusion", "ee_model_set_gap_fusion", "ee_model_gap_partials", "ee_model_head_launches", "ee_model_head_pools", "ee_model_set_stage_kernel", "ee_model_set_chain", "ee_model_set_timing", "ee_model_get_timing",
            "ee_model_plan", "ee_model_check", "ee_model_set_layer_variant", "ee_model_set_layer_splits", "ee_model_get_layer_config",
-           "ee_model_set_wait_limit", "ee_model_selftest_wait", "ee_wait_count", "ee_run_until_exit", "ee_status_string", "ee_last_cuda_error"]
+           "ee_model_set_wait_limit", "ee_model_selftest_wait", "ee_wait_count", "ee_run_until_exit", "ee_group_norm", "ee_adapted_linear",
+           "ee_adapted_linear_workspace_bytes", "ee_softmax", "ee_verify_drafts", "ee_operators_check", "ee_status_string", "ee_last_cuda_error"]
 
 
 class EEError(RuntimeError):
@@ -35,7 +36,8 @@ class EEError(RuntimeError):
 class LayerDesc(C.Structure):
     _fields_ = [("op", C.c_int), ("cin", C.c_int), ("cout", C.c_int), ("kh", C.c_int), ("kw", C.c_int), ("stride", C.c_int),
                 ("pad", C.c_int), ("act", C.c_int), ("input_from", C.c_int), ("residual_from", C.c_int),
-                ("weight", C.c_void_p), ("scale", C.c_void_p), ("bias", C.c_void_p), ("pad_w", C.c_int)]
+                ("weight", C.c_void_p), ("scale", C.c_void_p), ("bias", C.c_void_p), ("pad_w", C.c_int),
+                ("norm_groups", C.c_int), ("norm_eps", C.c_float)]
 
 
 class StageDesc(C.Structure):
@@ -117,6 +119,13 @@ def load_library() -> C.CDLL:
     L.ee_model_get_layer_config.argtypes = [vp, i, i, i, C.POINTER(i), C.POINTER(i), C.POINTER(i)]
     L.ee_model_set_wait_limit.argtypes = [vp, C.c_longlong]
     L.ee_model_selftest_wait.argtypes = [vp, C.c_longlong, vp]
+    L.ee_group_norm.argtypes = [i, vp, vp, i, i, i, i, vp, vp, C.c_float, i, vp, vp]
+    L.ee_adapted_linear.argtypes = [i, vp, i, i, vp, i, vp, vp, vp, i, i, vp, vp, vp, vp, C.c_size_t, vp]
+    L.ee_adapted_linear_workspace_bytes.argtypes = [i, i]
+    L.ee_adapted_linear_workspace_bytes.restype = C.c_size_t
+    L.ee_softmax.argtypes = [i, vp, i, i, vp, vp, vp]
+    L.ee_verify_drafts.argtypes = [vp, vp, vp, vp, vp, vp, i, i, i, vp, vp, vp]
+    L.ee_operators_check.argtypes = [vp]
     L.ee_status_string.argtypes = [i]
     L.ee_status_string.restype = C.c_char_p
     L.ee_last_cuda_error.restype = C.c_char_p
@@ -220,7 +229,8 @@ class EEModel:
             self._keep.append(layers)
             for li, l in enumerate(st.layers):
                 layers[li] = LayerDesc(l.op, l.cin, l.cout, l.kh, l.kw, l.stride, l.pad, l.act, l.input_from, l.residual_from,
-                                       host(l.weight, True), host(l.scale, False), host(l.bias, False), int(getattr(l, "pad_w", -1)))
+                                       host(l.weight, True), host(l.scale, False), host(l.bias, False), int(getattr(l, "pad_w", -1)),
+                                       int(getattr(l, "norm_groups", 0)), float(getattr(l, "norm_eps", 0.0)))
             stage_structs[si] = StageDesc(len(st.layers), layers, st.out_layer, st.n_classes, host(st.fc_weight, True),
                                           host(st.fc_bias, False), float(st.threshold), int(bool(st.always_exit)))
         desc = ModelDesc(1 if self.dtype == "bf16" else 0, spec.in_h, spec.in_w, spec.in_c, self.n_stages, stage_structs,
@@ -424,6 +434,78 @@ def apply_table(model: EEModel, spec, path: Optional[str] = None):
 def gather_survivors(feat, bytes_per_sample: int, survivor_idx, n_surv_dev, max_rows: int, feat_out, stream=None):
     _check(load_library().ee_gather_survivors(_ptr(feat), int(bytes_per_sample), _ptr(survivor_idx), _ptr(n_surv_dev),
                                               int(max_rows), _ptr(feat_out), _stream(stream)), "ee_gather_survivors")
+
+
+# ---- operators without a model (ee.h describes them).  Tensors are checked here for what the library cannot see: device, type,
+# contiguity and room for what the call reads or writes; integers are taken as device addresses, as everywhere in this module.
+
+_DTYPES = {"f32": 0, "bf16": 1}
+
+
+def _mem(where: str, t, dtype, count: int, device: int) -> Optional[int]:
+    if not isinstance(t, torch.Tensor):
+        return None if t is None else int(t)
+    if t.get_device() != device or t.dtype is not dtype or t.numel() < count or not t.is_contiguous():
+        raise EEError(1, where, f"an operand is not {count} contiguous values of {dtype} on device {device}: "
+                                f"{tuple(t.shape)} of {t.dtype}, strides {t.stride()}, on {t.device}")
+    return t.data_ptr()
+
+
+def _dtype(where: str, dtype: str):
+    if dtype not in _DTYPES:
+        raise EEError(1, where, f"dtype {dtype!r} is neither 'f32' nor 'bf16'")
+    return _DTYPES[dtype], torch_dtype(dtype)
+
+
+def group_norm(dtype: str, x, batch: int, hw: int, c: int, groups: int, gamma, beta, eps: float, act: int, out, residual=None, stream=None):
+    """ee_group_norm: act(gamma * (x - mean) / sqrt(var + eps) + beta (+ residual)) over [batch][hw][c], statistics per sample and group."""
+    f, d = "ee_group_norm", torch.cuda.current_device()
+    code, td = _dtype(f, dtype)
+    n = batch * hw * c
+    _check(load_library().ee_group_norm(code, _mem(f, x, td, n, d), _mem(f, residual, td, n, d), batch, hw, c, groups, _mem(f, gamma, torch.float32, c, d),
+                                        _mem(f, beta, torch.float32, c, d), eps, act, _mem(f, out, td, n, d), _stream(stream)), f)
+
+
+def adapted_linear_workspace_bytes(rows: int, rank: int) -> int:
+    return int(load_library().ee_adapted_linear_workspace_bytes(rows, rank))
+
+
+def adapted_linear(dtype: str, x, rows: int, c: int, weight, n: int, a, b, rank: int, n_adapters: int, adapter, out, workspace: Optional[torch.Tensor],
+                   bias=None, scale=None, stream=None):
+    """ee_adapted_linear: out[t] = weight x[t] + bias + scale[i] b[i] (a[i] x[t]), i = adapter[t].  ``workspace``: a device tensor of at least
+    adapted_linear_workspace_bytes(rows, rank) bytes behind its first 256-byte boundary, one for every call that may be in flight."""
+    f, d, f32 = "ee_adapted_linear", torch.cuda.current_device(), torch.float32
+    code, td = _dtype(f, dtype)
+    aligned, room = None, 0
+    if workspace is not None:
+        base = _mem(f, workspace, workspace.dtype, 0, d)
+        aligned = (base + 255) // 256 * 256
+        room = max(0, workspace.numel() * workspace.element_size() - (aligned - base))
+    _check(load_library().ee_adapted_linear(code, _mem(f, x, td, rows * c, d), rows, c, _mem(f, weight, td, n * c, d), n, _mem(f, bias, f32, n, d),
+                                            _mem(f, a, td, n_adapters * rank * c, d), _mem(f, b, td, n_adapters * n * rank, d), rank, n_adapters,
+                                            _mem(f, scale, f32, n_adapters, d), _mem(f, adapter, torch.int32, rows, d), _mem(f, out, td, rows * n, d),
+                                            aligned, room, _stream(stream)), f)
+
+
+def softmax(dtype: str, logits, rows: int, n: int, out, temperature=None, stream=None):
+    """ee_softmax: probabilities (fp32) of rows of logits at a temperature of each row's own."""
+    f, d = "ee_softmax", torch.cuda.current_device()
+    code, td = _dtype(f, dtype)
+    _check(load_library().ee_softmax(code, _mem(f, logits, td, rows * n, d), rows, n, _mem(f, temperature, torch.float32, rows, d),
+                                     _mem(f, out, torch.float32, rows * n, d), _stream(stream)), f)
+
+
+def verify_drafts(p, q, drafts, u, r, batch: int, k: int, n: int, tokens, n_accepted, n_draft=None, stream=None):
+    """ee_verify_drafts: which drafted tokens stand against the probabilities p, and the token that follows them."""
+    f, d, f32, i32 = "ee_verify_drafts", torch.cuda.current_device(), torch.float32, torch.int32
+    _check(load_library().ee_verify_drafts(_mem(f, p, f32, batch * (k + 1) * n, d), _mem(f, q, f32, batch * k * n, d), _mem(f, drafts, i32, batch * k, d),
+                                           _mem(f, u, f32, batch * k, d), _mem(f, r, f32, batch, d), _mem(f, n_draft, i32, batch, d), batch, k, n,
+                                           _mem(f, tokens, i32, batch * (k + 1), d), _mem(f, n_accepted, i32, batch, d), _stream(stream)), f)
+
+
+def operators_check(stream=None):
+    """ee_operators_check: raises when a bounded wait of an operator's kernel ran out since the last call."""
+    _check(load_library().ee_operators_check(_stream(stream)), "ee_operators_check")
 
 
 def to_device(model_dtype: str, a: np.ndarray, device="cuda") -> torch.Tensor:

@@ -2,8 +2,10 @@
 // plan, workspace layout), ee_stage_run, ee_batch_refill and the stand-alone head / gather calls.
 #include <atomic>
 #include <chrono>
+#include <cfloat>
 #include <cstdio>
 #include <cstring>
+#include <mutex>
 #include <new>
 #include <string>
 #include <vector>
@@ -19,6 +21,9 @@
 #include "conv_dw.cuh"
 #include "conv_xdw.cuh"
 #include "head.cuh"
+#include "norm.cuh"
+#include "lowrank.cuh"
+#include "draft.cuh"
 
 using namespace ee;
 
@@ -37,8 +42,8 @@ thread_local std::string g_cuda_err;
 
 constexpr int kBranchMaxBatch = 32;   // shortcut layers run on the branch stream up to this batch size
 
-enum KernelKind { KK_SIMT = 0, KK_TC = 1, KK_DW = 2, KK_POOL = 3, KK_TC_GATHER = 4, KK_F32 = 5 };
-const char* kKernelNames[] = {"conv_igemm_simt", "conv_igemm_tcgen05", "dwconv", "maxpool", "conv_igemm_tcgen05_gather", "conv_igemm_f64mma"};
+enum KernelKind { KK_SIMT = 0, KK_TC = 1, KK_DW = 2, KK_POOL = 3, KK_TC_GATHER = 4, KK_F32 = 5, KK_NORM = 6 };
+const char* kKernelNames[] = {"conv_igemm_simt", "conv_igemm_tcgen05", "dwconv", "maxpool", "conv_igemm_tcgen05_gather", "conv_igemm_f64mma", "group_norm"};
 
 struct LayerPlan {
   ee_layer_desc_t d;
@@ -323,6 +328,9 @@ ee_status_t launch_layer(ee_model* m, const LayerPlan& L, const void* src, const
         dwconv_kernel<T, 1><<<grid, 256, 0, st>>>((const T*)src, (const T*)L.w_dev, L.scale_dev, L.bias_dev, (T*)dst, g);
       break;
     }
+    case KK_NORM:
+      EE_CUDA(norm_launch<T>(src, res, dst, L.scale_dev, L.bias_dev, L.d.norm_eps, B, L.in_h * L.in_w, L.d.cin, L.d.norm_groups, L.d.act, L.tc.rev, st));
+      break;
     case KK_POOL: {
       if constexpr (sizeof(T) == 2) {
         if (dw_tma_supported(g, src, nullptr, dst)) {
@@ -349,6 +357,8 @@ ee_status_t launch_layer(ee_model* m, const LayerPlan& L, const void* src, const
 bool pair_entry_taken(const LayerPlan& L, int variant) {
   return L.kind == KK_TC && !L.tc.gather && !L.tc.halo && !L.tc.stem && L.pair_filters > (variant == TCV_PAIR256 ? 128 : 64);
 }
+
+bool valid_norm(int c, int groups, float eps) { return groups >= 1 && groups <= c && c % groups == 0 && eps >= 0.f && eps <= FLT_MAX; }
 
 bool host_memory(const void* p) {
   cudaPointerAttributes a;
@@ -906,11 +916,13 @@ ee_status_t ee_model_create(const ee_model_desc_t* desc, void* cuda_stream, ee_m
       if (d.pad_w < EE_PAD_W_SAME) return fail(EE_ERR_INVALID_ARG);
       if (L.d.pad_w == EE_PAD_W_SAME) L.d.pad_w = d.pad;              // from here on pad = rows, pad_w = columns
       if (d.op != EE_OP_CONV && L.d.pad_w != d.pad) return fail(EE_ERR_UNSUPPORTED);
-      if (d.op < EE_OP_CONV || d.op > EE_OP_MAXPOOL || d.kh < 1 || d.kw < 1 || d.stride < 1 || d.pad < 0 || d.cin < 1 ||
-          d.cout < 1 || d.act < EE_ACT_NONE || d.act > EE_ACT_RELU6 || d.input_from < EE_FROM_STAGE_INPUT ||
+      const bool norm = d.op == EE_OP_GROUPNORM;
+      if (d.op < EE_OP_CONV || d.op > EE_OP_GROUPNORM || d.kh < 1 || d.kw < 1 || d.stride < 1 || d.pad < 0 || d.cin < 1 ||
+          d.cout < 1 || d.act < EE_ACT_NONE || d.act > (norm ? EE_ACT_SILU : EE_ACT_RELU6) || d.input_from < EE_FROM_STAGE_INPUT ||
           d.input_from >= i || d.residual_from < EE_FROM_STAGE_INPUT || d.residual_from >= i)
         return fail(EE_ERR_INVALID_ARG);
-      if (d.op != EE_OP_MAXPOOL && !d.weight) return fail(EE_ERR_INVALID_ARG);
+      if (norm && (d.kh != 1 || d.kw != 1 || d.stride != 1 || d.pad != 0 || !valid_norm(d.cin, d.norm_groups, d.norm_eps))) return fail(EE_ERR_INVALID_ARG);
+      if (d.op != EE_OP_MAXPOOL && !norm && !d.weight) return fail(EE_ERR_INVALID_ARG);
       int ih, iw, ic, src = d.input_from;
       if (src == EE_FROM_STAGE_INPUT || (src == EE_FROM_PREV && i == 0)) {
         ih = h, iw = w, ic = c, src = -1;
@@ -920,7 +932,7 @@ ee_status_t ee_model_create(const ee_model_desc_t* desc, void* cuda_stream, ee_m
         last_use[src] = i;
       }
       if (ic != d.cin) return fail(EE_ERR_SHAPE);
-      if ((d.op == EE_OP_DWCONV || d.op == EE_OP_MAXPOOL) && d.cin != d.cout) return fail(EE_ERR_SHAPE);
+      if ((d.op == EE_OP_DWCONV || d.op == EE_OP_MAXPOOL || norm) && d.cin != d.cout) return fail(EE_ERR_SHAPE);
       L.in_h = ih;
       L.in_w = iw;
       L.out_h = (ih + 2 * d.pad - d.kh) / d.stride + 1;
@@ -932,7 +944,7 @@ ee_status_t ee_model_create(const ee_model_desc_t* desc, void* cuda_stream, ee_m
       if (rs == EE_NO_RESIDUAL) {
         L.res_slot = -2;
       } else {
-        if (d.op != EE_OP_CONV) return fail(EE_ERR_UNSUPPORTED);
+        if (d.op != EE_OP_CONV && !norm) return fail(EE_ERR_UNSUPPORTED);
         int rh, rw, rcn;
         if (rs == EE_FROM_STAGE_INPUT) {
           rh = h, rw = w, rcn = c;
@@ -944,7 +956,7 @@ ee_status_t ee_model_create(const ee_model_desc_t* desc, void* cuda_stream, ee_m
         }
         if (rh != L.out_h || rw != L.out_w || rcn != d.cout) return fail(EE_ERR_SHAPE);
       }
-      if (d.op != EE_OP_MAXPOOL) {
+      if (d.op != EE_OP_MAXPOOL && !norm) {
         const int cpg = d.op == EE_OP_DWCONV ? 1 : d.cin;
         sp.flops_per_sample += 2.0 * L.out_h * L.out_w * d.cout * (double)(d.kh * d.kw * cpg);
       }
@@ -1059,6 +1071,13 @@ ee_status_t ee_model_create(const ee_model_desc_t* desc, void* cuda_stream, ee_m
       const ee_layer_desc_t& d = L.d;
       if (d.op == EE_OP_MAXPOOL) {
         L.kind = KK_POOL;
+        continue;
+      }
+      if (d.op == EE_OP_GROUPNORM) {
+        L.kind = KK_NORM;
+        if (!norm_fits(norm_plan(L.in_h * L.in_w, d.cin, d.norm_groups, (int)es, true), desc->max_batch)) return fail(EE_ERR_UNSUPPORTED);
+        if ((rc = upload<float>(m, d.scale, d.cout, ondev, st, &L.scale_dev)) != EE_OK) return fail(rc);
+        if ((rc = upload<float>(m, d.bias, d.cout, ondev, st, &L.bias_dev)) != EE_OK) return fail(rc);
         continue;
       }
       const int cpg = d.op == EE_OP_DWCONV ? 1 : d.cin;
@@ -1681,9 +1700,10 @@ ee_status_t ee_model_plan(const ee_model_t* m, int stage, int batch, int cap, ee
     p.m = batch * L.out_h * L.out_w;
     p.n = L.d.cout;
     p.k = L.d.kh * L.d.kw * cpg;
-    p.flops = L.d.op == EE_OP_MAXPOOL ? 0.0 : 2.0 * p.m * (double)p.n * p.k;
+    const bool plain = L.d.op == EE_OP_MAXPOOL || L.d.op == EE_OP_GROUPNORM;   // no product
+    p.flops = plain ? 0.0 : 2.0 * p.m * (double)p.n * p.k;
     const double in_b = (double)batch * L.in_h * L.in_w * L.d.cin * es, out_b = (double)p.m * p.n * es;
-    const double w_b = L.d.op == EE_OP_MAXPOOL ? 0.0 : (double)L.d.cout * p.k * es;
+    const double w_b = plain ? 0.0 : (double)L.d.cout * p.k * es;
     p.bytes = in_b + out_b + w_b + (L.res_slot != -2 ? out_b : 0.0);
     p.launches = 1;
     if (L.pool_next) {   // the launch writes the pooled tensor instead of the convolution's output
@@ -1792,6 +1812,143 @@ ee_status_t ee_model_check(ee_model_t* m, void* cuda_stream) {
     return EE_ERR_TIMEOUT;
   }
   return EE_OK;
+}
+
+// ---- operators without a model
+
+static __device__ int g_operator_flag;   // EE_ERR_TIMEOUT once a bounded wait of an operator's kernel has run out
+
+namespace {
+
+struct OperatorContext {   // one per device, filled at its first call
+  std::atomic<int> ready{0};
+  LrContext lr;
+  int* flag = nullptr;
+};
+OperatorContext g_operators[kMaxDevices];
+std::mutex g_operators_lock;
+
+ee_status_t operator_context(const OperatorContext** out) {
+  int dev = -1;
+  EE_CUDA(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= kMaxDevices) return EE_ERR_UNSUPPORTED;
+  OperatorContext& c = g_operators[dev];
+  if (!c.ready.load(std::memory_order_acquire)) {
+    const std::lock_guard<std::mutex> hold(g_operators_lock);
+    if (!c.ready.load(std::memory_order_relaxed)) {
+      cudaDriverEntryPointQueryResult q;
+      void *f = nullptr, *flag = nullptr;
+      EE_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q));
+      EE_CUDA(cudaGetSymbolAddress(&flag, g_operator_flag));
+      if (!f || !flag) return EE_ERR_INTERNAL;
+      EE_CUDA(cudaDeviceGetAttribute(&c.lr.sm_count, cudaDevAttrMultiProcessorCount, dev));
+      EE_CUDA(lr_context_init());
+      if (f32_context_init() != EE_OK) return EE_ERR_CUDA;
+      c.lr.encode_tiled = (PFN_encodeTiled)f;
+      c.flag = (int*)flag;
+      c.ready.store(1, std::memory_order_release);
+    }
+  }
+  *out = &c;
+  return EE_OK;
+}
+
+bool aligned_to(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+bool apart(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  return (uintptr_t)a + a_bytes <= (uintptr_t)b || (uintptr_t)b + b_bytes <= (uintptr_t)a;
+}
+
+}  // namespace
+
+ee_status_t ee_group_norm(int dtype, const void* x, const void* residual, int batch, int hw, int c, int groups, const float* gamma, const float* beta,
+                          float eps, int act, void* y, void* cuda_stream) {
+  if ((dtype != EE_F32 && dtype != EE_BF16) || batch < 0 || hw < 1 || c < 1 || !valid_norm(c, groups, eps) || act < EE_ACT_NONE || act > EE_ACT_SILU)
+    return EE_ERR_INVALID_ARG;
+  if (batch == 0) return EE_OK;
+  const size_t es = esize(dtype), bytes = (size_t)batch * hw * c * es;
+  if (!x || !y || !aligned_to(x, es) || !aligned_to(y, es) || !aligned_to(residual, es) || !aligned_to(gamma, 4) || !aligned_to(beta, 4)) return EE_ERR_INVALID_ARG;
+  if ((y != x && !apart(x, bytes, y, bytes)) || (residual && y != residual && !apart(residual, bytes, y, bytes))) return EE_ERR_INVALID_ARG;
+  if (!norm_fits(norm_plan(hw, c, groups, (int)es, true), batch) || !norm_fits(norm_plan(hw, c, groups, (int)es, false), batch)) return EE_ERR_CAPACITY;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  EE_CUDA(dtype == EE_BF16 ? norm_launch<bf16>(x, residual, y, gamma, beta, eps, batch, hw, c, groups, act, false, st)
+                           : norm_launch<float>(x, residual, y, gamma, beta, eps, batch, hw, c, groups, act, false, st));
+  return EE_OK;
+}
+
+size_t ee_adapted_linear_workspace_bytes(int rows, int rank) {
+  return rows > 0 && rank > 0 ? (size_t)rows * rank * 4 : 0;   // a float, or two bf16 parts
+}
+
+ee_status_t ee_adapted_linear(int dtype, const void* x, int rows, int c, const void* weight, int n, const float* bias, const void* a, const void* b, int rank,
+                              int n_adapters, const float* scale, const int32_t* adapter, void* y, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if ((dtype != EE_F32 && dtype != EE_BF16) || rows < 0 || c < 1 || n < 1 || n_adapters < 0) return EE_ERR_INVALID_ARG;
+  if (n_adapters > 0 && (rank < 1 || rank > kLrMaxRank || (long)n_adapters * rank > 0x7fffffffL)) return EE_ERR_INVALID_ARG;
+  if (rows == 0) return EE_OK;
+  if (rows > 1 << 22) return EE_ERR_CAPACITY;
+  const size_t es = esize(dtype), xb = (size_t)rows * c * es, yb = (size_t)rows * n * es;
+  if (!x || !weight || !y || !aligned_to(x, es) || !aligned_to(weight, es) || !aligned_to(y, es) || !aligned_to(bias, 4) || !apart(x, xb, y, yb))
+    return EE_ERR_INVALID_ARG;
+  if (n_adapters > 0) {
+    if (!a || !b || !adapter || !workspace || !aligned_to(a, es) || !aligned_to(b, es) || !aligned_to(scale, 4) || !aligned_to(adapter, 4) || !aligned_to(workspace, 256))
+      return EE_ERR_INVALID_ARG;
+    const size_t need = ee_adapted_linear_workspace_bytes(rows, rank);
+    if (workspace_bytes < need) return EE_ERR_CAPACITY;
+    if (!apart(workspace, need, y, yb) || !apart(workspace, need, x, xb)) return EE_ERR_INVALID_ARG;
+  }
+  const OperatorContext* ctx;
+  const ee_status_t s = operator_context(&ctx);
+  if (s != EE_OK) return s;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  if (dtype == EE_F32) {
+    EE_CUDA(lr_run_f32(ctx->lr, (const float*)x, (const float*)weight, bias, (const float*)a, (const float*)b, scale, adapter, (float*)workspace, (float*)y, rows, c, n,
+                       rank, n_adapters, ctx->flag, st));
+    return EE_OK;
+  }
+  LrArgs p = {};
+  p.x = (const bf16*)x, p.w = (const bf16*)weight, p.bias = bias, p.a = (const bf16*)a, p.b = (const bf16*)b, p.scale = scale, p.which = adapter;
+  p.h = (bf16*)workspace, p.y = (bf16*)y, p.rows = rows, p.c = c, p.n = n, p.rank = n_adapters ? rank : 1, p.adapters = n_adapters, p.err_flag = ctx->flag;
+  EE_CUDA(lr_run_bf16(ctx->lr, p, st));
+  return EE_OK;
+}
+
+ee_status_t ee_softmax(int dtype, const void* logits, int rows, int n, const float* temperature, float* probs, void* cuda_stream) {
+  if ((dtype != EE_F32 && dtype != EE_BF16) || rows < 0 || n < 1) return EE_ERR_INVALID_ARG;
+  if (rows == 0) return EE_OK;
+  const size_t es = esize(dtype);
+  if (!logits || !probs || !aligned_to(logits, es) || !aligned_to(probs, 4) || !aligned_to(temperature, 4)) return EE_ERR_INVALID_ARG;
+  if (!(dtype == EE_F32 && logits == (const void*)probs) && !apart(logits, (size_t)rows * n * es, probs, (size_t)rows * n * 4)) return EE_ERR_INVALID_ARG;
+  if (n > (dtype == EE_BF16 ? softmax_most<bf16>() : softmax_most<float>()) || (long)rows * kSmMaxCluster > 0x7fffffffL) return EE_ERR_CAPACITY;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  EE_CUDA(dtype == EE_BF16 ? softmax_launch<bf16>((const bf16*)logits, temperature, probs, rows, n, st)
+                           : softmax_launch<float>((const float*)logits, temperature, probs, rows, n, st));
+  return EE_OK;
+}
+
+ee_status_t ee_verify_drafts(const float* p, const float* q, const int32_t* drafts, const float* u, const float* r, const int32_t* n_draft, int batch, int k,
+                             int n, int32_t* tokens, int32_t* n_accepted, void* cuda_stream) {
+  if (batch < 0 || k < 0 || n < 1) return EE_ERR_INVALID_ARG;
+  if (batch == 0) return EE_OK;
+  if (!p || !r || !tokens || !n_accepted || (k > 0 && (!drafts || !u))) return EE_ERR_INVALID_ARG;
+  if (!aligned_to(p, 4) || !aligned_to(q, 4) || !aligned_to(drafts, 4) || !aligned_to(u, 4) || !aligned_to(r, 4) || !aligned_to(n_draft, 4) ||
+      !aligned_to(tokens, 4) || !aligned_to(n_accepted, 4))
+    return EE_ERR_INVALID_ARG;
+  if ((long)batch * kVfMaxCluster > 0x7fffffffL || k > 0x7fffffff - 64) return EE_ERR_CAPACITY;
+  EE_CUDA(verify_launch({p, q, drafts, u, r, n_draft, tokens, n_accepted, k, n, 0}, batch, (cudaStream_t)cuda_stream));
+  return EE_OK;
+}
+
+ee_status_t ee_operators_check(void* cuda_stream) {
+  const OperatorContext* ctx;
+  const ee_status_t s = operator_context(&ctx);
+  if (s != EE_OK) return s;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  int flag = 0;
+  EE_CUDA(cudaMemcpyAsync(&flag, ctx->flag, sizeof(int), cudaMemcpyDeviceToHost, st));
+  EE_CUDA(cudaStreamSynchronize(st));
+  if (!flag) return EE_OK;
+  EE_CUDA(cudaMemsetAsync(ctx->flag, 0, sizeof(int), st));
+  EE_CUDA(cudaStreamSynchronize(st));
+  return EE_ERR_TIMEOUT;
 }
 
 }  // extern "C"

@@ -30,8 +30,8 @@ from typing import List, Optional
 
 import numpy as np
 
-OP_CONV, OP_DWCONV, OP_MAXPOOL = 0, 1, 2
-ACT_NONE, ACT_RELU, ACT_RELU6 = 0, 1, 2
+OP_CONV, OP_DWCONV, OP_MAXPOOL, OP_GROUPNORM = 0, 1, 2, 3
+ACT_NONE, ACT_RELU, ACT_RELU6, ACT_SILU = 0, 1, 2, 3
 FROM_PREV, FROM_STAGE_INPUT = -1, -2
 NO_RESIDUAL = -1
 
@@ -73,6 +73,8 @@ class Layer:
     scale: Optional[np.ndarray] = None    # [cout] folded-BN scale
     bias: Optional[np.ndarray] = None     # [cout] folded-BN bias
     pad_w: int = -1                       # padding of the columns; -1 = the same as ``pad`` (which pads the rows)
+    norm_groups: int = 0                  # group norm: groups that the channels fall into
+    norm_eps: float = 0.0                 # group norm: added to the variance
 
     @property
     def groups(self) -> int:
