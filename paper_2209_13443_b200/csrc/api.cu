@@ -329,7 +329,7 @@ ee_status_t launch_layer(ee_model* m, const LayerPlan& L, const void* src, const
       break;
     }
     case KK_NORM:
-      EE_CUDA(norm_launch<T>(src, res, dst, L.scale_dev, L.bias_dev, L.d.norm_eps, B, L.in_h * L.in_w, L.d.cin, L.d.norm_groups, L.d.act, L.tc.rev, st));
+      EE_CUDA(norm_launch<T>(src, res, dst, L.scale_dev, L.bias_dev, L.d.norm_eps, B, L.in_h * L.in_w, L.d.cin, L.d.norm_groups, L.d.act, L.tc.rev, m->err_flag, st));
       break;
     case KK_POOL: {
       if constexpr (sizeof(T) == 2) {
@@ -1869,9 +1869,12 @@ ee_status_t ee_group_norm(int dtype, const void* x, const void* residual, int ba
   if (!x || !y || !aligned_to(x, es) || !aligned_to(y, es) || !aligned_to(residual, es) || !aligned_to(gamma, 4) || !aligned_to(beta, 4)) return EE_ERR_INVALID_ARG;
   if ((y != x && !apart(x, bytes, y, bytes)) || (residual && y != residual && !apart(residual, bytes, y, bytes))) return EE_ERR_INVALID_ARG;
   if (!norm_fits(norm_plan(hw, c, groups, (int)es, true), batch) || !norm_fits(norm_plan(hw, c, groups, (int)es, false), batch)) return EE_ERR_CAPACITY;
+  const OperatorContext* ctx;
+  const ee_status_t s = operator_context(&ctx);
+  if (s != EE_OK) return s;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  EE_CUDA(dtype == EE_BF16 ? norm_launch<bf16>(x, residual, y, gamma, beta, eps, batch, hw, c, groups, act, false, st)
-                           : norm_launch<float>(x, residual, y, gamma, beta, eps, batch, hw, c, groups, act, false, st));
+  EE_CUDA(dtype == EE_BF16 ? norm_launch<bf16>(x, residual, y, gamma, beta, eps, batch, hw, c, groups, act, false, ctx->flag, st)
+                           : norm_launch<float>(x, residual, y, gamma, beta, eps, batch, hw, c, groups, act, false, ctx->flag, st));
   return EE_OK;
 }
 

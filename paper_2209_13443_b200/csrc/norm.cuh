@@ -1,12 +1,14 @@
 // Group norm with an activation on channels-last maps: y = act(gamma[c] * (x - mean_g) / sqrt(var_g + eps) + beta[c] (+ residual)),
 // mean and (biased) variance over the pixels of a sample and the channels of its group g.
 //
-// What bounds it is memory: x read once, y written once.  So a sample's slice of whole groups (about 128 bytes of channels) is
-// fetched into the shared memory of a cluster of up to eight CTAs, each with a range of the pixels, and stays there between the
-// statistics and the normalisation.  The statistics take two passes over what is in shared memory, the sum and then the squares
-// about the CTA's own mean, so that they do not cancel where a mean is large against its deviation; the CTAs exchange
-// (mean, sum of squares) through distributed shared memory and every CTA joins them in the same order:
-//   mean = sum n_i mean_i / n,   S = sum (S_i + n_i (mean_i - mean)^2).
+// What bounds it is memory: x read once, y written once.  So a unit, a sample's slice of whole groups (about 128 bytes of channels), is
+// fetched into the shared memory of a cluster of CTAs, each with a range of the pixels, and stays there between the
+// statistics and the normalisation.  Four small CTAs share an SM, so that one's loads and stores run beside another's barriers.  (Clusters that take one unit
+// after the other, the next one on its way into a second buffer, were slower: 91 against 63 us on 64 x 56 x 56 x 256 with a residual.)
+// Sums of squares would cancel where a mean is large against its deviation, so every part (a thread's
+// values, a warp's, a CTA's, the cluster's) is (mean, squares about it), and parts are joined, in a fixed order, as
+//   mean = sum n_i mean_i / n,   S = sum (S_i + n_i (mean_i - mean)^2);
+// the CTAs send each other theirs as asynchronous stores, which the receiver's barrier counts: nothing but the data is waited for.
 // All sums are fp32.  Slice, cluster and order of the sums follow from the map's shape alone, never from the batch: a sample's bits
 // do not depend on whom it rides with.
 //
@@ -16,23 +18,28 @@
 #include <algorithm>
 
 #include "common.cuh"
+#include "conv_tc.cuh"
 
 namespace ee {
 
-constexpr int kNormThreads = 256;
 constexpr int kNormMaxCluster = 8;
-constexpr int kNormChunk = 56 << 10;        // bytes of a CTA's part of a slice that a cluster is cut for: three CTAs share an SM
-constexpr int kNormMaxChunk = 192 << 10;    // beyond this, and at eight CTAs, the map is read again from global memory instead
+// Bytes of a CTA's part of a unit that a cluster is cut for, and up to which it stays in shared memory where eight CTAs are not enough for that: four CTAs then
+// share an SM.  Larger parts are read a second time, from L2.  us, 28 / 56 KB parts: 13 x 33 x 29 x 96 fp32 6.4 / 7.9; the second read in place of two CTAs an SM:
+// 32 x 112 x 112 x 96 84 -> 65 (parts of 150 KB), of four: 64 x 56 x 56 x 256 62 -> 68 (50 KB).
+constexpr int kNormChunk = 28 << 10;
+constexpr int kNormMaxChunk = 56 << 10;
 
 struct NormPlan {
   int v;             // elements per access
   int sv, slices;    // accesses per pixel of a slice, slices of a sample
   int groups;        // groups of a slice
   int cluster, rows; // CTAs of a slice, pixels of each
+  int threads;
   bool wide;         // a pixel of the slice is more than the CTA's threads take at once; the slice is then one group
   bool merged;       // an access lies in one group: its elements are summed together
   bool resident;
-  int smem, off_red, off_stat;
+  int chunk, red_rows, bins;   // bytes of a CTA's part; partial statistics: rows and columns
+  int smem() const { return chunk + red_rows * bins * 8 + groups * 8 * (cluster + 1) + 8; }
 };
 
 struct NormArgs {
@@ -43,7 +50,8 @@ struct NormArgs {
   const float* beta;
   float eps;
   int hw, c, cpg, act;
-  int sv, slices, groups, rows, off_red, off_stat;
+  int sv, slices, groups, rows, chunk, red_rows, bins;
+  int* err_flag;
   int rev;           // 1: from the last sample down (the newest samples of the input are the ones still in L2)
 };
 
@@ -55,6 +63,8 @@ inline int norm_gcd(int a, int b) {
   return a;
 }
 
+constexpr int kNormThreads = 256, kNormFew = 128;
+
 inline NormPlan norm_plan(int hw, int c, int groups, int es, bool aligned) {
   NormPlan p = {};
   const int cpg = c / groups;
@@ -62,8 +72,8 @@ inline NormPlan norm_plan(int hw, int c, int groups, int es, bool aligned) {
   int unit = cpg / norm_gcd(cpg, p.v) * p.v;               // channels that are whole groups and whole accesses
   if (unit / p.v > kNormThreads && cpg % p.v) p.v = 1, unit = cpg;
   p.wide = unit / p.v > kNormThreads;
-  // Wide enough for whole 128-byte lines, and on maps of few pixels for every thread to have something.
-  const long most = std::max<long>(128, (long)kNormThreads * 16 / std::max(hw, 1));
+  // Wide enough for whole 128-byte lines, and on maps of few pixels for 128 threads to have something.
+  const long most = std::max<long>(128, (long)kNormFew * 16 / std::max(hw, 1));
   const int units = c / unit;
   int m = 1;
   if (!p.wide)
@@ -76,9 +86,11 @@ inline NormPlan norm_plan(int hw, int c, int groups, int es, bool aligned) {
   while (p.cluster < kNormMaxCluster && p.cluster * 2 <= hw && ((long)hw + p.cluster - 1) / p.cluster * row > kNormChunk) p.cluster *= 2;
   p.rows = (hw + p.cluster - 1) / p.cluster;
   p.resident = p.rows * row <= kNormMaxChunk;
-  p.off_red = p.resident ? (int)align_up((size_t)(p.rows * row), 16) : 0;
-  p.off_stat = p.off_red + kNormThreads * (p.merged ? 1 : p.v) * 4;
-  p.smem = p.off_stat + p.groups * 4 * 4;                   // mean and squares of this CTA, of all
+  p.chunk = p.resident ? (int)align_up((size_t)(p.rows * row), 16) : 0;
+  // few accesses: few threads, so that each still has some
+  p.threads = p.resident && p.sv <= kNormFew && (long)p.rows * p.sv <= 4 * kNormFew ? kNormFew : kNormThreads;
+  p.bins = p.wide ? 1 : p.sv * (p.merged ? 1 : p.v);
+  p.red_rows = p.wide || p.sv <= 32 ? p.threads / 32 : p.threads / p.sv;
   return p;
 }
 
@@ -100,43 +112,81 @@ __device__ __forceinline__ void norm_unpack(const NormVec<T, V>& r, float* f) {
   }
 }
 
-// SiLU: the fast exponential is off by 2 + 1.2 |v| units in the last place, which weigh with exp(-v) / (1 + exp(-v)) where v > 0 and
-// relative to a vanishing result where v < 0; the fast quotient is 0 where exp(-v) passes 2^126, v < -87.
-__device__ __forceinline__ float norm_act(float v, int act) {
-  if (act == EE_ACT_SILU) return __fdividef(v, 1.f + __expf(-v));
-  return apply_act(v, act);
+// SiLU, v / (1 + exp(-v)): 2^x is off by 2 units in the last place and x = -v log2(e) by 1.2 |v| of them in the power, which weigh with exp(-v) / (1 + exp(-v))
+// where v > 0 and relative to a vanishing result where v < 0; the reciprocal adds one.
+// The other activations are clamps: to [lo, hi], NaN staying NaN.
+struct NormClamp {
+  float lo, hi;
+  __device__ __forceinline__ explicit NormClamp(int act) : lo(act == EE_ACT_NONE ? -INFINITY : 0.f), hi(act == EE_ACT_RELU6 ? 6.f : INFINITY) {}
+};
+template <bool SILU>
+__device__ __forceinline__ float norm_act(float v, const NormClamp& c) {
+  if constexpr (SILU) {
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    return v * r;
+  }
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(c.lo));
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(c.hi));
+  return v;
 }
-// Pairwise sum of an access.
-template <int V>
-__device__ __forceinline__ float norm_tree(const float* f) {
-  if constexpr (V == 1) return f[0];
-  else return norm_tree<V / 2>(f) + norm_tree<V / 2>(f + V / 2);
+template <bool B> struct Flag { static constexpr bool value = B; };
+// Two floats in one register pair: the packed instructions round each half like the scalar ones.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair_of(float lo, float hi) {
+  f32x2 d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void pair_split(f32x2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ f32x2 pair_add(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ f32x2 pair_fma(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
 }
 
-// V elements per access, MERGED and WIDE as in NormPlan; RESIDENT: the CTA's pixels stay in shared memory.
-template <typename T, int V, bool MERGED, bool WIDE, bool RESIDENT>
-__global__ void __launch_bounds__(kNormThreads)
-group_norm_kernel(NormArgs p) {
+// V elements per access, MERGED and WIDE as in NormPlan; RESIDENT: the CTA's pixels stay in shared memory; NT threads.
+template <typename T, int V, bool MERGED, bool WIDE, bool RESIDENT, int NT>
+__global__ void __launch_bounds__(NT, MERGED ? 1024 / NT : 768 / NT)
+group_norm_kernel(const __grid_constant__ NormArgs p) {
   static_assert(!WIDE || MERGED, "a wide slice is one group");
   typedef NormVec<T, V> Vec;
-  constexpr int K = MERGED ? 1 : V;      // sums per thread
+  constexpr int K = MERGED ? 1 : V;                    // sums per thread
+  constexpr int P = V > 1 ? V / 2 : 1;                 // pairs of an access
+  constexpr int NW = NT / 32;
   extern __shared__ __align__(16) uint8_t norm_smem[];
-  float* red = reinterpret_cast<float*>(norm_smem + p.off_red);
-  float* stat = reinterpret_cast<float*>(norm_smem + p.off_stat);   // [mean, squares] of this CTA, then [mean, 1 / deviation] of the slice
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  float2* red = reinterpret_cast<float2*>(norm_smem + p.chunk);
+  float2* stat = red + p.red_rows * p.bins;            // [groups][cluster]: (mean, squares) of every CTA
   uint32_t rank, cluster;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(cluster));
-  const long unit = (p.rev ? gridDim.x - 1 - blockIdx.x : blockIdx.x) / cluster;
-  const int slice = (int)(unit % p.slices);
-  const long sample = unit / p.slices;
-  const int row0 = min((int)rank * p.rows, p.hw), rows = min(p.rows, p.hw - row0);
-  const size_t first = ((size_t)sample * p.hw + row0) * p.c + (size_t)slice * p.sv * V;
-  const T* x = reinterpret_cast<const T*>(p.x) + first;
-  // this thread's accesses: column, pixel, and the step to the next one
-  const int ty_n = WIDE ? 1 : kNormThreads / p.sv;
-  const int col0 = WIDE ? tid : tid % p.sv, ty = WIDE ? 0 : tid / p.sv;
-  const bool active = WIDE || ty < ty_n;
+  float2* all = stat + p.groups * (int)cluster;    // [groups]: (mean, 1 / deviation) of the unit
+  const uint32_t arrived = (uint32_t)__cvta_generic_to_shared(all + p.groups);      // counts what the CTAs send
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (cluster > 1) {
+    if (tid == 0) {
+      mbar_init(arrived, 1);
+      mbar_expect_tx(arrived, (uint32_t)p.groups * cluster * 8u);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");    // waited for before anything is sent
+  }
+  const int rows = min(p.rows, p.hw - min((int)rank * p.rows, p.hw));
+  // This thread's accesses: its column, its first pixel, and the step to the next one.  Slices of up to 32 accesses: a warp has whole pixels.
+  const bool by_warp = !WIDE && p.sv <= 32;
+  const int warp_rows = by_warp ? 32 / p.sv : 1;
+  const int ty_n = WIDE ? 1 : by_warp ? NW * warp_rows : NT / p.sv;
+  const int lane_row = by_warp ? lane / p.sv : 0;
+  const int col0 = WIDE ? tid : by_warp ? lane - lane_row * p.sv : tid % p.sv;
+  const int ty = WIDE ? 0 : by_warp ? warp * warp_rows + lane_row : tid / p.sv;
+  const bool active = WIDE || (by_warp ? lane_row < warp_rows : ty < ty_n);
   auto each = [&](auto&& body) {
     if constexpr (WIDE) {
       for (int col = tid, row = 0; row < rows;) {
@@ -145,176 +195,279 @@ group_norm_kernel(NormArgs p) {
           if (++row >= rows) return;
         }
         body(row, col);
-        col += kNormThreads;
+        col += NT;
       }
     } else if (active) {
 #pragma unroll 4
       for (int row = ty; row < rows; row += ty_n) body(row, col0);
     }
   };
+  const long unit = (p.rev ? gridDim.x - 1 - blockIdx.x : blockIdx.x) / cluster, sample = unit / p.slices;
+  const int channel = (int)(unit - sample * p.slices) * p.sv * V;            // of the slice
+  const size_t first = ((size_t)sample * p.hw + min((int)rank * p.rows, p.hw)) * p.c + (size_t)channel;
+  const T* x = reinterpret_cast<const T*>(p.x) + first;
   auto held = [&](int row, int col) {
     if constexpr (RESIDENT)
-      return *reinterpret_cast<const Vec*>(norm_smem + ((size_t)row * p.sv + col) * sizeof(Vec));
+      return *reinterpret_cast<const Vec*>(norm_smem + (size_t)(row * p.sv + col) * sizeof(Vec));
     else
       return *reinterpret_cast<const Vec*>(x + (size_t)row * p.c + col * V);
   };
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if constexpr (RESIDENT) {   // a thread reads back what it fetched itself
-    const uint32_t at = (uint32_t)__cvta_generic_to_shared(norm_smem);
+  if constexpr (RESIDENT) {            // a thread reads back what it fetched itself: no barrier
+    const uint32_t smem_s = (uint32_t)__cvta_generic_to_shared(norm_smem);
     each([&](int row, int col) {
       const T* src = x + (size_t)row * p.c + col * V;
-      const uint32_t dst = at + (uint32_t)((row * p.sv + col) * (int)sizeof(Vec));
+      const uint32_t dst = smem_s + (uint32_t)((row * p.sv + col) * (int)sizeof(Vec));
       if constexpr (sizeof(Vec) == 16)
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
       else if constexpr (sizeof(Vec) == 4)
         asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
       else
-        *reinterpret_cast<Vec*>(norm_smem + ((size_t)row * p.sv + col) * sizeof(Vec)) = *reinterpret_cast<const Vec*>(src);
+        *reinterpret_cast<Vec*>(norm_smem + (size_t)(row * p.sv + col) * sizeof(Vec)) = *reinterpret_cast<const Vec*>(src);
     });
     cp_async_commit();
+    if (p.residual) {                  // on its way to L2 while the statistics are taken
+      const char* res = reinterpret_cast<const char*>(p.residual) + first * sizeof(T);
+      for (int row = tid; row < rows; row += NT)
+        for (int i = 0; i < p.sv * (int)sizeof(Vec); i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(res + (size_t)row * p.c * sizeof(T) + i));
+    }
     cp_async_wait<0>();
   }
-  // sums of the groups: each thread leaves its K sums in red, a warp adds up a group
-  const int bins = WIDE ? 1 : p.sv * K, per_group = bins / p.groups;   // bins of a pixel, of a group of it
-  const int reducers = WIDE ? kNormThreads : ty_n;                     // rows of red
-  float sum[K];
-  auto group_sums = [&](auto&& done) {
-    if (active) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) red[WIDE ? tid : ty * bins + col0 * K + k] = sum[k];
+  const float n_here = (float)rows * (float)p.cpg, inv_here = rows > 0 ? 1.f / n_here : 0.f, inv_all = 1.f / ((float)p.hw * (float)p.cpg);
+  const int lin = WIDE ? rows * p.sv : rows, step = WIDE ? NT : ty_n;    // thread r takes r, r + step, ... of lin
+  const int full = lin / step, more = lin - full * step;
+  auto count_of = [&](int r) { return (float)((full + (r < more ? 1 : 0)) * (MERGED ? V : 1)); };
+  // A row of red is a warp (its pixels together), or, where a pixel is more than a warp, the threads of one ty.
+  const int red_row = WIDE || by_warp ? warp : ty;
+  auto count_of_row = [&](int r) {
+    if (WIDE) {
+      float n = 0.f;
+      for (int i = 0; i < 32; ++i) n += count_of(r * 32 + i);
+      return n;
     }
-    __syncthreads();
-    const int n = reducers * per_group;
-    for (int g = warp; g < p.groups; g += kNormThreads / 32) {
+    return by_warp ? (float)((full * warp_rows + min(max(more - r * warp_rows, 0), warp_rows)) * (MERGED ? V : 1)) : count_of(r);
+  };
+  const int per_group = p.bins / p.groups;             // bins of a group
+  const int r_first = lane / per_group, r_step = 32 / per_group, b_first = lane - r_first * per_group, b_step = 32 - r_step * per_group;
+
+  // One pass: a thread sums d = x - shift and d^2 about its own first value of the group (or channel), which cancels as little as its few values
+  // allow: one of n values is at most sqrt(n) deviations off, so the squares lose at most n of the 2^24.
+  float shift[K], mean[K], m2[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) shift[k] = 0.f;
+  {
+    const int r0 = WIDE ? tid / p.sv : ty, c0 = WIDE ? tid % p.sv : col0;
+    if (active && r0 < rows) {
+      float f[V];
+      norm_unpack<T, V>(held(r0, c0), f);
+#pragma unroll
+      for (int k = 0; k < K; ++k) shift[k] = f[k];
+    }
+  }
+  if constexpr (V == 1) {
+    float s = 0.f, q = 0.f;
+    each([&](int row, int col) {
+      float f[1];
+      norm_unpack<T, V>(held(row, col), f);
+      const float d = f[0] - shift[0];
+      s += d, q = fmaf(d, d, q);
+    });
+    mean[0] = s, m2[0] = q;
+  } else {
+    constexpr int A = MERGED ? 2 : P;                // accumulators; an access has two chains where it is summed together
+    f32x2 s[A], q[A], less[MERGED ? 1 : P];
+#pragma unroll
+    for (int i = 0; i < A; ++i) s[i] = q[i] = 0ull;
+#pragma unroll
+    for (int i = 0; i < (MERGED ? 1 : P); ++i) less[i] = pair_of(-shift[MERGED ? 0 : 2 * i], -shift[MERGED ? 0 : 2 * i + 1]);
+    each([&](int row, int col) {
+      float f[V];
+      norm_unpack<T, V>(held(row, col), f);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const f32x2 d = pair_add(pair_of(f[2 * i], f[2 * i + 1]), less[MERGED ? 0 : i]);
+        s[MERGED ? i & 1 : i] = pair_add(s[MERGED ? i & 1 : i], d);
+        q[MERGED ? i & 1 : i] = pair_fma(d, d, q[MERGED ? i & 1 : i]);
+      }
+    });
+    if constexpr (MERGED) {
+      float u[4], v[4];
+      pair_split(s[0], u[0], u[1]), pair_split(s[1], u[2], u[3]), pair_split(q[0], v[0], v[1]), pair_split(q[1], v[2], v[3]);
+      mean[0] = (u[0] + u[1]) + (u[2] + u[3]), m2[0] = (v[0] + v[1]) + (v[2] + v[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < P; ++i) pair_split(s[i], mean[2 * i], mean[2 * i + 1]), pair_split(q[i], m2[2 * i], m2[2 * i + 1]);
+    }
+  }
+  // (mean, squares) of the thread's K columns; of a warp's, about the mean of its first pixel's thread; of a group, by one warp over the rows of red
+  {
+    const float n = active ? count_of(WIDE ? tid : ty) : 0.f, inv = n > 0.f ? 1.f / n : 0.f;
+    const float n_row = WIDE || by_warp ? count_of_row(warp) : n, inv_row = n_row > 0.f ? 1.f / n_row : 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const float s = mean[k];
+      float mu = shift[k] + s * inv, m = fmaxf(fmaf(-s * inv, s, m2[k]), 0.f);
+      if (WIDE || by_warp) {
+        const int stride = WIDE ? 1 : p.sv, others = WIDE ? 32 : warp_rows;
+        const float ref = __shfl_sync(0xffffffffu, mu, col0 & 31), d = n > 0.f ? mu - (WIDE ? __shfl_sync(0xffffffffu, mu, 0) : ref) : 0.f;
+        const float base = WIDE ? __shfl_sync(0xffffffffu, mu, 0) : ref;
+        float td = n * d, tq = fmaf(n * d, d, n > 0.f ? m : 0.f);
+        for (int left = others; left > 1;) {         // the pixels behind the half are added to those before it
+          const int half = (left + 1) >> 1;
+          const float od = __shfl_down_sync(0xffffffffu, td, half * stride), oq = __shfl_down_sync(0xffffffffu, tq, half * stride);
+          if ((WIDE ? lane : lane_row) + half < left) td += od, tq += oq;
+          left = half;
+        }
+        mu = fmaf(td, inv_row, base), m = fmaxf(fmaf(-td * inv_row, td, tq), 0.f);
+        if (n_row == 0.f) mu = m = 0.f;
+      } else if (n == 0.f) {
+        mu = m = 0.f;
+      }
+      if (WIDE ? lane == 0 : by_warp ? lane < p.sv : active) red[red_row * p.bins + (WIDE ? 0 : col0 * K + k)] = make_float2(mu, m);
+    }
+  }
+  __syncthreads();
+    bool lost = false;
+  if (cluster > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");    // every CTA's barrier is set up
+  for (int g = warp; g < p.groups; g += NW) {
+    auto over = [&](auto&& term) {       // the group's bins of every row, 32 at a time
       float s = 0.f;
-      for (int i = lane; i < n; i += 32) {
-        const int r = i / per_group;
-        s += red[r * bins + g * per_group + (i - r * per_group)];
+      const float2* at = red + r_first * p.bins + g * per_group + b_first;
+      for (int r = r_first, c = b_first; r < p.red_rows;) {
+        s += term(count_of_row(r), *at);
+        r += r_step, c += b_step, at += r_step * p.bins + b_step;
+        if (c >= per_group) c -= per_group, ++r, at += p.bins - per_group;
       }
 #pragma unroll
       for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-      if (lane == 0) done(g, s);
+      return s;
+    };
+    const float sum = over([&](float w, float2 v) { return w * v.x; });
+    const float mu = sum * inv_here;
+    const float squares = over([&](float w, float2 v) {
+      const float d = v.x - mu;
+      return fmaf(w * d, d, v.y);
+    });
+    if (cluster == 1) {
+      if (lane == 0) all[g] = make_float2(mu, rsqrtf(fmaf(squares, inv_here, p.eps)));
+    } else if (lane < (int)cluster) {
+      asm volatile(
+          "{\n .reg .b32 a, b;\n mapa.shared::cluster.u32 a, %0, %2;\n mapa.shared::cluster.u32 b, %1, %2;\n"
+          " st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [a], {%3, %4}, [b];\n}"
+          ::"r"((uint32_t)__cvta_generic_to_shared(stat + g * (int)cluster + (int)rank)), "r"(arrived), "r"(lane), "f"(mu), "f"(squares)
+          : "memory");
     }
-    __syncthreads();
-  };
-  const float n_here = (float)rows * (float)p.cpg;
-#pragma unroll
-  for (int k = 0; k < K; ++k) sum[k] = 0.f;
-  each([&](int row, int col) {
-    float f[V];
-    norm_unpack<T, V>(held(row, col), f);
-    if constexpr (MERGED) {
-      sum[0] += norm_tree<V>(f);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) sum[i] += f[i];
-    }
-  });
-  group_sums([&](int g, float s) { stat[2 * g] = rows > 0 ? s / n_here : 0.f; });
-  int group_of[K];     // the groups of this thread's columns; threads without a column take any
-  float mean[K];
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    group_of[k] = WIDE ? 0 : min((col0 * V + k) / p.cpg, p.groups - 1);
-    mean[k] = stat[2 * group_of[k]], sum[k] = 0.f;
   }
-  each([&](int row, int col) {
-    float f[V];
-    norm_unpack<T, V>(held(row, col), f);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float d = f[i] - mean[MERGED ? 0 : i];
-      if constexpr (MERGED) f[i] = d * d;
-      else sum[i] = fmaf(d, d, sum[i]);
-    }
-    if constexpr (MERGED) sum[0] += norm_tree<V>(f);
-  });
-  group_sums([&](int g, float s) { stat[2 * g + 1] = s; });
-  // the cluster's statistics
-  float* all = stat + 2 * p.groups;
+  // The cluster's statistics.
   if (cluster > 1) {
-    asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
-    const uint32_t stat_s = (uint32_t)__cvta_generic_to_shared(stat);
-    for (int g = tid; g < p.groups; g += kNormThreads) {
-      float m[kNormMaxCluster], q[kNormMaxCluster], s = 0.f;
+    for (int g0 = warp * 2; g0 < p.groups; g0 += NW * 2) {      // sixteen lanes a group
+      if (g0 == warp * 2 && !__all_sync(0xffffffffu, mbar_wait_cluster(arrived, 0, p.err_flag, kTcWaitCycles))) lost = true;
+      const int r = lane & 15, g = g0 + (lane >> 4);
+      const float w = r < (int)cluster ? (float)max(0, min(p.rows, p.hw - r * p.rows)) * (float)p.cpg : 0.f;
+      const float2 v = w > 0.f && g < p.groups ? stat[g * (int)cluster + r] : make_float2(0.f, 0.f);
+      float s = w * v.x;
 #pragma unroll
-      for (int r = 0; r < kNormMaxCluster; ++r)
-        if (r < (int)cluster) {
-          uint32_t from;
-          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(stat_s + 8u * g), "r"(r));
-          asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(m[r]), "=f"(q[r]) : "r"(from) : "memory");
-        }
-      const float n = (float)p.hw * (float)p.cpg;
+      for (int d = 8; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+      const float mu = s * inv_all;
+      s = w > 0.f ? fmaf(w * (v.x - mu), v.x - mu, v.y) : 0.f;
 #pragma unroll
-      for (int r = 0; r < kNormMaxCluster; ++r)
-        if (r < (int)cluster) s = fmaf((float)max(0, min(p.rows, p.hw - r * p.rows)) * (float)p.cpg, m[r], s);
-      const float mu = s / n;
-      s = 0.f;
-#pragma unroll
-      for (int r = 0; r < kNormMaxCluster; ++r)
-        if (r < (int)cluster) {
-          const float d = m[r] - mu;
-          s += fmaf((float)max(0, min(p.rows, p.hw - r * p.rows)) * (float)p.cpg, d * d, q[r]);
-        }
-      all[2 * g] = mu, all[2 * g + 1] = 1.f / sqrtf(s / n + p.eps);
+      for (int d = 8; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+      if (r == 0 && g < p.groups) all[g] = make_float2(mu, rsqrtf(fmaf(s, inv_all, p.eps)));
     }
-    asm volatile("barrier.cluster.arrive.release;" ::: "memory");   // this CTA reads no other one's memory any more
-    __syncthreads();
-  } else {
-    for (int g = tid; g < p.groups; g += kNormThreads) all[2 * g] = stat[2 * g], all[2 * g + 1] = 1.f / sqrtf(stat[2 * g + 1] / n_here + p.eps);
-    __syncthreads();
+  }
+  if (__syncthreads_or(lost)) {            // a wait that ran out: the status says so, and y stays as it is
+    cluster_drain(arrived, 0, p.err_flag);
+    return;
   }
   // y = (x - mean) * (gamma / deviation) + beta
   const T* res = p.residual ? reinterpret_cast<const T*>(p.residual) + first : nullptr;
   T* y = reinterpret_cast<T*>(p.y) + first;
+  // bf16: the mean goes into the offset, one operation less; that loses 2^-24 of it, far below the rounding of the result
+  constexpr bool kFolded = sizeof(T) == 2;
   float a[V], b[V];
   auto affine = [&](int col) {
-    const int c = slice * p.sv * V + col * V;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const float rstd = all[2 * group_of[MERGED ? 0 : i] + 1];
-      a[i] = p.gamma ? p.gamma[c + i] * rstd : rstd, b[i] = p.beta ? p.beta[c + i] : 0.f;
+      const int c = channel + col * V + i;
+      const float2 st = all[WIDE ? 0 : min((col * V + i) / p.cpg, p.groups - 1)];
+      a[i] = p.gamma ? p.gamma[c] * st.y : st.y, b[i] = p.beta ? p.beta[c] : 0.f;
+      if (i < K) mean[i] = st.x;
+      if (kFolded) b[i] = fmaf(-st.x, a[i], b[i]);
     }
   };
-#pragma unroll
-  for (int k = 0; k < K; ++k) mean[k] = all[2 * group_of[k]];
   if (!WIDE && active) affine(col0);
-  each([&](int row, int col) {
-    if (WIDE) affine(col);
-    const size_t at = (size_t)row * p.c + col * V;
-    Vec r;
-    if (res) r = *reinterpret_cast<const Vec*>(res + at);
-    float f[V], q[V];
-    norm_unpack<T, V>(held(row, col), f);
-    if (res) norm_unpack<T, V>(r, q);
+  const NormClamp clamp(p.act);
+  auto store = [&](auto act, auto with_residual) {
+    constexpr bool SILU = decltype(act)::value;
+    constexpr bool RES = decltype(with_residual)::value;
+    auto finish = [&](size_t at, const Vec& held_x, const Vec& r) {
+      float f[V], q[V];
+      norm_unpack<T, V>(held_x, f);
+      if (RES) norm_unpack<T, V>(r, q);
+      if constexpr (V == 1) {
+        float t = fmaf(kFolded ? f[0] : f[0] - mean[0], a[0], b[0]);
+        if (RES) t += q[0];
+        Elem<T>::st(y + at, norm_act<SILU>(t, clamp));
+      } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      float t = fmaf(f[i] - mean[MERGED ? 0 : i], a[i], b[i]);
-      if (res) t += q[i];
-      f[i] = norm_act(t, p.act);
-    }
-    if constexpr (V == 1) {
-      Elem<T>::st(y + at, f[0]);
-    } else {
-      Vec16<T> o;
+        for (int i = 0; i < P; ++i) {
+          f32x2 d = pair_of(f[2 * i], f[2 * i + 1]);
+          if (!kFolded) d = pair_add(d, pair_of(-mean[MERGED ? 0 : 2 * i], -mean[MERGED ? 0 : 2 * i + 1]));
+          f32x2 t = pair_fma(d, pair_of(a[2 * i], a[2 * i + 1]), pair_of(b[2 * i], b[2 * i + 1]));
+          if (RES) t = pair_add(t, pair_of(q[2 * i], q[2 * i + 1]));
+          pair_split(t, f[2 * i], f[2 * i + 1]);
+        }
+        Vec16<T> o;
 #pragma unroll
-      for (int i = 0; i < V; ++i) o.v[i] = f[i];
-      o.store(y + at);
+        for (int i = 0; i < V; ++i) o.v[i] = norm_act<SILU>(f[i], clamp);
+        o.store(y + at);
+      }
+    };
+    if constexpr (WIDE) {
+      each([&](int row, int col) {
+        affine(col);
+        const size_t at = (size_t)row * p.c + col * V;
+        Vec r;
+        if (RES) r = *reinterpret_cast<const Vec*>(res + at);
+        finish(at, held(row, col), r);
+      });
+    } else if (active) {
+      // Four pixels' loads before the first one's store: y may be the residual or x, so the compiler keeps loads behind stores.
+      constexpr int U = RES || !RESIDENT ? 4 : 1;
+      for (int row = ty; row < rows; row += U * ty_n) {
+        Vec h[U], r[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (row + u * ty_n < rows) {
+            if (!RESIDENT) h[u] = held(row + u * ty_n, col0);
+            if (RES) r[u] = *reinterpret_cast<const Vec*>(res + (size_t)(row + u * ty_n) * p.c + col0 * V);
+          }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (row + u * ty_n < rows) finish((size_t)(row + u * ty_n) * p.c + col0 * V, RESIDENT ? held(row + u * ty_n, col0) : h[u], r[u]);
+      }
     }
-  });
-  if (cluster > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");   // nobody reads this CTA's shared memory any more
+  };
+  if (p.act == EE_ACT_SILU) {
+    if (res) store(Flag<true>(), Flag<true>());
+    else store(Flag<true>(), Flag<false>());
+  } else {
+    if (res) store(Flag<false>(), Flag<true>());
+    else store(Flag<false>(), Flag<false>());
+  }
 }
 
-template <typename T, int V, bool MERGED, bool WIDE, bool RESIDENT>
-inline cudaError_t norm_launch_k(const NormPlan& pl, const NormArgs& a, long batch, cudaStream_t st) {
+template <typename T, int V, bool MERGED, bool WIDE, bool RESIDENT, int NT>
+inline cudaError_t norm_launch_k(const NormPlan& pl, const NormArgs& a, long units, cudaStream_t st) {
+  const auto kernel = group_norm_kernel<T, V, MERGED, WIDE, RESIDENT, NT>;
   cudaError_t e = cudaSuccess;
-  if (pl.smem > 48 << 10) e = cudaFuncSetAttribute(group_norm_kernel<T, V, MERGED, WIDE, RESIDENT>, cudaFuncAttributeMaxDynamicSharedMemorySize, pl.smem);
+  if (pl.smem() > 48 << 10) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, pl.smem());
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(batch * pl.slices * pl.cluster));
-  cfg.blockDim = dim3(kNormThreads);
-  cfg.dynamicSmemBytes = pl.smem;
+  cfg.gridDim = dim3((unsigned)(units * pl.cluster));
+  cfg.blockDim = dim3(NT);
+  cfg.dynamicSmemBytes = pl.smem();
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -323,15 +476,20 @@ inline cudaError_t norm_launch_k(const NormPlan& pl, const NormArgs& a, long bat
   attr[1].val.clusterDim.x = pl.cluster, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = pl.cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, group_norm_kernel<T, V, MERGED, WIDE, RESIDENT>, a);
+  return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
-template <typename T, int V>
-inline cudaError_t norm_launch_v(const NormPlan& pl, const NormArgs& a, long batch, cudaStream_t st) {
-  if (pl.wide) return pl.resident ? norm_launch_k<T, V, true, true, true>(pl, a, batch, st) : norm_launch_k<T, V, true, true, false>(pl, a, batch, st);
-  if (pl.merged) return pl.resident ? norm_launch_k<T, V, true, false, true>(pl, a, batch, st) : norm_launch_k<T, V, true, false, false>(pl, a, batch, st);
-  if constexpr (V > 1)
-    return pl.resident ? norm_launch_k<T, V, false, false, true>(pl, a, batch, st) : norm_launch_k<T, V, false, false, false>(pl, a, batch, st);
+template <typename T, int V, int NT>
+inline cudaError_t norm_launch_v(const NormPlan& pl, const NormArgs& a, long units, cudaStream_t st) {
+  if constexpr (NT == kNormThreads)
+    if (pl.wide) return pl.resident ? norm_launch_k<T, V, true, true, true, NT>(pl, a, units, st) : norm_launch_k<T, V, true, true, false, NT>(pl, a, units, st);
+  if constexpr (NT == kNormThreads)
+    if (!pl.resident) {
+      if (pl.merged) return norm_launch_k<T, V, true, false, false, NT>(pl, a, units, st);
+      if constexpr (V > 1) return norm_launch_k<T, V, false, false, false, NT>(pl, a, units, st);
+    }
+  if (pl.merged) return norm_launch_k<T, V, true, false, true, NT>(pl, a, units, st);
+  if constexpr (V > 1) return norm_launch_k<T, V, false, false, true, NT>(pl, a, units, st);
   return cudaErrorInvalidValue;
 }
 
@@ -340,12 +498,16 @@ inline bool norm_fits(const NormPlan& pl, long batch) { return batch * pl.slices
 
 template <typename T>
 inline cudaError_t norm_launch(const void* x, const void* residual, void* y, const float* gamma, const float* beta, float eps, long batch, int hw, int c,
-                               int groups, int act, bool rev, cudaStream_t st) {
+                               int groups, int act, bool rev, int* err_flag, cudaStream_t st) {
   const bool aligned = (((uintptr_t)x | (uintptr_t)residual | (uintptr_t)y) & 15) == 0;
   const NormPlan pl = norm_plan(hw, c, groups, (int)sizeof(T), aligned);
   if (!norm_fits(pl, batch)) return cudaErrorInvalidValue;
-  const NormArgs a = {x, residual, y, gamma, beta, eps, hw, c, c / groups, act, pl.sv, pl.slices, pl.groups, pl.rows, pl.off_red, pl.off_stat, rev ? 1 : 0};
-  return pl.v > 1 ? norm_launch_v<T, Elem<T>::kVec>(pl, a, batch, st) : norm_launch_v<T, 1>(pl, a, batch, st);
+  const NormArgs a = {x, residual, y, gamma, beta, eps, hw, c, c / groups, act, pl.sv, pl.slices, pl.groups, pl.rows, pl.chunk, pl.red_rows, pl.bins,
+                      err_flag, rev ? 1 : 0};
+  const long units = batch * pl.slices;
+  constexpr int V = Elem<T>::kVec;
+  if (pl.threads == kNormThreads) return pl.v > 1 ? norm_launch_v<T, V, kNormThreads>(pl, a, units, st) : norm_launch_v<T, 1, kNormThreads>(pl, a, units, st);
+  return pl.v > 1 ? norm_launch_v<T, V, kNormFew>(pl, a, units, st) : norm_launch_v<T, 1, kNormFew>(pl, a, units, st);
 }
 
 }  // namespace ee
