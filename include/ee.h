@@ -414,7 +414,7 @@ size_t ee_adapted_linear_workspace_bytes(int rows, int rank);
 /* Probabilities of rows of logits: probs[v] = exp((logits[v] - max) / t) / sum, t = temperature[row] (NULL = 1).  logits: [rows][n]
  * of dtype, probs: [rows][n] fp32.  A logit of -inf is masked: its probability is 0; a row with nothing else is all 0.
  * A temperature that is not above 0 puts 1 on the largest logit (the lowest index on ties).  A row that holds NaN or +inf is NaN
- * throughout.  probs may be logits (fp32); other overlaps are refused.  n up to 409600 (fp32) or 819200 (bf16).
+ * throughout.  probs may be logits (fp32); other overlaps are refused.  n up to 614400.
  * Errors: INVALID_ARG, CAPACITY (n or the grid too large), CUDA. */
 ee_status_t ee_softmax(int dtype, const void* logits, int rows, int n, const float* temperature, float* probs, void* cuda_stream);
 

@@ -1920,10 +1920,13 @@ ee_status_t ee_softmax(int dtype, const void* logits, int rows, int n, const flo
   const size_t es = esize(dtype);
   if (!logits || !probs || !aligned_to(logits, es) || !aligned_to(probs, 4) || !aligned_to(temperature, 4)) return EE_ERR_INVALID_ARG;
   if (!(dtype == EE_F32 && logits == (const void*)probs) && !apart(logits, (size_t)rows * n * es, probs, (size_t)rows * n * 4)) return EE_ERR_INVALID_ARG;
-  if (n > (dtype == EE_BF16 ? softmax_most<bf16>() : softmax_most<float>()) || (long)rows * kSmMaxCluster > 0x7fffffffL) return EE_ERR_CAPACITY;
+  if (n > kSmMost || (long)rows * kSmMaxCluster > 0x7fffffffL) return EE_ERR_CAPACITY;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  EE_CUDA(dtype == EE_BF16 ? softmax_launch<bf16>((const bf16*)logits, temperature, probs, rows, n, st)
-                           : softmax_launch<float>((const float*)logits, temperature, probs, rows, n, st));
+  const OperatorContext* ctx;
+  const ee_status_t s = operator_context(&ctx);
+  if (s != EE_OK) return s;
+  EE_CUDA(dtype == EE_BF16 ? softmax_launch<bf16>((const bf16*)logits, temperature, probs, rows, n, ctx->flag, st)
+                           : softmax_launch<float>((const float*)logits, temperature, probs, rows, n, ctx->flag, st));
   return EE_OK;
 }
 
@@ -1936,7 +1939,10 @@ ee_status_t ee_verify_drafts(const float* p, const float* q, const int32_t* draf
       !aligned_to(tokens, 4) || !aligned_to(n_accepted, 4))
     return EE_ERR_INVALID_ARG;
   if ((long)batch * kVfMaxCluster > 0x7fffffffL || k > 0x7fffffff - 64) return EE_ERR_CAPACITY;
-  EE_CUDA(verify_launch({p, q, drafts, u, r, n_draft, tokens, n_accepted, k, n, 0}, batch, (cudaStream_t)cuda_stream));
+  const OperatorContext* ctx;
+  const ee_status_t s = operator_context(&ctx);
+  if (s != EE_OK) return s;
+  EE_CUDA(verify_launch({p, q, drafts, u, r, n_draft, tokens, n_accepted, k, n, 0, 0, ctx->flag}, batch, (cudaStream_t)cuda_stream));
   return EE_OK;
 }
 

@@ -296,21 +296,21 @@ def softmax_exact(x, heat):
 
 
 def softmax_check(y, x, heat):
-    """The exponent (l - max) / t is off by 2 u of itself (difference, reciprocal, product: 3 u), the exponential by 2 units of 2 u; the sum's chain is n / 512 and its tree 16 long,
-    the quotient and its product 2 u.  What underflows is off by the smallest normal number."""
+    """The exponent (l - max) / t is off by 4 u of itself (difference, constant, quotient, product), the power by 2 units of 2 u, twice where a row is cut; the sum's chain is n / 512 and
+    its tree 16 long, the quotient and its product 2 u.  What underflows is off by the smallest normal number."""
     ref = softmax_exact(x, heat)
     n = x.shape[1]
     fin = ref.isfinite()
     assert torch.equal(fin, y.isfinite())
     d = torch.log(ref.clamp(min=1e-300)).abs()           # |l - max| / t + log(sum) >= |l - max| / t
-    tol = ref * U * (3 * d + 12 + n / 512 + 32) + 2.0 ** -126
+    tol = ref * U * (5 * d + 20 + n / 512 + 32) + 2.0 ** -126
     err = torch.where(fin, (y.double() - ref).abs(), torch.zeros_like(ref))
     assert bool((err <= tol)[fin].all()), f"off by {float((err / tol)[fin].max()):.3g} tolerances"
     assert bool((y[ref == 0] == 0).all())
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows,n", [(1, 1), (5, 2), (3, 31), (9, 128), (7, 129), (64, 1000), (3, 1024), (3, 1025), (4, 4099), (2, 16385), (3, 32769), (2, 50001), (3, 128001), (1, 262145), (1, 409600)])
+@pytest.mark.parametrize("rows,n", [(1, 1), (5, 2), (3, 31), (9, 128), (7, 129), (64, 1000), (3, 1024), (3, 1025), (4, 4099), (2, 16385), (3, 32769), (2, 50001), (3, 128001), (1, 262145), (2, 409600), (1, 614399)])
 def test_softmax(rows, n, dtype):
     g = gen(n)
     x = (3 * normal(g, rows, n)).to(TD[dtype])
@@ -438,7 +438,7 @@ def drafts_of(seed, b, k, n, spread=0.7):
 
 
 @pytest.mark.parametrize("dense", [True, False])
-@pytest.mark.parametrize("b,k,n", [(1, 1, 1), (3, 2, 2), (1, 0, 1000), (1, 1, 1000), (70, 4, 33), (5, 40, 100), (9, 3, 8192), (9, 3, 8193), (4, 2, 20001), (3, 5, 65537), (4, 5, 128001)])
+@pytest.mark.parametrize("b,k,n", [(1, 1, 1), (3, 2, 2), (1, 0, 1000), (1, 1, 1000), (70, 4, 33), (5, 40, 100), (9, 3, 8192), (9, 3, 8193), (4, 2, 20001), (3, 5, 65537), (4, 5, 128001), (1, 1, 2300001)])
 def test_verify_drafts(b, k, n, dense):
     p, q, d, u, r = drafts_of(b + k + n, b, k, n)
     verify_case(p, q if dense else None, d, u, r)

@@ -68,8 +68,8 @@ def test_softmax_refuses(changed):
 
 def test_softmax_of_nothing_and_of_too_much():
     assert call("ee_softmax", SOFTMAX, rows=0, logits=None, probs=None) == 0
-    assert call("ee_softmax", SOFTMAX, n=409601) == CAPACITY
-    assert call("ee_softmax", SOFTMAX, dtype=BF16, n=819201) == CAPACITY
+    assert call("ee_softmax", SOFTMAX, n=614401) == CAPACITY
+    assert call("ee_softmax", SOFTMAX, rows=2 ** 28, n=9, logits=1 << 50, probs=1 << 60) == CAPACITY
 
 
 VERIFY = dict(p=P[0], q=P[1], drafts=P[2], u=P[3], r=P[4], n_draft=P[5], batch=2, k=3, n=10, tokens=P[6], n_accepted=P[7], stream=None)
