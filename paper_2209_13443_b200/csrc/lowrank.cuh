@@ -7,12 +7,14 @@
 // their rank in additional K, and the sum is rounded once.  h is kept and multiplied as two bf16 parts, h and what its rounding left (2^-17
 // of h together, 2 rank columns): rounded to one part the adapter's share would carry a second rounding of the size of the result's.
 //
-// The tile is turned: 128 filters are the rows of the accumulator (lanes) and 16 to 256 rows of the batch its columns, so that few
+// The tile is turned: 128 filters are the rows of the accumulator (lanes) and 16 to 128 rows of the batch its columns, so that few
 // rows cost few columns, and W, which bounds small batches, is read once.  There K is cut over a cluster of up to eight CTAs, which
-// add their parts through distributed shared memory in fixed order.  The first launch is a product of the same shape, 128 rows of
+// send each other their parts as asynchronous stores and add them in fixed order.  The first launch is a product of the same shape, 128 rows of
 // stacked A_a over 64 rows of the batch; up to kLrSimtRows rows CUDA cores do it, a warp a row of A_a.
-// The second launch starts while the first runs and waits for it only before it fills in h.  The adapters' columns have
-// buffers of their own, beside the ring of the main loop: they are filled while that runs.
+// The second launch starts while the first runs and waits for it only before it fills in h.  The adapters' columns take ring slots behind the last channel's: the
+// producer of W, which walks the ring anyway, hands them to the four warps that gather the columns, while the products before them still run.  Grids of more than one
+// tile an SM use a ring of three slots, so that two CTAs share an SM and one's columns and stores lie under the other's products; smaller ones a
+// deep ring, for the bytes in flight.
 //
 // Channels that are not whole 16-byte vectors, or operands off a 16-byte boundary, cannot be fetched by TMA: eight warps then copy the
 // tiles (COPY), 2 or 4 bytes at a time.
@@ -45,19 +47,18 @@ struct LrArgs {
   int* err_flag;
 };
 
-template <int TN, bool SHRINK>
+template <int TN, bool DEEP>
 struct LrSmem {
   static constexpr int kABytes = 128 * 128, kBBytes = TN * 128, kStage = kABytes + kBBytes;
-  static constexpr int kStages = TN == 256 ? 3 : 4, kExt = SHRINK ? 0 : TN == 256 || TN == 128 ? 1 : 2;   // slots of the ring, of adapter columns
-  static constexpr int kOffExt = kStages * kStage;
-  // partial sums, over the drained ring: SHRINK, this CTA's h of its rows (up to 128 numbers each); else what the cluster's CTAs send
-  static constexpr int kPart = TN * 128 * 4;
-  static constexpr int kOffInts = kOffExt + kExt * kStage;
-  static constexpr int kInts = 3 * TN + 64 * (kExt + 1) + 16;       // adapter and slot of each row, adapters of the tile, column tables, masks and count
+  static constexpr int kStages = !DEEP ? 3 : TN == 128 ? 4 : 7;
+  static constexpr int kPart = TN * 128 * 4;                        // partial sums: a shrink's h of its rows (up to 128 numbers each); else what the cluster's CTAs send
+  static constexpr int kOffPart = kStages * kStage;
+  static constexpr int kOffInts = kOffPart + (DEEP ? kPart : 0);    // grids of a shallow ring do not cut K
+  static constexpr int kInts = 3 * TN + 16;                         // adapter and slot of each row, adapters of the tile, masks and counts
   static constexpr int kOffBars = kOffInts + kInts * 4;
-  static constexpr int kBytes = kOffBars + 8 * (2 * kStages + 2 * kExt + 2) + 1024;
-  static_assert(kPart <= kStages * kStage, "partial sums lie over the ring");
+  static constexpr int kBytes = kOffBars + 8 * (3 * kStages + 3) + 1024;
   static_assert(kBytes <= 227 * 1024, "exceeds the shared memory of an SM");
+  static_assert(DEEP || 2 * (kBytes + 1024) <= 228 * 1024, "two CTAs of a shallow ring share an SM");
 };
 
 __device__ __forceinline__ void mbar_arrive_n(uint32_t bar, uint32_t n) {
@@ -93,11 +94,12 @@ __device__ __noinline__ float lr_not_finite(const LrArgs& p, int t, int f, int a
 
 // tmA: rows of operand A (W in boxes of 128 filters; SHRINK: all adapters' A in boxes of r8 rows), tmX: rows of x in boxes of TN.
 // blockIdx.x: tile of filters (SHRINK: of stacked adapters), y: tile of rows, z: range of K.
-template <int TN, bool SHRINK, bool COPY>
+template <int TN, bool DEEP, bool SHRINK, bool COPY>
 __global__ void __launch_bounds__(COPY ? 192 + 32 * kLrCopyWarps : 224)
 lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmX, LrArgs p) {
-  using S = LrSmem<TN, SHRINK>;
-  constexpr int kStages = S::kStages, kExt = S::kExt;
+  static_assert(DEEP || !SHRINK, "a shrink keeps its partial sums beside the ring");
+  using S = LrSmem<TN, DEEP>;
+  constexpr int kStages = S::kStages;
   constexpr uint32_t kFull = COPY ? 32 * kLrCopyWarps : 2;   // arrivals that fill a slot
   extern __shared__ uint8_t lr_smem[];
   const uint32_t raw = smem_u32(lr_smem), base = (raw + 1023u) & ~1023u;
@@ -105,17 +107,15 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
   int* s_ad = reinterpret_cast<int*>(gen + S::kOffInts);     // [TN] adapter of a row, -1: none
   int* s_slot = s_ad + TN;                                   // [TN] its place among the tile's adapters
   int* s_list = s_slot + TN;                                 // [TN] the tile's adapters, in order of first occurrence
-  int* s_col = s_list + TN;                                  // [kExt][64] columns of the adapter slots
-  unsigned* s_mask = reinterpret_cast<unsigned*>(s_col + 64 * (kExt + 1));   // [8]
+  unsigned* s_mask = reinterpret_cast<unsigned*>(s_list + TN);   // [4]
   int* s_count = reinterpret_cast<int*>(s_mask) + 8;
   uint32_t* tmem_slot = s_mask + 9;
   int* s_bad = s_count + 2;                                  // set where a B_a of the tile holds infinities or NaN
   const uint32_t bar0 = base + S::kOffBars;
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (kStages + s); };
-  const uint32_t accum_bar = bar0 + 8u * (2 * kStages), list_bar = accum_bar + 8u;
-  auto ext_full = [&](int s) { return list_bar + 8u + 8u * s; };
-  auto ext_empty = [&](int s) { return list_bar + 8u + 8u * (kExt + s); };
+  auto grant_bar = [&](int s) { return bar0 + 8u * (2 * kStages + s); };     // the slot is free for adapter columns
+  const uint32_t accum_bar = bar0 + 8u * (3 * kStages), list_bar = accum_bar + 8u, part_bar = list_bar + 8u;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int t0 = (int)blockIdx.y * TN, n0 = (int)blockIdx.x * 128;
   const int z = (int)blockIdx.z, Z = (int)gridDim.z;
@@ -123,11 +123,12 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
   const int kb0 = (int)((long)kb_all * z / Z), num_kb = (int)((long)kb_all * (z + 1) / Z) - kb0;   // Z <= kb_all: never empty
 
   if (tid == 0) {
-    for (int s = 0; s < kStages; ++s) mbar_init(full_bar(s), kFull), mbar_init(empty_bar(s), 1);
+    for (int s = 0; s < kStages; ++s) mbar_init(full_bar(s), kFull), mbar_init(empty_bar(s), 1), mbar_init(grant_bar(s), 1);
     mbar_init(accum_bar, 1);
     mbar_init(list_bar, 1);
-    for (int s = 0; s < kExt; ++s) mbar_init(ext_full(s), 1), mbar_init(ext_empty(s), 1);
+    mbar_init(part_bar, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (!SHRINK && Z > 1) mbar_expect_tx(part_bar, (uint32_t)S::kPart);     // TN / Z columns from each of Z CTAs
   }
   constexpr uint32_t kCols = TN < 32 ? 32 : TN;
   if (warp == 1) {
@@ -139,6 +140,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   if (SHRINK) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (Z > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");       // waited for before anything is sent
 
   // The tile's adapters: a row is the first of its adapter, or refers to it.
   if (warp >= 2 && warp < 6) {
@@ -148,39 +150,31 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
       s_ad[i] = a >= 0 && a < p.adapters ? a : -1;
     }
     asm volatile("bar.sync 1, 128;" ::: "memory");
-    int first[TN > 128 ? 2 : 1];
-#pragma unroll
-    for (int h = 0; h < (TN > 128 ? 2 : 1); ++h) {
-      const int i = et + 128 * h;
-      const int a = i < TN ? s_ad[i] : -1;
-      int f = i;
-      if (a >= 0)
-        for (int u = 0; u < i; u += 4) {   // matches behind i are no smaller than f
-          const int4 o = *reinterpret_cast<const int4*>(s_ad + u);
-          if (o.w == a) f = min(f, u + 3);
-          if (o.z == a) f = min(f, u + 2);
-          if (o.y == a) f = min(f, u + 1);
-          if (o.x == a) f = min(f, u);
-        }
-      first[h] = a >= 0 ? f : -1;
-      const unsigned m = __ballot_sync(0xffffffffu, a >= 0 && f == i);
-      if (lane == 0 && i < TN) s_mask[i >> 5] = m;
-    }
+    const int a = et < TN ? s_ad[et] : -1;
+    int f = (et & ~31) + __ffs(__match_any_sync(0xffffffffu, a)) - 1;       // the first of its warp
+    if (a >= 0 && f == et)
+      for (int u = 0; u < (et & ~31); u += 4) {
+        const int4 o = *reinterpret_cast<const int4*>(s_ad + u);
+        if (o.w == a) f = min(f, u + 3);
+        if (o.z == a) f = min(f, u + 2);
+        if (o.y == a) f = min(f, u + 1);
+        if (o.x == a) f = min(f, u);
+      }
+    f = __shfl_sync(0xffffffffu, f, f >= (et & ~31) ? f & 31 : lane);       // the others of the warp take what their first found
+    const unsigned lead = __ballot_sync(0xffffffffu, a >= 0 && f == et);
+    if (lane == 0 && et < TN) s_mask[et >> 5] = lead;
     asm volatile("bar.sync 1, 128;" ::: "memory");
     int count = 0;
 #pragma unroll
     for (int k = 0; k < (TN + 31) / 32; ++k) count += __popc(s_mask[k]);
-#pragma unroll
-    for (int h = 0; h < (TN > 128 ? 2 : 1); ++h) {
-      const int i = et + 128 * h, f = first[h];
-      if (i >= TN) continue;
+    if (et < TN) {
       int slot = -1;
-      if (f >= 0) {
+      if (a >= 0) {
         slot = __popc(s_mask[f >> 5] & ((1u << (f & 31)) - 1u));
         for (int k = 0; k < f >> 5; ++k) slot += __popc(s_mask[k]);
-        if (f == i) s_list[slot] = s_ad[i];
+        if (f == et) s_list[slot] = a;
       }
-      s_slot[i] = slot;
+      s_slot[et] = slot;
     }
     if (et == 0) *s_count = count, *s_bad = 0;
     asm volatile("bar.sync 1, 128;" ::: "memory");
@@ -202,11 +196,12 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
 
   if (idle) {
   } else if (warp == 0) {
-    if (!COPY && elect_one()) {
+    if (elect_one()) {
       int s = 0;
       uint32_t ph = 1;
-      for (int i = 0; i < num_kb; ++i) {
-        if (i >= kStages && !mbar_wait(empty_bar(s), ph, p.err_flag)) break;
+      bool ok = true;
+      for (int i = 0; !COPY && i < num_kb; ++i) {
+        if (i >= kStages && !(ok = mbar_wait(empty_bar(s), ph, p.err_flag))) break;
         const uint32_t dst = base + (uint32_t)s * S::kStage;
         if (SHRINK) {
           mbar_expect_tx(full_bar(s), (uint32_t)(here * p.r8 * 128));
@@ -217,6 +212,14 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
           tma_load_2d(dst, &tmA, full_bar(s), (kb0 + i) * 64, n0);
         }
         if (++s == kStages) s = 0, ph ^= 1u;
+      }
+      if (!SHRINK && !COPY && ok && mbar_wait(list_bar, 0, p.err_flag)) {     // COPY: the first of its warps does this
+        const int ext = ext_blocks(*s_count);
+        for (int i = num_kb; i < num_kb + ext; ++i) {
+          if (i >= kStages && !mbar_wait(empty_bar(s), ph, p.err_flag)) break;
+          mbar_arrive_n(grant_bar(s), 1);
+          if (++s == kStages) s = 0, ph ^= 1u;
+        }
       }
     }
     __syncwarp();
@@ -267,14 +270,29 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
       mbar_arrive_n(full_bar(s), 1);
       if (++s == kStages) s = 0, ph ^= 1u;
     }
+    if (!SHRINK && cw == 0 && elect_one() && mbar_wait(list_bar, 0, p.err_flag)) {
+      const int ext = ext_blocks(*s_count);
+      for (int i = num_kb; i < num_kb + ext; ++i) {
+        if (i >= kStages && !mbar_wait(empty_bar(s), ph, p.err_flag)) break;
+        mbar_arrive_n(grant_bar(s), 1);
+        if (++s == kStages) s = 0, ph ^= 1u;
+      }
+    }
+    __syncwarp();
   } else if (warp == 1) {
     if (elect_one()) {
       constexpr uint32_t idesc = umma_idesc(TN);
       const uint64_t da0 = umma_desc(base), db0 = umma_desc(base + S::kABytes);
-      int s = 0;
+      int s = 0, blocks = num_kb;
       uint32_t ph = 0;
       bool ok = true;
-      for (int i = 0; i < num_kb && ok; ++i) {
+      for (int i = 0;; ++i) {
+        if (!SHRINK && i == num_kb) {                  // by now the list is long there
+          ok = mbar_wait(list_bar, 0, p.err_flag);
+          if (!ok) break;
+          blocks += ext_blocks(*s_count);
+        }
+        if (i >= blocks) break;
         ok = mbar_wait(full_bar(s), ph, p.err_flag);
         if (!ok) break;
         tc_fence_after();
@@ -282,19 +300,6 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
         umma_block(tmem, da0 + off, db0 + off, idesc, i != 0);
         umma_commit(empty_bar(s));
         if (++s == kStages) s = 0, ph ^= 1u;
-      }
-      if constexpr (!SHRINK) {
-        ok = ok && mbar_wait(list_bar, 0, p.err_flag);
-        const int ext = ok ? ext_blocks(*s_count) : 0;
-        for (int e = 0; e < ext; ++e) {
-          const int x = e % kExt;
-          ok = mbar_wait(ext_full(x), (uint32_t)(e / kExt) & 1u, p.err_flag);
-          if (!ok) break;
-          tc_fence_after();
-          const uint64_t off = (uint64_t)((S::kOffExt + x * S::kStage) >> 4);
-          umma_block(tmem, da0 + off, db0 + off, idesc, true);
-          umma_commit(ext_empty(x));
-        }
       }
       if (ok) umma_commit(accum_bar);
     }
@@ -304,68 +309,103 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     const int row = q * 32 + lane;                     // accumulator lane of this thread
     bool ok = true;
     if constexpr (!SHRINK) {
-      const int ext = ext_blocks(*s_count), all = *s_count * ext_cols;
-      const bool vec = p.rank % 8 == 0 && ((uintptr_t)p.b & 15) == 0;   // eight columns are one part of one adapter, and one load
-      const int f = n0 + et;
-      auto columns = [&](int e) {    // table of block e, then B_a of filter n0 + et
-        const int x = e % kExt, c0 = (z + e * Z) * 64;
-        int* col = s_col + 64 * x;
-        if (et < 64) {
-          const int c = c0 + et, slot = c / ext_cols, rem = c - slot * ext_cols;
-          col[et] = c < all ? slot << 8 | rem : -1;      // rem < 2 * 128
-        }
-        if (e >= kExt && ok) ok = mbar_wait(ext_empty(x), (uint32_t)(e / kExt - 1) & 1u, p.err_flag);
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        uint8_t* dst = gen + S::kOffExt + x * S::kStage + et * 128;
-#pragma unroll 4
-        for (int c8 = 0; c8 < 8; ++c8) {
-          uint4 o = make_uint4(0u, 0u, 0u, 0u);
-          if (vec) {
-            const int ck = col[c8 * 8], j = (ck & 255) < p.rank ? ck & 255 : (ck & 255) - p.rank;
-            if (ck >= 0 && f < p.n) o = *reinterpret_cast<const uint4*>(p.b + ((size_t)s_list[ck >> 8] * p.n + f) * p.rank + j);
-          } else {
+      // Block e of adapter columns goes into the ring as K block num_kb + e.  A thread has the 16-byte chunk et % 8 of 64 columns, in every sixteenth row of either operand.
+      const int ext = ext_blocks(*s_count), all = *s_count * ext_cols, c8 = et & 7, r0 = et >> 3;
+      const bool whole = p.rank % 8 == 0, vec = whole && ((uintptr_t)p.b & 15) == 0;   // eight columns are one part of one adapter; of B_a one load
+      auto place = [&](int r) { return (uint32_t)(r * 128 + ((c8 ^ (r & 7)) << 4)); };
+      auto column = [&](int e, int k, int& slot, int& rem) {       // adapter and place in its 2 * rank columns; slot -1: behind the last
+        const int c = (z + e * Z) * 64 + c8 * 8 + k;
+        slot = c / ext_cols, rem = c - slot * ext_cols;
+        if (c >= all) slot = -1;
+      };
+      auto fetch = [&](uint32_t dst, const void* src, bool in) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+      };
+      auto slot_of_block = [&](int e) { return (num_kb + e) % kStages; };
+      auto fill_b = [&](int e) {
+        const int s = slot_of_block(e);
+        // use u of this slot: the u-th grant of it follows those of the blocks of adapter columns before this one
+        ok = ok && mbar_wait(grant_bar(s), (uint32_t)(e / kStages) & 1u, p.err_flag);
+        uint8_t* tile = gen + (size_t)s * S::kStage;
+        int slot, rem;
+        if (vec) {
+          column(e, 0, slot, rem);
+          const bf16* src = slot >= 0 ? p.b + ((size_t)s_list[slot] * p.n + n0) * p.rank + (rem < p.rank ? rem : rem - p.rank) : p.b;
+#pragma unroll
+          for (int m = 0; m < 8; ++m) {
+            const int r = r0 + 16 * m;
+            const bool in = slot >= 0 && n0 + r < p.n;
+            fetch(base + (uint32_t)s * S::kStage + place(r), in ? src + (size_t)r * p.rank : p.b, in);
+          }
+        } else {
+          int ad[8], j[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            column(e, k, slot, rem);
+            ad[k] = slot >= 0 ? s_list[slot] : -1, j[k] = rem < p.rank ? rem : rem - p.rank;
+          }
+#pragma unroll 2
+          for (int m = 0; m < 8; ++m) {
+            const int r = r0 + 16 * m, f = n0 + r;
             uint32_t v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const int ck = col[c8 * 8 + k], j = (ck & 255) < p.rank ? ck & 255 : (ck & 255) - p.rank;
-              v[k] = ck >= 0 && f < p.n ? reinterpret_cast<const unsigned short*>(p.b)[((size_t)s_list[ck >> 8] * p.n + f) * p.rank + j] : 0u;
-            }
-            o = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+            for (int k = 0; k < 8; ++k) v[k] = ad[k] >= 0 && f < p.n ? reinterpret_cast<const unsigned short*>(p.b)[((size_t)ad[k] * p.n + f) * p.rank + j[k]] : 0u;
+            *reinterpret_cast<uint4*>(tile + place(r)) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
           }
-          // an infinity would turn the zeros of other adapters' rows into NaN: lr_not_finite adds it to its own rows
-          if (lr_drop(o.x) | lr_drop(o.y) | lr_drop(o.z) | lr_drop(o.w)) *s_bad = 1;
-          *reinterpret_cast<uint4*>(dst + ((c8 ^ (et & 7)) << 4)) = o;
         }
       };
-      for (int e = 0; e < ext && e < kExt; ++e) columns(e);      // no kernel writes B_a: before the wait for h
-      asm volatile("griddepcontrol.wait;" ::: "memory");
-      for (int e = 0; e < ext; ++e) {
-        const int x = e % kExt;
-        if (e >= kExt) columns(e);
-        const int* col = s_col + 64 * x;
-        uint8_t* dst = gen + S::kOffExt + x * S::kStage + S::kABytes;
+      auto fill_h = [&](int e) {
+        const int s = slot_of_block(e);
+        const uint32_t at = base + (uint32_t)s * S::kStage + S::kABytes;
+        int slot, rem;
+        if (whole) {                       // the workspace is aligned, and so are eight columns of a row
+          column(e, 0, slot, rem);
+#pragma unroll
+          for (int m = 0; m < TN / 16; ++m) {
+            const int t = r0 + 16 * m;
+            const bool in = slot >= 0 && s_slot[t] == slot;
+            fetch(at + place(t), in ? p.h + (size_t)(t0 + t) * ext_cols + rem : p.h, in);
+          }
+        } else {
+          int slots[8], rems[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) column(e, k, slots[k], rems[k]);
 #pragma unroll 2
-        for (int i = et; i < TN * 8; i += 128) {
-          const int t = i >> 3, c8 = i & 7, mine = s_slot[t];
-          const unsigned short* h = reinterpret_cast<const unsigned short*>(p.h) + (size_t)(t0 + t) * ext_cols;
-          uint4 o = make_uint4(0u, 0u, 0u, 0u);
-          if (p.rank % 8 == 0) {       // the workspace is aligned, and so are eight columns of a row
-            const int ck = col[c8 * 8];
-            if (ck >= 0 && ck >> 8 == mine) o = *reinterpret_cast<const uint4*>(h + (ck & 255));
-          } else {
+          for (int m = 0; m < TN / 16; ++m) {
+            const int t = r0 + 16 * m, mine = s_slot[t];
+            const unsigned short* h = reinterpret_cast<const unsigned short*>(p.h) + (size_t)(t0 + t) * ext_cols;
             uint32_t v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const int ck = col[c8 * 8 + k];
-              v[k] = ck >= 0 && ck >> 8 == mine ? h[ck & 255] : 0u;
-            }
-            o = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+            for (int k = 0; k < 8; ++k) v[k] = mine >= 0 && slots[k] == mine ? h[rems[k]] : 0u;
+            *reinterpret_cast<uint4*>(gen + (size_t)s * S::kStage + S::kABytes + place(t)) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
           }
-          *reinterpret_cast<uint4*>(dst + t * 128 + ((c8 ^ (t & 7)) << 4)) = o;
+        }
+        cp_async_commit();
+      };
+      auto finish = [&](int e) {           // what this thread fetched is here: an infinity would turn the zeros of other adapters' rows into NaN, so
+        const int s = slot_of_block(e);    // lr_not_finite adds it to its own rows
+        uint8_t* tile = gen + (size_t)s * S::kStage;
+#pragma unroll
+        for (int m = 0; m < 8; ++m) {
+          uint4* o = reinterpret_cast<uint4*>(tile + place(r0 + 16 * m));
+          uint4 v = *o;
+          if (lr_drop(v.x) | lr_drop(v.y) | lr_drop(v.z) | lr_drop(v.w)) *s_bad = 1, *o = v;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (et == 0) mbar_arrive_n(ext_full(x), 1);
+        if (et == 0) mbar_arrive_n(full_bar(s), kFull);
+      };
+      // B_a of the first blocks before the wait for h (no kernel writes it); then one block is fetched while the one before it is finished
+      constexpr int kAhead = 2;
+      for (int e = 0; e < ext && e < kAhead; ++e) fill_b(e);
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      if (ext > 0) fill_h(0);
+      if (ext > 1) fill_h(1);
+      for (int e = 0; e < ext; ++e) {
+        if (e + 1 < ext) cp_async_wait<1>();
+        else cp_async_wait<0>();
+        finish(e);
+        if (e + kAhead < ext) fill_b(e + kAhead), fill_h(e + kAhead);
       }
     }
     ok = __all_sync(0xffffffffu, mbar_wait(accum_bar, 0, p.err_flag));
@@ -375,7 +415,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     if constexpr (SHRINK) {
       // this CTA's part of h: [TN][r8] floats, of the rows whose adapter is in its tile
       const int k = row / p.r8, j = row - k * p.r8, slot = (int)blockIdx.x * per_tile + k;
-      float* part = reinterpret_cast<float*>(gen);
+      float* part = reinterpret_cast<float*>(gen + S::kOffPart);
 #pragma unroll 1
       for (int c = 0; c < TN; c += CH) {
         float v[CH];
@@ -390,63 +430,97 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
       const int f = n0 + row;
       const float bias = p.bias && f < p.n ? p.bias[f] : 0.f;
       const bool bad = *s_bad != 0 && f < p.n;
+      auto columns_of = [&](int c, float* v) {
+        if constexpr (CH == 32) tmem_ld32(lane_base + c, v);
+        else tmem_ld16(lane_base + c, v);
+        if (bad)
+#pragma unroll
+          for (int i = 0; i < CH; ++i) v[i] += lr_not_finite(p, t0 + c + i, f, s_ad[c + i], s_slot[c + i], z, Z);
+      };
       if (Z == 1) {
+        // Two neighbouring lanes trade: the even one stores both filters of the even rows, the odd one those of the odd rows, 4 bytes each.
+        const bool pairs = p.n % 2 == 0 && ((uintptr_t)p.y & 3) == 0;
 #pragma unroll 1
         for (int c = 0; c < TN; c += CH) {
           float v[CH];
-          if constexpr (CH == 32) tmem_ld32(lane_base + c, v);
-          else tmem_ld16(lane_base + c, v);
-          if (bad)
+          columns_of(c, v);
+          if (pairs) {
 #pragma unroll
-            for (int i = 0; i < CH; ++i) v[i] += lr_not_finite(p, t0 + c + i, f, s_ad[c + i], s_slot[c + i], z, Z);
-          if (ok && f < p.n)
+            for (int i = 0; i < CH; i += 2) {
+              const float give = (lane & 1 ? v[i] : v[i + 1]) + bias, keep = (lane & 1 ? v[i + 1] : v[i]) + bias, got = __shfl_xor_sync(0xffffffffu, give, 1);
+              const int t = t0 + c + i + (lane & 1);
+              if (ok && f < p.n && t < p.rows)         // n is even: both filters of a pair are there, or neither
+                *reinterpret_cast<uint32_t*>(p.y + (size_t)t * p.n + (f & ~1)) = lane & 1 ? pack_bf16x2(got, keep) : pack_bf16x2(keep, got);
+            }
+          } else if (ok && f < p.n) {
 #pragma unroll
             for (int i = 0; i < CH; ++i)
               if (t0 + c + i < p.rows) p.y[(size_t)(t0 + c + i) * p.n + f] = __float2bfloat16_rn(v[i] + bias);
+          }
         }
-      } else {
-        // CTA o of the cluster finishes columns [o * share, + share): everybody sends it its part of them
-        const int share = TN / Z;
-        asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");   // every CTA's products have left its ring
-        const uint32_t recv = base;
+      } else if constexpr (DEEP) {
+        // CTA o of the cluster finishes columns [o * share, + share): everybody sends it its part of them, in runs of four columns (two where a share has no more)
+        const int share = TN / Z, log_share = 31 - __clz(share);
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");      // every CTA's barriers are set up
+        const uint32_t recv = base + S::kOffPart;
 #pragma unroll 1
         for (int c = 0; c < TN; c += CH) {
           float v[CH];
-          if constexpr (CH == 32) tmem_ld32(lane_base + c, v);
-          else tmem_ld16(lane_base + c, v);
-          if (bad)
+          columns_of(c, v);
+          if (share >= 4) {
 #pragma unroll
-            for (int i = 0; i < CH; ++i) v[i] += lr_not_finite(p, t0 + c + i, f, s_ad[c + i], s_slot[c + i], z, Z);
+            for (int i = 0; i < CH; i += 4) {
+              const int o = (c + i) >> log_share, at = ((z * share + (c + i) - (o << log_share)) * 128 + row * 4) * 4;
+              asm volatile(
+                  "{\n .reg .b32 a, b;\n mapa.shared::cluster.u32 a, %0, %2;\n mapa.shared::cluster.u32 b, %1, %2;\n"
+                  " st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [a], {%3, %4, %5, %6}, [b];\n}"
+                  ::"r"(recv + (uint32_t)at), "r"(part_bar), "r"(o), "f"(v[i]), "f"(v[i + 1]), "f"(v[i + 2]), "f"(v[i + 3])
+                  : "memory");
+            }
+          } else {
 #pragma unroll
-          for (int i = 0; i < CH; ++i) {
-            const int o = (c + i) / share, at = (z * share + (c + i) - o * share) * 128 + row;
-            uint32_t to;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(recv + 4u * at), "r"(o));
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(v[i]) : "memory");
+            for (int i = 0; i < CH; i += 2) {
+              const int o = (c + i) >> 1, at = (z * 256 + row * 2) * 4;
+              asm volatile(
+                  "{\n .reg .b32 a, b;\n mapa.shared::cluster.u32 a, %0, %2;\n mapa.shared::cluster.u32 b, %1, %2;\n"
+                  " st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [a], {%3, %4}, [b];\n}"
+                  ::"r"(recv + (uint32_t)at), "r"(part_bar), "r"(o), "f"(v[i]), "f"(v[i + 1])
+                  : "memory");
+            }
           }
         }
-        asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
-        const float* in = reinterpret_cast<const float*>(gen);
-        for (int i = 0; i < share; ++i) {
-          const int t = t0 + z * share + i;
-          float sum = 0.f;
-          for (int k = 0; k < Z; ++k) sum += in[(k * share + i) * 128 + row];
-          if (ok && f < p.n && t < p.rows) p.y[(size_t)t * p.n + f] = __float2bfloat16_rn(sum + bias);
+        const bool sent = mbar_wait_cluster(part_bar, 0, p.err_flag, kTcWaitCycles) || mbar_wait_cluster(part_bar, 0, p.err_flag, kTcWaitCycles);
+        const float* in = reinterpret_cast<const float*>(gen + S::kOffPart);
+        const int run = min(share, 4);
+        for (int i = 0; i < share; i += run) {
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          for (int k = 0; k < Z; ++k) {
+            if (run == 4) {
+              const float4 o = *reinterpret_cast<const float4*>(in + (k * share + i) * 128 + row * 4);
+              sum[0] += o.x, sum[1] += o.y, sum[2] += o.z, sum[3] += o.w;
+            } else {
+              const float2 o = *reinterpret_cast<const float2*>(in + k * 256 + row * 2);
+              sum[0] += o.x, sum[1] += o.y;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int t = t0 + z * share + i + j;
+            if (j < run && ok && sent && f < p.n && t < p.rows) p.y[(size_t)t * p.n + f] = __float2bfloat16_rn(sum[j] + bias);
+          }
         }
       }
     }
     tc_fence_before();
   }
-  if (!SHRINK && Z > 1 && !(warp >= 2 && warp < 6)) {   // the other warps' part in the two barriers of the exchange
-    asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
-    asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
-  }
+  // The warps that send wait for what is sent to them; the others' part in the barrier at the start.
+  if (Z > 1 && (SHRINK || !(warp >= 2 && warp < 6))) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
   if constexpr (SHRINK) {
     if (!idle) {
       // The parts are complete in every CTA of the cluster; this one finishes every Z-th row.
       if (Z > 1) asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
       else __syncthreads();
-      const uint32_t part = base;
+      const uint32_t part = base + S::kOffPart;
       for (int i = tid; i < TN / Z * p.rank; i += (int)blockDim.x) {
         const int t = i / p.rank * Z + z, j = i - i / p.rank * p.rank, slot = s_slot[t] - (int)blockIdx.x * per_tile;
         if (slot < 0 || slot >= here) continue;
@@ -555,27 +629,27 @@ inline cudaError_t lr_context_init() {   // once per device
   auto set = [&](auto kernel, int bytes) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   };
-  set(lowrank_tcgen05_kernel<16, false, false>, LrSmem<16, false>::kBytes);
-  set(lowrank_tcgen05_kernel<16, false, true>, LrSmem<16, false>::kBytes);
-  set(lowrank_tcgen05_kernel<32, false, false>, LrSmem<32, false>::kBytes);
-  set(lowrank_tcgen05_kernel<32, false, true>, LrSmem<32, false>::kBytes);
-  set(lowrank_tcgen05_kernel<64, false, false>, LrSmem<64, false>::kBytes);
-  set(lowrank_tcgen05_kernel<64, false, true>, LrSmem<64, false>::kBytes);
-  set(lowrank_tcgen05_kernel<128, false, false>, LrSmem<128, false>::kBytes);
-  set(lowrank_tcgen05_kernel<128, false, true>, LrSmem<128, false>::kBytes);
-  set(lowrank_tcgen05_kernel<256, false, false>, LrSmem<256, false>::kBytes);
-  set(lowrank_tcgen05_kernel<256, false, true>, LrSmem<256, false>::kBytes);
-  set(lowrank_tcgen05_kernel<kLrShrinkTN, true, false>, LrSmem<kLrShrinkTN, true>::kBytes);
-  set(lowrank_tcgen05_kernel<kLrShrinkTN, true, true>, LrSmem<kLrShrinkTN, true>::kBytes);
+  set(lowrank_tcgen05_kernel<16, true, false, false>, LrSmem<16, true>::kBytes);
+  set(lowrank_tcgen05_kernel<16, true, false, true>, LrSmem<16, true>::kBytes);
+  set(lowrank_tcgen05_kernel<32, true, false, false>, LrSmem<32, true>::kBytes);
+  set(lowrank_tcgen05_kernel<32, true, false, true>, LrSmem<32, true>::kBytes);
+  set(lowrank_tcgen05_kernel<64, true, false, false>, LrSmem<64, true>::kBytes);
+  set(lowrank_tcgen05_kernel<64, true, false, true>, LrSmem<64, true>::kBytes);
+  set(lowrank_tcgen05_kernel<128, true, false, false>, LrSmem<128, true>::kBytes);
+  set(lowrank_tcgen05_kernel<128, true, false, true>, LrSmem<128, true>::kBytes);
+  set(lowrank_tcgen05_kernel<128, false, false, false>, LrSmem<128, false>::kBytes);
+  set(lowrank_tcgen05_kernel<128, false, false, true>, LrSmem<128, false>::kBytes);
+  set(lowrank_tcgen05_kernel<kLrShrinkTN, true, true, false>, LrSmem<kLrShrinkTN, true>::kBytes);
+  set(lowrank_tcgen05_kernel<kLrShrinkTN, true, true, true>, LrSmem<kLrShrinkTN, true>::kBytes);
   return e;
 }
 
-template <int TN, bool SHRINK, bool COPY>
+template <int TN, bool DEEP, bool SHRINK, bool COPY>
 inline cudaError_t lr_launch_k(const CUtensorMap& tmA, const CUtensorMap& tmX, const LrArgs& a, dim3 grid, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(COPY ? 192 + 32 * kLrCopyWarps : 224);
-  cfg.dynamicSmemBytes = LrSmem<TN, SHRINK>::kBytes;
+  cfg.dynamicSmemBytes = LrSmem<TN, DEEP>::kBytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   int n = 0;
@@ -590,25 +664,28 @@ inline cudaError_t lr_launch_k(const CUtensorMap& tmA, const CUtensorMap& tmX, c
   }
   cfg.attrs = attr;
   cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, lowrank_tcgen05_kernel<TN, SHRINK, COPY>, tmA, tmX, a);
+  return cudaLaunchKernelEx(&cfg, lowrank_tcgen05_kernel<TN, DEEP, SHRINK, COPY>, tmA, tmX, a);
 }
 
 struct LrPlan {
   int tn, splits;          // rows of a tile; CTAs that share its K
+  bool deep;               // ring: one tile an SM at most
   bool simt;               // h on CUDA cores
   int jn, h_splits;        // rows of A_a of a CTA there; CTAs that share the K of a tile on the tensor cores
 };
 
 inline LrPlan lr_plan(int rows, int c, int n, int rank, int adapters, int sms) {
   LrPlan p;
-  p.tn = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+  p.tn = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   const int kb = cdiv(c, 64);
   auto share = [&](long tiles) {           // twice as many CTAs while they fit side by side and each has four blocks of K
     int z = 1;
     while (z < kLrMaxSplits && tiles * z * 2 <= sms && kb >= z * 2 * 4) z *= 2;
     return z;
   };
-  p.splits = p.tn < 256 ? share((long)cdiv(n, 128) * cdiv(rows, p.tn)) : 1;
+  const long tiles = (long)cdiv(n, 128) * cdiv(rows, p.tn);
+  p.splits = share(tiles);
+  p.deep = p.tn < 128 || tiles <= sms;
   p.simt = rows <= kLrSimtRows;
   p.jn = 8;
   while (p.jn > 1 && (long)rows * cdiv(rank, p.jn) < 2L * sms) p.jn /= 2;
@@ -616,10 +693,10 @@ inline LrPlan lr_plan(int rows, int c, int n, int rank, int adapters, int sms) {
   return p;
 }
 
-template <int TN>
+template <int TN, bool DEEP>
 inline cudaError_t lr_expand(bool copy, const CUtensorMap& tmW, const CUtensorMap& tmX, const LrArgs& a, int splits, cudaStream_t st) {
   const dim3 grid(cdiv(a.n, 128), cdiv(a.rows, TN), splits);
-  return copy ? lr_launch_k<TN, false, true>(tmW, tmX, a, grid, st) : lr_launch_k<TN, false, false>(tmW, tmX, a, grid, st);
+  return copy ? lr_launch_k<TN, DEEP, false, true>(tmW, tmX, a, grid, st) : lr_launch_k<TN, DEEP, false, false>(tmW, tmX, a, grid, st);
 }
 
 template <typename T>
@@ -651,17 +728,16 @@ inline cudaError_t lr_run_bf16(const LrContext& ctx, LrArgs a, cudaStream_t st) 
   if (wide) {
     const int per_tile = 128 / a.r8;
     const dim3 grid(cdiv(std::min(a.adapters, kLrShrinkTN), per_tile), cdiv(a.rows, kLrShrinkTN), p.h_splits);
-    e = copy ? lr_launch_k<kLrShrinkTN, true, true>(tmA, tmH, a, grid, st) : lr_launch_k<kLrShrinkTN, true, false>(tmA, tmH, a, grid, st);
+    e = copy ? lr_launch_k<kLrShrinkTN, true, true, true>(tmA, tmH, a, grid, st) : lr_launch_k<kLrShrinkTN, true, true, false>(tmA, tmH, a, grid, st);
   } else if (a.adapters > 0) {
     e = lr_shrink_simt<bf16>(a.x, a.a, a.scale, a.which, a.h, a.rows, a.c, a.rank, a.adapters, p.jn, st);
   }
   if (e != cudaSuccess) return e;
   switch (p.tn) {
-    case 16: return lr_expand<16>(copy, tmW, tmX, a, p.splits, st);
-    case 32: return lr_expand<32>(copy, tmW, tmX, a, p.splits, st);
-    case 64: return lr_expand<64>(copy, tmW, tmX, a, p.splits, st);
-    case 128: return lr_expand<128>(copy, tmW, tmX, a, p.splits, st);
-    default: return lr_expand<256>(copy, tmW, tmX, a, p.splits, st);
+    case 16: return lr_expand<16, true>(copy, tmW, tmX, a, p.splits, st);
+    case 32: return lr_expand<32, true>(copy, tmW, tmX, a, p.splits, st);
+    case 64: return lr_expand<64, true>(copy, tmW, tmX, a, p.splits, st);
+    default: return p.deep ? lr_expand<128, true>(copy, tmW, tmX, a, p.splits, st) : lr_expand<128, false>(copy, tmW, tmX, a, p.splits, st);
   }
 }
 
