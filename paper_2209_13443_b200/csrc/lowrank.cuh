@@ -11,10 +11,11 @@
 // rows cost few columns, and W, which bounds small batches, is read once.  There K is cut over a cluster of up to eight CTAs, which
 // send each other their parts as asynchronous stores and add them in fixed order.  The first launch is a product of the same shape, 128 rows of
 // stacked A_a over 64 rows of the batch; up to kLrSimtRows rows CUDA cores do it, a warp a row of A_a.
-// The second launch starts while the first runs and waits for it only before it fills in h.  The adapters' columns take ring slots behind the last channel's: the
-// producer of W, which walks the ring anyway, hands them to the four warps that gather the columns, while the products before them still run.  Grids of more than one
-// tile an SM use a ring of three slots, so that two CTAs share an SM and one's columns and stores lie under the other's products; smaller ones a
-// deep ring, for the bytes in flight.
+// The second launch starts while the first runs and waits for it only before it fills in h.  The adapters' columns have slots of their own beside the ring of the
+// channels, which four warps fill while the channels are multiplied; they are multiplied at fixed places: behind the last channel, or, from a persistent CTA's second
+// tile on, spread over the second half of the channels, where they are long there.
+// Two forms.  At most one tile an SM: a deep ring, for the bytes in flight.  More: persistent CTAs with two accumulators, so that one tile's list of adapters, columns
+// and stores lie under the next one's products.  128 x 256 tiles where that takes less time: 128 x 128 ones ask 128 bytes a clock of L2 for every SM, and get 97.
 //
 // Channels that are not whole 16-byte vectors, or operands off a 16-byte boundary, cannot be fetched by TMA: eight warps then copy the
 // tiles (COPY), 2 or 4 bytes at a time.
@@ -47,18 +48,19 @@ struct LrArgs {
   int* err_flag;
 };
 
-template <int TN, bool DEEP>
+template <int TN, bool PERSIST, bool SHRINK = false>
 struct LrSmem {
   static constexpr int kABytes = 128 * 128, kBBytes = TN * 128, kStage = kABytes + kBBytes;
-  static constexpr int kStages = !DEEP ? 3 : TN == 128 ? 4 : 7;
+  static constexpr int kStages = SHRINK ? 3 : PERSIST ? (TN == 256 ? 3 : 5) : TN == 128 ? 4 : 5, kExt = SHRINK ? 0 : TN >= 128 ? 1 : 2;   // slots of the ring, of adapter columns
+  static constexpr int kAcc = PERSIST ? 2 : 1;                      // accumulators
   static constexpr int kPart = TN * 128 * 4;                        // partial sums: a shrink's h of its rows (up to 128 numbers each); else what the cluster's CTAs send
-  static constexpr int kOffPart = kStages * kStage;
-  static constexpr int kOffInts = kOffPart + (DEEP ? kPart : 0);    // grids of a shallow ring do not cut K
+  static constexpr int kOffExt = kStages * kStage, kOffPart = kOffExt + kExt * kStage;
+  static constexpr int kOffInts = kOffPart + (PERSIST ? 0 : kPart); // persistent CTAs do not cut K
   static constexpr int kInts = 3 * TN + 16;                         // adapter and slot of each row, adapters of the tile, masks and counts
   static constexpr int kOffBars = kOffInts + kInts * 4;
-  static constexpr int kBytes = kOffBars + 8 * (3 * kStages + 3) + 1024;
+  static constexpr int kBytes = kOffBars + 8 * (2 * kStages + 2 * kExt + 7) + 1024;
   static_assert(kBytes <= 227 * 1024, "exceeds the shared memory of an SM");
-  static_assert(DEEP || 2 * (kBytes + 1024) <= 228 * 1024, "two CTAs of a shallow ring share an SM");
+  static_assert(!SHRINK || 2 * (kBytes + 1024) <= 228 * 1024, "two CTAs of a shrink share an SM");
 };
 
 __device__ __forceinline__ void mbar_arrive_n(uint32_t bar, uint32_t n) {
@@ -73,12 +75,10 @@ __device__ __forceinline__ void lr_store(bf16* h, int t, int j, int rank, float 
 }
 __device__ __forceinline__ void lr_store(float* h, int t, int j, int rank, float v) { h[(size_t)t * rank + j] = v; }
 
-// Zeros in the place of infinities and NaN among two bf16 values; whether there were any.
-__device__ __forceinline__ uint32_t lr_drop(uint32_t& w) {
-  const uint32_t m = __vcmpeq2(w & 0x7f807f80u, 0x7f807f80u);
-  w &= ~m;
-  return m;
-}
+// Whether one of two bf16 values is an infinity or NaN: its exponent's carry.  Nonzero bits where so.
+__device__ __forceinline__ uint32_t lr_odd(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+// Zeros in their place.
+__device__ __forceinline__ uint32_t lr_drop(uint32_t w) { return w & ~__vcmpeq2(w & 0x7f807f80u, 0x7f807f80u); }
 // What the values dropped from B_a give row t and filter f, of the columns in the blocks of this CTA (z of Z); the second part of h would only make
 // inf - inf of an infinity.
 __device__ __noinline__ float lr_not_finite(const LrArgs& p, int t, int f, int ad, int slot, int z, int Z) {
@@ -93,13 +93,14 @@ __device__ __noinline__ float lr_not_finite(const LrArgs& p, int t, int f, int a
 }
 
 // tmA: rows of operand A (W in boxes of 128 filters; SHRINK: all adapters' A in boxes of r8 rows), tmX: rows of x in boxes of TN.
-// blockIdx.x: tile of filters (SHRINK: of stacked adapters), y: tile of rows, z: range of K.
-template <int TN, bool DEEP, bool SHRINK, bool COPY>
+// Tile: blockIdx.x of filters, y of rows, z: range of K.  Persistent: every gridDim.x-th tile, filters first.  SHRINK: a CTA takes the adapters of its rows in groups
+// that fill the 128 rows of operand A, one after the other; a row of x has one adapter, so all groups leave their numbers in the same array.
+template <int TN, bool PERSIST, bool SHRINK, bool COPY>
 __global__ void __launch_bounds__(COPY ? 192 + 32 * kLrCopyWarps : 224)
 lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmX, LrArgs p) {
-  static_assert(DEEP || !SHRINK, "a shrink keeps its partial sums beside the ring");
-  using S = LrSmem<TN, DEEP>;
-  constexpr int kStages = S::kStages;
+  using S = LrSmem<TN, PERSIST, SHRINK>;
+  constexpr int kStages = S::kStages, kExt = S::kExt, kAcc = S::kAcc;
+  constexpr bool kPersist = PERSIST;
   constexpr uint32_t kFull = COPY ? 32 * kLrCopyWarps : 2;   // arrivals that fill a slot
   extern __shared__ uint8_t lr_smem[];
   const uint32_t raw = smem_u32(lr_smem), base = (raw + 1023u) & ~1023u;
@@ -107,30 +108,41 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
   int* s_ad = reinterpret_cast<int*>(gen + S::kOffInts);     // [TN] adapter of a row, -1: none
   int* s_slot = s_ad + TN;                                   // [TN] its place among the tile's adapters
   int* s_list = s_slot + TN;                                 // [TN] the tile's adapters, in order of first occurrence
-  unsigned* s_mask = reinterpret_cast<unsigned*>(s_list + TN);   // [4]
-  int* s_count = reinterpret_cast<int*>(s_mask) + 8;
-  uint32_t* tmem_slot = s_mask + 9;
+  unsigned* s_mask = reinterpret_cast<unsigned*>(s_list + TN);   // [8]
+  int* s_count = reinterpret_cast<int*>(s_mask) + 8;         // [2] adapters of the tile, by its parity
   int* s_bad = s_count + 2;                                  // set where a B_a of the tile holds infinities or NaN
+  uint32_t* tmem_slot = s_mask + 11;
   const uint32_t bar0 = base + S::kOffBars;
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (kStages + s); };
-  auto grant_bar = [&](int s) { return bar0 + 8u * (2 * kStages + s); };     // the slot is free for adapter columns
-  const uint32_t accum_bar = bar0 + 8u * (3 * kStages), list_bar = accum_bar + 8u, part_bar = list_bar + 8u;
+  auto accum_bar = [&](int a) { return bar0 + 8u * (2 * kStages + a); };     // the accumulator is complete
+  auto drain_bar = [&](int a) { return bar0 + 8u * (2 * kStages + 2 + a); }; // and has been read
+  auto list_bar = [&](int i) { return bar0 + 8u * (2 * kStages + 4 + i); };  // the tile's adapters are known
+  const uint32_t part_bar = bar0 + 8u * (2 * kStages + 6);
+  auto ext_full = [&](int x) { return part_bar + 8u + 8u * x; };             // slots of adapter columns
+  auto ext_empty = [&](int x) { return part_bar + 8u + 8u * (kExt + x); };
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  const int t0 = (int)blockIdx.y * TN, n0 = (int)blockIdx.x * 128;
   const int z = (int)blockIdx.z, Z = (int)gridDim.z;
+  const int tiles_n = (p.n + 127) / 128;
+  int tiles = kPersist ? tiles_n * ((p.rows + TN - 1) / TN) : 1;
+  const int tile0 = kPersist ? (int)blockIdx.x : 0, tile_step = kPersist ? (int)gridDim.x : 1;
+  auto place_of = [&](int tile, int& n0, int& t0) {
+    n0 = (kPersist ? tile % tiles_n : (int)blockIdx.x) * 128, t0 = (kPersist ? tile / tiles_n : (int)blockIdx.y) * TN;
+  };
   const int kb_all = (p.c + 63) / 64;
   const int kb0 = (int)((long)kb_all * z / Z), num_kb = (int)((long)kb_all * (z + 1) / Z) - kb0;   // Z <= kb_all: never empty
+  int n_first, t_first;
+  place_of(tile0, n_first, t_first);
 
   if (tid == 0) {
-    for (int s = 0; s < kStages; ++s) mbar_init(full_bar(s), kFull), mbar_init(empty_bar(s), 1), mbar_init(grant_bar(s), 1);
-    mbar_init(accum_bar, 1);
-    mbar_init(list_bar, 1);
+    for (int s = 0; s < kStages; ++s) mbar_init(full_bar(s), kFull), mbar_init(empty_bar(s), 1);
+    for (int x = 0; x < kExt; ++x) mbar_init(ext_full(x), 1), mbar_init(ext_empty(x), 1);
+    for (int a = 0; a < 2; ++a) mbar_init(accum_bar(a), 1), mbar_init(drain_bar(a), 1), mbar_init(list_bar(a), 1);
     mbar_init(part_bar, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (!SHRINK && Z > 1) mbar_expect_tx(part_bar, (uint32_t)S::kPart);     // TN / Z columns from each of Z CTAs
   }
-  constexpr uint32_t kCols = TN < 32 ? 32 : TN;
+  constexpr uint32_t kCols = TN < 32 ? 32 : TN * kAcc;
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -142,371 +154,424 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
   if (SHRINK) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (Z > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");       // waited for before anything is sent
 
-  // The tile's adapters: a row is the first of its adapter, or refers to it.
-  if (warp >= 2 && warp < 6) {
-    const int et = tid - 64;
-    for (int i = et; i < TN; i += 128) {
-      const int t = t0 + i, a = t < p.rows && p.adapters > 0 ? p.which[t] : -1;
-      s_ad[i] = a >= 0 && a < p.adapters ? a : -1;
-    }
-    asm volatile("bar.sync 1, 128;" ::: "memory");
-    const int a = et < TN ? s_ad[et] : -1;
-    int f = (et & ~31) + __ffs(__match_any_sync(0xffffffffu, a)) - 1;       // the first of its warp
-    if (a >= 0 && f == et)
-      for (int u = 0; u < (et & ~31); u += 4) {
-        const int4 o = *reinterpret_cast<const int4*>(s_ad + u);
-        if (o.w == a) f = min(f, u + 3);
-        if (o.z == a) f = min(f, u + 2);
-        if (o.y == a) f = min(f, u + 1);
-        if (o.x == a) f = min(f, u);
-      }
-    f = __shfl_sync(0xffffffffu, f, f >= (et & ~31) ? f & 31 : lane);       // the others of the warp take what their first found
-    const unsigned lead = __ballot_sync(0xffffffffu, a >= 0 && f == et);
-    if (lane == 0 && et < TN) s_mask[et >> 5] = lead;
-    asm volatile("bar.sync 1, 128;" ::: "memory");
-    int count = 0;
-#pragma unroll
-    for (int k = 0; k < (TN + 31) / 32; ++k) count += __popc(s_mask[k]);
-    if (et < TN) {
-      int slot = -1;
-      if (a >= 0) {
-        slot = __popc(s_mask[f >> 5] & ((1u << (f & 31)) - 1u));
-        for (int k = 0; k < f >> 5; ++k) slot += __popc(s_mask[k]);
-        if (f == et) s_list[slot] = a;
-      }
-      s_slot[et] = slot;
-    }
-    if (et == 0) *s_count = count, *s_bad = 0;
-    asm volatile("bar.sync 1, 128;" ::: "memory");
-    if (et == 0) mbar_arrive_n(list_bar, 1);
-  }
-  const int per_tile = 128 / p.r8;               // SHRINK: adapters of a tile
-  int here = 0;
-  if (SHRINK) {
-    __syncthreads();
-    here = min(per_tile, *s_count - (int)blockIdx.x * per_tile);
-  }
-  const bool idle = SHRINK && here <= 0;         // this CTA's adapters do not occur
   const int ext_cols = kLrParts * p.rank;        // columns of an adapter
   // blocks of adapter columns that this CTA takes: z, z + Z, ...
   auto ext_blocks = [&](int count) {
     const int all = (int)(((long)count * ext_cols + 63) / 64);
     return all > z ? (all - z + Z - 1) / Z : 0;
   };
+  // The tile's adapters: a row is the first of its adapter, or refers to it.  Four warps.
+  auto list_adapters = [&](int t0, int par) {
+    const int et = tid - 64;
+    constexpr int H = TN > 128 ? TN / 128 : 1;
+    asm volatile("bar.sync 1, 128;" ::: "memory");       // the list of the tile before is not needed any more
+    for (int i = et; i < TN; i += 128) {
+      const int t = t0 + i, a = t < p.rows && p.adapters > 0 ? p.which[t] : -1;
+      s_ad[i] = a >= 0 && a < p.adapters ? a : -1;
+    }
+    asm volatile("bar.sync 1, 128;" ::: "memory");
+    int first[H];
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const int i = et + 128 * h, w0 = i & ~31;
+      const int a = i < TN ? s_ad[i] : -1;
+      int f = w0 + __ffs(__match_any_sync(0xffffffffu, a)) - 1;       // the first of its warp
+      if (a >= 0 && f == i)
+        for (int u = 0; u < w0; u += 4) {
+          const int4 o = *reinterpret_cast<const int4*>(s_ad + u);
+          if (o.w == a) f = min(f, u + 3);
+          if (o.z == a) f = min(f, u + 2);
+          if (o.y == a) f = min(f, u + 1);
+          if (o.x == a) f = min(f, u);
+        }
+      f = __shfl_sync(0xffffffffu, f, f >= w0 ? f & 31 : lane);       // the others of the warp take what their first found
+      const unsigned lead = __ballot_sync(0xffffffffu, a >= 0 && f == i);
+      if (lane == 0 && i < TN) s_mask[i >> 5] = lead;
+      first[h] = a >= 0 ? f : -1;
+    }
+    asm volatile("bar.sync 1, 128;" ::: "memory");
+    int count = 0;
+#pragma unroll
+    for (int k = 0; k < (TN + 31) / 32; ++k) count += __popc(s_mask[k]);
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const int i = et + 128 * h, f = first[h];
+      if (i >= TN) continue;
+      int slot = -1;
+      if (f >= 0) {
+        slot = __popc(s_mask[f >> 5] & ((1u << (f & 31)) - 1u));
+        for (int k = 0; k < f >> 5; ++k) slot += __popc(s_mask[k]);
+        if (f == i) s_list[slot] = s_ad[i];
+      }
+      s_slot[i] = slot;
+    }
+    if (et == 0) s_count[par] = count, *s_bad = 0;
+    asm volatile("bar.sync 1, 128;" ::: "memory");
+    if (et == 0) mbar_arrive_n(list_bar(par), 1);
+    return count;
+  };
+  const int per_tile = 128 / p.r8;               // SHRINK: adapters of a tile
+  if (SHRINK) {
+    if (warp >= 2 && warp < 6) list_adapters(t_first, 0);
+    __syncthreads();
+    tiles = (s_count[0] + per_tile - 1) / per_tile;
+  }
+  const bool idle = SHRINK && tiles == 0;        // no adapters here
+  auto here = [&](int group) { return min(per_tile, s_count[0] - group * per_tile); };      // adapters of a group
+
+  struct Walk {      // over the ring
+    int s;
+    uint32_t ph;
+    __device__ __forceinline__ void next() {
+      if (++s == kStages) s = 0, ph ^= 1u;
+    }
+  };
+  auto produce = [&](auto&& load) {
+    Walk w{0, 1u};
+    int used = 0;                                // slots start out free
+    for (int tile = tile0; tile < tiles; tile += tile_step) {
+      int n0, t0;
+      place_of(tile, n0, t0);
+      for (int i = 0; i < num_kb; ++i) {
+        if (used == kStages && !mbar_wait(empty_bar(w.s), w.ph, p.err_flag)) return;
+        load(w.s, kb0 + i, SHRINK ? tile : n0, t0);
+        used = min(used + 1, kStages), w.next();
+      }
+    }
+  };
 
   if (idle) {
   } else if (warp == 0) {
-    if (elect_one()) {
-      int s = 0;
-      uint32_t ph = 1;
-      bool ok = true;
-      for (int i = 0; !COPY && i < num_kb; ++i) {
-        if (i >= kStages && !(ok = mbar_wait(empty_bar(s), ph, p.err_flag))) break;
-        const uint32_t dst = base + (uint32_t)s * S::kStage;
-        if (SHRINK) {
-          mbar_expect_tx(full_bar(s), (uint32_t)(here * p.r8 * 128));
-          for (int k = 0; k < here; ++k)
-            tma_load_2d(dst + (uint32_t)(k * p.r8 * 128), &tmA, full_bar(s), (kb0 + i) * 64, s_list[(int)blockIdx.x * per_tile + k] * p.rank);
-        } else {
-          mbar_expect_tx(full_bar(s), S::kABytes);
-          tma_load_2d(dst, &tmA, full_bar(s), (kb0 + i) * 64, n0);
-        }
-        if (++s == kStages) s = 0, ph ^= 1u;
-      }
-      if (!SHRINK && !COPY && ok && mbar_wait(list_bar, 0, p.err_flag)) {     // COPY: the first of its warps does this
-        const int ext = ext_blocks(*s_count);
-        for (int i = num_kb; i < num_kb + ext; ++i) {
-          if (i >= kStages && !mbar_wait(empty_bar(s), ph, p.err_flag)) break;
-          mbar_arrive_n(grant_bar(s), 1);
-          if (++s == kStages) s = 0, ph ^= 1u;
-        }
-      }
-    }
+    if (!COPY && elect_one())
+      produce(
+              [&](int s, int kb, int n0, int) {
+                const uint32_t dst = base + (uint32_t)s * S::kStage;
+                if (SHRINK) {
+                  const int group = n0, n = here(group);
+                  mbar_expect_tx(full_bar(s), (uint32_t)(n * p.r8 * 128));
+                  for (int k = 0; k < n; ++k)
+                    tma_load_2d(dst + (uint32_t)(k * p.r8 * 128), &tmA, full_bar(s), kb * 64, s_list[group * per_tile + k] * p.rank);
+                } else {
+                  mbar_expect_tx(full_bar(s), S::kABytes);
+                  tma_load_2d(dst, &tmA, full_bar(s), kb * 64, n0);
+                }
+              });
     __syncwarp();
   } else if (!COPY && warp == 6) {
-    if (elect_one()) {
-      int s = 0;
-      uint32_t ph = 1;
-      for (int i = 0; i < num_kb; ++i) {
-        if (i >= kStages && !mbar_wait(empty_bar(s), ph, p.err_flag)) break;
-        mbar_expect_tx(full_bar(s), S::kBBytes);
-        tma_load_2d(base + (uint32_t)s * S::kStage + S::kABytes, &tmX, full_bar(s), (kb0 + i) * 64, t0);
-        if (++s == kStages) s = 0, ph ^= 1u;
-      }
-    }
+    if (elect_one())
+      produce(
+              [&](int s, int kb, int, int t0) {
+                mbar_expect_tx(full_bar(s), S::kBBytes);
+                tma_load_2d(base + (uint32_t)s * S::kStage + S::kABytes, &tmX, full_bar(s), kb * 64, t0);
+              });
     __syncwarp();
   } else if (COPY && warp >= 6) {
     const int cw = warp - 6;
-    int s = 0;
-    uint32_t ph = 1;
-    for (int i = 0; i < num_kb; ++i) {
-      if (i >= kStages && !mbar_wait(empty_bar(s), ph, p.err_flag)) break;
-      uint8_t* dst = gen + (size_t)s * S::kStage;
-      const int k0 = (kb0 + i) * 64 + 2 * lane;
+    produce(
+            [&](int s, int kb, int n0, int t0) {
+              uint8_t* dst = gen + (size_t)s * S::kStage;
+              const int k0 = kb * 64 + 2 * lane;
 #pragma unroll 8
-      for (int r = cw; r < 128 + TN; r += kLrCopyWarps) {
-        const bf16* src = nullptr;
-        if (r >= 128) {
-          if (t0 + r - 128 < p.rows) src = p.x + (size_t)(t0 + r - 128) * p.c;
-        } else if (SHRINK) {
-          const int k = r / p.r8, j = r - k * p.r8;
-          if (k < here && j < p.rank) src = p.a + ((size_t)s_list[(int)blockIdx.x * per_tile + k] * p.rank + j) * p.c;
-        } else if (n0 + r < p.n) {
-          src = p.w + (size_t)(n0 + r) * p.c;
-        }
-        uint32_t v = 0;
-        if (src) {
-          if (p.pairs) {                               // c is even: a pair lies inside the row or outside it
-            if (k0 < p.c) v = *reinterpret_cast<const uint32_t*>(src + k0);
-          } else {
-            const unsigned short* e = reinterpret_cast<const unsigned short*>(src);
-            if (k0 < p.c) v = e[k0];
-            if (k0 + 1 < p.c) v |= (uint32_t)e[k0 + 1] << 16;
-          }
-        }
-        *reinterpret_cast<uint32_t*>(dst + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) = v;
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      mbar_arrive_n(full_bar(s), 1);
-      if (++s == kStages) s = 0, ph ^= 1u;
-    }
-    if (!SHRINK && cw == 0 && elect_one() && mbar_wait(list_bar, 0, p.err_flag)) {
-      const int ext = ext_blocks(*s_count);
-      for (int i = num_kb; i < num_kb + ext; ++i) {
-        if (i >= kStages && !mbar_wait(empty_bar(s), ph, p.err_flag)) break;
-        mbar_arrive_n(grant_bar(s), 1);
-        if (++s == kStages) s = 0, ph ^= 1u;
-      }
-    }
-    __syncwarp();
+              for (int r = cw; r < 128 + TN; r += kLrCopyWarps) {
+                const bf16* src = nullptr;
+                if (r >= 128) {
+                  if (t0 + r - 128 < p.rows) src = p.x + (size_t)(t0 + r - 128) * p.c;
+                } else if (SHRINK) {
+                  const int k = r / p.r8, j = r - k * p.r8;
+                  if (k < here(n0) && j < p.rank) src = p.a + ((size_t)s_list[n0 * per_tile + k] * p.rank + j) * p.c;      // n0: the group
+                } else if (n0 + r < p.n) {
+                  src = p.w + (size_t)(n0 + r) * p.c;
+                }
+                uint32_t v = 0;
+                if (src) {
+                  if (p.pairs) {                               // c is even: a pair lies inside the row or outside it
+                    if (k0 < p.c) v = *reinterpret_cast<const uint32_t*>(src + k0);
+                  } else {
+                    const unsigned short* e = reinterpret_cast<const unsigned short*>(src);
+                    if (k0 < p.c) v = e[k0];
+                    if (k0 + 1 < p.c) v |= (uint32_t)e[k0 + 1] << 16;
+                  }
+                }
+                *reinterpret_cast<uint32_t*>(dst + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) = v;
+              }
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              mbar_arrive_n(full_bar(s), 1);
+            });
   } else if (warp == 1) {
     if (elect_one()) {
       constexpr uint32_t idesc = umma_idesc(TN);
       const uint64_t da0 = umma_desc(base), db0 = umma_desc(base + S::kABytes);
-      int s = 0, blocks = num_kb;
-      uint32_t ph = 0;
+      Walk w{0, 0u};
       bool ok = true;
-      for (int i = 0;; ++i) {
-        if (!SHRINK && i == num_kb) {                  // by now the list is long there
-          ok = mbar_wait(list_bar, 0, p.err_flag);
+      uint32_t xs = 0;                                 // blocks of adapter columns so far
+      for (int tile = tile0, it = 0; tile < tiles && ok; tile += tile_step, ++it) {
+        const int a = it & (kAcc - 1);
+        const uint32_t acc = tmem + (uint32_t)(a * TN);
+        if (it >= kAcc) ok = mbar_wait(drain_bar(a), (uint32_t)(it / kAcc - 1) & 1u, p.err_flag);
+        // Where the adapters' columns go, in K blocks: the list is asked for in the middle, or behind the last block.
+        const int ask = kPersist && it > 0 ? (num_kb + 1) / 2 : num_kb;
+        int ext = 0, e = 0;
+        for (int i = 0; i < num_kb && ok; ++i) {
+          ok = mbar_wait(full_bar(w.s), w.ph, p.err_flag);
           if (!ok) break;
-          blocks += ext_blocks(*s_count);
+          tc_fence_after();
+          const uint64_t off = (uint64_t)(w.s * (S::kStage >> 4));
+          umma_block(acc, da0 + off, db0 + off, idesc, i != 0);
+          umma_commit(empty_bar(w.s));
+          w.next();
+          if constexpr (!SHRINK) {
+            if (i + 1 == ask) {
+              ok = mbar_wait(list_bar(it & 1), (uint32_t)(it >> 1) & 1u, p.err_flag);
+              ext = ok ? ext_blocks(s_count[it & 1]) : 0;
+            }
+            for (; ok && e < ext && (i + 1 == num_kb || (long)(i + 1 - ask) * (ext + 1) >= (long)(e + 1) * (num_kb - ask)); ++e, ++xs) {
+              const int x = (int)(xs % kExt);
+              ok = mbar_wait(ext_full(x), xs / kExt & 1u, p.err_flag);
+              if (!ok) break;
+              tc_fence_after();
+              const uint64_t at = (uint64_t)((S::kOffExt + x * S::kStage) >> 4);
+              umma_block(acc, da0 + at, db0 + at, idesc, true);
+              umma_commit(ext_empty(x));
+            }
+          }
         }
-        if (i >= blocks) break;
-        ok = mbar_wait(full_bar(s), ph, p.err_flag);
-        if (!ok) break;
-        tc_fence_after();
-        const uint64_t off = (uint64_t)(s * (S::kStage >> 4));
-        umma_block(tmem, da0 + off, db0 + off, idesc, i != 0);
-        umma_commit(empty_bar(s));
-        if (++s == kStages) s = 0, ph ^= 1u;
+        if (ok) umma_commit(accum_bar(a));
       }
-      if (ok) umma_commit(accum_bar);
     }
     __syncwarp();
   } else {
     const int et = tid - 64, q = warp & 3;
     const int row = q * 32 + lane;                     // accumulator lane of this thread
-    bool ok = true;
-    if constexpr (!SHRINK) {
-      // Block e of adapter columns goes into the ring as K block num_kb + e.  A thread has the 16-byte chunk et % 8 of 64 columns, in every sixteenth row of either operand.
-      const int ext = ext_blocks(*s_count), all = *s_count * ext_cols, c8 = et & 7, r0 = et >> 3;
-      const bool whole = p.rank % 8 == 0, vec = whole && ((uintptr_t)p.b & 15) == 0;   // eight columns are one part of one adapter; of B_a one load
-      auto place = [&](int r) { return (uint32_t)(r * 128 + ((c8 ^ (r & 7)) << 4)); };
-      auto column = [&](int e, int k, int& slot, int& rem) {       // adapter and place in its 2 * rank columns; slot -1: behind the last
-        const int c = (z + e * Z) * 64 + c8 * 8 + k;
-        slot = c / ext_cols, rem = c - slot * ext_cols;
-        if (c >= all) slot = -1;
-      };
-      auto fetch = [&](uint32_t dst, const void* src, bool in) {
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
-      };
-      auto slot_of_block = [&](int e) { return (num_kb + e) % kStages; };
-      auto fill_b = [&](int e) {
-        const int s = slot_of_block(e);
-        // use u of this slot: the u-th grant of it follows those of the blocks of adapter columns before this one
-        ok = ok && mbar_wait(grant_bar(s), (uint32_t)(e / kStages) & 1u, p.err_flag);
-        uint8_t* tile = gen + (size_t)s * S::kStage;
-        int slot, rem;
-        if (vec) {
-          column(e, 0, slot, rem);
-          const bf16* src = slot >= 0 ? p.b + ((size_t)s_list[slot] * p.n + n0) * p.rank + (rem < p.rank ? rem : rem - p.rank) : p.b;
-#pragma unroll
-          for (int m = 0; m < 8; ++m) {
-            const int r = r0 + 16 * m;
-            const bool in = slot >= 0 && n0 + r < p.n;
-            fetch(base + (uint32_t)s * S::kStage + place(r), in ? src + (size_t)r * p.rank : p.b, in);
-          }
-        } else {
-          int ad[8], j[8];
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            column(e, k, slot, rem);
-            ad[k] = slot >= 0 ? s_list[slot] : -1, j[k] = rem < p.rank ? rem : rem - p.rank;
-          }
-#pragma unroll 2
-          for (int m = 0; m < 8; ++m) {
-            const int r = r0 + 16 * m, f = n0 + r;
-            uint32_t v[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = ad[k] >= 0 && f < p.n ? reinterpret_cast<const unsigned short*>(p.b)[((size_t)ad[k] * p.n + f) * p.rank + j[k]] : 0u;
-            *reinterpret_cast<uint4*>(tile + place(r)) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
-          }
-        }
-      };
-      auto fill_h = [&](int e) {
-        const int s = slot_of_block(e);
-        const uint32_t at = base + (uint32_t)s * S::kStage + S::kABytes;
-        int slot, rem;
-        if (whole) {                       // the workspace is aligned, and so are eight columns of a row
-          column(e, 0, slot, rem);
-#pragma unroll
-          for (int m = 0; m < TN / 16; ++m) {
-            const int t = r0 + 16 * m;
-            const bool in = slot >= 0 && s_slot[t] == slot;
-            fetch(at + place(t), in ? p.h + (size_t)(t0 + t) * ext_cols + rem : p.h, in);
-          }
-        } else {
-          int slots[8], rems[8];
-#pragma unroll
-          for (int k = 0; k < 8; ++k) column(e, k, slots[k], rems[k]);
-#pragma unroll 2
-          for (int m = 0; m < TN / 16; ++m) {
-            const int t = r0 + 16 * m, mine = s_slot[t];
-            const unsigned short* h = reinterpret_cast<const unsigned short*>(p.h) + (size_t)(t0 + t) * ext_cols;
-            uint32_t v[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = mine >= 0 && slots[k] == mine ? h[rems[k]] : 0u;
-            *reinterpret_cast<uint4*>(gen + (size_t)s * S::kStage + S::kABytes + place(t)) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
-          }
-        }
-        cp_async_commit();
-      };
-      auto finish = [&](int e) {           // what this thread fetched is here: an infinity would turn the zeros of other adapters' rows into NaN, so
-        const int s = slot_of_block(e);    // lr_not_finite adds it to its own rows
-        uint8_t* tile = gen + (size_t)s * S::kStage;
-#pragma unroll
-        for (int m = 0; m < 8; ++m) {
-          uint4* o = reinterpret_cast<uint4*>(tile + place(r0 + 16 * m));
-          uint4 v = *o;
-          if (lr_drop(v.x) | lr_drop(v.y) | lr_drop(v.z) | lr_drop(v.w)) *s_bad = 1, *o = v;
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (et == 0) mbar_arrive_n(full_bar(s), kFull);
-      };
-      // B_a of the first blocks before the wait for h (no kernel writes it); then one block is fetched while the one before it is finished
-      constexpr int kAhead = 2;
-      for (int e = 0; e < ext && e < kAhead; ++e) fill_b(e);
-      asm volatile("griddepcontrol.wait;" ::: "memory");
-      if (ext > 0) fill_h(0);
-      if (ext > 1) fill_h(1);
-      for (int e = 0; e < ext; ++e) {
-        if (e + 1 < ext) cp_async_wait<1>();
-        else cp_async_wait<0>();
-        finish(e);
-        if (e + kAhead < ext) fill_b(e + kAhead), fill_h(e + kAhead);
-      }
-    }
-    ok = __all_sync(0xffffffffu, mbar_wait(accum_bar, 0, p.err_flag));
-    tc_fence_after();
-    const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
     constexpr int CH = TN < 32 ? TN : 32;              // columns read at a time
+    bool ok = true;
     if constexpr (SHRINK) {
-      // this CTA's part of h: [TN][r8] floats, of the rows whose adapter is in its tile
-      const int k = row / p.r8, j = row - k * p.r8, slot = (int)blockIdx.x * per_tile + k;
+      // this CTA's part of h: [TN][r8] floats
+      const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
+      const int k = row / p.r8, j = row - k * p.r8;
       float* part = reinterpret_cast<float*>(gen + S::kOffPart);
+      for (int group = 0; group < tiles; ++group) {
+        ok = __all_sync(0xffffffffu, mbar_wait(accum_bar(0), (uint32_t)group & 1u, p.err_flag)) && ok;
+        tc_fence_after();
+        const int slot = k < per_tile ? group * per_tile + k : -2;
 #pragma unroll 1
-      for (int c = 0; c < TN; c += CH) {
-        float v[CH];
-        if constexpr (CH == 32) tmem_ld32(lane_base + c, v);
-        else tmem_ld16(lane_base + c, v);
-        if (k < here)
+        for (int c = 0; c < TN; c += CH) {
+          float v[CH];
+          if constexpr (CH == 32) tmem_ld32(lane_base + c, v);
+          else tmem_ld16(lane_base + c, v);
 #pragma unroll
           for (int i = 0; i < CH; ++i)
             if (s_slot[c + i] == slot) part[(c + i) * p.r8 + j] = v[i];
+        }
+        tc_fence_before();
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (et == 0) mbar_arrive_n(drain_bar(0), 1);
       }
     } else {
-      const int f = n0 + row;
-      const float bias = p.bias && f < p.n ? p.bias[f] : 0.f;
-      const bool bad = *s_bad != 0 && f < p.n;
-      auto columns_of = [&](int c, float* v) {
-        if constexpr (CH == 32) tmem_ld32(lane_base + c, v);
-        else tmem_ld16(lane_base + c, v);
-        if (bad)
-#pragma unroll
-          for (int i = 0; i < CH; ++i) v[i] += lr_not_finite(p, t0 + c + i, f, s_ad[c + i], s_slot[c + i], z, Z);
-      };
-      if (Z == 1) {
-        // Two neighbouring lanes trade: the even one stores both filters of the even rows, the odd one those of the odd rows, 4 bytes each.
-        const bool pairs = p.n % 2 == 0 && ((uintptr_t)p.y & 3) == 0;
+      uint32_t xs = 0;                                 // blocks of adapter columns so far
+      bool waited = false;                             // for h
+      for (int tile = tile0, it = 0; tile < tiles; tile += tile_step, ++it) {
+        int n0, t0;
+        place_of(tile, n0, t0);
+        const int count = list_adapters(t0, it & 1);
+        // A thread has the 16-byte chunk et % 8 of a block's 64 columns, in every sixteenth row of either operand.
+        const int ext = ext_blocks(count), all = count * ext_cols, c8 = et & 7, r0 = et >> 3;
+        const bool whole = p.rank % 8 == 0, vec = whole && ((uintptr_t)p.b & 15) == 0;   // eight columns are one part of one adapter; of B_a one load
+        // The code of this part is kept short (loops, not copies): it runs a few times a tile, and what it costs is its way into the instruction cache.
+        const uint32_t place0 = (uint32_t)(r0 * 128 + ((c8 ^ (r0 & 7)) << 4));      // of row r0; every sixteenth row is 2048 bytes on
+        const float per_col = 1.f / (float)ext_cols;
+        auto column = [&](int e, int k, int& slot, int& rem) {       // adapter and place in its 2 * rank columns; slot -1: behind the last
+          const int c = (z + e * Z) * 64 + c8 * 8 + k;
+          slot = (int)(((float)c + 0.5f) * per_col), rem = c - slot * ext_cols;      // c < 2^16: the quotient is off by less than half a column
+          if (c >= all) slot = -1;
+        };
+        auto fetch = [&](uint32_t dst, const void* src, bool in) {
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+        };
+        auto slot_of_block = [&](int e) { return (int)((xs + (uint32_t)e) % kExt); };
+        auto at_block = [&](int e) { return (uint32_t)(S::kOffExt + slot_of_block(e) * S::kStage); };
+        auto fill_b = [&](int e) {
+          const uint32_t use = xs + (uint32_t)e;
+          if (use >= kExt) ok = ok && mbar_wait(ext_empty(slot_of_block(e)), (use / kExt - 1) & 1u, p.err_flag);
+          if (vec) {
+            int slot, rem;
+            column(e, 0, slot, rem);
+            const bf16* src = p.b + ((size_t)(slot >= 0 ? s_list[slot] : 0) * p.n + n0 + r0) * p.rank + (rem < p.rank ? rem : rem - p.rank);
+            uint32_t dst = base + at_block(e) + place0;
 #pragma unroll 1
-        for (int c = 0; c < TN; c += CH) {
-          float v[CH];
-          columns_of(c, v);
-          if (pairs) {
-#pragma unroll
-            for (int i = 0; i < CH; i += 2) {
-              const float give = (lane & 1 ? v[i] : v[i + 1]) + bias, keep = (lane & 1 ? v[i + 1] : v[i]) + bias, got = __shfl_xor_sync(0xffffffffu, give, 1);
-              const int t = t0 + c + i + (lane & 1);
-              if (ok && f < p.n && t < p.rows)         // n is even: both filters of a pair are there, or neither
-                *reinterpret_cast<uint32_t*>(p.y + (size_t)t * p.n + (f & ~1)) = lane & 1 ? pack_bf16x2(got, keep) : pack_bf16x2(keep, got);
+            for (int f = n0 + r0; f < n0 + 128; f += 16, dst += 2048, src += 16 * p.rank) fetch(dst, slot >= 0 && f < p.n ? src : p.b, slot >= 0 && f < p.n);
+          } else {
+            unsigned short* dst = reinterpret_cast<unsigned short*>(gen + at_block(e) + place0);
+#pragma unroll 1
+            for (int k = 0; k < 8; ++k) {
+              int slot, rem;
+              column(e, k, slot, rem);
+              const unsigned short* src = reinterpret_cast<const unsigned short*>(p.b) + ((size_t)(slot >= 0 ? s_list[slot] : 0) * p.n + n0 + r0) * p.rank + (rem < p.rank ? rem : rem - p.rank);
+#pragma unroll 4
+              for (int m = 0; m < 8; ++m) dst[m * 1024 + k] = slot >= 0 && n0 + r0 + 16 * m < p.n ? src[(size_t)16 * m * p.rank] : (unsigned short)0;
             }
-          } else if (ok && f < p.n) {
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-              if (t0 + c + i < p.rows) p.y[(size_t)(t0 + c + i) * p.n + f] = __float2bfloat16_rn(v[i] + bias);
           }
-        }
-      } else if constexpr (DEEP) {
-        // CTA o of the cluster finishes columns [o * share, + share): everybody sends it its part of them, in runs of four columns (two where a share has no more)
-        const int share = TN / Z, log_share = 31 - __clz(share);
-        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");      // every CTA's barriers are set up
-        const uint32_t recv = base + S::kOffPart;
+        };
+        auto fill_h = [&](int e) {
+          if (whole) {                       // the workspace is aligned, and so are eight columns of a row
+            int slot, rem;
+            column(e, 0, slot, rem);
+            const bf16* src = p.h + (size_t)(t0 + r0) * ext_cols + rem;
+            uint32_t dst = base + at_block(e) + S::kABytes + place0;
 #pragma unroll 1
-        for (int c = 0; c < TN; c += CH) {
-          float v[CH];
-          columns_of(c, v);
-          if (share >= 4) {
-#pragma unroll
-            for (int i = 0; i < CH; i += 4) {
-              const int o = (c + i) >> log_share, at = ((z * share + (c + i) - (o << log_share)) * 128 + row * 4) * 4;
-              asm volatile(
-                  "{\n .reg .b32 a, b;\n mapa.shared::cluster.u32 a, %0, %2;\n mapa.shared::cluster.u32 b, %1, %2;\n"
-                  " st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [a], {%3, %4, %5, %6}, [b];\n}"
-                  ::"r"(recv + (uint32_t)at), "r"(part_bar), "r"(o), "f"(v[i]), "f"(v[i + 1]), "f"(v[i + 2]), "f"(v[i + 3])
-                  : "memory");
+            for (int t = r0; t < TN; t += 16, dst += 2048, src += 16 * ext_cols) {
+              const bool in = slot >= 0 && s_slot[t] == slot;
+              fetch(dst, in ? src : p.h, in);
             }
           } else {
-#pragma unroll
-            for (int i = 0; i < CH; i += 2) {
-              const int o = (c + i) >> 1, at = (z * 256 + row * 2) * 4;
-              asm volatile(
-                  "{\n .reg .b32 a, b;\n mapa.shared::cluster.u32 a, %0, %2;\n mapa.shared::cluster.u32 b, %1, %2;\n"
-                  " st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [a], {%3, %4}, [b];\n}"
-                  ::"r"(recv + (uint32_t)at), "r"(part_bar), "r"(o), "f"(v[i]), "f"(v[i + 1])
-                  : "memory");
+            unsigned short* dst = reinterpret_cast<unsigned short*>(gen + at_block(e) + S::kABytes + place0);
+#pragma unroll 1
+            for (int k = 0; k < 8; ++k) {
+              int slot, rem;
+              column(e, k, slot, rem);
+              const unsigned short* src = reinterpret_cast<const unsigned short*>(p.h) + (size_t)(t0 + r0) * ext_cols + rem;
+#pragma unroll 4
+              for (int m = 0; m < TN / 16; ++m) dst[m * 1024 + k] = slot >= 0 && s_slot[r0 + 16 * m] == slot ? src[(size_t)16 * m * ext_cols] : (unsigned short)0;
             }
           }
+        };
+        // What there is no slot for yet is on its way to L2.
+#pragma unroll 1
+        for (int e = kExt; e < ext; ++e) {
+          const int first = (z + e * Z) * 64 / ext_cols, last = min(((z + e * Z) * 64 + 63) / ext_cols, count - 1);
+          const int bytes = min(128, p.n - n0) * p.rank * 2, lines = (bytes + 127) / 128;
+          for (int k = first; k <= last; ++k)
+#pragma unroll 1
+            for (int i = et; i < lines; i += 128)
+              asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(p.b + ((size_t)s_list[k] * p.n + n0) * p.rank) + min(i * 128, bytes - 2)));
         }
-        const bool sent = mbar_wait_cluster(part_bar, 0, p.err_flag, kTcWaitCycles) || mbar_wait_cluster(part_bar, 0, p.err_flag, kTcWaitCycles);
-        const float* in = reinterpret_cast<const float*>(gen + S::kOffPart);
-        const int run = min(share, 4);
-        for (int i = 0; i < share; i += run) {
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
-          for (int k = 0; k < Z; ++k) {
-            if (run == 4) {
-              const float4 o = *reinterpret_cast<const float4*>(in + (k * share + i) * 128 + row * 4);
-              sum[0] += o.x, sum[1] += o.y, sum[2] += o.z, sum[3] += o.w;
-            } else {
-              const float2 o = *reinterpret_cast<const float2*>(in + k * 256 + row * 2);
-              sum[0] += o.x, sum[1] += o.y;
+        // Blocks of a batch are fetched together: B_a before the wait for h (no kernel writes it), then h.
+#pragma unroll 1
+        for (int e0 = 0; e0 < ext || !waited; e0 += kExt) {
+          const int e1 = min(e0 + kExt, ext);
+#pragma unroll 1
+          for (int e = e0; e < e1; ++e) fill_b(e);
+          if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+          waited = true;
+#pragma unroll 1
+          for (int e = e0; e < e1; ++e) fill_h(e);
+          cp_async_commit();
+          cp_async_wait<0>();
+          // what this thread fetched is here: an infinity would turn the zeros of other adapters' rows into NaN, so lr_not_finite adds it to its own rows
+#pragma unroll 1
+          for (int e = e0; e < e1; ++e) {
+            uint4* at = reinterpret_cast<uint4*>(gen + at_block(e) + place0);
+#pragma unroll 2
+            for (int m = 0; m < 8; ++m) {
+              const uint4 v = at[m * 128];
+              if (lr_odd(v.x) | lr_odd(v.y) | lr_odd(v.z) | lr_odd(v.w)) at[m * 128] = make_uint4(lr_drop(v.x), lr_drop(v.y), lr_drop(v.z), lr_drop(v.w)), *s_bad = 1;
             }
           }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          asm volatile("bar.sync 1, 128;" ::: "memory");
+          if (et == 0)
+            for (int e = e0; e < e1; ++e) mbar_arrive_n(ext_full(slot_of_block(e)), 1);
+        }
+        xs += (uint32_t)ext;
+
+        const int acc = it & (kAcc - 1);
+        ok = __all_sync(0xffffffffu, mbar_wait(accum_bar(acc), (uint32_t)(it / kAcc) & 1u, p.err_flag)) && ok;
+        tc_fence_after();
+        const uint32_t lane_base = tmem + (uint32_t)(acc * TN) + ((uint32_t)(q * 32) << 16);
+        const int f = n0 + row;
+        const float bias = p.bias && f < p.n ? p.bias[f] : 0.f;
+        const bool bad = *s_bad != 0 && f < p.n;
+        auto columns_of = [&](int c, float* v) {
+          if constexpr (CH == 32) tmem_ld32(lane_base + c, v);
+          else tmem_ld16(lane_base + c, v);
+          if (bad)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int t = t0 + z * share + i + j;
-            if (j < run && ok && sent && f < p.n && t < p.rows) p.y[(size_t)t * p.n + f] = __float2bfloat16_rn(sum[j] + bias);
+            for (int i = 0; i < CH; ++i) v[i] += lr_not_finite(p, t0 + c + i, f, s_ad[c + i], s_slot[c + i], z, Z);
+        };
+        // Two neighbouring lanes trade: the even one stores both filters of the even rows, the odd one those of the odd rows, 4 bytes each.
+        const bool pairs = p.n % 2 == 0 && ((uintptr_t)p.y & 3) == 0;
+        auto store2 = [&](int t, float v0, float v1) {       // of rows t and t + 1; n is even: both filters of a pair are there, or neither
+          const float give = lane & 1 ? v0 : v1, keep = lane & 1 ? v1 : v0, got = __shfl_xor_sync(0xffffffffu, give, 1);
+          t += lane & 1;
+          if (ok && f < p.n && t < p.rows) *reinterpret_cast<uint32_t*>(p.y + (size_t)t * p.n + (f & ~1)) = lane & 1 ? pack_bf16x2(got, keep) : pack_bf16x2(keep, got);
+        };
+        if (Z == 1) {
+#pragma unroll 1
+          for (int c = 0; c < TN; c += CH) {
+            float v[CH];
+            columns_of(c, v);
+            if (pairs) {
+#pragma unroll
+              for (int i = 0; i < CH; i += 2) store2(t0 + c + i, v[i] + bias, v[i + 1] + bias);
+            } else if (ok && f < p.n) {
+#pragma unroll
+              for (int i = 0; i < CH; ++i)
+                if (t0 + c + i < p.rows) p.y[(size_t)(t0 + c + i) * p.n + f] = __float2bfloat16_rn(v[i] + bias);
+            }
+          }
+          if (kPersist) {          // the accumulator is free for the tile after the next
+            tc_fence_before();
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            if (et == 0) mbar_arrive_n(drain_bar(acc), 1);
+          }
+        } else if constexpr (!kPersist) {
+          // CTA o of the cluster finishes columns [o * share, + share): everybody sends it its part of them, in runs of four columns (two where a share has no more)
+          const int share = TN / Z, log_share = 31 - __clz(share);
+          asm volatile("barrier.cluster.wait.acquire;" ::: "memory");      // every CTA's barriers are set up
+          const uint32_t recv = base + S::kOffPart;
+#pragma unroll 1
+          for (int c = 0; c < TN; c += CH) {
+            float v[CH];
+            columns_of(c, v);
+            if (share >= 4) {
+#pragma unroll
+              for (int i = 0; i < CH; i += 4) {
+                const int o = (c + i) >> log_share, at = ((z * share + (c + i) - (o << log_share)) * 128 + row * 4) * 4;
+                asm volatile(
+                    "{\n .reg .b32 a, b;\n mapa.shared::cluster.u32 a, %0, %2;\n mapa.shared::cluster.u32 b, %1, %2;\n"
+                    " st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [a], {%3, %4, %5, %6}, [b];\n}"
+                    ::"r"(recv + (uint32_t)at), "r"(part_bar), "r"(o), "f"(v[i]), "f"(v[i + 1]), "f"(v[i + 2]), "f"(v[i + 3])
+                    : "memory");
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < CH; i += 2) {
+                const int o = (c + i) >> 1, at = (z * 256 + row * 2) * 4;
+                asm volatile(
+                    "{\n .reg .b32 a, b;\n mapa.shared::cluster.u32 a, %0, %2;\n mapa.shared::cluster.u32 b, %1, %2;\n"
+                    " st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [a], {%3, %4}, [b];\n}"
+                    ::"r"(recv + (uint32_t)at), "r"(part_bar), "r"(o), "f"(v[i]), "f"(v[i + 1])
+                    : "memory");
+              }
+            }
+          }
+          ok = __all_sync(0xffffffffu, mbar_wait_cluster(part_bar, 0, p.err_flag, kTcWaitCycles) || mbar_wait_cluster(part_bar, 0, p.err_flag, kTcWaitCycles)) && ok;
+          const float* in = reinterpret_cast<const float*>(gen + S::kOffPart);
+          const int run = min(share, 4);
+#pragma unroll 1
+          for (int i = 0; i < share; i += run) {
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            if (run == 4) {
+#pragma unroll 2
+              for (int k = 0; k < Z; ++k) {
+                const float4 o = *reinterpret_cast<const float4*>(in + (k * share + i) * 128 + row * 4);
+                sum[0] += o.x, sum[1] += o.y, sum[2] += o.z, sum[3] += o.w;
+              }
+            } else {
+#pragma unroll 2
+              for (int k = 0; k < Z; ++k) {
+                const float2 o = *reinterpret_cast<const float2*>(in + k * 256 + row * 2);
+                sum[0] += o.x, sum[1] += o.y;
+              }
+            }
+            const int t = t0 + z * share + i;
+            if (pairs) {
+              store2(t, sum[0] + bias, sum[1] + bias);
+              if (run == 4) store2(t + 2, sum[2] + bias, sum[3] + bias);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (j < run && ok && f < p.n && t + j < p.rows) p.y[(size_t)(t + j) * p.n + f] = __float2bfloat16_rn(sum[j] + bias);
+            }
           }
         }
       }
@@ -522,8 +587,8 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
       else __syncthreads();
       const uint32_t part = base + S::kOffPart;
       for (int i = tid; i < TN / Z * p.rank; i += (int)blockDim.x) {
-        const int t = i / p.rank * Z + z, j = i - i / p.rank * p.rank, slot = s_slot[t] - (int)blockIdx.x * per_tile;
-        if (slot < 0 || slot >= here) continue;
+        const int t = i / p.rank * Z + z, j = i - i / p.rank * p.rank;
+        if (s_slot[t] < 0) continue;
         float sum = 0.f;
         for (int r = 0; r < Z; ++r) {
           uint32_t from;
@@ -532,7 +597,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
           asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(from) : "memory");
           sum += v;
         }
-        lr_store(p.h, t0 + t, j, p.rank, p.scale ? sum * p.scale[s_ad[t]] : sum);
+        lr_store(p.h, t_first + t, j, p.rank, p.scale ? sum * p.scale[s_ad[t]] : sum);
       }
       if (Z > 1) asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");   // nobody reads this CTA's part any more
     }
@@ -629,27 +694,29 @@ inline cudaError_t lr_context_init() {   // once per device
   auto set = [&](auto kernel, int bytes) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   };
-  set(lowrank_tcgen05_kernel<16, true, false, false>, LrSmem<16, true>::kBytes);
-  set(lowrank_tcgen05_kernel<16, true, false, true>, LrSmem<16, true>::kBytes);
-  set(lowrank_tcgen05_kernel<32, true, false, false>, LrSmem<32, true>::kBytes);
-  set(lowrank_tcgen05_kernel<32, true, false, true>, LrSmem<32, true>::kBytes);
-  set(lowrank_tcgen05_kernel<64, true, false, false>, LrSmem<64, true>::kBytes);
-  set(lowrank_tcgen05_kernel<64, true, false, true>, LrSmem<64, true>::kBytes);
-  set(lowrank_tcgen05_kernel<128, true, false, false>, LrSmem<128, true>::kBytes);
-  set(lowrank_tcgen05_kernel<128, true, false, true>, LrSmem<128, true>::kBytes);
+  set(lowrank_tcgen05_kernel<16, false, false, false>, LrSmem<16, false>::kBytes);
+  set(lowrank_tcgen05_kernel<16, false, false, true>, LrSmem<16, false>::kBytes);
+  set(lowrank_tcgen05_kernel<32, false, false, false>, LrSmem<32, false>::kBytes);
+  set(lowrank_tcgen05_kernel<32, false, false, true>, LrSmem<32, false>::kBytes);
+  set(lowrank_tcgen05_kernel<64, false, false, false>, LrSmem<64, false>::kBytes);
+  set(lowrank_tcgen05_kernel<64, false, false, true>, LrSmem<64, false>::kBytes);
   set(lowrank_tcgen05_kernel<128, false, false, false>, LrSmem<128, false>::kBytes);
   set(lowrank_tcgen05_kernel<128, false, false, true>, LrSmem<128, false>::kBytes);
-  set(lowrank_tcgen05_kernel<kLrShrinkTN, true, true, false>, LrSmem<kLrShrinkTN, true>::kBytes);
-  set(lowrank_tcgen05_kernel<kLrShrinkTN, true, true, true>, LrSmem<kLrShrinkTN, true>::kBytes);
+  set(lowrank_tcgen05_kernel<128, true, false, false>, LrSmem<128, true>::kBytes);
+  set(lowrank_tcgen05_kernel<128, true, false, true>, LrSmem<128, true>::kBytes);
+  set(lowrank_tcgen05_kernel<256, true, false, false>, LrSmem<256, true>::kBytes);
+  set(lowrank_tcgen05_kernel<256, true, false, true>, LrSmem<256, true>::kBytes);
+  set(lowrank_tcgen05_kernel<kLrShrinkTN, false, true, false>, LrSmem<kLrShrinkTN, false, true>::kBytes);
+  set(lowrank_tcgen05_kernel<kLrShrinkTN, false, true, true>, LrSmem<kLrShrinkTN, false, true>::kBytes);
   return e;
 }
 
-template <int TN, bool DEEP, bool SHRINK, bool COPY>
+template <int TN, bool PERSIST, bool SHRINK, bool COPY>
 inline cudaError_t lr_launch_k(const CUtensorMap& tmA, const CUtensorMap& tmX, const LrArgs& a, dim3 grid, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(COPY ? 192 + 32 * kLrCopyWarps : 224);
-  cfg.dynamicSmemBytes = LrSmem<TN, DEEP>::kBytes;
+  cfg.dynamicSmemBytes = LrSmem<TN, PERSIST, SHRINK>::kBytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   int n = 0;
@@ -664,39 +731,41 @@ inline cudaError_t lr_launch_k(const CUtensorMap& tmA, const CUtensorMap& tmX, c
   }
   cfg.attrs = attr;
   cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, lowrank_tcgen05_kernel<TN, DEEP, SHRINK, COPY>, tmA, tmX, a);
+  return cudaLaunchKernelEx(&cfg, lowrank_tcgen05_kernel<TN, PERSIST, SHRINK, COPY>, tmA, tmX, a);
 }
 
 struct LrPlan {
   int tn, splits;          // rows of a tile; CTAs that share its K
-  bool deep;               // ring: one tile an SM at most
+  bool persist;            // more tiles than SMs
   bool simt;               // h on CUDA cores
   int jn, h_splits;        // rows of A_a of a CTA there; CTAs that share the K of a tile on the tensor cores
 };
 
 inline LrPlan lr_plan(int rows, int c, int n, int rank, int adapters, int sms) {
   LrPlan p;
-  p.tn = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  // Clocks a K block of a tile takes in a full grid, 470 of 128 rows and 750 of 256, times the tiles an SM gets.
+  auto rounds = [&](int tn) { return ((long)cdiv(n, 128) * cdiv(rows, tn) + sms - 1) / sms; };
+  p.tn = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rounds(256) * 750 <= rounds(128) * 470 ? 256 : 128;
   const int kb = cdiv(c, 64);
-  auto share = [&](long tiles) {           // twice as many CTAs while they fit side by side and each has four blocks of K
+  auto share = [&](long tiles, int per_sm) {           // twice as many CTAs while they fit side by side and each has four blocks of K
     int z = 1;
-    while (z < kLrMaxSplits && tiles * z * 2 <= sms && kb >= z * 2 * 4) z *= 2;
+    while (z < kLrMaxSplits && tiles * z * 2 <= (long)sms * per_sm && kb >= z * 2 * 4) z *= 2;
     return z;
   };
   const long tiles = (long)cdiv(n, 128) * cdiv(rows, p.tn);
-  p.splits = share(tiles);
-  p.deep = p.tn < 128 || tiles <= sms;
+  p.persist = p.tn == 256 || (p.tn == 128 && tiles > sms);
+  p.splits = p.persist ? 1 : share(tiles, 1);
   p.simt = rows <= kLrSimtRows;
   p.jn = 8;
   while (p.jn > 1 && (long)rows * cdiv(rank, p.jn) < 2L * sms) p.jn /= 2;
-  p.h_splits = share((long)cdiv(rows, kLrShrinkTN) * cdiv(std::min(adapters, kLrShrinkTN), 128 / (int)align_up(rank, 8)));
+  p.h_splits = share(cdiv(rows, kLrShrinkTN), 2);
   return p;
 }
 
-template <int TN, bool DEEP>
-inline cudaError_t lr_expand(bool copy, const CUtensorMap& tmW, const CUtensorMap& tmX, const LrArgs& a, int splits, cudaStream_t st) {
-  const dim3 grid(cdiv(a.n, 128), cdiv(a.rows, TN), splits);
-  return copy ? lr_launch_k<TN, DEEP, false, true>(tmW, tmX, a, grid, st) : lr_launch_k<TN, DEEP, false, false>(tmW, tmX, a, grid, st);
+template <int TN, bool PERSIST>
+inline cudaError_t lr_expand(bool copy, const CUtensorMap& tmW, const CUtensorMap& tmX, const LrArgs& a, int splits, int sms, cudaStream_t st) {
+  const dim3 grid = PERSIST ? dim3(std::min(sms, cdiv(a.n, 128) * cdiv(a.rows, TN))) : dim3(cdiv(a.n, 128), cdiv(a.rows, TN), splits);
+  return copy ? lr_launch_k<TN, PERSIST, false, true>(tmW, tmX, a, grid, st) : lr_launch_k<TN, PERSIST, false, false>(tmW, tmX, a, grid, st);
 }
 
 template <typename T>
@@ -726,18 +795,18 @@ inline cudaError_t lr_run_bf16(const LrContext& ctx, LrArgs a, cudaStream_t st) 
     if (e != cudaSuccess) return e;
   }
   if (wide) {
-    const int per_tile = 128 / a.r8;
-    const dim3 grid(cdiv(std::min(a.adapters, kLrShrinkTN), per_tile), cdiv(a.rows, kLrShrinkTN), p.h_splits);
-    e = copy ? lr_launch_k<kLrShrinkTN, true, true, true>(tmA, tmH, a, grid, st) : lr_launch_k<kLrShrinkTN, true, true, false>(tmA, tmH, a, grid, st);
+    const dim3 grid(1, cdiv(a.rows, kLrShrinkTN), p.h_splits);
+    e = copy ? lr_launch_k<kLrShrinkTN, false, true, true>(tmA, tmH, a, grid, st) : lr_launch_k<kLrShrinkTN, false, true, false>(tmA, tmH, a, grid, st);
   } else if (a.adapters > 0) {
     e = lr_shrink_simt<bf16>(a.x, a.a, a.scale, a.which, a.h, a.rows, a.c, a.rank, a.adapters, p.jn, st);
   }
   if (e != cudaSuccess) return e;
   switch (p.tn) {
-    case 16: return lr_expand<16, true>(copy, tmW, tmX, a, p.splits, st);
-    case 32: return lr_expand<32, true>(copy, tmW, tmX, a, p.splits, st);
-    case 64: return lr_expand<64, true>(copy, tmW, tmX, a, p.splits, st);
-    default: return p.deep ? lr_expand<128, true>(copy, tmW, tmX, a, p.splits, st) : lr_expand<128, false>(copy, tmW, tmX, a, p.splits, st);
+    case 16: return lr_expand<16, false>(copy, tmW, tmX, a, p.splits, ctx.sm_count, st);
+    case 32: return lr_expand<32, false>(copy, tmW, tmX, a, p.splits, ctx.sm_count, st);
+    case 64: return lr_expand<64, false>(copy, tmW, tmX, a, p.splits, ctx.sm_count, st);
+    case 128: return p.persist ? lr_expand<128, true>(copy, tmW, tmX, a, p.splits, ctx.sm_count, st) : lr_expand<128, false>(copy, tmW, tmX, a, p.splits, ctx.sm_count, st);
+    default: return lr_expand<256, true>(copy, tmW, tmX, a, p.splits, ctx.sm_count, st);
   }
 }
 
