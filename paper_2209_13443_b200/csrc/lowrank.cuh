@@ -12,8 +12,8 @@
 // send each other their parts as asynchronous stores and add them in fixed order.  The first launch is a product of the same shape, 128 rows of
 // stacked A_a over 64 rows of the batch; up to kLrSimtRows rows CUDA cores do it, a warp a row of A_a.
 // The second launch starts while the first runs and waits for it only before it fills in h.  The adapters' columns have slots of their own beside the ring of the
-// channels, which four warps fill while the channels are multiplied; they are multiplied at fixed places: behind the last channel, or, from a persistent CTA's second
-// tile on, spread over the second half of the channels, where they are long there.
+// channels, which four warps fill while the channels are multiplied; they are multiplied at fixed places, spread over the later channels, or behind the last one where h is
+// not there before (a persistent CTA's first tile, short K).
 // Two forms.  At most one tile an SM: a deep ring, for the bytes in flight.  More: persistent CTAs with two accumulators, so that one tile's list of adapters, columns
 // and stores lie under the next one's products.  128 x 256 tiles where that takes less time: 128 x 128 ones ask 128 bytes a clock of L2 for every SM, and get 97.
 //
@@ -134,6 +134,10 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
   int n_first, t_first;
   place_of(tile0, n_first, t_first);
 
+  if (!COPY && (warp == 0 || warp == 6) && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmA) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmX) : "memory");
+  }
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) mbar_init(full_bar(s), kFull), mbar_init(empty_bar(s), 1);
     for (int x = 0; x < kExt; ++x) mbar_init(ext_full(x), 1), mbar_init(ext_empty(x), 1);
@@ -147,10 +151,17 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  // The producer of W needs nothing but its barriers: it goes ahead while the others wait for the accumulator's address, about 1600 clocks.
+  constexpr int kThreads = COPY ? 192 + 32 * kLrCopyWarps : 224;
+  if (warp == 0) {
+    __syncwarp();
+    asm volatile("bar.arrive 2, %0;" ::"n"(kThreads) : "memory");
+  } else {
+    tc_fence_before();
+    asm volatile("bar.sync 2, %0;" ::"n"(kThreads) : "memory");
+    tc_fence_after();
+  }
+  const uint32_t tmem = warp == 0 ? 0u : *tmem_slot;
   if (SHRINK) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (Z > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");       // waited for before anything is sent
 
@@ -308,8 +319,8 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
         const int a = it & (kAcc - 1);
         const uint32_t acc = tmem + (uint32_t)(a * TN);
         if (it >= kAcc) ok = mbar_wait(drain_bar(a), (uint32_t)(it / kAcc - 1) & 1u, p.err_flag);
-        // Where the adapters' columns go, in K blocks: the list is asked for in the middle, or behind the last block.
-        const int ask = kPersist && it > 0 ? (num_kb + 1) / 2 : num_kb;
+        // Where the adapters' columns go, in K blocks: spread from where the list is asked for, or behind the last block, if h is not there before.
+        const int ask = kPersist ? (it > 0 ? (num_kb + 1) / 2 : num_kb) : num_kb >= 8 ? num_kb * 5 / 8 : num_kb;
         int ext = 0, e = 0;
         for (int i = 0; i < num_kb && ok; ++i) {
           ok = mbar_wait(full_bar(w.s), w.ph, p.err_flag);
