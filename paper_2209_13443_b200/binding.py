@@ -148,9 +148,9 @@ def _ptr(t) -> Optional[int]:
     return int(t)
 
 
-def _stream(stream) -> Optional[int]:
+def _stream(stream, device: Optional[int] = None) -> Optional[int]:
     if stream is None:   # what torch.cuda.current_stream().cuda_stream is, without the object: 0.1 us in place of 3.3
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -463,7 +463,7 @@ def group_norm(dtype: str, x, batch: int, hw: int, c: int, groups: int, gamma, b
     code, td = _dtype(f, dtype)
     n = batch * hw * c
     _check(load_library().ee_group_norm(code, _mem(f, x, td, n, d), _mem(f, residual, td, n, d), batch, hw, c, groups, _mem(f, gamma, torch.float32, c, d),
-                                        _mem(f, beta, torch.float32, c, d), eps, act, _mem(f, out, td, n, d), _stream(stream)), f)
+                                        _mem(f, beta, torch.float32, c, d), eps, act, _mem(f, out, td, n, d), _stream(stream, d)), f)
 
 
 def adapted_linear_workspace_bytes(rows: int, rank: int) -> int:
@@ -484,7 +484,7 @@ def adapted_linear(dtype: str, x, rows: int, c: int, weight, n: int, a, b, rank:
     _check(load_library().ee_adapted_linear(code, _mem(f, x, td, rows * c, d), rows, c, _mem(f, weight, td, n * c, d), n, _mem(f, bias, f32, n, d),
                                             _mem(f, a, td, n_adapters * rank * c, d), _mem(f, b, td, n_adapters * n * rank, d), rank, n_adapters,
                                             _mem(f, scale, f32, n_adapters, d), _mem(f, adapter, torch.int32, rows, d), _mem(f, out, td, rows * n, d),
-                                            aligned, room, _stream(stream)), f)
+                                            aligned, room, _stream(stream, d)), f)
 
 
 def softmax(dtype: str, logits, rows: int, n: int, out, temperature=None, stream=None):
@@ -492,7 +492,7 @@ def softmax(dtype: str, logits, rows: int, n: int, out, temperature=None, stream
     f, d = "ee_softmax", torch.cuda.current_device()
     code, td = _dtype(f, dtype)
     _check(load_library().ee_softmax(code, _mem(f, logits, td, rows * n, d), rows, n, _mem(f, temperature, torch.float32, rows, d),
-                                     _mem(f, out, torch.float32, rows * n, d), _stream(stream)), f)
+                                     _mem(f, out, torch.float32, rows * n, d), _stream(stream, d)), f)
 
 
 def verify_drafts(p, q, drafts, u, r, batch: int, k: int, n: int, tokens, n_accepted, n_draft=None, stream=None):
@@ -500,7 +500,7 @@ def verify_drafts(p, q, drafts, u, r, batch: int, k: int, n: int, tokens, n_acce
     f, d, f32, i32 = "ee_verify_drafts", torch.cuda.current_device(), torch.float32, torch.int32
     _check(load_library().ee_verify_drafts(_mem(f, p, f32, batch * (k + 1) * n, d), _mem(f, q, f32, batch * k * n, d), _mem(f, drafts, i32, batch * k, d),
                                            _mem(f, u, f32, batch * k, d), _mem(f, r, f32, batch, d), _mem(f, n_draft, i32, batch, d), batch, k, n,
-                                           _mem(f, tokens, i32, batch * (k + 1), d), _mem(f, n_accepted, i32, batch, d), _stream(stream)), f)
+                                           _mem(f, tokens, i32, batch * (k + 1), d), _mem(f, n_accepted, i32, batch, d), _stream(stream, d)), f)
 
 
 def operators_check(stream=None):
