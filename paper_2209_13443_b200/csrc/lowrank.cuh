@@ -10,7 +10,7 @@
 // The tile is turned: 128 filters are the rows of the accumulator (lanes) and 16 to 128 rows of the batch its columns, so that few
 // rows cost few columns, and W, which bounds small batches, is read once.  There K is cut over a cluster of up to eight CTAs, which
 // send each other their parts as asynchronous stores and add them in fixed order.  The first launch is a product of the same shape, 128 rows of
-// stacked A_a over 64 rows of the batch; up to kLrSimtRows rows CUDA cores do it, a warp a row of A_a.
+// stacked A_a over 64 rows of the batch; up to kLrSimtWork products CUDA cores do it, a warp a row of A_a.
 // The second launch starts while the first runs and waits for it only before it fills in h.  The adapters' columns have slots of their own beside the ring of the
 // channels, which four warps fill while the channels are multiplied; they are multiplied at fixed places, spread over the later channels, or behind the last one where h is
 // not there before (a persistent CTA's first tile, short K).
@@ -18,7 +18,8 @@
 // and stores lie under the next one's products.  128 x 256 tiles where that takes less time: 128 x 128 ones ask 128 bytes a clock of L2 for every SM, and get 97.
 //
 // Channels that are not whole 16-byte vectors, or operands off a 16-byte boundary, cannot be fetched by TMA: eight warps then copy the
-// tiles (COPY), 2 or 4 bytes at a time.
+// tiles (COPY), 8 or 4 bytes at a time without waiting for them, or 2 where a row may start between two words.  Ranks, too, need not be whole vectors: columns are
+// fetched in the widest units (8, 4, 2 or 1 values) that divide the rank.
 #pragma once
 #include "common.cuh"
 #include "conv_f32.cuh"
@@ -30,7 +31,7 @@ constexpr int kLrParts = 2;            // bf16 parts of h
 constexpr int kLrMaxRank = 128;
 constexpr int kLrMaxSplits = 8;        // CTAs of a cluster
 constexpr int kLrShrinkTN = 64;        // rows of a tile of the first launch
-constexpr int kLrSimtRows = 96;
+constexpr long kLrSimtWork = 24L << 20;  // products of the first launch up to which CUDA cores take it: every row of x reads its adapter from L2
 constexpr int kLrCopyWarps = 8;
 
 struct LrArgs {
@@ -44,14 +45,14 @@ struct LrArgs {
   bf16* h;             // [rows][2][rank]: the two parts
   bf16* y;             // [rows][n]
   int rows, c, n, rank, r8, adapters;
-  bool pairs;          // COPY: rows start on 4-byte boundaries
+  int unit;            // COPY: bytes of a copy, 8, 4 or 2: rows are whole units and start on their boundaries
   int* err_flag;
 };
 
 template <int TN, bool PERSIST, bool SHRINK = false>
 struct LrSmem {
   static constexpr int kABytes = 128 * 128, kBBytes = TN * 128, kStage = kABytes + kBBytes;
-  static constexpr int kStages = SHRINK ? 3 : PERSIST ? (TN == 256 ? 3 : 5) : TN == 128 ? 4 : 5, kExt = SHRINK ? 0 : TN >= 128 ? 1 : 2;   // slots of the ring, of adapter columns
+  static constexpr int kStages = SHRINK ? 3 : PERSIST ? (TN == 256 ? 3 : 4) : TN == 128 ? 3 : 5, kExt = SHRINK ? 0 : TN == 256 ? 1 : 2;   // slots of the ring, of adapter columns
   static constexpr int kAcc = PERSIST ? 2 : 1;                      // accumulators
   static constexpr int kPart = TN * 128 * 4;                        // partial sums: a shrink's h of its rows (up to 128 numbers each); else what the cluster's CTAs send
   static constexpr int kOffExt = kStages * kStage, kOffPart = kOffExt + kExt * kStage;
@@ -277,37 +278,64 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
               });
     __syncwarp();
   } else if (COPY && warp >= 6) {
-    const int cw = warp - 6;
-    produce(
-            [&](int s, int kb, int n0, int t0) {
-              uint8_t* dst = gen + (size_t)s * S::kStage;
-              const int k0 = kb * 64 + 2 * lane;
-#pragma unroll 8
-              for (int r = cw; r < 128 + TN; r += kLrCopyWarps) {
-                const bf16* src = nullptr;
-                if (r >= 128) {
-                  if (t0 + r - 128 < p.rows) src = p.x + (size_t)(t0 + r - 128) * p.c;
-                } else if (SHRINK) {
-                  const int k = r / p.r8, j = r - k * p.r8;
-                  if (k < here(n0) && j < p.rank) src = p.a + ((size_t)s_list[n0 * per_tile + k] * p.rank + j) * p.c;      // n0: the group
-                } else if (n0 + r < p.n) {
-                  src = p.w + (size_t)(n0 + r) * p.c;
-                }
-                uint32_t v = 0;
-                if (src) {
-                  if (p.pairs) {                               // c is even: a pair lies inside the row or outside it
-                    if (k0 < p.c) v = *reinterpret_cast<const uint32_t*>(src + k0);
-                  } else {
-                    const unsigned short* e = reinterpret_cast<const unsigned short*>(src);
-                    if (k0 < p.c) v = e[k0];
-                    if (k0 + 1 < p.c) v |= (uint32_t)e[k0 + 1] << 16;
-                  }
-                }
-                *reinterpret_cast<uint32_t*>(dst + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) = v;
-              }
-              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-              mbar_arrive_n(full_bar(s), 1);
-            });
+    const int ct = tid - 192;
+    int late = -1;                       // slot whose copies are on their way
+    auto landed = [&]() {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      mbar_arrive_n(full_bar(late), 1);
+    };
+    produce([&](int s, int kb, int n0, int t0) {
+      uint8_t* dst = gen + (size_t)s * S::kStage;
+      const uint32_t dst_s = base + (uint32_t)s * S::kStage;
+      const int shift = p.unit == 8 ? 4 : 5, col = ct & ((1 << shift) - 1);      // copies of a row: 16 of 8 bytes, 32 of 4 (or of 2 x 2)
+      const int k0 = kb * 64 + col * (64 >> shift);
+      const uint32_t chunk = (uint32_t)(col >> (shift - 3)), within = (uint32_t)(col & ((1 << (shift - 3)) - 1)) * (uint32_t)(128 >> shift);
+      auto row_of = [&](int r) -> const bf16* {
+        if (r >= 128) return t0 + r - 128 < p.rows ? p.x + (size_t)(t0 + r - 128) * p.c : nullptr;
+        if (SHRINK) {                    // n0: the group
+          const int k = r / p.r8, j = r - k * p.r8;
+          return k < here(n0) && j < p.rank ? p.a + ((size_t)s_list[n0 * per_tile + k] * p.rank + j) * p.c : nullptr;
+        }
+        return n0 + r < p.n ? p.w + (size_t)(n0 + r) * p.c : nullptr;
+      };
+      auto place = [&](int r) { return (uint32_t)r * 128 + ((chunk ^ (uint32_t)(r & 7)) << 4) + within; };
+      if (p.unit > 2) {
+#pragma unroll 4
+        for (int r = ct >> shift; r < 128 + TN; r += 32 * kLrCopyWarps >> shift) {
+          const bf16* src = row_of(r);
+          const bool in = src && k0 < p.c;               // rows are whole units: one lies inside its row or outside it
+          if (p.unit == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst_s + place(r)), "l"(in ? src + k0 : p.x), "r"(in ? 8 : 0) : "memory");
+          else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst_s + place(r)), "l"(in ? src + k0 : p.x), "r"(in ? 4 : 0) : "memory");
+        }
+      } else {
+#pragma unroll 1
+        for (int r0 = ct >> 5; r0 < 128 + TN; r0 += 8 * kLrCopyWarps) {      // eight rows' values on their way before the first is stored
+          unsigned short lo[8], hi[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = r0 + i * kLrCopyWarps;
+            const unsigned short* src = r < 128 + TN ? reinterpret_cast<const unsigned short*>(row_of(r)) : nullptr;
+            lo[i] = src && k0 < p.c ? src[k0] : (unsigned short)0;
+            hi[i] = src && k0 + 1 < p.c ? src[k0 + 1] : (unsigned short)0;
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = r0 + i * kLrCopyWarps;
+            if (r < 128 + TN) *reinterpret_cast<uint32_t*>(dst + place(r)) = (uint32_t)lo[i] | (uint32_t)hi[i] << 16;
+          }
+        }
+      }
+      cp_async_commit();
+      if (late >= 0) {                   // one block behind
+        cp_async_wait<1>();
+        landed();
+      }
+      late = s;
+    });
+    if (late >= 0) {
+      cp_async_wait<0>();
+      landed();
+    }
   } else if (warp == 1) {
     if (elect_one()) {
       constexpr uint32_t idesc = umma_idesc(TN);
@@ -386,7 +414,10 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
         const int count = list_adapters(t0, it & 1);
         // A thread has the 16-byte chunk et % 8 of a block's 64 columns, in every sixteenth row of either operand.
         const int ext = ext_blocks(count), all = count * ext_cols, c8 = et & 7, r0 = et >> 3;
-        const bool whole = p.rank % 8 == 0, vec = whole && ((uintptr_t)p.b & 15) == 0;   // eight columns are one part of one adapter; of B_a one load
+        // values of a unit of B_a, of h: they lie in one part of one adapter
+        const int unit_h = p.rank % 8 == 0 ? 8 : p.rank % 4 == 0 ? 4 : p.rank % 2 == 0 ? 2 : 1;
+        int unit_b = unit_h;
+        while ((uintptr_t)p.b & (unit_b * 2 - 1)) unit_b >>= 1;
         // The code of this part is kept short (loops, not copies): it runs a few times a tile, and what it costs is its way into the instruction cache.
         const uint32_t place0 = (uint32_t)(r0 * 128 + ((c8 ^ (r0 & 7)) << 4));      // of row r0; every sixteenth row is 2048 bytes on
         const float per_col = 1.f / (float)ext_cols;
@@ -395,53 +426,53 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
           slot = (int)(((float)c + 0.5f) * per_col), rem = c - slot * ext_cols;      // c < 2^16: the quotient is off by less than half a column
           if (c >= all) slot = -1;
         };
-        auto fetch = [&](uint32_t dst, const void* src, bool in) {
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+        auto fetch = [&](uint32_t dst, const void* src, bool in, int bytes) {
+          if (bytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+          else if (bytes == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(in ? 8 : 0) : "memory");
+          else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(in ? 4 : 0) : "memory");
         };
         auto slot_of_block = [&](int e) { return (int)((xs + (uint32_t)e) % kExt); };
         auto at_block = [&](int e) { return (uint32_t)(S::kOffExt + slot_of_block(e) * S::kStage); };
         auto fill_b = [&](int e) {
           const uint32_t use = xs + (uint32_t)e;
           if (use >= kExt) ok = ok && mbar_wait(ext_empty(slot_of_block(e)), (use / kExt - 1) & 1u, p.err_flag);
-          if (vec) {
+#pragma unroll 1
+          for (int k = 0; k < 8; k += unit_b) {
             int slot, rem;
-            column(e, 0, slot, rem);
+            column(e, k, slot, rem);
             const bf16* src = p.b + ((size_t)(slot >= 0 ? s_list[slot] : 0) * p.n + n0 + r0) * p.rank + (rem < p.rank ? rem : rem - p.rank);
-            uint32_t dst = base + at_block(e) + place0;
+            if (unit_b > 1) {
+              uint32_t dst = base + at_block(e) + place0 + 2 * k;
 #pragma unroll 1
-            for (int f = n0 + r0; f < n0 + 128; f += 16, dst += 2048, src += 16 * p.rank) fetch(dst, slot >= 0 && f < p.n ? src : p.b, slot >= 0 && f < p.n);
-          } else {
-            unsigned short* dst = reinterpret_cast<unsigned short*>(gen + at_block(e) + place0);
-#pragma unroll 1
-            for (int k = 0; k < 8; ++k) {
-              int slot, rem;
-              column(e, k, slot, rem);
-              const unsigned short* src = reinterpret_cast<const unsigned short*>(p.b) + ((size_t)(slot >= 0 ? s_list[slot] : 0) * p.n + n0 + r0) * p.rank + (rem < p.rank ? rem : rem - p.rank);
-#pragma unroll 4
-              for (int m = 0; m < 8; ++m) dst[m * 1024 + k] = slot >= 0 && n0 + r0 + 16 * m < p.n ? src[(size_t)16 * m * p.rank] : (unsigned short)0;
+              for (int f = n0 + r0; f < n0 + 128; f += 16, dst += 2048, src += 16 * p.rank) fetch(dst, slot >= 0 && f < p.n ? src : p.b, slot >= 0 && f < p.n, unit_b * 2);
+            } else {
+              unsigned short* dst = reinterpret_cast<unsigned short*>(gen + at_block(e) + place0) + k;
+              unsigned short v[8];
+#pragma unroll
+              for (int m = 0; m < 8; ++m) v[m] = slot >= 0 && n0 + r0 + 16 * m < p.n ? reinterpret_cast<const unsigned short*>(src)[(size_t)16 * m * p.rank] : (unsigned short)0;
+#pragma unroll
+              for (int m = 0; m < 8; ++m) dst[m * 1024] = v[m];
             }
           }
         };
-        auto fill_h = [&](int e) {
-          if (whole) {                       // the workspace is aligned, and so are eight columns of a row
+        auto fill_h = [&](int e) {         // the workspace is aligned
+#pragma unroll 1
+          for (int k = 0; k < 8; k += unit_h) {
             int slot, rem;
-            column(e, 0, slot, rem);
+            column(e, k, slot, rem);
             const bf16* src = p.h + (size_t)(t0 + r0) * ext_cols + rem;
-            uint32_t dst = base + at_block(e) + S::kABytes + place0;
+            if (unit_h > 1) {
+              uint32_t dst = base + at_block(e) + S::kABytes + place0 + 2 * k;
 #pragma unroll 1
-            for (int t = r0; t < TN; t += 16, dst += 2048, src += 16 * ext_cols) {
-              const bool in = slot >= 0 && s_slot[t] == slot;
-              fetch(dst, in ? src : p.h, in);
-            }
-          } else {
-            unsigned short* dst = reinterpret_cast<unsigned short*>(gen + at_block(e) + S::kABytes + place0);
-#pragma unroll 1
-            for (int k = 0; k < 8; ++k) {
-              int slot, rem;
-              column(e, k, slot, rem);
-              const unsigned short* src = reinterpret_cast<const unsigned short*>(p.h) + (size_t)(t0 + r0) * ext_cols + rem;
+              for (int t = r0; t < TN; t += 16, dst += 2048, src += 16 * ext_cols) {
+                const bool in = slot >= 0 && s_slot[t] == slot;
+                fetch(dst, in ? src : p.h, in, unit_h * 2);
+              }
+            } else {
+              unsigned short* dst = reinterpret_cast<unsigned short*>(gen + at_block(e) + S::kABytes + place0) + k;
 #pragma unroll 4
-              for (int m = 0; m < TN / 16; ++m) dst[m * 1024 + k] = slot >= 0 && s_slot[r0 + 16 * m] == slot ? src[(size_t)16 * m * ext_cols] : (unsigned short)0;
+              for (int m = 0; m < TN / 16; ++m)
+                dst[m * 1024] = slot >= 0 && s_slot[r0 + 16 * m] == slot ? reinterpret_cast<const unsigned short*>(src)[(size_t)16 * m * ext_cols] : (unsigned short)0;
             }
           }
         };
@@ -641,6 +672,17 @@ lowrank_shrink_kernel(const T* __restrict__ x, const T* __restrict__ a, const fl
       if (k < c) {                              // V divides c
         if constexpr (V == 1) {
           sum = acc_fma(Elem<T>::ld(xr + k), Elem<T>::ld(ar + k), sum);
+        } else if constexpr (V * sizeof(T) == 8) {       // four bf16, or two floats
+          const uint2 u = *reinterpret_cast<const uint2*>(xr + k), v = *reinterpret_cast<const uint2*>(ar + k);
+          if constexpr (sizeof(T) == 2) {
+            sum = acc_fma(__uint_as_float(u.x << 16), __uint_as_float(v.x << 16), sum);
+            sum = acc_fma(__uint_as_float(u.x & 0xffff0000u), __uint_as_float(v.x & 0xffff0000u), sum);
+            sum = acc_fma(__uint_as_float(u.y << 16), __uint_as_float(v.y << 16), sum);
+            sum = acc_fma(__uint_as_float(u.y & 0xffff0000u), __uint_as_float(v.y & 0xffff0000u), sum);
+          } else {
+            sum = acc_fma(__uint_as_float(u.x), __uint_as_float(v.x), sum);
+            sum = acc_fma(__uint_as_float(u.y), __uint_as_float(v.y), sum);
+          }
         } else {
           Vec16<T> u, v;
           u.load(xr + k);
@@ -752,21 +794,24 @@ struct LrPlan {
   int jn, h_splits;        // rows of A_a of a CTA there; CTAs that share the K of a tile on the tensor cores
 };
 
-inline LrPlan lr_plan(int rows, int c, int n, int rank, int adapters, int sms) {
+inline LrPlan lr_plan(int rows, int c, int n, int rank, int sms) {
   LrPlan p;
   // Clocks a K block of a tile takes in a full grid, 470 of 128 rows and 750 of 256, times the tiles an SM gets.
   auto rounds = [&](int tn) { return ((long)cdiv(n, 128) * cdiv(rows, tn) + sms - 1) / sms; };
   p.tn = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rounds(256) * 750 <= rounds(128) * 470 ? 256 : 128;
   const int kb = cdiv(c, 64);
-  auto share = [&](long tiles, int per_sm) {           // twice as many CTAs while they fit side by side and each has four blocks of K
+  // Twice as many CTAs while they fit side by side and each has a block of K: an exchange costs less than what further CTAs take off the adapters' columns and the copies.
+  // us, one / two / four blocks at least: 160x360x1756 with 23 adapters of rank 32 19 / 27 / 37, 1166x444x184 16 / 20 / 24, 7x304x300 12 / 16 / 21, 196x312x35
+  // 14 / 16 / 13.  The adapters have no say: rows without one come out the same whatever the others have.
+  auto share = [&](long tiles, int per_sm) {
     int z = 1;
-    while (z < kLrMaxSplits && tiles * z * 2 <= (long)sms * per_sm && kb >= z * 2 * 4) z *= 2;
+    while (z < kLrMaxSplits && tiles * z * 2 <= (long)sms * per_sm && kb >= z * 2) z *= 2;
     return z;
   };
   const long tiles = (long)cdiv(n, 128) * cdiv(rows, p.tn);
   p.persist = p.tn == 256 || (p.tn == 128 && tiles > sms);
   p.splits = p.persist ? 1 : share(tiles, 1);
-  p.simt = rows <= kLrSimtRows;
+  p.simt = (long)rows * rank * c <= kLrSimtWork;
   p.jn = 8;
   while (p.jn > 1 && (long)rows * cdiv(rank, p.jn) < 2L * sms) p.jn /= 2;
   p.h_splits = share(cdiv(rows, kLrShrinkTN), 2);
@@ -782,18 +827,19 @@ inline cudaError_t lr_expand(bool copy, const CUtensorMap& tmW, const CUtensorMa
 template <typename T>
 inline cudaError_t lr_shrink_simt(const T* x, const T* a, const float* scale, const int32_t* which, T* h, int rows, int c, int rank, int adapters, int jn, cudaStream_t st) {
   constexpr int V = Elem<T>::kVec;
-  const bool vec = c % V == 0 && (((uintptr_t)x | (uintptr_t)a) & 15) == 0;
+  const uintptr_t bits = (uintptr_t)x | (uintptr_t)a;
   const dim3 grid(rows, cdiv(rank, jn));
-  if (vec) lowrank_shrink_kernel<T, V><<<grid, 256, 0, st>>>(x, a, scale, which, h, c, rank, adapters, jn);
+  if (c % V == 0 && (bits & 15) == 0) lowrank_shrink_kernel<T, V><<<grid, 256, 0, st>>>(x, a, scale, which, h, c, rank, adapters, jn);
+  else if (c % (V / 2) == 0 && (bits & 7) == 0) lowrank_shrink_kernel<T, V / 2><<<grid, 256, 0, st>>>(x, a, scale, which, h, c, rank, adapters, jn);
   else lowrank_shrink_kernel<T, 1><<<grid, 256, 0, st>>>(x, a, scale, which, h, c, rank, adapters, jn);
   return cudaGetLastError();
 }
 
 inline cudaError_t lr_run_bf16(const LrContext& ctx, LrArgs a, cudaStream_t st) {
-  const LrPlan p = lr_plan(a.rows, a.c, a.n, a.rank, a.adapters, ctx.sm_count);
+  const LrPlan p = lr_plan(a.rows, a.c, a.n, a.rank, ctx.sm_count);
   const uintptr_t bits = (uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.a;
   const bool copy = a.c % 8 != 0 || (bits & 15) != 0;
-  a.pairs = a.c % 2 == 0 && (bits & 3) == 0;
+  a.unit = a.c % 4 == 0 && (bits & 7) == 0 ? 8 : a.c % 2 == 0 && (bits & 3) == 0 ? 4 : 2;
   a.r8 = (int)align_up(a.rank, 8);
   const bool wide = a.adapters > 0 && !p.simt;         // h on the tensor cores
   CUtensorMap tmW = {}, tmX = {}, tmA = {}, tmH = {};
@@ -825,7 +871,7 @@ inline cudaError_t lr_run_bf16(const LrContext& ctx, LrArgs a, cudaStream_t st) 
 // the fp32 model as a 1x1 layer of one pixel a row, which adds that share.
 inline cudaError_t lr_run_f32(const LrContext& ctx, const float* x, const float* w, const float* bias, const float* a, const float* b, const float* scale,
                               const int32_t* which, float* h, float* y, int rows, int c, int n, int rank, int adapters, int* err_flag, cudaStream_t st) {
-  const LrPlan p = lr_plan(rows, c, n, std::max(rank, 1), adapters, ctx.sm_count);
+  const LrPlan p = lr_plan(rows, c, n, std::max(rank, 1), ctx.sm_count);
   if (adapters > 0) {
     cudaError_t e = lr_shrink_simt<float>(x, a, scale, which, h, rows, c, rank, adapters, p.jn, st);
     if (e != cudaSuccess) return e;
