@@ -299,7 +299,7 @@ conv_igemm_f64mma_kernel(const float* __restrict__ x, const float* __restrict__ 
 
 template <int WM, int WN, int KG, int MF, int NF, int V>
 inline cudaError_t f32_launch_t(const F32Plan& p, const float* x, const float* w, const float* scale, const float* bias, const float* residual,
-                                float* y, const ConvGeom& g, int* err_flag, long long wait_cycles, cudaStream_t st) {
+                                float* y, const ConvGeom& g, int* err_flag, long long wait_cycles, cudaStream_t st, bool early) {
   using S = F32Tile<WM, WN, KG, MF, NF>;
   if (p.z > 1 && S::kRecv == 0) return cudaErrorInvalidValue;   // no room for what a cluster's CTAs send
   const int K = g.kh * g.kw * g.Cin;
@@ -311,7 +311,7 @@ inline cudaError_t f32_launch_t(const F32Plan& p, const float* x, const float* w
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[0].val.programmaticStreamSerializationAllowed = early ? 1 : 0;
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = p.z;
@@ -322,19 +322,21 @@ inline cudaError_t f32_launch_t(const F32Plan& p, const float* x, const float* w
 
 template <int V>
 inline cudaError_t f32_launch_v(const F32Plan& p, const float* x, const float* w, const float* scale, const float* bias, const float* residual,
-                                float* y, const ConvGeom& g, int* err_flag, long long wait_cycles, cudaStream_t st) {
+                                float* y, const ConvGeom& g, int* err_flag, long long wait_cycles, cudaStream_t st, bool early) {
   switch (p.tile) {
-    case 1: return f32_launch_t<2, 2, 2, 2, 4, V>(p, x, w, scale, bias, residual, y, g, err_flag, wait_cycles, st);
-    case 2: return f32_launch_t<1, 1, 8, 2, 4, V>(p, x, w, scale, bias, residual, y, g, err_flag, wait_cycles, st);
-    case 3: return f32_launch_t<1, 1, 8, 1, 4, V>(p, x, w, scale, bias, residual, y, g, err_flag, wait_cycles, st);
-    default: return f32_launch_t<4, 2, 1, 1, 2, V>(p, x, w, scale, bias, residual, y, g, err_flag, wait_cycles, st);
+    case 1: return f32_launch_t<2, 2, 2, 2, 4, V>(p, x, w, scale, bias, residual, y, g, err_flag, wait_cycles, st, early);
+    case 2: return f32_launch_t<1, 1, 8, 2, 4, V>(p, x, w, scale, bias, residual, y, g, err_flag, wait_cycles, st, early);
+    case 3: return f32_launch_t<1, 1, 8, 1, 4, V>(p, x, w, scale, bias, residual, y, g, err_flag, wait_cycles, st, early);
+    default: return f32_launch_t<4, 2, 1, 1, 2, V>(p, x, w, scale, bias, residual, y, g, err_flag, wait_cycles, st, early);
   }
 }
 
+// early: before the kernel in front of it has finished; its weights, scale and bias are then no output of a kernel that may still run.
 inline cudaError_t f32_launch(const F32Plan& p, const float* x, const float* w, const float* scale, const float* bias, const float* residual,
-                              float* y, const ConvGeom& g, int* err_flag, long long wait_cycles, cudaStream_t st) {
+                              float* y, const ConvGeom& g, int* err_flag, long long wait_cycles, cudaStream_t st, bool early = true) {
   const bool vec = g.Cin % 4 == 0 && (((uintptr_t)x | (uintptr_t)w) & 15) == 0;
-  return vec ? f32_launch_v<4>(p, x, w, scale, bias, residual, y, g, err_flag, wait_cycles, st) : f32_launch_v<1>(p, x, w, scale, bias, residual, y, g, err_flag, wait_cycles, st);
+  return vec ? f32_launch_v<4>(p, x, w, scale, bias, residual, y, g, err_flag, wait_cycles, st, early)
+             : f32_launch_v<1>(p, x, w, scale, bias, residual, y, g, err_flag, wait_cycles, st, early);
 }
 
 inline ee_status_t f32_context_init() {

@@ -889,7 +889,8 @@ inline cudaError_t lr_run_f32(const LrContext& ctx, const float* x, const float*
   }
   const bool vec = c % 4 == 0 && (((uintptr_t)x | (uintptr_t)w) & 15) == 0;
   const ConvGeom g{rows, 1, 1, c, 1, 1, n, 1, 1, 1, 0, 0, EE_ACT_NONE};
-  return f32_launch(f32_plan(rows, n, c, ctx.sm_count, vec), x, w, nullptr, bias, adapters > 0 ? y : nullptr, y, g, err_flag, kTcWaitCycles, st);
+  // Behind the adapters' launches, which the stream's past is over for, W and the bias may be fetched early; behind anything else they may be its output.
+  return f32_launch(f32_plan(rows, n, c, ctx.sm_count, vec), x, w, nullptr, bias, adapters > 0 ? y : nullptr, y, g, err_flag, kTcWaitCycles, st, adapters > 0);
 }
 
 }  // namespace ee

@@ -674,3 +674,30 @@ def test_silu_is_for_group_norm_alone():
     spec.stages[0].layers[0].act = wl.ACT_SILU
     with pytest.raises(eb.EEError):
         eb.EEModel(spec)
+
+
+# ----------------------------------------------------------------------------- calls behind one another
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("adapters", [0, 2])
+def test_a_projection_whose_weight_the_call_before_it_writes(dtype, adapters):
+    """weight = W2 (the first call's output), bias = probabilities (the second call's): both are there when they are read."""
+    rows, c, n, rank = 4, 1024, 384, 8
+    x, w, _, a, b, _, which = linear_operands(5, rows, c, n, rank, 2, dtype)
+    inner = (normal(gen(6), c, 512) * 512 ** -0.5).to(TD[dtype])
+    logits = normal(gen(7), 1, n)
+    w2, bias, y = torch.zeros_like(w), torch.zeros((1, n), device="cuda"), torch.zeros((rows, n), dtype=TD[dtype], device="cuda")
+    outer = (normal(gen(8), n, 512) * 512 ** -0.5).to(TD[dtype])
+    ws = torch.empty(eb.adapted_linear_workspace_bytes(rows, rank), dtype=torch.uint8, device="cuda")
+
+    def run():
+        eb.adapted_linear(dtype, outer, n, 512, inner, c, None, None, 0, 0, None, w2, None)
+        eb.softmax("f32", logits, 1, n, bias)
+        eb.adapted_linear(dtype, x, rows, c, w2, n, a if adapters else None, b if adapters else None, rank, adapters, which if adapters else None, y,
+                          ws if adapters else None, bias=bias)
+
+    for times in range(5):
+        w2.zero_(), bias.zero_(), y.zero_()
+        run()
+        linear_check(y, x, w2, bias[0], a[:adapters], b[:adapters], None, which, dtype)
+        assert bool((w2 != 0).any())
