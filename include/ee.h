@@ -392,7 +392,7 @@ ee_status_t ee_model_check(ee_model_t* model, void* cuda_stream);
  * statistics and sums in fp32, one rounding to the model dtype.  x, residual (or NULL), y: [batch][hw][c]; gamma (NULL = 1)
  * and beta (NULL = 0): [c] fp32.  Unlike a folded batch norm it takes its statistics from the sample itself, so it suits a batch
  * that shrinks and is refilled: the bits of a sample do not depend on the batch.  y may be x or residual (in place); other
- * overlaps are refused.  act: ee_act_t.  Errors: INVALID_ARG, CAPACITY (a grid beyond 2^31 - 1 blocks), CUDA. */
+ * overlaps are refused.  act: ee_act_t.  Errors: INVALID_ARG, CAPACITY (a grid beyond 2^31 - 1 blocks, a block beyond as many loads), CUDA. */
 ee_status_t ee_group_norm(int dtype, const void* x, const void* residual, int batch, int hw, int c, int groups, const float* gamma,
                           const float* beta, float eps, int act, void* y, void* cuda_stream);
 
@@ -404,8 +404,9 @@ ee_status_t ee_group_norm(int dtype, const void* x, const void* residual, int ba
  * in fp32 (a x enters the second product as two bf16 parts, 2^-17 of it), fp32 products in fp64; one rounding to dtype.
  * rank: 1 to 128.  n_adapters = 0 is the plain projection (a, b, adapter and workspace may be NULL).  `workspace` (256-byte
  * aligned): at least ee_adapted_linear_workspace_bytes(rows, rank) bytes, undefined afterwards; calls that may overlap (two
- * streams, or two captured graphs) need one each.  y must not overlap x or the workspace.  How the sums are grouped depends
- * on the number of rows, so a row's last bit may.  Errors: INVALID_ARG, CAPACITY (workspace too small, more than 2^22 rows), CUDA. */
+ * streams, or two captured graphs) need one each.  y and the workspace must not overlap anything else.  How the sums are grouped depends
+ * on the number of rows, so a row's last bit may.  Errors: INVALID_ARG, CAPACITY (workspace too small, more than 2^22 rows, c or
+ * n above 2^20), CUDA. */
 ee_status_t ee_adapted_linear(int dtype, const void* x, int rows, int c, const void* weight, int n, const float* bias, const void* a,
                               const void* b, int rank, int n_adapters, const float* scale, const int32_t* adapter, void* y,
                               void* workspace, size_t workspace_bytes, void* cuda_stream);
@@ -429,7 +430,7 @@ ee_status_t ee_softmax(int dtype, const void* logits, int rows, int n, const flo
  *   leaves nothing; where all are, from p[n_draft], the row behind them.  The draw is the first v whose running sum (fp64)
  *   exceeds r times the total; values that are not positive and finite weigh nothing; -1 where nothing weighs anything.
  * tokens: [batch][k + 1]: the accepted drafts, the drawn token, then -1.  n_accepted: [batch].  p may hold anything in rows behind
- * the one drawn from, and q too.  k = 0 draws from p (q, drafts and u may be NULL).  Errors: INVALID_ARG, CAPACITY, CUDA. */
+ * the one drawn from, and q too.  k = 0 draws from p (q, drafts and u may be NULL).  tokens and n_accepted must not overlap anything else.  Errors: INVALID_ARG, CAPACITY, CUDA. */
 ee_status_t ee_verify_drafts(const float* p, const float* q, const int32_t* drafts, const float* u, const float* r, const int32_t* n_draft,
                              int batch, int k, int n, int32_t* tokens, int32_t* n_accepted, void* cuda_stream);
 

@@ -1887,16 +1887,21 @@ ee_status_t ee_adapted_linear(int dtype, const void* x, int rows, int c, const v
   if ((dtype != EE_F32 && dtype != EE_BF16) || rows < 0 || c < 1 || n < 1 || n_adapters < 0) return EE_ERR_INVALID_ARG;
   if (n_adapters > 0 && (rank < 1 || rank > kLrMaxRank || (long)n_adapters * rank > 0x7fffffffL)) return EE_ERR_INVALID_ARG;
   if (rows == 0) return EE_OK;
-  if (rows > 1 << 22) return EE_ERR_CAPACITY;
+  if (rows > 1 << 22 || c > 1 << 20 || n > 1 << 20) return EE_ERR_CAPACITY;
   const size_t es = esize(dtype), xb = (size_t)rows * c * es, yb = (size_t)rows * n * es;
-  if (!x || !weight || !y || !aligned_to(x, es) || !aligned_to(weight, es) || !aligned_to(y, es) || !aligned_to(bias, 4) || !apart(x, xb, y, yb))
+  if (!x || !weight || !y || !aligned_to(x, es) || !aligned_to(weight, es) || !aligned_to(y, es) || !aligned_to(bias, 4) || !apart(x, xb, y, yb) ||
+      !apart(weight, (size_t)n * c * es, y, yb) || !apart(bias, (size_t)n * 4, y, yb))
     return EE_ERR_INVALID_ARG;
   if (n_adapters > 0) {
     if (!a || !b || !adapter || !workspace || !aligned_to(a, es) || !aligned_to(b, es) || !aligned_to(scale, 4) || !aligned_to(adapter, 4) || !aligned_to(workspace, 256))
       return EE_ERR_INVALID_ARG;
     const size_t need = ee_adapted_linear_workspace_bytes(rows, rank);
     if (workspace_bytes < need) return EE_ERR_CAPACITY;
-    if (!apart(workspace, need, y, yb) || !apart(workspace, need, x, xb)) return EE_ERR_INVALID_ARG;
+    auto clear = [&](const void* p, size_t bytes) { return !p || (apart(p, bytes, y, yb) && apart(p, bytes, workspace, need)); };
+    if (!apart(workspace, need, y, yb) || !clear(x, xb) || !clear(weight, (size_t)n * c * es) || !clear(bias, (size_t)n * 4) ||
+        !clear(a, (size_t)n_adapters * rank * c * es) || !clear(b, (size_t)n_adapters * n * rank * es) || !clear(scale, (size_t)n_adapters * 4) ||
+        !clear(adapter, (size_t)rows * 4))
+      return EE_ERR_INVALID_ARG;
   }
   const OperatorContext* ctx;
   const ee_status_t s = operator_context(&ctx);
@@ -1920,6 +1925,7 @@ ee_status_t ee_softmax(int dtype, const void* logits, int rows, int n, const flo
   const size_t es = esize(dtype);
   if (!logits || !probs || !aligned_to(logits, es) || !aligned_to(probs, 4) || !aligned_to(temperature, 4)) return EE_ERR_INVALID_ARG;
   if (!(dtype == EE_F32 && logits == (const void*)probs) && !apart(logits, (size_t)rows * n * es, probs, (size_t)rows * n * 4)) return EE_ERR_INVALID_ARG;
+  if (!(temperature == nullptr || apart(temperature, (size_t)rows * 4, probs, (size_t)rows * n * 4))) return EE_ERR_INVALID_ARG;
   if (n > kSmMost || (long)rows * kSmMaxCluster > 0x7fffffffL) return EE_ERR_CAPACITY;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   const OperatorContext* ctx;
@@ -1939,6 +1945,11 @@ ee_status_t ee_verify_drafts(const float* p, const float* q, const int32_t* draf
       !aligned_to(tokens, 4) || !aligned_to(n_accepted, 4))
     return EE_ERR_INVALID_ARG;
   if ((long)batch * kVfMaxCluster > 0x7fffffffL || k > 0x7fffffff - 64) return EE_ERR_CAPACITY;
+  const size_t all = (size_t)batch * k * 4, row = (size_t)batch * 4;
+  auto clear = [&](const void* in, size_t bytes) { return !in || (apart(in, bytes, tokens, all + row) && apart(in, bytes, n_accepted, row)); };
+  if (!apart(tokens, all + row, n_accepted, row) || !clear(p, (all + row) * n) || !clear(q, all * n) || !clear(drafts, all) || !clear(u, all) || !clear(r, row) ||
+      !clear(n_draft, row))
+    return EE_ERR_INVALID_ARG;
   const OperatorContext* ctx;
   const ee_status_t s = operator_context(&ctx);
   if (s != EE_OK) return s;

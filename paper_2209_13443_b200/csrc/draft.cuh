@@ -304,7 +304,7 @@ struct VerifyArgs {
 // The weight of one value: what the draw goes by.  Values that are not positive and finite weigh nothing.
 __device__ __forceinline__ double verify_weight(float p, float q) {
   const double w = (double)p - (double)q;
-  return w > 0.0 && p < INFINITY ? w : 0.0;
+  return w > 0.0 && w < INFINITY ? w : 0.0;     // an infinite p or q: infinite, or NaN
 }
 
 __device__ __forceinline__ double warp_scan(double v, int lane) {   // inclusive

@@ -72,7 +72,8 @@ __device__ __forceinline__ void mbar_arrive_n(uint32_t bar, uint32_t n) {
 __device__ __forceinline__ void lr_store(bf16* h, int t, int j, int rank, float v) {
   const bf16 hi = __float2bfloat16_rn(v);
   h[((size_t)t * 2) * rank + j] = hi;
-  h[((size_t)t * 2 + 1) * rank + j] = __float2bfloat16_rn(v - __bfloat162float(hi));
+  const float rest = v - __bfloat162float(hi);
+  h[((size_t)t * 2 + 1) * rank + j] = __float2bfloat16_rn(isfinite(rest) ? rest : 0.f);   // of an infinity nothing is left
 }
 __device__ __forceinline__ void lr_store(float* h, int t, int j, int rank, float v) { h[(size_t)t * rank + j] = v; }
 
@@ -94,7 +95,7 @@ __device__ __noinline__ float lr_not_finite(const LrArgs& p, int t, int f, int a
 }
 
 // tmA: rows of operand A (W in boxes of 128 filters; SHRINK: all adapters' A in boxes of r8 rows), tmX: rows of x in boxes of TN.
-// Tile: blockIdx.x of filters, y of rows, z: range of K.  Persistent: every gridDim.x-th tile, filters first.  SHRINK: a CTA takes the adapters of its rows in groups
+// Tile: blockIdx.x of filters, y of rows, z: range of K.  Persistent: every gridDim.x-th tile, filters first.  SHRINK: blockIdx.x of rows; a CTA takes the adapters of its rows in groups
 // that fill the 128 rows of operand A, one after the other; a row of x has one adapter, so all groups leave their numbers in the same array.
 template <int TN, bool PERSIST, bool SHRINK, bool COPY>
 __global__ void __launch_bounds__(COPY ? 192 + 32 * kLrCopyWarps : 224)
@@ -128,6 +129,10 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
   int tiles = kPersist ? tiles_n * ((p.rows + TN - 1) / TN) : 1;
   const int tile0 = kPersist ? (int)blockIdx.x : 0, tile_step = kPersist ? (int)gridDim.x : 1;
   auto place_of = [&](int tile, int& n0, int& t0) {
+    if (SHRINK) {
+      n0 = 0, t0 = (int)blockIdx.x * TN;
+      return;
+    }
     n0 = (kPersist ? tile % tiles_n : (int)blockIdx.x) * 128, t0 = (kPersist ? tile / tiles_n : (int)blockIdx.y) * TN;
   };
   const int kb_all = (p.c + 63) / 64;
@@ -852,7 +857,7 @@ inline cudaError_t lr_run_bf16(const LrContext& ctx, LrArgs a, cudaStream_t st) 
     if (e != cudaSuccess) return e;
   }
   if (wide) {
-    const dim3 grid(1, cdiv(a.rows, kLrShrinkTN), p.h_splits);
+    const dim3 grid(cdiv(a.rows, kLrShrinkTN), 1, p.h_splits);
     e = copy ? lr_launch_k<kLrShrinkTN, false, true, true>(tmA, tmH, a, grid, st) : lr_launch_k<kLrShrinkTN, false, true, false>(tmA, tmH, a, grid, st);
   } else if (a.adapters > 0) {
     e = lr_shrink_simt<bf16>(a.x, a.a, a.scale, a.which, a.h, a.rows, a.c, a.rank, a.adapters, p.jn, st);

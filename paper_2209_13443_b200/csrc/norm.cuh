@@ -84,7 +84,7 @@ inline NormPlan norm_plan(int hw, int c, int groups, int es, bool aligned) {
   p.cluster = 1;
   const long row = (long)s * es;
   while (p.cluster < kNormMaxCluster && p.cluster * 2 <= hw && ((long)hw + p.cluster - 1) / p.cluster * row > kNormChunk) p.cluster *= 2;
-  p.rows = (hw + p.cluster - 1) / p.cluster;
+  p.rows = (int)(((long)hw + p.cluster - 1) / p.cluster);
   p.resident = p.rows * row <= kNormMaxChunk;
   p.chunk = p.resident ? (int)align_up((size_t)(p.rows * row), 16) : 0;
   // few accesses: few threads, so that each still has some
@@ -328,7 +328,7 @@ group_norm_kernel(const __grid_constant__ NormArgs p) {
     }
   }
   __syncthreads();
-    bool lost = false;
+  bool lost = false;
   if (cluster > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");    // every CTA's barrier is set up
   for (int g = warp; g < p.groups; g += NW) {
     auto over = [&](auto&& term) {       // the group's bins of every row, 32 at a time
@@ -493,8 +493,8 @@ inline cudaError_t norm_launch_v(const NormPlan& pl, const NormArgs& a, long uni
   return cudaErrorInvalidValue;
 }
 
-// Whether a grid holds a call's blocks: its limit is 2^31 - 1.
-inline bool norm_fits(const NormPlan& pl, long batch) { return batch * pl.slices * pl.cluster <= 0x7fffffffL; }
+// Whether a grid holds a call's blocks, and an int a CTA's accesses: the limit is 2^31 - 1.
+inline bool norm_fits(const NormPlan& pl, long batch) { return batch * pl.slices * pl.cluster <= 0x7fffffffL && (long)pl.rows * pl.sv <= 0x7fffffffL - 4096; }
 
 template <typename T>
 inline cudaError_t norm_launch(const void* x, const void* residual, void* y, const float* gamma, const float* beta, float eps, long batch, int hw, int c,

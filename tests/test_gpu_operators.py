@@ -392,7 +392,7 @@ def verify_exact(p, q, drafts, u, r, count, tokens, accepted):
         def weights(minus):
             with np.errstate(invalid="ignore"):
                 w = p[i, j] - minus
-            w[~((w > 0) & (p[i, j] < np.inf))] = 0.0
+            w[~((w > 0) & (w < np.inf))] = 0.0
             return w
         w = weights(0.0)
         if j < have:
@@ -701,3 +701,41 @@ def test_a_projection_whose_weight_the_call_before_it_writes(dtype, adapters):
         run()
         linear_check(y, x, w2, bias[0], a[:adapters], b[:adapters], None, which, dtype)
         assert bool((w2 != 0).any())
+
+
+# ----------------------------------------------------------------------------- at the ends of what they take
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_adapted_linear_of_the_most_rows(dtype):
+    """2^22 rows: more blocks than the second and third dimension of a grid take."""
+    rows, c, n = 1 << 22, 8, 1
+    ops = linear_operands(3, rows, c, n, 2, 3, dtype)
+    linear_run(dtype, ops)
+
+
+@pytest.mark.parametrize("shape", [(300, 520, 4099, 24, 7), (700, 70, 5000, 16, 30), (700, 71, 5000, 3, 30), (290, 264, 9000, 5, 3)], ids=str)
+def test_adapted_linear_of_more_tiles_than_processors(shape):
+    linear_run("bf16", linear_operands(sum(shape), *shape, "bf16"))
+
+
+@pytest.mark.parametrize("rows", [6, 200])
+def test_adapted_linear_of_an_infinite_sum(rows):
+    """a x is an infinity: the row is one, with the sign of b, and the others are not touched."""
+    x, w, bias, a, b, scale, which = linear_operands(4, rows, 256, 130, 1, 2, "bf16")
+    x, a = x.abs(), a.abs()
+    b[b == 0] = 1.0
+    scale[1] = float("inf")
+    y, _ = out_like((rows, 130), torch.bfloat16)
+    ws = torch.empty(eb.adapted_linear_workspace_bytes(rows, 1), dtype=torch.uint8, device="cuda")
+    eb.adapted_linear("bf16", x, rows, 256, w, 130, a, b, 1, 2, which, y, ws, bias=bias, scale=scale)
+    hit = which == 1
+    assert bool(hit.any()) and torch.equal(y[hit], torch.copysign(torch.full_like(y[hit], float("inf")), b[1, :, 0].expand(int(hit.sum()), 130)))
+    linear_check(y[~hit], x[~hit], w, bias, a, b, torch.ones_like(scale) * scale[0], torch.where(which == 1, -1, which)[~hit], "bf16")
+
+
+@pytest.mark.parametrize("n", [70, 9000])
+def test_verify_drafts_where_the_early_probabilities_are_infinite(n):
+    p, q, d, u, r = drafts_of(n, 6, 2, n)
+    q[0, :, 3::2], q[1, :, ::3], q[2] = -float("inf"), float("inf"), -float("inf")
+    verify_case(p, q, d, u * 0 + 1 - 2.0 ** -24, r)
+    verify_case(p, q, d, u, r)

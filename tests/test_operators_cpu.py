@@ -33,6 +33,9 @@ def test_group_norm_of_nothing_and_of_too_much():
     assert call("ee_group_norm", NORM, batch=0, x=None, y=None, residual=None) == 0
     # a slice a block at the least: 2^31 - 1 samples of two slices are more blocks than a grid has
     assert call("ee_group_norm", NORM, batch=2 ** 31 - 1, hw=256, c=256, groups=2, residual=None, x=1 << 50, y=1 << 60) == CAPACITY
+    # a group of 2^22 pixels of 65521 odd rows: 2^35 loads of a block
+    assert call("ee_group_norm", NORM, batch=1, hw=1 << 22, c=65521, groups=1, residual=None, x=1 << 50, y=1 << 60) == CAPACITY
+    assert call("ee_group_norm", NORM, batch=2 ** 31 - 1, hw=2 ** 31 - 1, c=1, groups=1, residual=None, x=1 << 40, y=1 << 60) == CAPACITY
 
 
 LINEAR = dict(dtype=BF16, x=P[0], rows=5, c=64, weight=P[1], n=40, bias=P[2], a=P[3], b=P[4], rank=8, n_adapters=3, scale=P[5], adapter=P[6], y=P[7], workspace=P[8],
@@ -55,13 +58,21 @@ def test_adapted_linear_workspace():
     assert call("ee_adapted_linear", LINEAR, workspace_bytes=5 * 8 * 4 - 1) == CAPACITY
     assert call("ee_adapted_linear", LINEAR, rows=(1 << 22) + 1) == CAPACITY
     assert call("ee_adapted_linear", LINEAR, rows=0, x=None, weight=None, y=None) == 0
+    for size in ("c", "n"):
+        assert call("ee_adapted_linear", LINEAR, **{size: (1 << 20) + 1}) == CAPACITY
+
+
+@pytest.mark.parametrize("changed", [dict(y=P[1] + 40 * 64 * 2 - 2), dict(y=P[2] + 40 * 4 - 2), dict(y=P[3]), dict(y=P[4] + 3 * 40 * 8 * 2 - 2), dict(y=P[5]), dict(y=P[6] + 2), dict(workspace=P[1]),
+                                     dict(workspace=P[2]), dict(workspace=P[3] + 256), dict(workspace=P[4]), dict(workspace=P[5]), dict(workspace=P[6])])
+def test_adapted_linear_refuses_outputs_on_top_of_inputs(changed):
+    assert call("ee_adapted_linear", LINEAR, **changed) == INVALID
 
 
 SOFTMAX = dict(dtype=F32, logits=P[0], rows=3, n=100, temperature=P[1], probs=P[2], stream=None)
 
 
 @pytest.mark.parametrize("changed", [dict(dtype=3), dict(rows=-1), dict(n=0), dict(logits=None), dict(probs=None), dict(logits=P[0] + 2), dict(probs=P[2] + 2), dict(temperature=P[1] + 1),
-                                     dict(probs=P[0] + 4), dict(dtype=BF16, probs=P[0])])
+                                     dict(probs=P[0] + 4), dict(dtype=BF16, probs=P[0]), dict(temperature=P[2] + 1196)])
 def test_softmax_refuses(changed):
     assert call("ee_softmax", SOFTMAX, **changed) == INVALID
 
@@ -79,6 +90,12 @@ VERIFY = dict(p=P[0], q=P[1], drafts=P[2], u=P[3], r=P[4], n_draft=P[5], batch=2
                                      dict(p=P[0] + 2), dict(q=P[1] + 1), dict(drafts=P[2] + 2), dict(u=P[3] + 2), dict(r=P[4] + 1), dict(n_draft=P[5] + 2), dict(tokens=P[6] + 2),
                                      dict(n_accepted=P[7] + 2)])
 def test_verify_drafts_refuses(changed):
+    assert call("ee_verify_drafts", VERIFY, **changed) == INVALID
+
+
+@pytest.mark.parametrize("changed", [dict(tokens=P[0] + 2 * 4 * 10 * 4 - 4), dict(tokens=P[1]), dict(tokens=P[2]), dict(tokens=P[3] + 20), dict(tokens=P[4] + 4), dict(tokens=P[5]), dict(tokens=P[7] - 4),
+                                     dict(n_accepted=P[2] + 20), dict(n_accepted=P[5]), dict(n_accepted=P[6] + 28)])
+def test_verify_drafts_refuses_outputs_on_top_of_inputs(changed):
     assert call("ee_verify_drafts", VERIFY, **changed) == INVALID
 
 
