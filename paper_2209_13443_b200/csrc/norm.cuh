@@ -25,7 +25,8 @@ namespace ee {
 constexpr int kNormMaxCluster = 8;
 // Bytes of a CTA's part of a unit that a cluster is cut for, and up to which it stays in shared memory where eight CTAs are not enough for that: four CTAs then
 // share an SM.  Larger parts are read a second time, from L2.  us, 28 / 56 KB parts: 13 x 33 x 29 x 96 fp32 6.4 / 7.9; the second read in place of two CTAs an SM:
-// 32 x 112 x 112 x 96 84 -> 65 (parts of 150 KB), of four: 64 x 56 x 56 x 256 62 -> 68 (50 KB).
+// 32 x 112 x 112 x 96 84 -> 65 (parts of 150 KB), of four: 64 x 56 x 56 x 256 62 -> 68 (50 KB).  Parts of up to 104 KB kept by CTAs of 512 threads won and lost:
+// 64 x 80 x 80 x 128 63 -> 56, 16 of them 18.6 -> 19.8, 32 x 72 x 72 x 96 28.8 -> 30.
 constexpr int kNormChunk = 28 << 10;
 constexpr int kNormMaxChunk = 56 << 10;
 
@@ -36,7 +37,7 @@ struct NormPlan {
   int cluster, rows; // CTAs of a slice, pixels of each
   int threads;
   bool wide;         // a pixel of the slice is more than the CTA's threads take at once; the slice is then one group
-  bool merged;       // an access lies in one group: its elements are summed together
+  int parts;         // an access falls into so many runs that lie in one group each and are summed together
   bool resident;
   int chunk, red_rows, bins;   // bytes of a CTA's part; partial statistics: rows and columns
   int smem() const { return chunk + red_rows * bins * 8 + groups * 8 * (cluster + 1) + 8; }
@@ -63,7 +64,9 @@ inline int norm_gcd(int a, int b) {
   return a;
 }
 
-constexpr int kNormThreads = 256, kNormFew = 128;
+// Threads of a CTA: many where the part does not stay in shared memory and is read twice, for the loads in flight of few samples.  us, 256 / 512 threads there:
+// 4 x 128 x 128 x 128 30 / 22.5, 1 x 224 x 224 x 32 33 / 24, 16 x 112 x 112 x 64 28.5 / 23.4, 32 x 112 x 112 x 96 51 / 54 (1024: 76).
+constexpr int kNormThreads = 256, kNormFew = 128, kNormMany = 512;
 
 inline NormPlan norm_plan(int hw, int c, int groups, int es, bool aligned) {
   NormPlan p = {};
@@ -80,7 +83,7 @@ inline NormPlan norm_plan(int hw, int c, int groups, int es, bool aligned) {
     for (int d = 1; d <= units; ++d)
       if (units % d == 0 && (long)unit * d * es <= most && unit * d / p.v <= kNormThreads) m = d;
   const int s = unit * m;
-  p.sv = s / p.v, p.slices = c / s, p.groups = s / cpg, p.merged = cpg % p.v == 0;
+  p.sv = s / p.v, p.slices = c / s, p.groups = s / cpg, p.parts = p.v / norm_gcd(p.v, cpg);
   p.cluster = 1;
   const long row = (long)s * es;
   while (p.cluster < kNormMaxCluster && p.cluster * 2 <= hw && ((long)hw + p.cluster - 1) / p.cluster * row > kNormChunk) p.cluster *= 2;
@@ -88,8 +91,8 @@ inline NormPlan norm_plan(int hw, int c, int groups, int es, bool aligned) {
   p.resident = p.rows * row <= kNormMaxChunk;
   p.chunk = p.resident ? (int)align_up((size_t)(p.rows * row), 16) : 0;
   // few accesses: few threads, so that each still has some
-  p.threads = p.resident && p.sv <= kNormFew && (long)p.rows * p.sv <= 4 * kNormFew ? kNormFew : kNormThreads;
-  p.bins = p.wide ? 1 : p.sv * (p.merged ? 1 : p.v);
+  p.threads = !p.resident ? kNormMany : p.sv <= kNormFew && (long)p.rows * p.sv <= 4 * kNormFew ? kNormFew : kNormThreads;
+  p.bins = p.wide ? 1 : p.sv * p.parts;
   p.red_rows = p.wide || p.sv <= 32 ? p.threads / 32 : p.threads / p.sv;
   return p;
 }
@@ -151,13 +154,15 @@ __device__ __forceinline__ f32x2 pair_fma(f32x2 a, f32x2 b, f32x2 c) {
   return d;
 }
 
-// V elements per access, MERGED and WIDE as in NormPlan; RESIDENT: the CTA's pixels stay in shared memory; NT threads.
-template <typename T, int V, bool MERGED, bool WIDE, bool RESIDENT, int NT>
-__global__ void __launch_bounds__(NT, MERGED ? 1024 / NT : 768 / NT)
+// V elements per access in K parts, WIDE as in NormPlan; RESIDENT: the CTA's pixels stay in shared memory; NT threads.  With up to two
+// sums, or four of pairs, a thread's state leaves room for 1024 threads an SM (64 registers): 64 x 56 x 56 x 192 in groups of 6 60 -> 51 us; four single ones, 13 x 33 x 29 x 96 fp32
+// in groups of 3, take 6.4 us with 80 registers and 8.1 with 64.
+template <typename T, int V, int K, bool WIDE, bool RESIDENT, int NT>
+__global__ void __launch_bounds__(NT, !RESIDENT || K <= 2 || (K == 4 && V == 8) ? 1024 / NT : 768 / NT)
 group_norm_kernel(const __grid_constant__ NormArgs p) {
-  static_assert(!WIDE || MERGED, "a wide slice is one group");
+  static_assert(!WIDE || K == 1, "a wide slice is one group");
   typedef NormVec<T, V> Vec;
-  constexpr int K = MERGED ? 1 : V;                    // sums per thread
+  constexpr int G = V / K;                             // elements of a part
   constexpr int P = V > 1 ? V / 2 : 1;                 // pairs of an access
   constexpr int NW = NT / 32;
   extern __shared__ __align__(16) uint8_t norm_smem[];
@@ -237,7 +242,7 @@ group_norm_kernel(const __grid_constant__ NormArgs p) {
   const float n_here = (float)rows * (float)p.cpg, inv_here = rows > 0 ? 1.f / n_here : 0.f, inv_all = 1.f / ((float)p.hw * (float)p.cpg);
   const int lin = WIDE ? rows * p.sv : rows, step = WIDE ? NT : ty_n;    // thread r takes r, r + step, ... of lin
   const int full = lin / step, more = lin - full * step;
-  auto count_of = [&](int r) { return (float)((full + (r < more ? 1 : 0)) * (MERGED ? V : 1)); };
+  auto count_of = [&](int r) { return (float)((full + (r < more ? 1 : 0)) * G); };
   // A row of red is a warp (its pixels together), or, where a pixel is more than a warp, the threads of one ty.
   const int red_row = WIDE || by_warp ? warp : ty;
   auto count_of_row = [&](int r) {
@@ -246,7 +251,7 @@ group_norm_kernel(const __grid_constant__ NormArgs p) {
       for (int i = 0; i < 32; ++i) n += count_of(r * 32 + i);
       return n;
     }
-    return by_warp ? (float)((full * warp_rows + min(max(more - r * warp_rows, 0), warp_rows)) * (MERGED ? V : 1)) : count_of(r);
+    return by_warp ? (float)((full * warp_rows + min(max(more - r * warp_rows, 0), warp_rows)) * G) : count_of(r);
   };
   const int per_group = p.bins / p.groups;             // bins of a group
   const int r_first = lane / per_group, r_step = 32 / per_group, b_first = lane - r_first * per_group, b_step = 32 - r_step * per_group;
@@ -262,7 +267,7 @@ group_norm_kernel(const __grid_constant__ NormArgs p) {
       float f[V];
       norm_unpack<T, V>(held(r0, c0), f);
 #pragma unroll
-      for (int k = 0; k < K; ++k) shift[k] = f[k];
+      for (int k = 0; k < K; ++k) shift[k] = f[k * G];
     }
   }
   if constexpr (V == 1) {
@@ -275,29 +280,36 @@ group_norm_kernel(const __grid_constant__ NormArgs p) {
     });
     mean[0] = s, m2[0] = q;
   } else {
-    constexpr int A = MERGED ? 2 : P;                // accumulators; an access has two chains where it is summed together
-    f32x2 s[A], q[A], less[MERGED ? 1 : P];
+    // Pairs of accumulators: of one part, two elements of it (and two chains where an access is summed together); else of two neighbouring parts.
+    constexpr int A = K == 1 ? 2 : G > 1 ? K : P;
+    f32x2 s[A], q[A], less[P];
 #pragma unroll
     for (int i = 0; i < A; ++i) s[i] = q[i] = 0ull;
 #pragma unroll
-    for (int i = 0; i < (MERGED ? 1 : P); ++i) less[i] = pair_of(-shift[MERGED ? 0 : 2 * i], -shift[MERGED ? 0 : 2 * i + 1]);
+    for (int i = 0; i < P; ++i) less[i] = pair_of(-shift[2 * i / G], -shift[(2 * i + 1) / G]);
     each([&](int row, int col) {
       float f[V];
       norm_unpack<T, V>(held(row, col), f);
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        const f32x2 d = pair_add(pair_of(f[2 * i], f[2 * i + 1]), less[MERGED ? 0 : i]);
-        s[MERGED ? i & 1 : i] = pair_add(s[MERGED ? i & 1 : i], d);
-        q[MERGED ? i & 1 : i] = pair_fma(d, d, q[MERGED ? i & 1 : i]);
+        const int at = K == 1 ? i & 1 : G > 1 ? 2 * i / G : i;
+        const f32x2 d = pair_add(pair_of(f[2 * i], f[2 * i + 1]), less[i]);
+        s[at] = pair_add(s[at], d);
+        q[at] = pair_fma(d, d, q[at]);
       }
     });
-    if constexpr (MERGED) {
+    if constexpr (K == 1) {
       float u[4], v[4];
       pair_split(s[0], u[0], u[1]), pair_split(s[1], u[2], u[3]), pair_split(q[0], v[0], v[1]), pair_split(q[1], v[2], v[3]);
       mean[0] = (u[0] + u[1]) + (u[2] + u[3]), m2[0] = (v[0] + v[1]) + (v[2] + v[3]);
     } else {
 #pragma unroll
-      for (int i = 0; i < P; ++i) pair_split(s[i], mean[2 * i], mean[2 * i + 1]), pair_split(q[i], m2[2 * i], m2[2 * i + 1]);
+      for (int i = 0; i < A; ++i) {
+        float u[2], v[2];
+        pair_split(s[i], u[0], u[1]), pair_split(q[i], v[0], v[1]);
+        if constexpr (G > 1) mean[i] = u[0] + u[1], m2[i] = v[0] + v[1];
+        else mean[2 * i] = u[0], mean[2 * i + 1] = u[1], m2[2 * i] = v[0], m2[2 * i + 1] = v[1];
+      }
     }
   }
   // (mean, squares) of the thread's K columns; of a warp's, about the mean of its first pixel's thread; of a group, by one warp over the rows of red
@@ -392,7 +404,7 @@ group_norm_kernel(const __grid_constant__ NormArgs p) {
       const int c = channel + col * V + i;
       const float2 st = all[WIDE ? 0 : min((col * V + i) / p.cpg, p.groups - 1)];
       a[i] = p.gamma ? p.gamma[c] * st.y : st.y, b[i] = p.beta ? p.beta[c] : 0.f;
-      if (i < K) mean[i] = st.x;
+      if (i % G == 0) mean[i / G] = st.x;
       if (kFolded) b[i] = fmaf(-st.x, a[i], b[i]);
     }
   };
@@ -413,7 +425,7 @@ group_norm_kernel(const __grid_constant__ NormArgs p) {
 #pragma unroll
         for (int i = 0; i < P; ++i) {
           f32x2 d = pair_of(f[2 * i], f[2 * i + 1]);
-          if (!kFolded) d = pair_add(d, pair_of(-mean[MERGED ? 0 : 2 * i], -mean[MERGED ? 0 : 2 * i + 1]));
+          if (!kFolded) d = pair_add(d, pair_of(-mean[2 * i / G], -mean[(2 * i + 1) / G]));
           f32x2 t = pair_fma(d, pair_of(a[2 * i], a[2 * i + 1]), pair_of(b[2 * i], b[2 * i + 1]));
           if (RES) t = pair_add(t, pair_of(q[2 * i], q[2 * i + 1]));
           pair_split(t, f[2 * i], f[2 * i + 1]);
@@ -434,7 +446,7 @@ group_norm_kernel(const __grid_constant__ NormArgs p) {
       });
     } else if (active) {
       // Four pixels' loads before the first one's store: y may be the residual or x, so the compiler keeps loads behind stores.
-      constexpr int U = RES || !RESIDENT ? 4 : 1;
+      constexpr int U = RES && !RESIDENT ? 2 : RES || !RESIDENT ? 4 : 1;
       for (int row = ty; row < rows; row += U * ty_n) {
         Vec h[U], r[U];
 #pragma unroll
@@ -458,9 +470,9 @@ group_norm_kernel(const __grid_constant__ NormArgs p) {
   }
 }
 
-template <typename T, int V, bool MERGED, bool WIDE, bool RESIDENT, int NT>
+template <typename T, int V, int K, bool WIDE, bool RESIDENT, int NT>
 inline cudaError_t norm_launch_k(const NormPlan& pl, const NormArgs& a, long units, cudaStream_t st) {
-  const auto kernel = group_norm_kernel<T, V, MERGED, WIDE, RESIDENT, NT>;
+  const auto kernel = group_norm_kernel<T, V, K, WIDE, RESIDENT, NT>;
   cudaError_t e = cudaSuccess;
   if (pl.smem() > 48 << 10) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, pl.smem());
   if (e != cudaSuccess) return e;
@@ -479,17 +491,21 @@ inline cudaError_t norm_launch_k(const NormPlan& pl, const NormArgs& a, long uni
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
-template <typename T, int V, int NT>
+template <typename T, int V, int K>
+inline cudaError_t norm_launch_p(const NormPlan& pl, const NormArgs& a, long units, cudaStream_t st) {
+  if (pl.threads == kNormMany) return norm_launch_k<T, V, K, false, false, kNormMany>(pl, a, units, st);
+  return pl.threads == kNormFew ? norm_launch_k<T, V, K, false, true, kNormFew>(pl, a, units, st) : norm_launch_k<T, V, K, false, true, kNormThreads>(pl, a, units, st);
+}
+
+template <typename T, int V>
 inline cudaError_t norm_launch_v(const NormPlan& pl, const NormArgs& a, long units, cudaStream_t st) {
-  if constexpr (NT == kNormThreads)
-    if (pl.wide) return pl.resident ? norm_launch_k<T, V, true, true, true, NT>(pl, a, units, st) : norm_launch_k<T, V, true, true, false, NT>(pl, a, units, st);
-  if constexpr (NT == kNormThreads)
-    if (!pl.resident) {
-      if (pl.merged) return norm_launch_k<T, V, true, false, false, NT>(pl, a, units, st);
-      if constexpr (V > 1) return norm_launch_k<T, V, false, false, false, NT>(pl, a, units, st);
-    }
-  if (pl.merged) return norm_launch_k<T, V, true, false, true, NT>(pl, a, units, st);
-  if constexpr (V > 1) return norm_launch_k<T, V, false, false, true, NT>(pl, a, units, st);
+  if (pl.wide) return pl.resident ? norm_launch_k<T, V, 1, true, true, kNormThreads>(pl, a, units, st) : norm_launch_k<T, V, 1, true, false, kNormMany>(pl, a, units, st);
+  if (pl.parts == 1) return norm_launch_p<T, V, 1>(pl, a, units, st);
+  if constexpr (V > 1)
+    if (pl.parts == 2) return norm_launch_p<T, V, 2>(pl, a, units, st);
+  if constexpr (V > 2)
+    if (pl.parts == 4) return norm_launch_p<T, V, 4>(pl, a, units, st);
+  if constexpr (V > 4) return norm_launch_p<T, V, 8>(pl, a, units, st);
   return cudaErrorInvalidValue;
 }
 
@@ -506,8 +522,7 @@ inline cudaError_t norm_launch(const void* x, const void* residual, void* y, con
                       err_flag, rev ? 1 : 0};
   const long units = batch * pl.slices;
   constexpr int V = Elem<T>::kVec;
-  if (pl.threads == kNormThreads) return pl.v > 1 ? norm_launch_v<T, V, kNormThreads>(pl, a, units, st) : norm_launch_v<T, 1, kNormThreads>(pl, a, units, st);
-  return pl.v > 1 ? norm_launch_v<T, V, kNormFew>(pl, a, units, st) : norm_launch_v<T, 1, kNormFew>(pl, a, units, st);
+  return pl.v > 1 ? norm_launch_v<T, V>(pl, a, units, st) : norm_launch_v<T, 1>(pl, a, units, st);
 }
 
 }  // namespace ee
