@@ -32,7 +32,8 @@ constexpr int kLrMaxRank = 128;
 constexpr int kLrMaxSplits = 8;        // CTAs of a cluster
 constexpr int kLrShrinkTN = 64;        // rows of a tile of the first launch
 constexpr long kLrSimtWork = 24L << 20;  // products of the first launch up to which CUDA cores take it: every row of x reads its adapter from L2
-constexpr int kLrCopyWarps = 8;
+constexpr int kLrCopyWarps = 8, kLrFillWarps = 8;
+template <bool COPY, bool SHRINK> constexpr int kLrThreads = 192 + 32 * (COPY ? kLrCopyWarps : 1) + (SHRINK ? 0 : 32 * kLrFillWarps);
 
 struct LrArgs {
   const bf16* x;       // [rows][c]
@@ -57,9 +58,9 @@ struct LrSmem {
   static constexpr int kPart = TN * 128 * 4;                        // partial sums: a shrink's h of its rows (up to 128 numbers each); else what the cluster's CTAs send
   static constexpr int kOffExt = kStages * kStage, kOffPart = kOffExt + kExt * kStage;
   static constexpr int kOffInts = kOffPart + (PERSIST ? 0 : kPart); // persistent CTAs do not cut K
-  static constexpr int kInts = 3 * TN + 16;                         // adapter and slot of each row, adapters of the tile, masks and counts
+  static constexpr int kInts = (2 * kAcc + 1) * TN + 16;            // adapter and slot of each row of a tile (and the next), adapters of the tile, masks and counts
   static constexpr int kOffBars = kOffInts + kInts * 4;
-  static constexpr int kBytes = kOffBars + 8 * (2 * kStages + 2 * kExt + 7) + 1024;
+  static constexpr int kBytes = kOffBars + 8 * (2 * kStages + 2 * kExt + 9) + 1024;
   static_assert(kBytes <= 227 * 1024, "exceeds the shared memory of an SM");
   static_assert(!SHRINK || 2 * (kBytes + 1024) <= 228 * 1024, "two CTAs of a shrink share an SM");
 };
@@ -98,7 +99,7 @@ __device__ __noinline__ float lr_not_finite(const LrArgs& p, int t, int f, int a
 // Tile: blockIdx.x of filters, y of rows, z: range of K.  Persistent: every gridDim.x-th tile, filters first.  SHRINK: blockIdx.x of rows; a CTA takes the adapters of its rows in groups
 // that fill the 128 rows of operand A, one after the other; a row of x has one adapter, so all groups leave their numbers in the same array.
 template <int TN, bool PERSIST, bool SHRINK, bool COPY>
-__global__ void __launch_bounds__(COPY ? 192 + 32 * kLrCopyWarps : 224)
+__global__ void __launch_bounds__(kLrThreads<COPY, SHRINK>)
 lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmX, LrArgs p) {
   using S = LrSmem<TN, PERSIST, SHRINK>;
   constexpr int kStages = S::kStages, kExt = S::kExt, kAcc = S::kAcc;
@@ -107,13 +108,13 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
   extern __shared__ uint8_t lr_smem[];
   const uint32_t raw = smem_u32(lr_smem), base = (raw + 1023u) & ~1023u;
   uint8_t* gen = lr_smem + (base - raw);
-  int* s_ad = reinterpret_cast<int*>(gen + S::kOffInts);     // [TN] adapter of a row, -1: none
-  int* s_slot = s_ad + TN;                                   // [TN] its place among the tile's adapters
-  int* s_list = s_slot + TN;                                 // [TN] the tile's adapters, in order of first occurrence
+  int* s_ad0 = reinterpret_cast<int*>(gen + S::kOffInts);    // [kAcc][TN] adapter of a row, -1: none
+  int* s_slot0 = s_ad0 + kAcc * TN;                          // [kAcc][TN] its place among the tile's adapters
+  int* s_list = s_slot0 + kAcc * TN;                         // [TN] the tile's adapters, in order of first occurrence
   unsigned* s_mask = reinterpret_cast<unsigned*>(s_list + TN);   // [8]
   int* s_count = reinterpret_cast<int*>(s_mask) + 8;         // [2] adapters of the tile, by its parity
-  int* s_bad = s_count + 2;                                  // set where a B_a of the tile holds infinities or NaN
-  uint32_t* tmem_slot = s_mask + 11;
+  int* s_bad = s_count + 2;                                  // [2] set where a B_a of the tile holds infinities or NaN
+  uint32_t* tmem_slot = s_mask + 12;
   const uint32_t bar0 = base + S::kOffBars;
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (kStages + s); };
@@ -123,6 +124,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
   const uint32_t part_bar = bar0 + 8u * (2 * kStages + 6);
   auto ext_full = [&](int x) { return part_bar + 8u + 8u * x; };             // slots of adapter columns
   auto ext_empty = [&](int x) { return part_bar + 8u + 8u * (kExt + x); };
+  auto filled_bar = [&](int i) { return part_bar + 8u + 8u * (2 * kExt + i); };   // all that the tile's epilogue reads of its adapters is there
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int z = (int)blockIdx.z, Z = (int)gridDim.z;
   const int tiles_n = (p.n + 127) / 128;
@@ -147,7 +149,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) mbar_init(full_bar(s), kFull), mbar_init(empty_bar(s), 1);
     for (int x = 0; x < kExt; ++x) mbar_init(ext_full(x), 1), mbar_init(ext_empty(x), 1);
-    for (int a = 0; a < 2; ++a) mbar_init(accum_bar(a), 1), mbar_init(drain_bar(a), 1), mbar_init(list_bar(a), 1);
+    for (int a = 0; a < 2; ++a) mbar_init(accum_bar(a), 1), mbar_init(drain_bar(a), 1), mbar_init(list_bar(a), 1), mbar_init(filled_bar(a), 1);
     mbar_init(part_bar, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (!SHRINK && Z > 1) mbar_expect_tx(part_bar, (uint32_t)S::kPart);     // TN / Z columns from each of Z CTAs
@@ -158,7 +160,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   // The producer of W needs nothing but its barriers: it goes ahead while the others wait for the accumulator's address, about 1600 clocks.
-  constexpr int kThreads = COPY ? 192 + 32 * kLrCopyWarps : 224;
+  constexpr int kThreads = kLrThreads<COPY, SHRINK>, kFill0 = COPY ? 6 + kLrCopyWarps : 7;
   if (warp == 0) {
     __syncwarp();
     asm volatile("bar.arrive 2, %0;" ::"n"(kThreads) : "memory");
@@ -177,59 +179,51 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     const int all = (int)(((long)count * ext_cols + 63) / 64);
     return all > z ? (all - z + Z - 1) / Z : 0;
   };
-  // The tile's adapters: a row is the first of its adapter, or refers to it.  Four warps.
-  auto list_adapters = [&](int t0, int par) {
-    const int et = tid - 64;
-    constexpr int H = TN > 128 ? TN / 128 : 1;
-    asm volatile("bar.sync 1, 128;" ::: "memory");       // the list of the tile before is not needed any more
-    for (int i = et; i < TN; i += 128) {
-      const int t = t0 + i, a = t < p.rows && p.adapters > 0 ? p.which[t] : -1;
-      s_ad[i] = a >= 0 && a < p.adapters ? a : -1;
+  // The tile's adapters: a row is the first of its adapter, or refers to it.  By the kList threads from `et` = 0 on.
+  constexpr int kList = SHRINK ? 128 : 32 * kLrFillWarps;
+  auto list_adapters = [&](int et, int t0, int par) {
+    static_assert(TN <= kList, "a thread has a row");
+    int *s_ad = s_ad0 + (par & (kAcc - 1)) * TN, *s_slot = s_slot0 + (par & (kAcc - 1)) * TN;
+    asm volatile("bar.sync 1, %0;" ::"n"(kList) : "memory");       // the list of the tile before is not needed any more
+    if (et < TN) {
+      const int t = t0 + et, a = t < p.rows && p.adapters > 0 ? p.which[t] : -1;
+      s_ad[et] = a >= 0 && a < p.adapters ? a : -1;
     }
-    asm volatile("bar.sync 1, 128;" ::: "memory");
-    int first[H];
-#pragma unroll
-    for (int h = 0; h < H; ++h) {
-      const int i = et + 128 * h, w0 = i & ~31;
-      const int a = i < TN ? s_ad[i] : -1;
-      int f = w0 + __ffs(__match_any_sync(0xffffffffu, a)) - 1;       // the first of its warp
-      if (a >= 0 && f == i)
-        for (int u = 0; u < w0; u += 4) {
-          const int4 o = *reinterpret_cast<const int4*>(s_ad + u);
-          if (o.w == a) f = min(f, u + 3);
-          if (o.z == a) f = min(f, u + 2);
-          if (o.y == a) f = min(f, u + 1);
-          if (o.x == a) f = min(f, u);
-        }
-      f = __shfl_sync(0xffffffffu, f, f >= w0 ? f & 31 : lane);       // the others of the warp take what their first found
-      const unsigned lead = __ballot_sync(0xffffffffu, a >= 0 && f == i);
-      if (lane == 0 && i < TN) s_mask[i >> 5] = lead;
-      first[h] = a >= 0 ? f : -1;
-    }
-    asm volatile("bar.sync 1, 128;" ::: "memory");
+    asm volatile("bar.sync 1, %0;" ::"n"(kList) : "memory");
+    const int w0 = et & ~31, a = et < TN ? s_ad[et] : -1;
+    int f = w0 + __ffs(__match_any_sync(0xffffffffu, a)) - 1;       // the first of its warp
+    if (a >= 0 && f == et)
+      for (int u = 0; u < w0; u += 4) {
+        const int4 o = *reinterpret_cast<const int4*>(s_ad + u);
+        if (o.w == a) f = min(f, u + 3);
+        if (o.z == a) f = min(f, u + 2);
+        if (o.y == a) f = min(f, u + 1);
+        if (o.x == a) f = min(f, u);
+      }
+    f = __shfl_sync(0xffffffffu, f, f >= w0 ? f & 31 : lane);       // the others of the warp take what their first found
+    const unsigned lead = __ballot_sync(0xffffffffu, a >= 0 && f == et);
+    if (lane == 0 && et < TN) s_mask[et >> 5] = lead;
+    asm volatile("bar.sync 1, %0;" ::"n"(kList) : "memory");
     int count = 0;
 #pragma unroll
     for (int k = 0; k < (TN + 31) / 32; ++k) count += __popc(s_mask[k]);
-#pragma unroll
-    for (int h = 0; h < H; ++h) {
-      const int i = et + 128 * h, f = first[h];
-      if (i >= TN) continue;
+    if (et < TN) {
       int slot = -1;
-      if (f >= 0) {
+      if (a >= 0) {
         slot = __popc(s_mask[f >> 5] & ((1u << (f & 31)) - 1u));
         for (int k = 0; k < f >> 5; ++k) slot += __popc(s_mask[k]);
-        if (f == i) s_list[slot] = s_ad[i];
+        if (f == et) s_list[slot] = a;
       }
-      s_slot[i] = slot;
+      s_slot[et] = slot;
     }
-    if (et == 0) s_count[par] = count, *s_bad = 0;
-    asm volatile("bar.sync 1, 128;" ::: "memory");
+    if (et == 0) s_count[par] = count, s_bad[par] = 0;
+    asm volatile("bar.sync 1, %0;" ::"n"(kList) : "memory");
     if (et == 0) mbar_arrive_n(list_bar(par), 1);
     return count;
   };
   const int per_tile = 128 / p.r8;               // SHRINK: adapters of a tile
   if (SHRINK) {
-    if (warp >= 2 && warp < 6) list_adapters(t_first, 0);
+    if (warp >= 2 && warp < 6) list_adapters(tid - 64, t_first, 0);
     __syncthreads();
     tiles = (s_count[0] + per_tile - 1) / per_tile;
   }
@@ -282,7 +276,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
                 tma_load_2d(base + (uint32_t)s * S::kStage + S::kABytes, &tmX, full_bar(s), kb * 64, t0);
               });
     __syncwarp();
-  } else if (COPY && warp >= 6) {
+  } else if (COPY && warp >= 6 && warp < 6 + kLrCopyWarps) {
     const int ct = tid - 192;
     int late = -1;                       // slot whose copies are on their way
     auto landed = [&]() {
@@ -353,7 +347,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
         const uint32_t acc = tmem + (uint32_t)(a * TN);
         if (it >= kAcc) ok = mbar_wait(drain_bar(a), (uint32_t)(it / kAcc - 1) & 1u, p.err_flag);
         // Where the adapters' columns go, in K blocks: spread from where the list is asked for, or behind the last block, if h is not there before.
-        const int ask = kPersist ? (it > 0 ? (num_kb + 1) / 2 : num_kb) : num_kb >= 8 ? num_kb * 5 / 8 : num_kb;
+        const int ask = kPersist ? (it > 0 ? (num_kb + 3) / 4 : num_kb) : num_kb >= 8 ? num_kb * 5 / 8 : num_kb;
         int ext = 0, e = 0;
         for (int i = 0; i < num_kb && ok; ++i) {
           ok = mbar_wait(full_bar(w.s), w.ph, p.err_flag);
@@ -383,48 +377,26 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
       }
     }
     __syncwarp();
-  } else {
-    const int et = tid - 64, q = warp & 3;
-    const int row = q * 32 + lane;                     // accumulator lane of this thread
-    constexpr int CH = TN < 32 ? TN : 32;              // columns read at a time
-    bool ok = true;
-    if constexpr (SHRINK) {
-      // this CTA's part of h: [TN][r8] floats
-      const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
-      const int k = row / p.r8, j = row - k * p.r8;
-      float* part = reinterpret_cast<float*>(gen + S::kOffPart);
-      for (int group = 0; group < tiles; ++group) {
-        ok = __all_sync(0xffffffffu, mbar_wait(accum_bar(0), (uint32_t)group & 1u, p.err_flag)) && ok;
-        tc_fence_after();
-        const int slot = k < per_tile ? group * per_tile + k : -2;
-#pragma unroll 1
-        for (int c = 0; c < TN; c += CH) {
-          float v[CH];
-          if constexpr (CH == 32) tmem_ld32(lane_base + c, v);
-          else tmem_ld16(lane_base + c, v);
-#pragma unroll
-          for (int i = 0; i < CH; ++i)
-            if (s_slot[c + i] == slot) part[(c + i) * p.r8 + j] = v[i];
-        }
-        tc_fence_before();
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (et == 0) mbar_arrive_n(drain_bar(0), 1);
-      }
-    } else {
+  } else if (!SHRINK && warp >= kFill0) {
+    if constexpr (!SHRINK) {
+      const int et = tid - 32 * kFill0;
+      bool ok = true;
       uint32_t xs = 0;                                 // blocks of adapter columns so far
       bool waited = false;                             // for h
       for (int tile = tile0, it = 0; tile < tiles; tile += tile_step, ++it) {
         int n0, t0;
         place_of(tile, n0, t0);
-        const int count = list_adapters(t0, it & 1);
-        // A thread has the 16-byte chunk et % 8 of a block's 64 columns, in every sixteenth row of either operand.
+        if (it >= kAcc) ok = ok && mbar_wait(drain_bar(it & (kAcc - 1)), (uint32_t)(it / kAcc - 1) & 1u, p.err_flag);    // the list of that tile is not needed any more
+        const int count = list_adapters(et, t0, it & 1);
+        const int* s_slot = s_slot0 + (it & (kAcc - 1)) * TN;
+        // A thread has the 16-byte chunk et % 8 of a block's 64 columns, in every 32nd row of either operand.
         const int ext = ext_blocks(count), all = count * ext_cols, c8 = et & 7, r0 = et >> 3;
         // values of a unit of B_a, of h: they lie in one part of one adapter
         const int unit_h = p.rank % 8 == 0 ? 8 : p.rank % 4 == 0 ? 4 : p.rank % 2 == 0 ? 2 : 1;
         int unit_b = unit_h;
         while ((uintptr_t)p.b & (unit_b * 2 - 1)) unit_b >>= 1;
         // The code of this part is kept short (loops, not copies): it runs a few times a tile, and what it costs is its way into the instruction cache.
-        const uint32_t place0 = (uint32_t)(r0 * 128 + ((c8 ^ (r0 & 7)) << 4));      // of row r0; every sixteenth row is 2048 bytes on
+        const uint32_t place0 = (uint32_t)(r0 * 128 + ((c8 ^ (r0 & 7)) << 4));      // of row r0; every 32nd row is 4096 bytes on
         const float per_col = 1.f / (float)ext_cols;
         auto column = [&](int e, int k, int& slot, int& rem) {       // adapter and place in its 2 * rank columns; slot -1: behind the last
           const int c = (z + e * Z) * 64 + c8 * 8 + k;
@@ -449,14 +421,14 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
             if (unit_b > 1) {
               uint32_t dst = base + at_block(e) + place0 + 2 * k;
 #pragma unroll 1
-              for (int f = n0 + r0; f < n0 + 128; f += 16, dst += 2048, src += 16 * p.rank) fetch(dst, slot >= 0 && f < p.n ? src : p.b, slot >= 0 && f < p.n, unit_b * 2);
+              for (int f = n0 + r0; f < n0 + 128; f += 32, dst += 4096, src += 32 * p.rank) fetch(dst, slot >= 0 && f < p.n ? src : p.b, slot >= 0 && f < p.n, unit_b * 2);
             } else {
               unsigned short* dst = reinterpret_cast<unsigned short*>(gen + at_block(e) + place0) + k;
-              unsigned short v[8];
+              unsigned short v[4];
 #pragma unroll
-              for (int m = 0; m < 8; ++m) v[m] = slot >= 0 && n0 + r0 + 16 * m < p.n ? reinterpret_cast<const unsigned short*>(src)[(size_t)16 * m * p.rank] : (unsigned short)0;
+              for (int m = 0; m < 4; ++m) v[m] = slot >= 0 && n0 + r0 + 32 * m < p.n ? reinterpret_cast<const unsigned short*>(src)[(size_t)32 * m * p.rank] : (unsigned short)0;
 #pragma unroll
-              for (int m = 0; m < 8; ++m) dst[m * 1024] = v[m];
+              for (int m = 0; m < 4; ++m) dst[m * 2048] = v[m];
             }
           }
         };
@@ -469,15 +441,14 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
             if (unit_h > 1) {
               uint32_t dst = base + at_block(e) + S::kABytes + place0 + 2 * k;
 #pragma unroll 1
-              for (int t = r0; t < TN; t += 16, dst += 2048, src += 16 * ext_cols) {
+              for (int t = r0; t < TN; t += 32, dst += 4096, src += 32 * ext_cols) {
                 const bool in = slot >= 0 && s_slot[t] == slot;
                 fetch(dst, in ? src : p.h, in, unit_h * 2);
               }
             } else {
               unsigned short* dst = reinterpret_cast<unsigned short*>(gen + at_block(e) + S::kABytes + place0) + k;
 #pragma unroll 4
-              for (int m = 0; m < TN / 16; ++m)
-                dst[m * 1024] = slot >= 0 && s_slot[r0 + 16 * m] == slot ? reinterpret_cast<const unsigned short*>(src)[(size_t)16 * m * ext_cols] : (unsigned short)0;
+              for (int t = r0; t < TN; t += 32, dst += 2048, src += 32 * ext_cols) *dst = slot >= 0 && s_slot[t] == slot ? *reinterpret_cast<const unsigned short*>(src) : (unsigned short)0;
             }
           }
         };
@@ -488,45 +459,85 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
           const int bytes = min(128, p.n - n0) * p.rank * 2, lines = (bytes + 127) / 128;
           for (int k = first; k <= last; ++k)
 #pragma unroll 1
-            for (int i = et; i < lines; i += 128)
+            for (int i = et; i < lines; i += kList)
               asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(p.b + ((size_t)s_list[k] * p.n + n0) * p.rank) + min(i * 128, bytes - 2)));
         }
-        // Blocks of a batch are fetched together: B_a before the wait for h (no kernel writes it), then h.
-#pragma unroll 1
-        for (int e0 = 0; e0 < ext || !waited; e0 += kExt) {
-          const int e1 = min(e0 + kExt, ext);
-#pragma unroll 1
-          for (int e = e0; e < e1; ++e) fill_b(e);
-          if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
-          waited = true;
-#pragma unroll 1
-          for (int e = e0; e < e1; ++e) fill_h(e);
-          cp_async_commit();
-          cp_async_wait<0>();
+        // A block is fetched while the one before it arrives.  B_a, which no kernel in front writes, is fetched before the wait for h.
+        auto finish = [&](int e) {
           // what this thread fetched is here: an infinity would turn the zeros of other adapters' rows into NaN, so lr_not_finite adds it to its own rows
-#pragma unroll 1
-          for (int e = e0; e < e1; ++e) {
-            uint4* at = reinterpret_cast<uint4*>(gen + at_block(e) + place0);
+          uint4* at = reinterpret_cast<uint4*>(gen + at_block(e) + place0);
 #pragma unroll 2
-            for (int m = 0; m < 8; ++m) {
-              const uint4 v = at[m * 128];
-              if (lr_odd(v.x) | lr_odd(v.y) | lr_odd(v.z) | lr_odd(v.w)) at[m * 128] = make_uint4(lr_drop(v.x), lr_drop(v.y), lr_drop(v.z), lr_drop(v.w)), *s_bad = 1;
-            }
+          for (int m = 0; m < 4; ++m) {
+            const uint4 v = at[m * 256];
+            if (lr_odd(v.x) | lr_odd(v.y) | lr_odd(v.z) | lr_odd(v.w)) at[m * 256] = make_uint4(lr_drop(v.x), lr_drop(v.y), lr_drop(v.z), lr_drop(v.w)), s_bad[it & 1] = 1;
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          asm volatile("bar.sync 1, 128;" ::: "memory");
-          if (et == 0)
-            for (int e = e0; e < e1; ++e) mbar_arrive_n(ext_full(slot_of_block(e)), 1);
+          asm volatile("bar.sync 1, %0;" ::"n"(kList) : "memory");
+          if (et == 0) mbar_arrive_n(ext_full(slot_of_block(e)), 1);
+        };
+        constexpr int kBehind = kExt - 1;      // blocks on their way behind the one that is finished
+        int have = 0;                          // blocks whose B_a is on its way
+#pragma unroll 1
+        for (int e = 0; e < ext + kBehind; ++e) {
+          if (e < ext) {
+            const int to = waited ? e + 1 : min(kExt, ext);
+#pragma unroll 1
+            for (; have < to; ++have) fill_b(have);
+            if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+            waited = true;
+            fill_h(e);
+          }
+          cp_async_commit();
+          if (e >= kBehind) {
+            cp_async_wait<kBehind>();
+            finish(e - kBehind);
+          }
         }
         xs += (uint32_t)ext;
-
+        if (et == 0) mbar_arrive_n(filled_bar(it & 1), 1);
+      }
+    }
+  } else {
+    const int et = tid - 64, q = warp & 3;
+    const int row = q * 32 + lane;                     // accumulator lane of this thread
+    constexpr int CH = TN < 32 ? TN : 32;              // columns read at a time
+    bool ok = true;
+    if constexpr (SHRINK) {
+      // this CTA's part of h: [TN][r8] floats
+      const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
+      const int k = row / p.r8, j = row - k * p.r8;
+      float* part = reinterpret_cast<float*>(gen + S::kOffPart);
+      for (int group = 0; group < tiles; ++group) {
+        ok = __all_sync(0xffffffffu, mbar_wait(accum_bar(0), (uint32_t)group & 1u, p.err_flag)) && ok;
+        tc_fence_after();
+        const int slot = k < per_tile ? group * per_tile + k : -2;
+#pragma unroll 1
+        for (int c = 0; c < TN; c += CH) {
+          float v[CH];
+          if constexpr (CH == 32) tmem_ld32(lane_base + c, v);
+          else tmem_ld16(lane_base + c, v);
+#pragma unroll
+          for (int i = 0; i < CH; ++i)
+            if (s_slot0[c + i] == slot) part[(c + i) * p.r8 + j] = v[i];
+        }
+        tc_fence_before();
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (et == 0) mbar_arrive_n(drain_bar(0), 1);
+      }
+    } else {
+      asm volatile("griddepcontrol.wait;" ::: "memory");      // nothing is stored before, nor h read
+      for (int tile = tile0, it = 0; tile < tiles; tile += tile_step, ++it) {
+        int n0, t0;
+        place_of(tile, n0, t0);
+        const int* s_ad = s_ad0 + (it & (kAcc - 1)) * TN;
+        const int* s_slot = s_slot0 + (it & (kAcc - 1)) * TN;
         const int acc = it & (kAcc - 1);
-        ok = __all_sync(0xffffffffu, mbar_wait(accum_bar(acc), (uint32_t)(it / kAcc) & 1u, p.err_flag)) && ok;
+        ok = __all_sync(0xffffffffu, mbar_wait(accum_bar(acc), (uint32_t)(it / kAcc) & 1u, p.err_flag) && mbar_wait(filled_bar(it & 1), (uint32_t)(it >> 1) & 1u, p.err_flag)) && ok;
         tc_fence_after();
         const uint32_t lane_base = tmem + (uint32_t)(acc * TN) + ((uint32_t)(q * 32) << 16);
         const int f = n0 + row;
         const float bias = p.bias && f < p.n ? p.bias[f] : 0.f;
-        const bool bad = *s_bad != 0 && f < p.n;
+        const bool bad = s_bad[it & 1] != 0 && f < p.n;
         auto columns_of = [&](int c, float* v) {
           if constexpr (CH == 32) tmem_ld32(lane_base + c, v);
           else tmem_ld16(lane_base + c, v);
@@ -557,7 +568,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
           }
           if (kPersist) {          // the accumulator is free for the tile after the next
             tc_fence_before();
-            asm volatile("bar.sync 1, 128;" ::: "memory");
+            asm volatile("bar.sync 3, 128;" ::: "memory");
             if (et == 0) mbar_arrive_n(drain_bar(acc), 1);
           }
         } else if constexpr (!kPersist) {
@@ -635,7 +646,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
       const uint32_t part = base + S::kOffPart;
       for (int i = tid; i < TN / Z * p.rank; i += (int)blockDim.x) {
         const int t = i / p.rank * Z + z, j = i - i / p.rank * p.rank;
-        if (s_slot[t] < 0) continue;
+        if (s_slot0[t] < 0) continue;
         float sum = 0.f;
         for (int r = 0; r < Z; ++r) {
           uint32_t from;
@@ -644,7 +655,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
           asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(from) : "memory");
           sum += v;
         }
-        lr_store(p.h, t_first + t, j, p.rank, p.scale ? sum * p.scale[s_ad[t]] : sum);
+        lr_store(p.h, t_first + t, j, p.rank, p.scale ? sum * p.scale[s_ad0[t]] : sum);
       }
       if (Z > 1) asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");   // nobody reads this CTA's part any more
     }
@@ -773,7 +784,7 @@ template <int TN, bool PERSIST, bool SHRINK, bool COPY>
 inline cudaError_t lr_launch_k(const CUtensorMap& tmA, const CUtensorMap& tmX, const LrArgs& a, dim3 grid, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
-  cfg.blockDim = dim3(COPY ? 192 + 32 * kLrCopyWarps : 224);
+  cfg.blockDim = dim3(kLrThreads<COPY, SHRINK>);
   cfg.dynamicSmemBytes = LrSmem<TN, PERSIST, SHRINK>::kBytes;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
