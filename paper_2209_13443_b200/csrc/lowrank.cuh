@@ -12,10 +12,14 @@
 // send each other their parts as asynchronous stores and add them in fixed order.  The first launch is a product of the same shape, 128 rows of
 // stacked A_a over 64 rows of the batch; up to kLrSimtWork products CUDA cores do it, a warp a row of A_a.
 // The second launch starts while the first runs and waits for it only before it fills in h.  The adapters' columns have slots of their own beside the ring of the
-// channels, which four warps fill while the channels are multiplied; they are multiplied at fixed places, spread over the later channels, or behind the last one where h is
-// not there before (a persistent CTA's first tile, short K).
+// channels: eight warps list the adapters of a tile and fill the slots, a tile ahead of the four that store; the blocks are multiplied at fixed places, spread over the later
+// channels, or behind the last one where h is not there before (a persistent CTA's first tile, short K).  Four warps that filled and stored in turn took 139 us
+// in place of 131 for 4096 x 4096 x 4096 with nine adapters of rank 64, 90 in place of 68 for 2048 x 1024 x 4096 with eight of 32 in mixed order, and 6.9 in place of 7.3 for
+// one row of 2048 x 1000.
 // Two forms.  At most one tile an SM: a deep ring, for the bytes in flight.  More: persistent CTAs with two accumulators, so that one tile's list of adapters, columns
 // and stores lie under the next one's products.  128 x 256 tiles where that takes less time: 128 x 128 ones ask 128 bytes a clock of L2 for every SM, and get 97.
+// What bounds it: few rows the latency of the two launches, 64 x 4096 x 4096 the bytes of W (9.3 of 19.8 us at the rate of memory), thousands of rows the tensor cores; rows in mixed
+// order the fill of h, whose columns are zero in the rows of other adapters (about 190 clocks for 32 rows of a block).
 //
 // Channels that are not whole 16-byte vectors, or operands off a 16-byte boundary, cannot be fetched by TMA: eight warps then copy the
 // tiles (COPY), 8 or 4 bytes at a time without waiting for them, or 2 where a row may start between two words.  Ranks, too, need not be whole vectors: columns are
@@ -96,8 +100,8 @@ __device__ __noinline__ float lr_not_finite(const LrArgs& p, int t, int f, int a
 }
 
 // tmA: rows of operand A (W in boxes of 128 filters; SHRINK: all adapters' A in boxes of r8 rows), tmX: rows of x in boxes of TN.
-// Tile: blockIdx.x of filters, y of rows, z: range of K.  Persistent: every gridDim.x-th tile, filters first.  SHRINK: blockIdx.x of rows; a CTA takes the adapters of its rows in groups
-// that fill the 128 rows of operand A, one after the other; a row of x has one adapter, so all groups leave their numbers in the same array.
+// Tile: blockIdx.x of filters, y of rows, z: range of K.  Persistent: every gridDim.x-th tile, filters first.  SHRINK: blockIdx.x of rows; their adapters in groups
+// that fill the 128 rows of operand A, every gridDim.y-th from blockIdx.y on; a row of x has one adapter, so all groups of a CTA leave their numbers in the same array.
 template <int TN, bool PERSIST, bool SHRINK, bool COPY>
 __global__ void __launch_bounds__(kLrThreads<COPY, SHRINK>)
 lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmX, LrArgs p) {
@@ -129,7 +133,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
   const int z = (int)blockIdx.z, Z = (int)gridDim.z;
   const int tiles_n = (p.n + 127) / 128;
   int tiles = kPersist ? tiles_n * ((p.rows + TN - 1) / TN) : 1;
-  const int tile0 = kPersist ? (int)blockIdx.x : 0, tile_step = kPersist ? (int)gridDim.x : 1;
+  const int tile0 = kPersist ? (int)blockIdx.x : SHRINK ? (int)blockIdx.y : 0, tile_step = kPersist ? (int)gridDim.x : SHRINK ? (int)gridDim.y : 1;
   auto place_of = [&](int tile, int& n0, int& t0) {
     if (SHRINK) {
       n0 = 0, t0 = (int)blockIdx.x * TN;
@@ -227,7 +231,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     __syncthreads();
     tiles = (s_count[0] + per_tile - 1) / per_tile;
   }
-  const bool idle = SHRINK && tiles == 0;        // no adapters here
+  const bool idle = SHRINK && tiles <= tile0;    // no adapters here
   auto here = [&](int group) { return min(per_tile, s_count[0] - group * per_tile); };      // adapters of a group
 
   struct Walk {      // over the ring
@@ -419,9 +423,12 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
             column(e, k, slot, rem);
             const bf16* src = p.b + ((size_t)(slot >= 0 ? s_list[slot] : 0) * p.n + n0 + r0) * p.rank + (rem < p.rank ? rem : rem - p.rank);
             if (unit_b > 1) {
-              uint32_t dst = base + at_block(e) + place0 + 2 * k;
-#pragma unroll 1
-              for (int f = n0 + r0; f < n0 + 128; f += 32, dst += 4096, src += 32 * p.rank) fetch(dst, slot >= 0 && f < p.n ? src : p.b, slot >= 0 && f < p.n, unit_b * 2);
+              const uint32_t dst = base + at_block(e) + place0 + 2 * k;
+#pragma unroll
+              for (int m = 0; m < 4; ++m) {
+                const bool in = slot >= 0 && n0 + r0 + 32 * m < p.n;
+                fetch(dst + 4096 * m, in ? src + (size_t)32 * m * p.rank : p.b, in, unit_b * 2);
+              }
             } else {
               unsigned short* dst = reinterpret_cast<unsigned short*>(gen + at_block(e) + place0) + k;
               unsigned short v[4];
@@ -440,7 +447,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
             const bf16* src = p.h + (size_t)(t0 + r0) * ext_cols + rem;
             if (unit_h > 1) {
               uint32_t dst = base + at_block(e) + S::kABytes + place0 + 2 * k;
-#pragma unroll 1
+#pragma unroll 4
               for (int t = r0; t < TN; t += 32, dst += 4096, src += 32 * ext_cols) {
                 const bool in = slot >= 0 && s_slot[t] == slot;
                 fetch(dst, in ? src : p.h, in, unit_h * 2);
@@ -507,8 +514,8 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
       const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
       const int k = row / p.r8, j = row - k * p.r8;
       float* part = reinterpret_cast<float*>(gen + S::kOffPart);
-      for (int group = 0; group < tiles; ++group) {
-        ok = __all_sync(0xffffffffu, mbar_wait(accum_bar(0), (uint32_t)group & 1u, p.err_flag)) && ok;
+      for (int group = tile0, it = 0; group < tiles; group += tile_step, ++it) {
+        ok = __all_sync(0xffffffffu, mbar_wait(accum_bar(0), (uint32_t)it & 1u, p.err_flag)) && ok;
         tc_fence_after();
         const int slot = k < per_tile ? group * per_tile + k : -2;
 #pragma unroll 1
@@ -646,7 +653,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
       const uint32_t part = base + S::kOffPart;
       for (int i = tid; i < TN / Z * p.rank; i += (int)blockDim.x) {
         const int t = i / p.rank * Z + z, j = i - i / p.rank * p.rank;
-        if (s_slot0[t] < 0) continue;
+        if (s_slot0[t] < 0 || s_slot0[t] / per_tile % tile_step != tile0) continue;
         float sum = 0.f;
         for (int r = 0; r < Z; ++r) {
           uint32_t from;
@@ -807,10 +814,11 @@ struct LrPlan {
   int tn, splits;          // rows of a tile; CTAs that share its K
   bool persist;            // more tiles than SMs
   bool simt;               // h on CUDA cores
-  int jn, h_splits;        // rows of A_a of a CTA there; CTAs that share the K of a tile on the tensor cores
+  int jn;                  // rows of A_a of a CTA there
+  int h_groups, h_splits;  // on the tensor cores: CTAs that share a tile's groups of adapters, and the K of one
 };
 
-inline LrPlan lr_plan(int rows, int c, int n, int rank, int sms) {
+inline LrPlan lr_plan(int rows, int c, int n, int rank, int adapters, int sms) {
   LrPlan p;
   // Clocks a K block of a tile takes in a full grid, 470 of 128 rows and 750 of 256, times the tiles an SM gets.
   auto rounds = [&](int tn) { return ((long)cdiv(n, 128) * cdiv(rows, tn) + sms - 1) / sms; };
@@ -830,7 +838,12 @@ inline LrPlan lr_plan(int rows, int c, int n, int rank, int sms) {
   p.simt = (long)rows * rank * c <= kLrSimtWork;
   p.jn = 8;
   while (p.jn > 1 && (long)rows * cdiv(rank, p.jn) < 2L * sms) p.jn /= 2;
-  p.h_splits = share(cdiv(rows, kLrShrinkTN), 2);
+  // A tile whose rows are sorted has a group or two, one of mixed rows up to all: where there may be several, K is cut for four CTAs at the most, and further ones take
+  // the groups side by side.  us of a call, sorted / mixed rows, eight CTAs to a group / so: 256 x 4096 x 4096 with eight adapters of rank 64 40 / 54, 35 / 40,
+  // 1402 x 2288 x 1802 with ten 52 / 94, 53 / 85.
+  const int h_tiles = cdiv(rows, kLrShrinkTN), groups = cdiv(std::min(adapters, kLrShrinkTN), 128 / (int)align_up(rank, 8));
+  p.h_splits = std::min(share(h_tiles, 2), groups > 1 ? 4 : kLrMaxSplits);
+  p.h_groups = std::max(1, std::min(groups, 2 * sms / (h_tiles * p.h_splits)));
   return p;
 }
 
@@ -852,7 +865,7 @@ inline cudaError_t lr_shrink_simt(const T* x, const T* a, const float* scale, co
 }
 
 inline cudaError_t lr_run_bf16(const LrContext& ctx, LrArgs a, cudaStream_t st) {
-  const LrPlan p = lr_plan(a.rows, a.c, a.n, a.rank, ctx.sm_count);
+  const LrPlan p = lr_plan(a.rows, a.c, a.n, a.rank, a.adapters, ctx.sm_count);
   const uintptr_t bits = (uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.a;
   const bool copy = a.c % 8 != 0 || (bits & 15) != 0;
   a.unit = a.c % 4 == 0 && (bits & 7) == 0 ? 8 : a.c % 2 == 0 && (bits & 3) == 0 ? 4 : 2;
@@ -868,7 +881,7 @@ inline cudaError_t lr_run_bf16(const LrContext& ctx, LrArgs a, cudaStream_t st) 
     if (e != cudaSuccess) return e;
   }
   if (wide) {
-    const dim3 grid(cdiv(a.rows, kLrShrinkTN), 1, p.h_splits);
+    const dim3 grid(cdiv(a.rows, kLrShrinkTN), p.h_groups, p.h_splits);
     e = copy ? lr_launch_k<kLrShrinkTN, false, true, true>(tmA, tmH, a, grid, st) : lr_launch_k<kLrShrinkTN, false, true, false>(tmA, tmH, a, grid, st);
   } else if (a.adapters > 0) {
     e = lr_shrink_simt<bf16>(a.x, a.a, a.scale, a.which, a.h, a.rows, a.c, a.rank, a.adapters, p.jn, st);
@@ -887,7 +900,7 @@ inline cudaError_t lr_run_bf16(const LrContext& ctx, LrArgs a, cudaStream_t st) 
 // the fp32 model as a 1x1 layer of one pixel a row, which adds that share.
 inline cudaError_t lr_run_f32(const LrContext& ctx, const float* x, const float* w, const float* bias, const float* a, const float* b, const float* scale,
                               const int32_t* which, float* h, float* y, int rows, int c, int n, int rank, int adapters, int* err_flag, cudaStream_t st) {
-  const LrPlan p = lr_plan(rows, c, n, std::max(rank, 1), ctx.sm_count);
+  const LrPlan p = lr_plan(rows, c, n, std::max(rank, 1), adapters, ctx.sm_count);
   if (adapters > 0) {
     cudaError_t e = lr_shrink_simt<float>(x, a, scale, which, h, rows, c, rank, adapters, p.jn, st);
     if (e != cudaSuccess) return e;
