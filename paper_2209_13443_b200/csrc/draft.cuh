@@ -303,8 +303,7 @@ struct VerifyArgs {
 
 // The weight of one value: what the draw goes by.  Values that are not positive and finite weigh nothing.
 __device__ __forceinline__ double verify_weight(float p, float q) {
-  const double w = (double)p - (double)q;
-  return w > 0.0 && w < INFINITY ? w : 0.0;     // an infinite p or q: infinite, or NaN
+  return p > q && p < INFINITY && q > -INFINITY ? (double)p - (double)q : 0.0;     // compared as floats: fp64 comparisons took 33 us in place of 20 for 64 rows of 128001
 }
 
 __device__ __forceinline__ double warp_scan(double v, int lane) {   // inclusive
