@@ -1842,7 +1842,7 @@ ee_status_t operator_context(const OperatorContext** out) {
       EE_CUDA(cudaGetSymbolAddress(&flag, g_operator_flag));
       if (!f || !flag) return EE_ERR_INTERNAL;
       EE_CUDA(cudaDeviceGetAttribute(&c.lr.sm_count, cudaDevAttrMultiProcessorCount, dev));
-      EE_CUDA(lr_context_init());
+      EE_CUDA(lr_context_init(c.lr));
       if (f32_context_init() != EE_OK) return EE_ERR_CUDA;
       c.lr.encode_tiled = (PFN_encodeTiled)f;
       c.flag = (int*)flag;

@@ -33,7 +33,7 @@ namespace ee {
 
 constexpr int kLrParts = 2;            // bf16 parts of h
 constexpr int kLrMaxRank = 128;
-constexpr int kLrMaxSplits = 8;        // CTAs of a cluster
+constexpr int kLrMaxSplits = 8;        // CTAs of a cluster, at most
 constexpr int kLrShrinkTN = 64;        // rows of a tile of the first launch
 constexpr long kLrSimtWork = 24L << 20;  // products of the first launch up to which CUDA cores take it: every row of x reads its adapter from L2
 constexpr int kLrCopyWarps = 8, kLrFillWarps = 8;
@@ -752,6 +752,7 @@ lowrank_delta_kernel(const float* __restrict__ b, const int32_t* __restrict__ wh
 struct LrContext {
   PFN_encodeTiled encode_tiled = nullptr;
   int sm_count = 148;
+  int fit[4] = {};   // clusters of 1, 2, 4 and 8 CTAs, one an SM, that run side by side: what a group of SMs has left over is too few for another
 };
 
 inline cudaError_t lr_map(const LrContext& c, CUtensorMap* tm, const void* base, long rows, int cols, int box_rows) {
@@ -765,7 +766,7 @@ inline cudaError_t lr_map(const LrContext& c, CUtensorMap* tm, const void* base,
              : cudaErrorInvalidValue;
 }
 
-inline cudaError_t lr_context_init() {   // once per device
+inline cudaError_t lr_context_init(LrContext& ctx) {   // once per device
   cudaError_t e = cudaSuccess;
   auto set = [&](auto kernel, int bytes) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -784,6 +785,19 @@ inline cudaError_t lr_context_init() {   // once per device
   set(lowrank_tcgen05_kernel<256, true, false, true>, LrSmem<256, true>::kBytes);
   set(lowrank_tcgen05_kernel<kLrShrinkTN, false, true, false>, LrSmem<kLrShrinkTN, false, true>::kBytes);
   set(lowrank_tcgen05_kernel<kLrShrinkTN, false, true, true>, LrSmem<kLrShrinkTN, false, true>::kBytes);
+  for (int i = 0; i < 4 && e == cudaSuccess; ++i) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1u << i;
+    cfg.gridDim = dim3(1, 1, 1u << i);
+    cfg.blockDim = dim3(kLrThreads<false, false>);
+    cfg.dynamicSmemBytes = LrSmem<64, false>::kBytes;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&ctx.fit[i], lowrank_tcgen05_kernel<64, false, false, false>, &cfg);
+  }
   return e;
 }
 
@@ -818,19 +832,20 @@ struct LrPlan {
   int h_groups, h_splits;  // on the tensor cores: CTAs that share a tile's groups of adapters, and the K of one
 };
 
-inline LrPlan lr_plan(int rows, int c, int n, int rank, int adapters, int sms) {
+inline LrPlan lr_plan(int rows, int c, int n, int rank, int adapters, const LrContext& ctx) {
+  const int sms = ctx.sm_count;
   LrPlan p;
   // Clocks a K block of a tile takes in a full grid, 470 of 128 rows and 750 of 256, times the tiles an SM gets.
   auto rounds = [&](int tn) { return ((long)cdiv(n, 128) * cdiv(rows, tn) + sms - 1) / sms; };
   p.tn = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rounds(256) * 750 <= rounds(128) * 470 ? 256 : 128;
   const int kb = cdiv(c, 64);
-  // Twice as many CTAs while they fit side by side and each has a block of K: an exchange costs less than what further CTAs take off the adapters' columns and the copies.
+  // Twice as many CTAs while their clusters fit side by side (16 of eight CTAs do not: 16 x 2048 x 2048 13.6 us, with clusters of four 8.5) and each has a block of K: an exchange costs less than what further CTAs take off the adapters' columns and the copies.
   // us, one / two / four blocks at least: 160x360x1756 with 23 adapters of rank 32 19 / 27 / 37, 1166x444x184 16 / 20 / 24, 7x304x300 12 / 16 / 21, 196x312x35
   // 14 / 16 / 13.  The adapters have no say: rows without one come out the same whatever the others have.
   auto share = [&](long tiles, int per_sm) {
-    int z = 1;
-    while (z < kLrMaxSplits && tiles * z * 2 <= (long)sms * per_sm && kb >= z * 2) z *= 2;
-    return z;
+    int i = 0;
+    while (i < 3 && tiles <= ctx.fit[i + 1] * per_sm && kb >= 2 << i) ++i;
+    return 1 << i;
   };
   const long tiles = (long)cdiv(n, 128) * cdiv(rows, p.tn);
   p.persist = p.tn == 256 || (p.tn == 128 && tiles > sms);
@@ -838,11 +853,11 @@ inline LrPlan lr_plan(int rows, int c, int n, int rank, int adapters, int sms) {
   p.simt = (long)rows * rank * c <= kLrSimtWork;
   p.jn = 8;
   while (p.jn > 1 && (long)rows * cdiv(rank, p.jn) < 2L * sms) p.jn /= 2;
-  // A tile whose rows are sorted has a group or two, one of mixed rows up to all: where there may be several, K is cut for four CTAs at the most, and further ones take
-  // the groups side by side.  us of a call, sorted / mixed rows, eight CTAs to a group / so: 256 x 4096 x 4096 with eight adapters of rank 64 40 / 54, 35 / 40,
-  // 1402 x 2288 x 1802 with ten 52 / 94, 53 / 85.
+  // A tile whose rows are sorted has a group or two, one of mixed rows up to all: K is cut for two groups a tile, or for four CTAs, and further ones take what groups there
+  // are side by side.  us of a call, sorted / mixed rows, all for the cut and one group after the other / so: 256 x 4096 x 4096 with eight adapters of rank 64 40 / 54, 35 / 40,
+  // 1402 x 2288 x 1802 with ten 52 / 94, 50 / 85; 4096 x 4096 x 4096 with nine, never more than half for the cut / so: 141 / 257, 134 / 262.
   const int h_tiles = cdiv(rows, kLrShrinkTN), groups = cdiv(std::min(adapters, kLrShrinkTN), 128 / (int)align_up(rank, 8));
-  p.h_splits = std::min(share(h_tiles, 2), groups > 1 ? 4 : kLrMaxSplits);
+  p.h_splits = std::max(share((long)h_tiles * std::min(std::max(groups, 1), 2), 2), std::min(share(h_tiles, 2), 4));
   p.h_groups = std::max(1, std::min(groups, 2 * sms / (h_tiles * p.h_splits)));
   return p;
 }
@@ -865,7 +880,7 @@ inline cudaError_t lr_shrink_simt(const T* x, const T* a, const float* scale, co
 }
 
 inline cudaError_t lr_run_bf16(const LrContext& ctx, LrArgs a, cudaStream_t st) {
-  const LrPlan p = lr_plan(a.rows, a.c, a.n, a.rank, a.adapters, ctx.sm_count);
+  const LrPlan p = lr_plan(a.rows, a.c, a.n, a.rank, a.adapters, ctx);
   const uintptr_t bits = (uintptr_t)a.x | (uintptr_t)a.w | (uintptr_t)a.a;
   const bool copy = a.c % 8 != 0 || (bits & 15) != 0;
   a.unit = a.c % 4 == 0 && (bits & 7) == 0 ? 8 : a.c % 2 == 0 && (bits & 3) == 0 ? 4 : 2;
@@ -900,7 +915,7 @@ inline cudaError_t lr_run_bf16(const LrContext& ctx, LrArgs a, cudaStream_t st) 
 // the fp32 model as a 1x1 layer of one pixel a row, which adds that share.
 inline cudaError_t lr_run_f32(const LrContext& ctx, const float* x, const float* w, const float* bias, const float* a, const float* b, const float* scale,
                               const int32_t* which, float* h, float* y, int rows, int c, int n, int rank, int adapters, int* err_flag, cudaStream_t st) {
-  const LrPlan p = lr_plan(rows, c, n, std::max(rank, 1), adapters, ctx.sm_count);
+  const LrPlan p = lr_plan(rows, c, n, std::max(rank, 1), adapters, ctx);
   if (adapters > 0) {
     cudaError_t e = lr_shrink_simt<float>(x, a, scale, which, h, rows, c, rank, adapters, p.jn, st);
     if (e != cudaSuccess) return e;
