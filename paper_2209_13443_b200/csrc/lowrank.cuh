@@ -19,7 +19,8 @@
 // Two forms.  At most one tile an SM: a deep ring, for the bytes in flight.  More: persistent CTAs with two accumulators, so that one tile's list of adapters, columns
 // and stores lie under the next one's products.  128 x 256 tiles where that takes less time: 128 x 128 ones ask 128 bytes a clock of L2 for every SM, and get 97.
 // What bounds it: few rows the latency of the two launches, 64 x 4096 x 4096 the bytes of W (9.3 of 19.8 us at the rate of memory), thousands of rows the tensor cores; rows in mixed
-// order the fill of h, whose columns are zero in the rows of other adapters (about 190 clocks for 32 rows of a block).
+// order the columns of all their adapters, most of them zero: a block of 64 takes the filling warps about 2600 clocks (addresses 500, h 900, the look for infinities and the hand-over
+// 700, the slot 400; plain stores in place of copies of zeros change nothing), its products 470.
 //
 // Channels that are not whole 16-byte vectors, or operands off a 16-byte boundary, cannot be fetched by TMA: eight warps then copy the
 // tiles (COPY), 8 or 4 bytes at a time without waiting for them, or 2 where a row may start between two words.  Ranks, too, need not be whole vectors: columns are
@@ -33,7 +34,6 @@ namespace ee {
 
 constexpr int kLrParts = 2;            // bf16 parts of h
 constexpr int kLrMaxRank = 128;
-constexpr int kLrMaxSplits = 8;        // CTAs of a cluster, at most
 constexpr int kLrShrinkTN = 64;        // rows of a tile of the first launch
 constexpr long kLrSimtWork = 24L << 20;  // products of the first launch up to which CUDA cores take it: every row of x reads its adapter from L2
 constexpr int kLrCopyWarps = 8, kLrFillWarps = 8;
