@@ -739,3 +739,41 @@ def test_verify_drafts_where_the_early_probabilities_are_infinite(n):
     q[0, :, 3::2], q[1, :, ::3], q[2] = -float("inf"), float("inf"), -float("inf")
     verify_case(p, q, d, u * 0 + 1 - 2.0 ** -24, r)
     verify_case(p, q, d, u, r)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 500, 48, 8), (1, 20000, 48, 8), (3, 77, 64, 32), (1, 9000, 640, 64), (2, 300, 80, 4), (1, 30000, 64, 16), (1, 25001, 24, 12), (4, 6, 96, 16), (1, 40000, 40, 8)], ids=str)
+def test_group_norm_of_groups_that_share_accesses(shape, dtype):
+    """Groups of 2, 4, 5, 6, 10 and 20 channels: a 16-byte access holds two, four or eight runs of one group each, on maps that stay and that are read twice."""
+    b, hw, c, groups = shape
+    g = gen(sum(shape))
+    x = (normal(g, b, hw, c) * (0.5 + normal(g, c).abs()) + 2 * normal(g, c)).to(TD[dtype])
+    gamma, beta, res = 1 + 0.3 * normal(g, c), 0.5 * normal(g, c), normal(g, b, hw, c).to(TD[dtype])
+    for act, residual in ((3, None), (1, res)):
+        y, raw = out_like(x.shape, TD[dtype])
+        eb.group_norm(dtype, x, b, hw, c, groups, gamma, beta, 1e-5, act, y, residual=residual)
+        norm_check(y, x, gamma, beta, groups, 1e-5, act, dtype, residual)
+        assert untouched(raw, 0, x.numel())
+    eb.operators_check()
+
+
+@pytest.mark.parametrize("order", ["mixed", "runs", "none", "one"])
+@pytest.mark.parametrize("shape", [(300, 2048, 200, 64, 12), (300, 2050, 130, 64, 9), (200, 2047, 77, 70, 12), (700, 1024, 64, 128, 20), (130, 3600, 300, 57, 130), (1500, 4096, 260, 8, 40)], ids=str)
+def test_adapted_linear_of_much_work_for_the_adapters(shape, order):
+    """a x on the tensor cores: groups of adapters that fill a tile, side by side and one after the other."""
+    linear_run("bf16", linear_operands(sum(shape), *shape, "bf16", order))
+
+
+def test_adapted_linear_of_much_work_keeps_other_rows_out_of_a_row():
+    rows, c, n, rank, adapters = 400, 2048, 260, 48, 9
+    x, w, bias, a, b, scale, which = linear_operands(8, rows, c, n, rank, adapters, "bf16")
+    y = linear_run("bf16", (x, w, bias, a, b, scale, which))
+    x, a, b = x.clone(), a.clone(), b.clone()
+    a[2], b[1], x[77] = float("nan"), float("inf"), float("inf")
+    bad, _ = out_like(y.shape, torch.bfloat16)
+    ws = torch.empty(eb.adapted_linear_workspace_bytes(rows, rank), dtype=torch.uint8, device="cuda")
+    eb.adapted_linear("bf16", x, rows, c, w, n, a, b, rank, adapters, which, bad, ws, bias=bias, scale=scale)
+    clean = (which != 1) & (which != 2)
+    clean[77] = False
+    assert torch.equal(bad[clean], y[clean]) and bool(bad[which == 2].isnan().all()) and bool((~bad[which == 1].isfinite()).all())
+    eb.operators_check()
