@@ -1076,6 +1076,7 @@ ee_status_t ee_model_create(const ee_model_desc_t* desc, void* cuda_stream, ee_m
       if (d.op == EE_OP_GROUPNORM) {
         L.kind = KK_NORM;
         if (!norm_fits(norm_plan(L.in_h * L.in_w, d.cin, d.norm_groups, (int)es, true), desc->max_batch)) return fail(EE_ERR_UNSUPPORTED);
+        if (norm_context_init() != cudaSuccess) return fail(EE_ERR_CUDA);
         if ((rc = upload<float>(m, d.scale, d.cout, ondev, st, &L.scale_dev)) != EE_OK) return fail(rc);
         if ((rc = upload<float>(m, d.bias, d.cout, ondev, st, &L.bias_dev)) != EE_OK) return fail(rc);
         continue;
@@ -1843,6 +1844,8 @@ ee_status_t operator_context(const OperatorContext** out) {
       if (!f || !flag) return EE_ERR_INTERNAL;
       EE_CUDA(cudaDeviceGetAttribute(&c.lr.sm_count, cudaDevAttrMultiProcessorCount, dev));
       EE_CUDA(lr_context_init(c.lr));
+      EE_CUDA(norm_context_init());
+      EE_CUDA(softmax_context_init());
       if (f32_context_init() != EE_OK) return EE_ERR_CUDA;
       c.lr.encode_tiled = (PFN_encodeTiled)f;
       c.flag = (int*)flag;

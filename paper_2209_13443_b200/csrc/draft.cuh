@@ -251,6 +251,21 @@ softmax_cluster_kernel(const T* x, const float* __restrict__ heat, float* y, int
 constexpr int kSmMost = kSmMaxCluster * kSmMaxPart;     // longest row that softmax takes
 
 template <typename T>
+inline size_t softmax_smem(int per) { return align_up((size_t)per * sizeof(T) + 16, 16); }
+
+// Once per device, before the first launch: set by a launch to its own need, it would be lowered under the launch of another host thread.
+inline cudaError_t softmax_context_init() {
+  cudaError_t e = cudaSuccess;
+  auto set = [&](auto kernel, size_t bytes) {
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  };
+  set(softmax_cluster_kernel<bf16>, softmax_smem<bf16>(kSmMaxPart));
+  set(softmax_cluster_kernel<float>, softmax_smem<float>(kSmMaxPart));
+  return e;
+}
+
+template <typename T>
 inline cudaError_t softmax_launch(const T* x, const float* heat, float* y, long rows, int n, int* err_flag, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.stream = st;
@@ -274,11 +289,7 @@ inline cudaError_t softmax_launch(const T* x, const float* heat, float* y, long 
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = cluster, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
-  cfg.dynamicSmemBytes = align_up((size_t)per * sizeof(T) + 16, 16);
-  cudaError_t e = cudaSuccess;
-  if (cfg.dynamicSmemBytes > 47 << 10) e = cudaFuncSetAttribute(softmax_cluster_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
-  if (e == cudaSuccess && cluster > 8) e = cudaFuncSetAttribute(softmax_cluster_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-  if (e != cudaSuccess) return e;
+  cfg.dynamicSmemBytes = softmax_smem<T>(per);
   return cudaLaunchKernelEx(&cfg, softmax_cluster_kernel<T>, x, heat, y, n, per, err_flag);
 }
 

@@ -29,6 +29,9 @@ constexpr int kNormMaxCluster = 8;
 // 64 x 80 x 80 x 128 63 -> 56, 16 of them 18.6 -> 19.8, 32 x 72 x 72 x 96 28.8 -> 30.
 constexpr int kNormChunk = 28 << 10;
 constexpr int kNormMaxChunk = 56 << 10;
+// What a CTA asks for at most: its part, 16 KB of partial statistics of 256 threads (8 bytes for each of up to eight runs of an access), and 8 bytes for each group and
+// CTA, of which there are 1024 where one CTA has the whole slice (of 2 KB) and 64 where eight have.
+constexpr int kNormMaxSmem = 80 << 10;
 
 struct NormPlan {
   int v;             // elements per access
@@ -472,10 +475,6 @@ group_norm_kernel(const __grid_constant__ NormArgs p) {
 
 template <typename T, int V, int K, bool WIDE, bool RESIDENT, int NT>
 inline cudaError_t norm_launch_k(const NormPlan& pl, const NormArgs& a, long units, cudaStream_t st) {
-  const auto kernel = group_norm_kernel<T, V, K, WIDE, RESIDENT, NT>;
-  cudaError_t e = cudaSuccess;
-  if (pl.smem() > 48 << 10) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, pl.smem());
-  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(units * pl.cluster));
   cfg.blockDim = dim3(NT);
@@ -488,7 +487,7 @@ inline cudaError_t norm_launch_k(const NormPlan& pl, const NormArgs& a, long uni
   attr[1].val.clusterDim.x = pl.cluster, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = pl.cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, a);
+  return cudaLaunchKernelEx(&cfg, group_norm_kernel<T, V, K, WIDE, RESIDENT, NT>, a);
 }
 
 template <typename T, int V, int K>
@@ -510,7 +509,35 @@ inline cudaError_t norm_launch_v(const NormPlan& pl, const NormArgs& a, long uni
 }
 
 // Whether a grid holds a call's blocks, and an int a CTA's accesses: the limit is 2^31 - 1.
-inline bool norm_fits(const NormPlan& pl, long batch) { return batch * pl.slices * pl.cluster <= 0x7fffffffL && (long)pl.rows * pl.sv <= 0x7fffffffL - 4096; }
+inline bool norm_fits(const NormPlan& pl, long batch) {
+  return batch * pl.slices * pl.cluster <= 0x7fffffffL && (long)pl.rows * pl.sv <= 0x7fffffffL - 4096 && pl.smem() <= kNormMaxSmem;
+}
+
+// Once per device, before the first launch.  What a kernel may ask for is the kernel's, not the launch's: a call that set it to its own need would lower it under
+// the launch of another host thread.  Parts that are read again need no more than the 48 KB that every kernel has.
+template <typename T, int V, int K, bool WIDE>
+inline cudaError_t norm_allow() {
+  cudaError_t e = cudaFuncSetAttribute(group_norm_kernel<T, V, K, WIDE, true, kNormThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormMaxSmem);
+  if constexpr (!WIDE)
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(group_norm_kernel<T, V, K, false, true, kNormFew>, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormMaxSmem);
+  return e;
+}
+inline cudaError_t norm_context_init() {
+  cudaError_t e = norm_allow<bf16, 8, 1, false>();
+  if (e == cudaSuccess) e = norm_allow<bf16, 8, 2, false>();
+  if (e == cudaSuccess) e = norm_allow<bf16, 8, 4, false>();
+  if (e == cudaSuccess) e = norm_allow<bf16, 8, 8, false>();
+  if (e == cudaSuccess) e = norm_allow<bf16, 8, 1, true>();
+  if (e == cudaSuccess) e = norm_allow<bf16, 1, 1, false>();
+  if (e == cudaSuccess) e = norm_allow<bf16, 1, 1, true>();
+  if (e == cudaSuccess) e = norm_allow<float, 4, 1, false>();
+  if (e == cudaSuccess) e = norm_allow<float, 4, 2, false>();
+  if (e == cudaSuccess) e = norm_allow<float, 4, 4, false>();
+  if (e == cudaSuccess) e = norm_allow<float, 4, 1, true>();
+  if (e == cudaSuccess) e = norm_allow<float, 1, 1, false>();
+  if (e == cudaSuccess) e = norm_allow<float, 1, 1, true>();
+  return e;
+}
 
 template <typename T>
 inline cudaError_t norm_launch(const void* x, const void* residual, void* y, const float* gamma, const float* beta, float eps, long batch, int hw, int c,

@@ -1,0 +1,73 @@
+"""What ee.h promises of the operators that need no model, where a plain comparison of results does not look: calls from several host threads, values at the ends
+of their types, statistics of extreme maps, what a row may depend on."""
+import ctypes as C
+import subprocess
+
+import pytest
+import torch
+
+from paper_2209_13443_b200 import binding as eb
+from tests.test_gpu_operators import gen, normal
+
+pytestmark = pytest.mark.gpu
+
+# ----------------------------------------------------------------------------- several host threads
+
+HAMMER = r"""
+#include <thread>
+typedef int (*softmax_fn)(int, const void*, int, int, const float*, float*, void*);
+typedef int (*norm_fn)(int, const void*, const void*, int, int, int, int, const float*, const float*, float, int, void*, void*);
+struct Work { const void* x; void* y; int n; void* stream; };
+// Two host threads, each with calls of its own size on a stream of its own; returns how many calls failed.
+template <typename F>
+static int both(F call, const Work* w, int times) {
+  int bad[2] = {0, 0};
+  std::thread t[2];
+  for (int i = 0; i < 2; ++i)
+    t[i] = std::thread([=, &bad] {
+      for (int k = 0; k < times; ++k) bad[i] += call(w[i]) != 0;
+    });
+  for (auto& x : t) x.join();
+  return bad[0] + bad[1];
+}
+extern "C" int hammer_softmax(void* f, const Work* w, int times) {
+  return both([f](const Work& k) { return ((softmax_fn)f)(0, k.x, 1, k.n, nullptr, (float*)k.y, k.stream); }, w, times);
+}
+extern "C" int hammer_norm(void* f, const Work* w, int times) {
+  return both([f](const Work& k) { return ((norm_fn)f)(0, k.x, nullptr, 1, k.n, 32, 1, nullptr, nullptr, 1e-5f, 0, k.y, k.stream); }, w, times);
+}
+"""
+
+
+class Work(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("n", C.c_int), ("stream", C.c_void_p)]
+
+
+@pytest.mark.parametrize("op,sizes", [("softmax", (600000, 128001)), ("norm", (3500, 3200))])
+def test_two_host_threads_with_calls_of_different_sizes(op, sizes, tmp_path):
+    """Two lengths of a row, two sizes of a map, of one kernel, both beyond the 48 KB of shared memory that a launch has without asking."""
+    src, so = tmp_path / "hammer.cpp", tmp_path / "hammer.so"
+    src.write_text(HAMMER)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-pthread", "-o", str(so), str(src)], check=True)
+    width = 1 if op == "softmax" else 32
+    xs = [normal(gen(n), n * width) for n in sizes]
+    ys = [torch.empty_like(x) for x in xs]
+    streams = [torch.cuda.Stream() for _ in sizes]
+
+    def alone(x, n):
+        y = torch.empty_like(x)
+        if op == "softmax":
+            eb.softmax("f32", x, 1, n, y)
+        else:
+            eb.group_norm("f32", x, 1, n, 32, 1, None, None, 1e-5, 0, y)
+        return y
+
+    want = [alone(x, n) for x, n in zip(xs, sizes)]
+    torch.cuda.synchronize()
+    work = (Work * 2)(*[Work(x.data_ptr(), y.data_ptr(), n, s.cuda_stream) for x, y, n, s in zip(xs, ys, sizes, streams)])
+    lib = eb.load_library()
+    entry = C.cast(lib.ee_softmax if op == "softmax" else lib.ee_group_norm, C.c_void_p)
+    failed = getattr(C.CDLL(str(so)), "hammer_" + op)(entry, work, 4000)
+    torch.cuda.synchronize()
+    assert failed == 0, f"{failed} of 8000 calls failed"
+    assert all(torch.equal(a, b) for a, b in zip(ys, want))
