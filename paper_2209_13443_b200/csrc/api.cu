@@ -1871,6 +1871,7 @@ ee_status_t ee_group_norm(int dtype, const void* x, const void* residual, int ba
   const size_t es = esize(dtype), bytes = (size_t)batch * hw * c * es;
   if (!x || !y || !aligned_to(x, es) || !aligned_to(y, es) || !aligned_to(residual, es) || !aligned_to(gamma, 4) || !aligned_to(beta, 4)) return EE_ERR_INVALID_ARG;
   if ((y != x && !apart(x, bytes, y, bytes)) || (residual && y != residual && !apart(residual, bytes, y, bytes))) return EE_ERR_INVALID_ARG;
+  if ((gamma && !apart(gamma, (size_t)c * 4, y, bytes)) || (beta && !apart(beta, (size_t)c * 4, y, bytes))) return EE_ERR_INVALID_ARG;
   if (!norm_fits(norm_plan(hw, c, groups, (int)es, true), batch) || !norm_fits(norm_plan(hw, c, groups, (int)es, false), batch)) return EE_ERR_CAPACITY;
   const OperatorContext* ctx;
   const ee_status_t s = operator_context(&ctx);

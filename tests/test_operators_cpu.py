@@ -29,6 +29,11 @@ def test_group_norm_refuses(changed):
     assert call("ee_group_norm", NORM, **changed) == INVALID
 
 
+@pytest.mark.parametrize("changed", [dict(y=P[2]), dict(y=P[3]), dict(y=P[2] + 11 * 4), dict(gamma=P[4] + 2 * 9 * 12 * 4 - 4), dict(beta=P[4] - 11 * 4), dict(gamma=P[4] + 16), dict(beta=P[4])])
+def test_group_norm_refuses_an_output_on_top_of_gamma_or_beta(changed):
+    assert call("ee_group_norm", NORM, **changed) == INVALID
+
+
 def test_group_norm_of_nothing_and_of_too_much():
     assert call("ee_group_norm", NORM, batch=0, x=None, y=None, residual=None) == 0
     # a slice a block at the least: 2^31 - 1 samples of two slices are more blocks than a grid has
