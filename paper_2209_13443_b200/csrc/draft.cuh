@@ -44,22 +44,24 @@ __device__ __forceinline__ F warp_total(F v) {
 }
 
 // A row's temperature: heat > 0 divides; anything else puts the whole mass on the first of the largest logits.
-// weight = exp((l - top) / t) as 2^((l - top) c), c = log2(e) / t.  The difference is taken first: the largest logit weighs exactly 1 however cold the row.
-// c is kept finite, so that 0 * c is 0, and above 0, so that a masked logit (-inf) weighs nothing however hot.  NaN and +inf make NaN.  Off by 2 u |l - top| / t of the
+// weight = exp((l - top) / t) as 2^((l / 2 - top / 2) c), c = 2 log2(e) / t.  The difference is taken first: the largest logit weighs exactly 1 however cold the row; and
+// of halves, in one multiply-add, which is exact where l - top is and does not overflow where that does (logits of -3e38 and 3e38 in a hot row).
+// c is kept finite, so that 0 * c is 0, and above 0, so that a masked logit (-inf) weighs nothing however hot: at t = inf, where it is 2^-149, a weight is off by
+// 3.4e38 * 2^-149 * ln 2 = 3.3e-7 (5.6 u) at most, and where c is below 2^-126 by the rounding of c, half of that.  NaN and +inf make NaN.  Off by 2 u |l - top| / t of the
 // product's two roundings and 2 units of the power; what is below 2^-126 is 0.
 struct SmScale {
   float c;
   bool greedy;
-  __device__ __forceinline__ SmScale(const float* heat, long row) : c(1.4426950408889634f), greedy(false) {
+  __device__ __forceinline__ SmScale(const float* heat, long row) : c(2.f * 1.4426950408889634f), greedy(false) {
     if (heat) {
       const float t = heat[row];
       greedy = !(t > 0.f);
-      c = fmaxf(fminf(1.4426950408889634f / t, FLT_MAX), FLT_MIN);
+      c = fmaxf(fminf(2.f * 1.4426950408889634f / t, FLT_MAX), __int_as_float(1));
     }
   }
   __device__ __forceinline__ float weight(float l, float top) const {
     float e;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"((l - top) * c));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fmaf(l, 0.5f, -0.5f * top) * c));
     return e;
   }
   // What the weights of a part are taken from: its maximum, or any number where everything is masked.

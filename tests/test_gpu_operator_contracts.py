@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2209_13443_b200 import binding as eb
-from tests.test_gpu_operators import gen, normal
+from tests.test_gpu_operators import TD, U, gen, normal, out_like, untouched
 
 pytestmark = pytest.mark.gpu
 
@@ -71,3 +71,32 @@ def test_two_host_threads_with_calls_of_different_sizes(op, sizes, tmp_path):
     torch.cuda.synchronize()
     assert failed == 0, f"{failed} of 8000 calls failed"
     assert all(torch.equal(a, b) for a, b in zip(ys, want))
+
+
+# ----------------------------------------------------------------------------- softmax at the ends of its types
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [40, 900, 5000, 70001])
+@pytest.mark.parametrize("t", [float("inf"), 3.4e38, 1.5e38, 1e38, 2e37, 1e36])
+def test_softmax_so_hot_that_the_lowest_values_count(dtype, n, t):
+    """Masks of the type's lowest value are numbers: at temperatures of their size they weigh what the formula says, infinities as masks still nothing.  Tolerance: that of
+    (l - max) / t and of its power as ever (5 u of it + 52 u + the sum's chain of n / 512), and of a factor that is a subnormal number half its step, 2^-150, of
+    at most 3.4e38 halves: 2.8 u, 5.6 u where t is infinite; each twice, for the value and for the sum."""
+    inf, low = float("inf"), torch.finfo(TD[dtype]).min
+    x = normal(gen(n), 5, n).to(TD[dtype])
+    x[0, 7:] = low
+    x[1, 5:] = -inf
+    x[2], x[2, ::2] = low, -low                            # further apart than the type's largest value
+    x[3, 3:9], x[3, 9:] = low, -inf
+    x[4] = low
+    y, raw = out_like((5, n), torch.float32)
+    eb.softmax(dtype, x, 5, n, y, temperature=torch.full((5,), t, device="cuda"))
+    z = x.double()
+    d = (z.amax(1, keepdim=True) - z) / torch.tensor(t, device="cuda").double()       # finite / inf = 0
+    d = torch.where(z == -inf, torch.full_like(d, inf), d)
+    e = torch.exp(-d)
+    ref = e / e.sum(1, keepdim=True)
+    tol = ref * U * (5 * torch.where(d < 200, d, torch.zeros_like(d)) + 52 + n / 512 + 11.2) + 2.0 ** -126
+    err = (y.double() - ref).abs()
+    assert bool((err <= tol).all()), f"off by {float((err / tol).max()):.3g} tolerances"
+    assert bool((y[x == -inf] == 0).all()) and untouched(raw, 0, 5 * n)
