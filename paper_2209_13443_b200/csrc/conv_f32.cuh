@@ -76,10 +76,11 @@ __device__ __forceinline__ void st_async_f64x2(uint32_t addr, uint32_t bar, uint
 }
 
 // V: floats per copy (4 when Cin is a multiple of 4 and the pointers are 16-byte aligned, else 1).  k_per: K range of a CTA.
+// residual may be y, and what the launch in front, beside whose end this one starts, writes: neither is __restrict__.
 template <int WM, int WN, int KG, int MF, int NF, int V>
 __global__ void __launch_bounds__(kF32Threads, KG == 1 || KG == 8 ? 2 : 1)   // two CTAs an SM, which the plan counts on: 128 registers
 conv_igemm_f64mma_kernel(const float* __restrict__ x, const float* __restrict__ w, const float* __restrict__ scale,
-                         const float* __restrict__ bias, const float* __restrict__ residual, float* __restrict__ y, ConvGeom g, int k_per,
+                         const float* __restrict__ bias, const float* residual, float* y, ConvGeom g, int k_per,
                          int* err_flag, long long wait_cycles) {
   using S = F32Tile<WM, WN, KG, MF, NF>;
   constexpr int BM = S::kBM, BN = S::kBN, KS = S::kKS, STAGES = S::kStages;

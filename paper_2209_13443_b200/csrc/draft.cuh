@@ -68,9 +68,10 @@ struct SmScale {
   __device__ __forceinline__ static float base(float top) { return top == -INFINITY ? 0.f : top; }
 };
 
+// Nothing that is read here is __restrict__: the kernel starts while the one in front, which may write it, still runs.
 template <typename T, int N>   // N values a lane
 __global__ void __launch_bounds__(128)
-softmax_warp_kernel(const T* x, const float* __restrict__ heat, float* y, long rows, int n) {
+softmax_warp_kernel(const T* x, const float* heat, float* y, long rows, int n) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const long row = (long)blockIdx.x * 4 + (threadIdx.x >> 5);
@@ -150,7 +151,7 @@ __device__ __forceinline__ float sm_word_max(uint4 w, float top) {
 // per: elements of a CTA's part (the last one's is shorter, or empty).
 template <typename T>
 __global__ void __launch_bounds__(kSmThreads, 7)
-softmax_cluster_kernel(const T* x, const float* __restrict__ heat, float* y, int n, int per, int* err_flag) {
+softmax_cluster_kernel(const T* x, const float* heat, float* y, int n, int per, int* err_flag) {
   constexpr int NW = kSmThreads / 32;
   extern __shared__ __align__(16) uint8_t sm_smem[];
   __shared__ float tops[NW];

@@ -726,9 +726,10 @@ lowrank_shrink_kernel(const T* __restrict__ x, const T* __restrict__ a, const fl
   lr_store(h, t, j, rank, scale ? f * scale[ad] : f);
 }
 
-// fp32: y[t] = s_a B_a h[t], 0 without an adapter; the projection's launch adds it as its residual operand.
+// fp32: y[t] = s_a B_a h[t], 0 without an adapter; the projection's launch adds it as its residual operand.  Starts while the launch that writes h runs: h must not be
+// __restrict__, which would promise that nobody writes it for as long as this kernel lives.
 __global__ void __launch_bounds__(256)
-lowrank_delta_kernel(const float* __restrict__ b, const int32_t* __restrict__ which, const float* __restrict__ h, float* __restrict__ y, int n, int rank, int adapters) {
+lowrank_delta_kernel(const float* __restrict__ b, const int32_t* __restrict__ which, const float* h, float* y, int n, int rank, int adapters) {
   __shared__ float s_h[kLrMaxRank];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");

@@ -122,3 +122,23 @@ def test_prototypes_match_the_header():
         decl = re.search(r"\b" + name + r"\s*\((.*?)\)\s*;", src, flags=re.S).group(1)
         want = [C.c_void_p if "*" in a else C.c_float if "float" in a else C.c_size_t if "size_t" in a else C.c_int for a in decl.split(",")]
         assert getattr(lib, name).argtypes == want, name
+
+
+def test_what_a_launch_in_front_may_write_is_not_declared_read_only():
+    """A kernel that starts before the one in front has ended must not promise (`__restrict__`) that nobody writes its inputs while it lives: such loads may be served by
+    a cache that the wait for that kernel does not clear.  Operands that only the past of the stream writes may keep it."""
+    import os
+    import re
+
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2209_13443_b200", "csrc")
+    past = {"lowrank_delta_kernel": {"b", "which"}, "conv_igemm_f64mma_kernel": {"x", "w", "scale", "bias"}}     # of the former, a plain launch is in between; of the latter, x is only copied
+    seen = 0
+    for name in ("norm.cuh", "draft.cuh", "lowrank.cuh", "conv_f32.cuh"):
+        src = open(os.path.join(csrc, name)).read()
+        for m in re.finditer(r"__global__ void[^;{]*?\n(\w+)\(([^{]*?)\) \{(.*?)\n\}\n", src, flags=re.S):
+            if "griddepcontrol.wait" not in m.group(3):
+                continue
+            seen += 1
+            only = {re.search(r"(\w+)\s*$", a).group(1) for a in m.group(2).split(",") if "__restrict__" in a}
+            assert only <= past.get(m.group(1), set()), (m.group(1), only)
+    assert seen >= 6
