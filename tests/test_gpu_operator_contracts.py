@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2209_13443_b200 import binding as eb
-from tests.test_gpu_operators import TD, U, gen, normal, out_like, untouched
+from tests.test_gpu_operators import TD, U, gen, norm_check, norm_exact, normal, out_like, untouched
 
 pytestmark = pytest.mark.gpu
 
@@ -100,3 +100,36 @@ def test_softmax_so_hot_that_the_lowest_values_count(dtype, n, t):
     err = (y.double() - ref).abs()
     assert bool((err <= tol).all()), f"off by {float((err / tol).max()):.3g} tolerances"
     assert bool((y[x == -inf] == 0).all()) and untouched(raw, 0, 5 * n)
+
+
+# ----------------------------------------------------------------------------- group norm of groups that hardly vary, and of lone extremes
+
+FLAT = [(2, 40, 16, 4), (3, 957, 96, 32), (1, 12544, 96, 8), (1, 60001, 64, 4), (2, 9, 1001, 1), (1, 20000, 3, 1), (1, 30, 6006, 1), (1, 10, 4096, 1), (1, 30000, 520, 40), (2, 3136, 64, 64), (3, 100, 30, 30)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", FLAT, ids=str)
+def test_group_norm_of_constant_groups_is_beta(shape, dtype):
+    """x - mean is 0 in every value, so the result is beta and nothing else, however large the constant and however small eps."""
+    b, hw, c, groups = shape
+    beta = normal(gen(2), c)
+    y, raw = out_like((b, hw, c), TD[dtype])
+    for value in (1000.0, 3008.0, 100.0, 0.3, -7e6):
+        x = torch.full((b, hw, c), value, device="cuda").to(TD[dtype])
+        for eps in (1e-5, 1e-12):
+            eb.group_norm(dtype, x, b, hw, c, groups, None, beta, eps, 0, y)
+            assert torch.equal(y, beta.to(TD[dtype]).expand_as(y)), (value, eps, float((y.float() - beta).abs().max()))
+    assert untouched(raw, 0, x.numel())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", FLAT, ids=str)
+def test_group_norm_of_groups_that_hardly_vary(shape, dtype):
+    """Some values one step of bf16 above the others."""
+    b, hw, c, groups = shape
+    x = torch.full((b, hw, c), 1000.0, device="cuda")
+    x[torch.rand((b, hw, c), generator=gen(4), device="cuda") < 0.02] = 1004.0
+    x = x.to(TD[dtype])
+    y, _ = out_like(x.shape, TD[dtype])
+    eb.group_norm(dtype, x, b, hw, c, groups, None, None, 1e-5, 0, y)
+    norm_check(y, x, None, None, groups, 1e-5, 0, dtype)
