@@ -259,40 +259,44 @@ group_norm_kernel(const __grid_constant__ NormArgs p) {
   const int per_group = p.bins / p.groups;             // bins of a group
   const int r_first = lane / per_group, r_step = 32 / per_group, b_first = lane - r_first * per_group, b_step = 32 - r_step * per_group;
 
-  // One pass: a thread sums d = x - shift and d^2 about its own first value of the group (or channel), which cancels as little as its few values
-  // allow: one of n values is at most sqrt(n) deviations off, so the squares lose at most n of the 2^24.
-  float shift[K], mean[K], m2[K];
+  // One pass, in runs of kRun accesses: a thread sums d = x - mean and d^2, about its own first value of the group (or channel) in the first run and its mean so far in
+  // the later ones.  With s and q the run's sums and N the thread's values with it, the mean moves by s / N and the squares grow by q - s^2 / N.  In short runs, because
+  // where the first value is an extreme one, n values in chains of m lose n m / 2 roundings (u = 2^-24) of what they say of it: 512 u with 16 fp32 accesses (32 of one
+  // value), 8192 u with 32 of bf16, an eighth of the result's own rounding; without runs 2 % of the deviation of a map of 1024 x 1024.
+  float mean[K], m2[K];                                // mean: what the differences are from
 #pragma unroll
-  for (int k = 0; k < K; ++k) shift[k] = 0.f;
+  for (int k = 0; k < K; ++k) mean[k] = m2[k] = 0.f;
   {
     const int r0 = WIDE ? tid / p.sv : ty, c0 = WIDE ? tid % p.sv : col0;
     if (active && r0 < rows) {
       float f[V];
       norm_unpack<T, V>(held(r0, c0), f);
 #pragma unroll
-      for (int k = 0; k < K; ++k) shift[k] = f[k * G];
+      for (int k = 0; k < K; ++k) mean[k] = f[k * G];
     }
   }
-  if constexpr (V == 1) {
-    float s = 0.f, q = 0.f;
-    each([&](int row, int col) {
-      float f[1];
-      norm_unpack<T, V>(held(row, col), f);
-      const float d = f[0] - shift[0];
-      s += d, q = fmaf(d, d, q);
-    });
-    mean[0] = s, m2[0] = q;
-  } else {
-    // Pairs of accumulators: of one part, two elements of it (and two chains where an access is summed together); else of two neighbouring parts.
-    constexpr int A = K == 1 ? 2 : G > 1 ? K : P;
-    f32x2 s[A], q[A], less[P];
+  // Pairs of accumulators: of one part, two elements of it (and two chains where an access is summed together); else of two neighbouring parts.
+  constexpr int A = K == 1 ? 2 : G > 1 ? K : P;
+  constexpr int kRun = V == 4 ? 16 : 32;
+  f32x2 s[A], q[A], less[P];
+  float s1 = 0.f, q1 = 0.f;              // V = 1
+  auto begin = [&]() {
+    if constexpr (V == 1) {
+      s1 = q1 = 0.f;
+    } else {
 #pragma unroll
-    for (int i = 0; i < A; ++i) s[i] = q[i] = 0ull;
+      for (int i = 0; i < A; ++i) s[i] = q[i] = 0ull;
 #pragma unroll
-    for (int i = 0; i < P; ++i) less[i] = pair_of(-shift[2 * i / G], -shift[(2 * i + 1) / G]);
-    each([&](int row, int col) {
-      float f[V];
-      norm_unpack<T, V>(held(row, col), f);
+      for (int i = 0; i < P; ++i) less[i] = pair_of(-mean[2 * i / G], -mean[(2 * i + 1) / G]);
+    }
+  };
+  auto add = [&](int row, int col) {
+    float f[V];
+    norm_unpack<T, V>(held(row, col), f);
+    if constexpr (V == 1) {
+      const float d = f[0] - mean[0];
+      s1 += d, q1 = fmaf(d, d, q1);
+    } else {
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         const int at = K == 1 ? i & 1 : G > 1 ? 2 * i / G : i;
@@ -300,29 +304,56 @@ group_norm_kernel(const __grid_constant__ NormArgs p) {
         s[at] = pair_add(s[at], d);
         q[at] = pair_fma(d, d, q[at]);
       }
-    });
-    if constexpr (K == 1) {
+    }
+  };
+  auto end = [&](float inv) {            // 1 / N
+    auto join = [&](int k, float u, float v) {
+      m2[k] += fmaxf(fmaf(-u * inv, u, v), 0.f);
+      mean[k] = fmaf(u, inv, mean[k]);
+    };
+    if constexpr (V == 1) {
+      join(0, s1, q1);
+    } else if constexpr (K == 1) {
       float u[4], v[4];
       pair_split(s[0], u[0], u[1]), pair_split(s[1], u[2], u[3]), pair_split(q[0], v[0], v[1]), pair_split(q[1], v[2], v[3]);
-      mean[0] = (u[0] + u[1]) + (u[2] + u[3]), m2[0] = (v[0] + v[1]) + (v[2] + v[3]);
+      join(0, (u[0] + u[1]) + (u[2] + u[3]), (v[0] + v[1]) + (v[2] + v[3]));
     } else {
 #pragma unroll
       for (int i = 0; i < A; ++i) {
         float u[2], v[2];
         pair_split(s[i], u[0], u[1]), pair_split(q[i], v[0], v[1]);
-        if constexpr (G > 1) mean[i] = u[0] + u[1], m2[i] = v[0] + v[1];
-        else mean[2 * i] = u[0], mean[2 * i + 1] = u[1], m2[2 * i] = v[0], m2[2 * i + 1] = v[1];
+        if constexpr (G > 1) join(i, u[0] + u[1], v[0] + v[1]);
+        else join(2 * i, u[0], v[0]), join(2 * i + 1, u[1], v[1]);
       }
+    }
+  };
+  const int mine = active ? full + ((WIDE ? tid : ty) < more ? 1 : 0) : 0;     // accesses of this thread
+  if constexpr (WIDE) {
+    for (int done = 0, col = tid, row = 0; done < mine;) {
+      const int last = mine - done > kRun ? done + kRun : mine;
+      begin();
+      for (; done < last; ++done, col += NT) {
+        while (col >= p.sv) col -= p.sv, ++row;
+        add(row, col);
+      }
+      end(1.f / ((float)done * (float)G));
+    }
+  } else {
+    for (int done = 0, row = ty; done < mine;) {
+      const int last = mine - done > kRun ? done + kRun : mine;
+      begin();
+#pragma unroll 4
+      for (; done < last; ++done, row += ty_n) add(row, col0);
+      end(1.f / ((float)done * (float)G));
     }
   }
   // (mean, squares) of the thread's K columns; of a warp's, about the mean of its first pixel's thread; of a group, by one warp over the rows of red
   {
-    const float n = active ? count_of(WIDE ? tid : ty) : 0.f, inv = n > 0.f ? 1.f / n : 0.f;
+    const float n = (float)mine * (float)G;
     const float n_row = WIDE || by_warp ? count_of_row(warp) : n, inv_row = n_row > 0.f ? 1.f / n_row : 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const float s = mean[k];
-      float mu = shift[k] + s * inv, m = fmaxf(fmaf(-s * inv, s, m2[k]), 0.f);
+      float mu = mean[k], m = m2[k];
       if (WIDE || by_warp) {
         const int stride = WIDE ? 1 : p.sv, others = WIDE ? 32 : warp_rows;
         const float ref = __shfl_sync(0xffffffffu, mu, col0 & 31), d = n > 0.f ? mu - (WIDE ? __shfl_sync(0xffffffffu, mu, 0) : ref) : 0.f;

@@ -133,3 +133,23 @@ def test_group_norm_of_groups_that_hardly_vary(shape, dtype):
     y, _ = out_like(x.shape, TD[dtype])
     eb.group_norm(dtype, x, b, hw, c, groups, None, None, 1e-5, 0, y)
     norm_check(y, x, None, None, groups, 1e-5, 0, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 1 << 20, 64, 8), (1, 1 << 18, 64, 1), (1, 50176, 32, 4), (1, 90000, 37, 1), (2, 2401, 37, 1), (1, 100003, 24, 8), (1, 70000, 64, 64), (1, 12544, 4096, 2)], ids=str)
+def test_group_norm_of_one_extreme_pixel(shape, dtype):
+    """A map of zeros but for its first pixel, of 10000: all differences but one are alike, and extreme, where they are taken from the first value.  A run of r accesses
+    of V values, in four chains (one where V = 1), loses up to (r V)^2 / 8 u (r^2 / 2 u) of the mean and of the squares of its thread: with V = 4, r = 16 (fp32) and V = 1, r = 32
+    512 u, with V = 8, r = 32 (bf16) 8192 u; half of the squares' goes into the deviation.  The sums of up to 300 later runs lose r V / 4 k u (r / k u) of the mean in the k-th
+    (ln 300 + 1 < 7 of them), and its rounding one u each; the joins of threads, warps and CTAs below 100 u."""
+    b, hw, c, groups = shape
+    x = torch.zeros(b, hw, c, device="cuda")
+    x[:, 0] = 1e4
+    x = x.to(TD[dtype])
+    y, _ = out_like(x.shape, TD[dtype])
+    eb.group_norm(dtype, x, b, hw, c, groups, None, None, 1e-5, 0, y)
+    ref = norm_exact(x, None, None, groups, 1e-5, 0)[0]
+    lost = (1.5 * (512 if dtype == "f32" else 8192) + 7 * 64 + 300 + 100) * U
+    tol = ref.abs() * (lost + (0 if dtype == "f32" else 2.0 ** -8 * (1 + lost))) + U * 1e-3
+    err = (y.double() - ref).abs()
+    assert bool((err <= tol).all()), f"off by {float((err / tol).max()):.3g} tolerances"
