@@ -34,6 +34,7 @@ namespace ee {
 
 constexpr int kLrParts = 2;            // bf16 parts of h
 constexpr int kLrMaxRank = 128;
+constexpr float kLrBf16Max = 3.3895313892515355e38f;   // the largest bf16
 constexpr int kLrShrinkTN = 64;        // rows of a tile of the first launch
 constexpr long kLrSimtWork = 24L << 20;  // products of the first launch up to which CUDA cores take it: every row of x reads its adapter from L2
 constexpr int kLrCopyWarps = 8, kLrFillWarps = 8;
@@ -75,7 +76,7 @@ __device__ __forceinline__ void mbar_arrive_n(uint32_t bar, uint32_t n) {
 
 // Number j of row t's h: for the bf16 product as two parts, for the fp32 one as it is.
 __device__ __forceinline__ void lr_store(bf16* h, int t, int j, int rank, float v) {
-  const bf16 hi = __float2bfloat16_rn(v);
+  const bf16 hi = isfinite(v) && fabsf(v) > kLrBf16Max ? __float2bfloat16_rz(v) : __float2bfloat16_rn(v);   // what would round to an infinity is cut: the rest has the remainder
   h[((size_t)t * 2) * rank + j] = hi;
   const float rest = v - __bfloat162float(hi);
   h[((size_t)t * 2 + 1) * rank + j] = __float2bfloat16_rn(isfinite(rest) ? rest : 0.f);   // of an infinity nothing is left

@@ -102,6 +102,25 @@ def test_softmax_so_hot_that_the_lowest_values_count(dtype, n, t):
     assert bool((y[x == -inf] == 0).all()) and untouched(raw, 0, 5 * n)
 
 
+# ----------------------------------------------------------------------------- adapted projection
+
+@pytest.mark.parametrize("rows,c,rank", [(3, 8, 1), (100, 8, 1), (300, 4096, 48)])
+@pytest.mark.parametrize("scale", [3.4e38, -3.4e38, 3.395e38])
+def test_adapted_linear_of_the_largest_finite_sums(rows, c, rank, scale):
+    """scale * a x is a float above the largest bf16: its two bf16 parts are that and the remainder, not an infinity.  b brings it back, so y = scale * 2^-127: off by 2^-17 of it for
+    the two parts and half a step of bf16."""
+    n = 16
+    x, w, a, b = (torch.zeros(s, dtype=torch.bfloat16, device="cuda") for s in ((rows, c), (n, c), (1, rank, c), (1, n, rank)))
+    x[:, 0], a[0, rank - 1, 0] = 1.0, 1.0
+    b[0, :, rank - 1] = 2.0 ** -127
+    y, raw = out_like((rows, n), torch.bfloat16)
+    ws = torch.empty(eb.adapted_linear_workspace_bytes(rows, rank) + 256, dtype=torch.uint8, device="cuda")
+    which = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    eb.adapted_linear("bf16", x, rows, c, w, n, a, b, rank, 1, which, y, ws, scale=torch.tensor([scale], device="cuda"))
+    want = float(torch.tensor(scale, dtype=torch.float32)) * 2.0 ** -127
+    assert bool(((y.double() - want).abs() <= abs(want) * (2.0 ** -17 + 2.0 ** -8)).all()) and untouched(raw, 0, rows * n)
+
+
 # ----------------------------------------------------------------------------- group norm of groups that hardly vary, and of lone extremes
 
 FLAT = [(2, 40, 16, 4), (3, 957, 96, 32), (1, 12544, 96, 8), (1, 60001, 64, 4), (2, 9, 1001, 1), (1, 20000, 3, 1), (1, 30, 6006, 1), (1, 10, 4096, 1), (1, 30000, 520, 40), (2, 3136, 64, 64), (3, 100, 30, 30)]
