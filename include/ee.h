@@ -401,7 +401,8 @@ ee_status_t ee_group_norm(int dtype, const void* x, const void* residual, int ba
  * a row whose adapter[t] is negative or >= n_adapters has none.  x: [rows][c], weight: [n][c], a: [n_adapters][rank][c],
  * b: [n_adapters][n][rank], y: [rows][n], all of dtype; bias: [n] fp32 (NULL = 0), scale: [n_adapters] fp32 (NULL = 1),
  * adapter: [rows].  Rows need not be sorted by adapter (rows of one adapter beside one another cost least).  Sums: bf16 products
- * in fp32 (a x enters the second product as two bf16 parts, 2^-17 of it), fp32 products in fp64; one rounding to dtype.
+ * in fp32 (scale * a x enters the second product as two bf16 parts, 2^-17 of it) and one rounding to bf16; fp32 products in fp64, with
+ * scale * a x and the adapter's share of y rounded to fp32 on their way (2^-24 of each), and their sum with the rest once more.
  * rank: 1 to 128.  n_adapters = 0 is the plain projection (a, b, adapter and workspace may be NULL).  `workspace` (256-byte
  * aligned): at least ee_adapted_linear_workspace_bytes(rows, rank) bytes, undefined afterwards; calls that may overlap (two
  * streams, or two captured graphs) need one each.  y and the workspace must not overlap anything else.  How the sums are grouped depends

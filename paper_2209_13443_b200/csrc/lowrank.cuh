@@ -723,8 +723,7 @@ lowrank_shrink_kernel(const T* __restrict__ x, const T* __restrict__ a, const fl
   __syncthreads();
   if (lane != 0 || part != 0 || j >= rank) return;
   for (int k = 1; k < parts; ++k) sum += s_sum[warp + k * jn];
-  const float f = (float)sum;
-  lr_store(h, t, j, rank, scale ? f * scale[ad] : f);
+  lr_store(h, t, j, rank, (float)(scale ? sum * (acc_t)scale[ad] : sum));
 }
 
 // fp32: y[t] = s_a B_a h[t], 0 without an adapter; the projection's launch adds it as its residual operand.  Starts while the launch that writes h runs: h must not be

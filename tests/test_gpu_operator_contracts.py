@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2209_13443_b200 import binding as eb
-from tests.test_gpu_operators import TD, U, gen, norm_check, norm_exact, normal, out_like, untouched
+from tests.test_gpu_operators import TD, U, gen, linear_operands, norm_check, norm_exact, normal, out_like, untouched
 
 pytestmark = pytest.mark.gpu
 
@@ -119,6 +119,21 @@ def test_adapted_linear_of_the_largest_finite_sums(rows, c, rank, scale):
     eb.adapted_linear("bf16", x, rows, c, w, n, a, b, rank, 1, which, y, ws, scale=torch.tensor([scale], device="cuda"))
     want = float(torch.tensor(scale, dtype=torch.float32)) * 2.0 ** -127
     assert bool(((y.double() - want).abs() <= abs(want) * (2.0 ** -17 + 2.0 ** -8)).all()) and untouched(raw, 0, rows * n)
+
+
+@pytest.mark.parametrize("shape", [(300, 64, 40, 5), (9, 1001, 300, 3)], ids=str)
+def test_adapted_linear_f32_rounds_the_scaled_sum_once(shape):
+    """Rank 1, b = 1 and no shared weight leave y = scale * a x rounded to fp32.  The sum itself is off by c 2^-53 of its magnitudes, so one value in 2^29 / c, times what cancels in it,
+    could round the other way: none of the few hundred here, and of c = 1001 at most one."""
+    rows, c, n, m = shape
+    x, w, _, a, b, scale, which = linear_operands(1, rows, c, n, 1, m, "f32")
+    w, b = torch.zeros_like(w), torch.ones_like(b)
+    y, raw = out_like((rows, n), torch.float32)
+    ws = torch.empty(eb.adapted_linear_workspace_bytes(rows, 1) + 256, dtype=torch.uint8, device="cuda")
+    eb.adapted_linear("f32", x, rows, c, w, n, a, b, 1, m, which, y, ws, scale=scale)
+    at = which.long().clamp(min=0)
+    want = torch.where(which >= 0, (x.double() * a[at, 0].double()).sum(1) * scale[at].double(), torch.zeros(rows, dtype=torch.float64, device="cuda")).float()
+    assert int((y[:, 0] != want).sum()) <= (1 if c > 1000 else 0) and torch.equal(y, y[:, :1].expand_as(y)) and untouched(raw, 0, rows * n)
 
 
 # ----------------------------------------------------------------------------- group norm of groups that hardly vary, and of lone extremes
