@@ -406,7 +406,9 @@ ee_status_t ee_group_norm(int dtype, const void* x, const void* residual, int ba
  * rank: 1 to 128.  n_adapters = 0 is the plain projection (a, b, adapter and workspace may be NULL).  `workspace` (256-byte
  * aligned): at least ee_adapted_linear_workspace_bytes(rows, rank) bytes, undefined afterwards; calls that may overlap (two
  * streams, or two captured graphs) need one each.  y and the workspace must not overlap anything else.  How the sums are grouped depends
- * on the number of rows, so a row's last bit may.  Errors: INVALID_ARG, CAPACITY (workspace too small, more than 2^22 rows, c or
+ * on the number of rows and, for a row with an adapter, on n_adapters, on its place among the rows and on the adapters that the others name: its
+ * last bits may (about three of 100 000 bf16 values, by one step, when the others change theirs).  A row without an adapter has the bits of the
+ * plain projection of as many rows.  Errors: INVALID_ARG, CAPACITY (workspace too small, more than 2^22 rows, c or
  * n above 2^20), CUDA. */
 ee_status_t ee_adapted_linear(int dtype, const void* x, int rows, int c, const void* weight, int n, const float* bias, const void* a,
                               const void* b, int rank, int n_adapters, const float* scale, const int32_t* adapter, void* y,

@@ -4,7 +4,8 @@
 // Two launches.  The first forms h[t] = s_a A_a x[t], rank numbers a row, in the caller's workspace; the second is the product with W on
 // tcgen05, whose K loop goes on behind the last channel: for the adapters that occur in its tile of rows it appends columns, of
 // B_a on one side and of h[t] on the other, zero in the rows of other adapters.  So the adapters of a tile, in any order and mix, cost
-// their rank in additional K, and the sum is rounded once.  h is kept and multiplied as two bf16 parts, h and what its rounding left (2^-17
+// their rank in additional K, and the sum is rounded once.  Where in the sum a row's columns come, and in which CTA of a cluster, follows from the place of its adapter in
+// the tile's list: its fp32 sum is grouped by what the other rows of the tile name.  Columns of zeros change no sum: a row without an adapter is not touched by them.  h is kept and multiplied as two bf16 parts, h and what its rounding left (2^-17
 // of h together, 2 rank columns): rounded to one part the adapter's share would carry a second rounding of the size of the result's.
 //
 // The tile is turned: 128 filters are the rows of the accumulator (lanes) and 16 to 128 rows of the batch its columns, so that few

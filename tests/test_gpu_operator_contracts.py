@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2209_13443_b200 import binding as eb
-from tests.test_gpu_operators import TD, U, gen, linear_operands, norm_check, norm_exact, normal, out_like, untouched
+from tests.test_gpu_operators import TD, U, gen, linear_operands, linear_run, norm_check, norm_exact, normal, out_like, untouched
 
 pytestmark = pytest.mark.gpu
 
@@ -134,6 +134,33 @@ def test_adapted_linear_f32_rounds_the_scaled_sum_once(shape):
     at = which.long().clamp(min=0)
     want = torch.where(which >= 0, (x.double() * a[at, 0].double()).sum(1) * scale[at].double(), torch.zeros(rows, dtype=torch.float64, device="cuda")).float()
     assert int((y[:, 0] != want).sum()) <= (1 if c > 1000 else 0) and torch.equal(y, y[:, :1].expand_as(y)) and untouched(raw, 0, rows * n)
+
+
+@pytest.mark.parametrize("shape", [(64, 4096, 512, 16, 32), (300, 520, 4099, 24, 7), (20, 512, 256, 5, 4), (256, 4096, 1024, 64, 9), (200, 2047, 300, 8, 12)], ids=str)
+def test_adapted_linear_of_rows_beside_others_adapters(shape):
+    """Half of the rows keep their adapters while the other half change theirs, and while the pool of adapters grows.  Rows without one keep their bits, the others what the
+    order of a sum in fp32 moves: each call's values are within linear_check's bound (linear_run), so two calls' within twice that, the roundings to bf16 included."""
+    rows, c, n, rank, m = shape
+    x, w, bias, a, b, scale, which = linear_operands(8, *shape, "bf16")
+    which[::8] = -1
+    keep = torch.arange(rows, device="cuda") % 2 == 0
+    first = linear_run("bf16", (x, w, bias, a, b, scale, which))
+    has, none = keep & (which >= 0), keep & (which < 0)
+    assert bool(has.any()) and bool(none.any())
+    for seed in range(3):
+        others = torch.randint(-1, m, (rows,), generator=gen(seed), device="cuda").int()
+        changed = torch.where(keep, which, others)
+        if seed == 2:
+            a, b, scale = (torch.cat([t, torch.zeros((40,) + t.shape[1:], dtype=t.dtype, device="cuda")]) for t in (a, b, scale))
+        y = linear_run("bf16", (x, w, bias, a, b, scale, changed))
+        assert torch.equal(y[none], first[none])
+        mag = x.double().abs() @ w.double().abs().t() + bias.double().abs()
+        at = which.long().clamp(min=0)
+        h = torch.bmm(a[at].double().abs(), x.double().abs()[:, :, None])
+        share = torch.bmm(b[at].double().abs(), h)[:, :, 0] * scale[at, None].double()
+        lost = (c / 16 + 20) * 2 * U * (mag + 2 * share) + 2.0 ** -17 * share
+        off = (y.double() - first.double()).abs()
+        assert bool((off <= 2 * (lost + 2.0 ** -8 * (first.double().abs() + lost)))[has].all())
 
 
 # ----------------------------------------------------------------------------- group norm of groups that hardly vary, and of lone extremes
