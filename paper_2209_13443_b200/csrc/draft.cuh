@@ -332,7 +332,7 @@ __device__ __forceinline__ double warp_scan(double v, int lane) {   // inclusive
 
 __global__ void __launch_bounds__(kVfThreads, 4)
 verify_drafts_kernel(VerifyArgs a) {
-  __shared__ int s_got, s_count, s_again;
+  __shared__ int s_got, s_count, s_next;
   __shared__ double s_block[kVfBlocks], s_total[2][kVfMaxCluster];
   __shared__ uint64_t bars[2];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -427,7 +427,6 @@ verify_drafts_kernel(VerifyArgs a) {
               ::"r"(smem_u32(&s_total[round][rank])), "r"(here), "r"(lane), "l"(__double_as_longlong(mine))
               : "memory");
         ok = __all_sync(0xffffffffu, mbar_wait_cluster(here, 0, a.err_flag, kTcWaitCycles));
-        if (!ok) ok = __all_sync(0xffffffffu, mbar_wait_cluster(here, 0, a.err_flag, kTcWaitCycles));   // stays until what is sent to it has landed
         total = 0.0;
         for (int c = 0; c < (int)cluster; ++c) {
           const double o = s_total[round][c];
@@ -476,10 +475,13 @@ verify_drafts_kernel(VerifyArgs a) {
         for (int i = lane; i <= a.k; i += 32) out[i] = i < got ? a.drafts[(size_t)b * a.k + i] : i == got ? token : -1;
         if (lane == 0) a.accepted[b] = got;
       }
-      if (lane == 0) s_again = again;
+      if (lane == 0) s_next = ok ? again : 2;
     }
     __syncthreads();
-    if (!s_again) break;
+    if (s_next != 1) {
+      if (s_next == 2) cluster_drain(arrived + 8u * round, 0, a.err_flag);      // the status says so, and where the token would have been of this part, the outputs stay as they are
+      break;
+    }
   }
 }
 

@@ -234,6 +234,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     tiles = (s_count[0] + per_tile - 1) / per_tile;
   }
   const bool idle = SHRINK && tiles <= tile0;    // no adapters here
+  bool lost = false;                             // the cluster's parts have not come
   auto here = [&](int group) { return min(per_tile, s_count[0] - group * per_tile); };      // adapters of a group
 
   struct Walk {      // over the ring
@@ -611,7 +612,8 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
               }
             }
           }
-          ok = __all_sync(0xffffffffu, mbar_wait_cluster(part_bar, 0, p.err_flag, kTcWaitCycles) || mbar_wait_cluster(part_bar, 0, p.err_flag, kTcWaitCycles)) && ok;
+          lost = !__all_sync(0xffffffffu, mbar_wait_cluster(part_bar, 0, p.err_flag, kTcWaitCycles));
+          ok = ok && !lost;
           const float* in = reinterpret_cast<const float*>(gen + S::kOffPart);
           const int run = min(share, 4);
 #pragma unroll 1
@@ -669,7 +671,11 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
       if (Z > 1) asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");   // nobody reads this CTA's part any more
     }
   }
-  __syncthreads();
+  if (!SHRINK && !kPersist) {
+    if (__syncthreads_or(lost)) cluster_drain(part_bar, 0, p.err_flag);      // the status says so, and y stays as it is
+  } else {
+    __syncthreads();
+  }
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols) : "memory");
 }
 

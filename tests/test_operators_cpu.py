@@ -142,3 +142,19 @@ def test_what_a_launch_in_front_may_write_is_not_declared_read_only():
             only = {re.search(r"(\w+)\s*$", a).group(1) for a in m.group(2).split(",") if "__restrict__" in a}
             assert only <= past.get(m.group(1), set()), (m.group(1), only)
     assert seen >= 6
+
+
+def test_a_block_whose_wait_for_its_cluster_runs_out_stays_until_the_stores_to_it_have_landed():
+    """Every kernel that waits for other CTAs' asynchronous stores meets them (cluster_drain) before it leaves without them: stores that land in the shared
+    memory of a CTA that has gone are a fault."""
+    import os
+    import re
+
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2209_13443_b200", "csrc")
+    seen = 0
+    for name in ("norm.cuh", "draft.cuh", "lowrank.cuh", "conv_f32.cuh", "head.cuh"):
+        for m in re.finditer(r"__global__ void[^;{]*?\n(\w+)\([^{]*?\) \{(.*?)\n\}\n", open(os.path.join(csrc, name)).read(), flags=re.S):
+            if "mbar_wait_cluster(" in m.group(2):
+                seen += 1
+                assert "cluster_drain(" in m.group(2), m.group(1)
+    assert seen >= 6
