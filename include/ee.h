@@ -437,8 +437,14 @@ ee_status_t ee_softmax(int dtype, const void* logits, int rows, int n, const flo
 ee_status_t ee_verify_drafts(const float* p, const float* q, const int32_t* drafts, const float* u, const float* r, const int32_t* n_draft,
                              int batch, int k, int n, int32_t* tokens, int32_t* n_accepted, void* cuda_stream);
 
+/* Limit, in SM clock cycles, of a block's wait for the others of its cluster in the operators above, on the current device (default about 2 s):
+ * what ee_model_set_wait_limit is for a model.  For the calls that follow; a captured one keeps what it was captured with.  Where a wait runs out, a
+ * block leaves its part of the outputs as it is.  Errors: INVALID_ARG, CUDA. */
+ee_status_t ee_operators_set_wait_limit(long long cycles);
+
 /* Synchronises the stream and reports what ee_model_check reports, for the operators above on the current device:
- * EE_ERR_TIMEOUT when a bounded wait of one of their kernels ran out since the last call. */
+ * EE_ERR_TIMEOUT when a bounded wait of one of their kernels ran out since the last call.  A device has one such flag for all of its callers, and the
+ * call clears it: callers that share a device have to tell each other. */
 ee_status_t ee_operators_check(void* cuda_stream);
 
 const char* ee_status_string(ee_status_t s);

@@ -23,7 +23,7 @@ EXPORTS = ["ee_model_create", "ee_model_destroy", "ee_model_query", "ee_stage_ru
            "ee_exit_head_scratch_bytes", "ee_exit_head_static", "ee_gather_survivors", "ee_model_set_graphs", "ee_model_set_branches", "ee_model_set_fused_head", "ee_model_set_proj_fusion", "ee_model_set_gap_fusion", "ee_model_gap_partials", "ee_model_head_launches", "ee_model_head_pools", "ee_model_set_stage_kernel", "ee_model_set_chain", "ee_model_set_timing", "ee_model_get_timing",
            "ee_model_plan", "ee_model_check", "ee_model_set_layer_variant", "ee_model_set_layer_splits", "ee_model_get_layer_config",
            "ee_model_set_wait_limit", "ee_model_selftest_wait", "ee_wait_count", "ee_run_until_exit", "ee_group_norm", "ee_adapted_linear",
-           "ee_adapted_linear_workspace_bytes", "ee_softmax", "ee_verify_drafts", "ee_operators_check", "ee_status_string", "ee_last_cuda_error"]
+           "ee_adapted_linear_workspace_bytes", "ee_softmax", "ee_verify_drafts", "ee_operators_set_wait_limit", "ee_operators_check", "ee_status_string", "ee_last_cuda_error"]
 
 
 class EEError(RuntimeError):
@@ -125,6 +125,7 @@ def load_library() -> C.CDLL:
     L.ee_adapted_linear_workspace_bytes.restype = C.c_size_t
     L.ee_softmax.argtypes = [i, vp, i, i, vp, vp, vp]
     L.ee_verify_drafts.argtypes = [vp, vp, vp, vp, vp, vp, i, i, i, vp, vp, vp]
+    L.ee_operators_set_wait_limit.argtypes = [C.c_longlong]
     L.ee_operators_check.argtypes = [vp]
     L.ee_status_string.argtypes = [i]
     L.ee_status_string.restype = C.c_char_p
@@ -503,8 +504,13 @@ def verify_drafts(p, q, drafts, u, r, batch: int, k: int, n: int, tokens, n_acce
                                            _mem(f, tokens, i32, batch * (k + 1), d), _mem(f, n_accepted, i32, batch, d), _stream(stream, d)), f)
 
 
+def operators_set_wait_limit(cycles: int):
+    """ee_operators_set_wait_limit: how long, in SM clock cycles, a block of an operator's kernel waits for the others of its cluster."""
+    _check(load_library().ee_operators_set_wait_limit(int(cycles)), "ee_operators_set_wait_limit")
+
+
 def operators_check(stream=None):
-    """ee_operators_check: raises when a bounded wait of an operator's kernel ran out since the last call."""
+    """ee_operators_check: raises when a bounded wait of an operator's kernel ran out since the last call (by any caller on this device)."""
     _check(load_library().ee_operators_check(_stream(stream)), "ee_operators_check")
 
 

@@ -191,7 +191,7 @@ struct ee_model {
   bool proj_fusion = true;             // projection shortcuts computed inside the layer that adds them, where that applies
   int fc_room = 1;                     // clusters of the FC kernel that run side by side
   bool fused_head = false;             // bf16 models: pool + FC + decision + scan as one cluster kernel where the shape allows (an option)
-  long long wait_cycles = kTcWaitCycles;   // limit of the bounded device-side waits of the pair kernel, of the exchanges of fp32 convolutions and exit heads and of the self-test
+  long long wait_cycles = kTcWaitCycles;   // limit of the bounded device-side waits of the pair kernel, of the exchanges of fp32 convolutions, group norms and exit heads and of the self-test
   int device = -1;           // the GPU the model lives on
   bool timing = false;
   bool graphs = true;  // replay stages as CUDA graphs on capturable streams
@@ -329,7 +329,8 @@ ee_status_t launch_layer(ee_model* m, const LayerPlan& L, const void* src, const
       break;
     }
     case KK_NORM:
-      EE_CUDA(norm_launch<T>(src, res, dst, L.scale_dev, L.bias_dev, L.d.norm_eps, B, L.in_h * L.in_w, L.d.cin, L.d.norm_groups, L.d.act, L.tc.rev, m->err_flag, st));
+      EE_CUDA(norm_launch<T>(src, res, dst, L.scale_dev, L.bias_dev, L.d.norm_eps, B, L.in_h * L.in_w, L.d.cin, L.d.norm_groups, L.d.act, L.tc.rev, m->err_flag,
+                             m->wait_cycles, st));
       break;
     case KK_POOL: {
       if constexpr (sizeof(T) == 2) {
@@ -1825,11 +1826,12 @@ struct OperatorContext {   // one per device, filled at its first call
   std::atomic<int> ready{0};
   LrContext lr;
   int* flag = nullptr;
+  std::atomic<long long> wait_cycles{kTcWaitCycles};   // limit of a block's wait for the others of its cluster
 };
 OperatorContext g_operators[kMaxDevices];
 std::mutex g_operators_lock;
 
-ee_status_t operator_context(const OperatorContext** out) {
+ee_status_t operator_context(OperatorContext** out) {
   int dev = -1;
   EE_CUDA(cudaGetDevice(&dev));
   if (dev < 0 || dev >= kMaxDevices) return EE_ERR_UNSUPPORTED;
@@ -1873,12 +1875,12 @@ ee_status_t ee_group_norm(int dtype, const void* x, const void* residual, int ba
   if ((y != x && !apart(x, bytes, y, bytes)) || (residual && y != residual && !apart(residual, bytes, y, bytes))) return EE_ERR_INVALID_ARG;
   if ((gamma && !apart(gamma, (size_t)c * 4, y, bytes)) || (beta && !apart(beta, (size_t)c * 4, y, bytes))) return EE_ERR_INVALID_ARG;
   if (!norm_fits(norm_plan(hw, c, groups, (int)es, true), batch) || !norm_fits(norm_plan(hw, c, groups, (int)es, false), batch)) return EE_ERR_CAPACITY;
-  const OperatorContext* ctx;
+  OperatorContext* ctx;
   const ee_status_t s = operator_context(&ctx);
   if (s != EE_OK) return s;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  EE_CUDA(dtype == EE_BF16 ? norm_launch<bf16>(x, residual, y, gamma, beta, eps, batch, hw, c, groups, act, false, ctx->flag, st)
-                           : norm_launch<float>(x, residual, y, gamma, beta, eps, batch, hw, c, groups, act, false, ctx->flag, st));
+  EE_CUDA(dtype == EE_BF16 ? norm_launch<bf16>(x, residual, y, gamma, beta, eps, batch, hw, c, groups, act, false, ctx->flag, ctx->wait_cycles, st)
+                           : norm_launch<float>(x, residual, y, gamma, beta, eps, batch, hw, c, groups, act, false, ctx->flag, ctx->wait_cycles, st));
   return EE_OK;
 }
 
@@ -1907,18 +1909,18 @@ ee_status_t ee_adapted_linear(int dtype, const void* x, int rows, int c, const v
         !clear(adapter, (size_t)rows * 4))
       return EE_ERR_INVALID_ARG;
   }
-  const OperatorContext* ctx;
+  OperatorContext* ctx;
   const ee_status_t s = operator_context(&ctx);
   if (s != EE_OK) return s;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   if (dtype == EE_F32) {
     EE_CUDA(lr_run_f32(ctx->lr, (const float*)x, (const float*)weight, bias, (const float*)a, (const float*)b, scale, adapter, (float*)workspace, (float*)y, rows, c, n,
-                       rank, n_adapters, ctx->flag, st));
+                       rank, n_adapters, ctx->flag, ctx->wait_cycles, st));
     return EE_OK;
   }
   LrArgs p = {};
   p.x = (const bf16*)x, p.w = (const bf16*)weight, p.bias = bias, p.a = (const bf16*)a, p.b = (const bf16*)b, p.scale = scale, p.which = adapter;
-  p.h = (bf16*)workspace, p.y = (bf16*)y, p.rows = rows, p.c = c, p.n = n, p.rank = n_adapters ? rank : 1, p.adapters = n_adapters, p.err_flag = ctx->flag;
+  p.h = (bf16*)workspace, p.y = (bf16*)y, p.rows = rows, p.c = c, p.n = n, p.rank = n_adapters ? rank : 1, p.adapters = n_adapters, p.err_flag = ctx->flag, p.wait_cycles = ctx->wait_cycles;
   EE_CUDA(lr_run_bf16(ctx->lr, p, st));
   return EE_OK;
 }
@@ -1932,11 +1934,11 @@ ee_status_t ee_softmax(int dtype, const void* logits, int rows, int n, const flo
   if (!(temperature == nullptr || apart(temperature, (size_t)rows * 4, probs, (size_t)rows * n * 4))) return EE_ERR_INVALID_ARG;
   if (n > kSmMost || (long)rows * kSmMaxCluster > 0x7fffffffL) return EE_ERR_CAPACITY;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  const OperatorContext* ctx;
+  OperatorContext* ctx;
   const ee_status_t s = operator_context(&ctx);
   if (s != EE_OK) return s;
-  EE_CUDA(dtype == EE_BF16 ? softmax_launch<bf16>((const bf16*)logits, temperature, probs, rows, n, ctx->flag, st)
-                           : softmax_launch<float>((const float*)logits, temperature, probs, rows, n, ctx->flag, st));
+  EE_CUDA(dtype == EE_BF16 ? softmax_launch<bf16>((const bf16*)logits, temperature, probs, rows, n, ctx->flag, ctx->wait_cycles, st)
+                           : softmax_launch<float>((const float*)logits, temperature, probs, rows, n, ctx->flag, ctx->wait_cycles, st));
   return EE_OK;
 }
 
@@ -1954,15 +1956,24 @@ ee_status_t ee_verify_drafts(const float* p, const float* q, const int32_t* draf
   if (!apart(tokens, all + row, n_accepted, row) || !clear(p, (all + row) * n) || !clear(q, all * n) || !clear(drafts, all) || !clear(u, all) || !clear(r, row) ||
       !clear(n_draft, row))
     return EE_ERR_INVALID_ARG;
-  const OperatorContext* ctx;
+  OperatorContext* ctx;
   const ee_status_t s = operator_context(&ctx);
   if (s != EE_OK) return s;
-  EE_CUDA(verify_launch({p, q, drafts, u, r, n_draft, tokens, n_accepted, k, n, 0, 0, ctx->flag}, batch, (cudaStream_t)cuda_stream));
+  EE_CUDA(verify_launch({p, q, drafts, u, r, n_draft, tokens, n_accepted, k, n, 0, 0, ctx->flag, ctx->wait_cycles}, batch, (cudaStream_t)cuda_stream));
+  return EE_OK;
+}
+
+ee_status_t ee_operators_set_wait_limit(long long cycles) {
+  if (cycles < 1) return EE_ERR_INVALID_ARG;
+  OperatorContext* ctx;
+  const ee_status_t s = operator_context(&ctx);
+  if (s != EE_OK) return s;
+  ctx->wait_cycles = cycles;
   return EE_OK;
 }
 
 ee_status_t ee_operators_check(void* cuda_stream) {
-  const OperatorContext* ctx;
+  OperatorContext* ctx;
   const ee_status_t s = operator_context(&ctx);
   if (s != EE_OK) return s;
   cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -151,7 +151,7 @@ __device__ __forceinline__ float sm_word_max(uint4 w, float top) {
 // per: elements of a CTA's part (the last one's is shorter, or empty).
 template <typename T>
 __global__ void __launch_bounds__(kSmThreads, 7)
-softmax_cluster_kernel(const T* x, const float* heat, float* y, int n, int per, int* err_flag) {
+softmax_cluster_kernel(const T* x, const float* heat, float* y, int n, int per, int* err_flag, long long wait_cycles) {
   constexpr int NW = kSmThreads / 32;
   extern __shared__ __align__(16) uint8_t sm_smem[];
   __shared__ float tops[NW];
@@ -229,7 +229,7 @@ softmax_cluster_kernel(const T* x, const float* heat, float* y, int n, int per, 
             " st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [a], {%3, %4, %5, %4}, [b];\n}"
             ::"r"(smem_u32(&parts[rank])), "r"(arrived), "r"(lane), "f"(all.top), "f"(all.sum), "f"(all.at)
             : "memory");
-      lost = !__all_sync(0xffffffffu, mbar_wait_cluster(arrived, 0, err_flag, kTcWaitCycles));
+      lost = !__all_sync(0xffffffffu, mbar_wait_cluster(arrived, 0, err_flag, wait_cycles));
       const float4 o = lane < (int)cluster ? parts[lane] : make_float4(-INFINITY, 0.f, 1e9f, 0.f);
       all = sm_join(sc, SmJoin{o.x, o.y, o.z});
     }
@@ -269,7 +269,7 @@ inline cudaError_t softmax_context_init() {
 }
 
 template <typename T>
-inline cudaError_t softmax_launch(const T* x, const float* heat, float* y, long rows, int n, int* err_flag, cudaStream_t st) {
+inline cudaError_t softmax_launch(const T* x, const float* heat, float* y, long rows, int n, int* err_flag, long long wait_cycles, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -293,7 +293,7 @@ inline cudaError_t softmax_launch(const T* x, const float* heat, float* y, long 
   attr[1].val.clusterDim.x = cluster, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
   cfg.dynamicSmemBytes = softmax_smem<T>(per);
-  return cudaLaunchKernelEx(&cfg, softmax_cluster_kernel<T>, x, heat, y, n, per, err_flag);
+  return cudaLaunchKernelEx(&cfg, softmax_cluster_kernel<T>, x, heat, y, n, per, err_flag, wait_cycles);
 }
 
 // ----------------------------------------------------------------------------- verification of drafts
@@ -314,6 +314,7 @@ struct VerifyArgs {
   int32_t* accepted;       // [batch]
   int k, n, per, block;    // values of a CTA's part, of a block (a multiple of 512)
   int* err_flag;
+  long long wait_cycles;   // limit of the waits for the cluster's totals
 };
 
 // The weight of one value: what the draw goes by.  Values that are not positive and finite weigh nothing.
@@ -426,7 +427,7 @@ verify_drafts_kernel(VerifyArgs a) {
               " st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [a], %3, [b];\n}"
               ::"r"(smem_u32(&s_total[round][rank])), "r"(here), "r"(lane), "l"(__double_as_longlong(mine))
               : "memory");
-        ok = __all_sync(0xffffffffu, mbar_wait_cluster(here, 0, a.err_flag, kTcWaitCycles));
+        ok = __all_sync(0xffffffffu, mbar_wait_cluster(here, 0, a.err_flag, a.wait_cycles));
         total = 0.0;
         for (int c = 0; c < (int)cluster; ++c) {
           const double o = s_total[round][c];

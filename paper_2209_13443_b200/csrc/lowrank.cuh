@@ -54,6 +54,7 @@ struct LrArgs {
   int rows, c, n, rank, r8, adapters;
   int unit;            // COPY: bytes of a copy, 8, 4 or 2: rows are whole units and start on their boundaries
   int* err_flag;
+  long long wait_cycles;   // limit of the wait for the cluster's partial sums
 };
 
 template <int TN, bool PERSIST, bool SHRINK = false>
@@ -612,7 +613,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
               }
             }
           }
-          lost = !__all_sync(0xffffffffu, mbar_wait_cluster(part_bar, 0, p.err_flag, kTcWaitCycles));
+          lost = !__all_sync(0xffffffffu, mbar_wait_cluster(part_bar, 0, p.err_flag, p.wait_cycles));
           ok = ok && !lost;
           const float* in = reinterpret_cast<const float*>(gen + S::kOffPart);
           const int run = min(share, 4);
@@ -922,7 +923,8 @@ inline cudaError_t lr_run_bf16(const LrContext& ctx, LrArgs a, cudaStream_t st) 
 // fp32: h and the adapters' share on CUDA cores (summed in fp64, like everything of the fp32 model), then the projection on the convolution kernel of
 // the fp32 model as a 1x1 layer of one pixel a row, which adds that share.
 inline cudaError_t lr_run_f32(const LrContext& ctx, const float* x, const float* w, const float* bias, const float* a, const float* b, const float* scale,
-                              const int32_t* which, float* h, float* y, int rows, int c, int n, int rank, int adapters, int* err_flag, cudaStream_t st) {
+                              const int32_t* which, float* h, float* y, int rows, int c, int n, int rank, int adapters, int* err_flag, long long wait_cycles,
+                              cudaStream_t st) {
   const LrPlan p = lr_plan(rows, c, n, std::max(rank, 1), adapters, ctx);
   if (adapters > 0) {
     cudaError_t e = lr_shrink_simt<float>(x, a, scale, which, h, rows, c, rank, adapters, p.jn, st);
@@ -942,7 +944,7 @@ inline cudaError_t lr_run_f32(const LrContext& ctx, const float* x, const float*
   const bool vec = c % 4 == 0 && (((uintptr_t)x | (uintptr_t)w) & 15) == 0;
   const ConvGeom g{rows, 1, 1, c, 1, 1, n, 1, 1, 1, 0, 0, EE_ACT_NONE};
   // Behind the adapters' launches, which the stream's past is over for, W and the bias may be fetched early; behind anything else they may be its output.
-  return f32_launch(f32_plan(rows, n, c, ctx.sm_count, vec), x, w, nullptr, bias, adapters > 0 ? y : nullptr, y, g, err_flag, kTcWaitCycles, st, adapters > 0);
+  return f32_launch(f32_plan(rows, n, c, ctx.sm_count, vec), x, w, nullptr, bias, adapters > 0 ? y : nullptr, y, g, err_flag, wait_cycles, st, adapters > 0);
 }
 
 }  // namespace ee

@@ -56,6 +56,7 @@ struct NormArgs {
   int hw, c, cpg, act;
   int sv, slices, groups, rows, chunk, red_rows, bins;
   int* err_flag;
+  long long wait_cycles;   // limit of the wait for the cluster's statistics
   int rev;           // 1: from the last sample down (the newest samples of the input are the ones still in L2)
 };
 
@@ -408,7 +409,7 @@ group_norm_kernel(const __grid_constant__ NormArgs p) {
   // The cluster's statistics.
   if (cluster > 1) {
     for (int g0 = warp * 2; g0 < p.groups; g0 += NW * 2) {      // sixteen lanes a group
-      if (g0 == warp * 2 && !__all_sync(0xffffffffu, mbar_wait_cluster(arrived, 0, p.err_flag, kTcWaitCycles))) lost = true;
+      if (g0 == warp * 2 && !__all_sync(0xffffffffu, mbar_wait_cluster(arrived, 0, p.err_flag, p.wait_cycles))) lost = true;
       const int r = lane & 15, g = g0 + (lane >> 4);
       const float w = r < (int)cluster ? (float)max(0, min(p.rows, p.hw - r * p.rows)) * (float)p.cpg : 0.f;
       const float2 v = w > 0.f && g < p.groups ? stat[g * (int)cluster + r] : make_float2(0.f, 0.f);
@@ -571,12 +572,12 @@ inline cudaError_t norm_context_init() {
 
 template <typename T>
 inline cudaError_t norm_launch(const void* x, const void* residual, void* y, const float* gamma, const float* beta, float eps, long batch, int hw, int c,
-                               int groups, int act, bool rev, int* err_flag, cudaStream_t st) {
+                               int groups, int act, bool rev, int* err_flag, long long wait_cycles, cudaStream_t st) {
   const bool aligned = (((uintptr_t)x | (uintptr_t)residual | (uintptr_t)y) & 15) == 0;
   const NormPlan pl = norm_plan(hw, c, groups, (int)sizeof(T), aligned);
   if (!norm_fits(pl, batch)) return cudaErrorInvalidValue;
   const NormArgs a = {x, residual, y, gamma, beta, eps, hw, c, c / groups, act, pl.sv, pl.slices, pl.groups, pl.rows, pl.chunk, pl.red_rows, pl.bins,
-                      err_flag, rev ? 1 : 0};
+                      err_flag, wait_cycles, rev ? 1 : 0};
   const long units = batch * pl.slices;
   constexpr int V = Elem<T>::kVec;
   return pl.v > 1 ? norm_launch_v<T, V>(pl, a, units, st) : norm_launch_v<T, 1>(pl, a, units, st);

@@ -3,11 +3,13 @@ of their types, statistics of extreme maps, what a row may depend on."""
 import ctypes as C
 import subprocess
 
+import numpy as np
 import pytest
 import torch
 
 from paper_2209_13443_b200 import binding as eb
-from tests.test_gpu_operators import TD, U, gen, linear_operands, linear_run, norm_check, norm_exact, normal, out_like, untouched
+from paper_2209_13443_b200 import workloads as wl
+from tests.test_gpu_operators import TD, U, drafts_of, gen, linear_operands, linear_run, norm_check, norm_exact, normal, out_like, untouched
 
 pytestmark = pytest.mark.gpu
 
@@ -214,3 +216,95 @@ def test_group_norm_of_one_extreme_pixel(shape, dtype):
     tol = ref.abs() * (lost + (0 if dtype == "f32" else 2.0 ** -8 * (1 + lost))) + U * 1e-3
     err = (y.double() - ref).abs()
     assert bool((err <= tol).all()), f"off by {float((err / tol).max()):.3g} tolerances"
+
+
+# ----------------------------------------------------------------------------- waits that run out
+
+def _late(call, outs):
+    """`call` with a limit of one clock on the waits between the blocks of a cluster, until a wait has run out (a block that happens to be its cluster's last has nothing to wait
+    for), from outputs filled with 77; then with the limit back.  What a block that gave up left is 77, everything else right."""
+    for o in outs:
+        o.fill_(77)
+    call()
+    eb.operators_check()
+    want = [o.clone() for o in outs]
+    eb.operators_set_wait_limit(1)
+    try:
+        seen = False
+        for _ in range(20):
+            for o in outs:
+                o.fill_(77)
+            call()
+            torch.cuda.synchronize()
+            try:
+                eb.operators_check()
+            except eb.EEError as e:
+                assert e.status == 7                                   # EE_ERR_TIMEOUT
+                seen = True
+            for o, w in zip(outs, want):
+                assert bool(((o == w) | (o == 77)).all())
+            if seen:
+                break
+        assert seen
+    finally:
+        eb.operators_set_wait_limit(4_000_000_000)
+    for o in outs:
+        o.fill_(77)
+    call()
+    eb.operators_check()
+    assert all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 3136, 64, 8), (1, 30000, 520, 40), (3, 957, 96, 32)], ids=str)
+def test_group_norm_whose_exchange_runs_out_of_time(shape, dtype):
+    b, hw, c, groups = shape
+    x = normal(gen(1), b, hw, c).to(TD[dtype])
+    y = torch.empty_like(x)
+    _late(lambda: eb.group_norm(dtype, x, b, hw, c, groups, None, None, 1e-5, 3, y), [y])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [32769, 128001, 614399])
+def test_softmax_whose_exchange_runs_out_of_time(n, dtype):
+    x, y = normal(gen(n), 3, n).to(TD[dtype]), torch.empty((3, n), device="cuda")
+    for heat in (None, torch.zeros(3, device="cuda")):
+        _late(lambda: eb.softmax(dtype, x, 3, n, y, temperature=heat), [y])
+
+
+@pytest.mark.parametrize("dtype,shape", [("bf16", (1, 2048, 1000, 8, 16)), ("bf16", (64, 4096, 512, 16, 32)), ("bf16", (40, 1001, 300, 3, 4)), ("bf16", (256, 4096, 256, 64, 9)), ("f32", (37, 2048, 1000, 5, 7))], ids=str)
+def test_adapted_linear_whose_exchange_runs_out_of_time(dtype, shape):
+    rows, c, n, rank, m = shape
+    x, w, bias, a, b, scale, which = linear_operands(2, *shape, dtype)
+    y, ws = torch.empty((rows, n), dtype=TD[dtype], device="cuda"), torch.empty(eb.adapted_linear_workspace_bytes(rows, rank) + 256, dtype=torch.uint8, device="cuda")
+    _late(lambda: eb.adapted_linear(dtype, x, rows, c, w, n, a, b, rank, m, which, y, ws, bias=bias, scale=scale), [y])
+
+
+@pytest.mark.parametrize("n", [20001, 128001])
+def test_verify_drafts_whose_exchange_runs_out_of_time(n):
+    p, q, d, u, r = drafts_of(n, 9, 3, n)
+    p[3], q[4, 0] = 0.0, 2.0                               # a second round: p - q leaves nothing
+    tokens, accepted = torch.empty((9, 4), dtype=torch.int32, device="cuda"), torch.empty(9, dtype=torch.int32, device="cuda")
+    _late(lambda: eb.verify_drafts(p, q, d, u, r, 9, 3, n, tokens, accepted), [tokens, accepted])
+
+
+def test_a_models_group_norms_go_by_its_limit():
+    """As its other layers do: with a limit of one clock the wait for a cluster's statistics runs out and is reported once."""
+    spec = wl.Model("norm", "bf16", 256, 256, 64, [wl.Stage([wl.Layer(wl.OP_GROUPNORM, 64, 64, act=wl.ACT_RELU, norm_groups=8, norm_eps=1e-5)], 10, np.zeros((10, 64), np.float32),
+                                                           np.zeros(10, np.float32), 0.0, True)], 2)
+    m = eb.EEModel(spec)
+    ws = m.workspace()
+    x = normal(gen(0), 2, 256, 256, 64).to(torch.bfloat16)
+    y, want = torch.full_like(x, 77), torch.empty_like(x)
+    m.layer_run(0, 0, x, None, 2, want, ws)
+    m.check()
+    m.set_wait_limit(1)
+    m.layer_run(0, 0, x, None, 2, y, ws)
+    with pytest.raises(eb.EEError) as e:
+        m.check()
+    assert e.value.status == 7 and bool(((y == want) | (y == 77)).all())
+    m.set_wait_limit(4_000_000_000)
+    m.layer_run(0, 0, x, None, 2, y, ws)
+    m.check()
+    assert torch.equal(y, want)
+    m.close()

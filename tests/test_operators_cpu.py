@@ -110,6 +110,11 @@ def test_verify_drafts_of_nothing_and_of_too_much():
     assert call("ee_verify_drafts", VERIFY, k=2 ** 31 - 1) == CAPACITY
 
 
+@pytest.mark.parametrize("cycles", [0, -1, -2 ** 62])
+def test_a_limit_of_the_waits_is_positive(cycles):
+    assert eb.load_library().ee_operators_set_wait_limit(cycles) == INVALID
+
+
 def test_prototypes_match_the_header():
     """As many arguments in the binding as in the header, pointers where it has pointers."""
     import os
