@@ -218,6 +218,25 @@ def test_group_norm_of_one_extreme_pixel(shape, dtype):
     assert bool((err <= tol).all()), f"off by {float((err / tol).max()):.3g} tolerances"
 
 
+@pytest.mark.parametrize("offset", [100.0, -3000.0, 1e5])
+@pytest.mark.parametrize("residual", [False, True])
+def test_group_norm_keeps_the_digits_below_a_large_mean(offset, residual):
+    """fp32, a mean of thousands of deviations.  Differences from a value (or mean) nearby are exact, so the mean is rounded once in each join: threads, warps, CTAs, cluster: 4 u of
+    it, and what its parts' roundings do to the squares between the parts is at most 2 u |mean| / deviation of them where a part's mean lies within half a deviation.  Sums
+    of differences: chains of 12 accesses, four lanes, eight warps and CTAs, below 512 u of the deviation."""
+    b, hw, c, groups = 2, 3000, 32, 2
+    g = gen(9)
+    x = normal(g, b, hw, c) + offset
+    res = normal(g, b, hw, c) if residual else None
+    y, _ = out_like(x.shape, torch.float32)
+    eb.group_norm("f32", x, b, hw, c, groups, None, None, 1e-5, 0, y, residual=res)
+    ref, t, z, mean, var = norm_exact(x, None, None, groups, 1e-5, 0, res)
+    far = (mean.abs() / torch.sqrt(var)).expand(b, hw, groups, c // groups).reshape(b, hw, c) + z.abs()
+    tol = U * far * (4.5 + z.abs()) + 512 * U * (1 + z.abs()) + 4 * U * ref.abs()
+    err = (y.double() - ref).abs()
+    assert bool((err <= tol).all()), f"off by {float((err / tol).max()):.3g} tolerances"
+
+
 # ----------------------------------------------------------------------------- waits that run out
 
 def _late(call, outs):
