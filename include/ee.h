@@ -391,7 +391,8 @@ ee_status_t ee_model_check(ee_model_t* model, void* cuda_stream);
  *   y = act(gamma[c] * (x - mean) / sqrt(var + eps) + beta[c] (+ residual)),   var biased (divided by the count),
  * statistics and sums in fp32, one rounding to the model dtype.  x, residual (or NULL), y: [batch][hw][c]; gamma (NULL = 1)
  * and beta (NULL = 0): [c] fp32.  Unlike a folded batch norm it takes its statistics from the sample itself, so it suits a batch
- * that shrinks and is refilled: the bits of a sample do not depend on the batch.  y may be x or residual (in place); other
+ * that shrinks and is refilled: the bits of a sample do not depend on the batch (with operands off 16-byte boundaries the sums are grouped
+ * otherwise).  y may be x or residual (in place); other
  * overlaps are refused.  act: ee_act_t.  Errors: INVALID_ARG, CAPACITY (a grid beyond 2^31 - 1 blocks, a block beyond as many loads), CUDA. */
 ee_status_t ee_group_norm(int dtype, const void* x, const void* residual, int batch, int hw, int c, int groups, const float* gamma,
                           const float* beta, float eps, int act, void* y, void* cuda_stream);
@@ -418,7 +419,7 @@ size_t ee_adapted_linear_workspace_bytes(int rows, int rank);
 /* Probabilities of rows of logits: probs[v] = exp((logits[v] - max) / t) / sum, t = temperature[row] (NULL = 1).  logits: [rows][n]
  * of dtype, probs: [rows][n] fp32.  A logit of -inf is masked: its probability is 0; a row with nothing else is all 0.
  * A temperature that is not above 0 puts 1 on the largest logit (the lowest index on ties).  A row that holds NaN or +inf is NaN
- * throughout.  probs may be logits (fp32); other overlaps are refused.  n up to 614400.
+ * throughout.  Probabilities below 2^-126 come out as 0.  probs may be logits (fp32); other overlaps are refused.  n up to 614400.
  * Errors: INVALID_ARG, CAPACITY (n or the grid too large), CUDA. */
 ee_status_t ee_softmax(int dtype, const void* logits, int rows, int n, const float* temperature, float* probs, void* cuda_stream);
 

@@ -1,20 +1,22 @@
 // Class probabilities, and the verification of classes (tokens) that an early exit drafted against the probabilities of a later one.
 //
 // softmax: p[v] = exp((l[v] - max) / t) / sum, a row at a time.  Bound by memory: a logit read once, a probability written once, and not far behind by
-// instructions: about fifteen an element, so the joins are kept off the threads' path.  A short row is one warp's, in registers.  A long one is cut over a cluster of
-// CTAs, up to seven of which share an SM so that one's loads run beside another's barriers.  A CTA fetches its part into shared memory, takes its maximum and the sum of the
+// instructions, so the joins are kept off the threads' path.  A short row is one warp's, in registers.  A long one is cut over a cluster of
+// CTAs, up to six of which share an SM so that one's loads run beside another's barriers.  A CTA fetches its part into shared memory, takes its maximum and the sum of the
 // exponentials against that, sends both to the other CTAs, and writes exp((l - max) / t) / sum once it has theirs.  Rows of any length and any alignment: whole 16-byte
 // words are fetched, the odd elements in front of and behind them one by one (one element a lane takes 4 us for 32 of them: 2-byte loads); exponentials are taken and
 // probabilities leave one element a lane, 128 bytes a warp, so that the order of the sum does not follow the row's alignment.  How a row is cut follows from its length
-// alone, so its bits do not depend on the other rows.  320 x 128001 bf16: 50.5 us, 4.9 TB/s; 64 x 1000 fp32: 1.7 us.
+// alone, so its bits do not depend on the other rows.  320 x 128001 bf16: 50.8 us, 4.8 TB/s; fp32 73.7, 4.4; 64 x 1000 fp32: 1.8 us.  An SM issues 60 % of the
+// time; of the 17 cycles from one issue of a warp to its next 3.9 are barriers, 4.2 shared memory, 2.1 loads: fetch, maximum, sum and stores of a part
+// follow one another, and six CTAs cover them in part.
 //
 // verify: draft i of a sequence is accepted while u_i q_i(x_i) < p_i(x_i); at the first rejection a token is drawn from max(p_i - q_i, 0), where
 // all hold from the row behind the last draft, as the first v whose running sum exceeds r times the total.  What is compared is exact: u q in fp64 is the
 // exact product of two floats, and the sums are fp64, because a draw must not depend on how a sum over a hundred thousand floats was grouped
 // (2^-53 against steps of about 1e-5).  It reads one row of p and one of q per sequence: which row it is (two dependent loads), then the sums of blocks of
 // 512 values, all CTAs of 64 sequences side by side; the CTAs send each other their totals, and the one in whose part the sum crosses scans its block sums
-// and then that one block.  64 sequences of 5 drafts, 128001 tokens: 21 us, 3.1 TB/s of the two rows that are read, of which the dependent loads, the exchange and the scan are
-// about half; one sequence of 1000: 4.7 us.
+// and then that one block.  64 sequences of 5 drafts, 128001 tokens: 21.8 us, 3.0 TB/s of the two rows that are read, of which the dependent loads, the exchange and the scan are
+// about half (an SM issues 42 % of the time; loads and barriers are 4.4 and 3.7 of a warp's 14.6 cycles an issue); certain drafts 20.2; one sequence of 1000: 5.7 us.
 #pragma once
 #include <float.h>
 
@@ -27,7 +29,7 @@ namespace ee {
 
 constexpr int kSmWarpMost = 1024;        // longest row of the one-warp form: 32 values a lane
 constexpr int kSmThreads = 256;
-constexpr int kSmPart = 16384;           // elements of a CTA's part that a cluster is cut for: seven CTAs an SM (fp32: three)
+constexpr int kSmPart = 16384;           // elements of a CTA's part that a cluster is cut for: six CTAs an SM (fp32: three)
 constexpr int kSmMaxCluster = 16;        // above eight, the portable size, the kernel asks
 constexpr int kSmMaxPart = 38400;        // elements that a CTA has room for
 

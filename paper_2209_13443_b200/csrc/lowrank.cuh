@@ -19,7 +19,7 @@
 // one row of 2048 x 1000.
 // Two forms.  At most one tile an SM: a deep ring, for the bytes in flight.  More: persistent CTAs with two accumulators, so that one tile's list of adapters, columns
 // and stores lie under the next one's products.  128 x 256 tiles where that takes less time: 128 x 128 ones ask 128 bytes a clock of L2 for every SM, and get 97.
-// What bounds it: few rows the latency of the two launches, 64 x 4096 x 4096 the bytes of W (9.3 of 19.8 us at the rate of memory), thousands of rows the tensor cores; rows in mixed
+// What bounds it: few rows the latency of the two launches, 64 x 4096 x 4096 the bytes of W (9.3 of 19.8 us, at 3.6 TB/s), thousands of rows the tensor cores; rows in mixed
 // order the columns of all their adapters, most of them zero: a block of 64 takes the filling warps about 2600 clocks (addresses 500, h 900, the look for infinities and the hand-over
 // 700, the slot 400; plain stores in place of copies of zeros change nothing), its products 470.
 //

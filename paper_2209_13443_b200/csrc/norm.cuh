@@ -9,8 +9,8 @@
 // values, a warp's, a CTA's, the cluster's) is (mean, squares about it), and parts are joined, in a fixed order, as
 //   mean = sum n_i mean_i / n,   S = sum (S_i + n_i (mean_i - mean)^2);
 // the CTAs send each other theirs as asynchronous stores, which the receiver's barrier counts: nothing but the data is waited for.
-// All sums are fp32.  Slice, cluster and order of the sums follow from the map's shape alone, never from the batch: a sample's bits
-// do not depend on whom it rides with.  64 x 56 x 56 x 256 bf16 with a residual 62.4 us (4.9 TB/s), 32 x 112 x 112 x 96 53, 1 x 7 x 7 x 2048 3.2.
+// All sums are fp32.  Slice, cluster and order of the sums follow from the map's shape and from whether rows lie on 16-byte boundaries, never from the batch: a sample's
+// bits do not depend on whom it rides with.  64 x 56 x 56 x 256 bf16 with a residual 62.7 us (4.9 TB/s), 32 x 112 x 112 x 96 53.0, 1 x 7 x 7 x 2048 3.3.
 //
 // A thread keeps one column of 16 bytes of channels and walks down the pixels, so gamma and beta live in registers and a vector may
 // hold several groups or parts of them.  Rows that are not whole 16-byte vectors, or pointers off a 16-byte boundary, take one element at a time.
