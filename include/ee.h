@@ -438,6 +438,46 @@ ee_status_t ee_softmax(int dtype, const void* logits, int rows, int n, const flo
 ee_status_t ee_verify_drafts(const float* p, const float* q, const int32_t* drafts, const float* u, const float* r, const int32_t* n_draft,
                              int batch, int k, int n, int32_t* tokens, int32_t* n_accepted, void* cuda_stream);
 
+/* Rows in 8 bits, each with a scale of its own: what a parked batch (Section III-B, "Preemption": the activations of halted samples stay in memory) is kept in at half or a
+ * quarter of its bytes, and what ee_int8_linear multiplies.  x: [rows][c] of dtype; q: [rows][ee_int8_row_bytes(c)], 16-byte aligned, what lies behind a row's c
+ * values is set to 0; scale: [rows].
+ *   scale = max |x| * (1 / 127), both rounded to fp32;  q = the integer nearest to x / scale, the even one of two, from -127 to 127;  0 where scale is 0.
+ * A row that holds NaN or an infinity has the scale NaN and zeros.  c up to 131071.  Errors: INVALID_ARG (overlaps too), CAPACITY, CUDA. */
+ee_status_t ee_quantize_rows(int dtype, const void* x, int rows, int c, int8_t* q, float* scale, void* cuda_stream);
+/* Bytes from one quantised row to the next: c rounded up to whole 16 bytes; 0 for a c out of range. */
+size_t ee_int8_row_bytes(int c);
+/* The same rows read back: y[t] = q[i] * scale[i], i = index[t] (NULL: t), rounded to dtype (fp32 in between).  q: [pool][ee_int8_row_bytes(c)], scale: [pool], index:
+ * [rows], any order, the same row as often as wanted; y: [rows][c].  A row of y whose index lies outside [0, pool) is left as it is; without an index pool must be at
+ * least rows.  Errors: INVALID_ARG, CAPACITY, CUDA. */
+ee_status_t ee_dequantize_rows(int dtype, const int8_t* q, const float* scale, int pool, int c, const int32_t* index, int rows, void* y, void* cuda_stream);
+
+/* A projection in 8-bit integers with a scale for each row and each channel:
+ *   y[t][f] = x_scale[t] * weight_scale[f] * sum_k x[t][k] * weight[f][k] + bias[f].
+ * weight: [n][ee_int8_row_bytes(c)] (ee_quantize_rows of the matrix, once), 16-byte aligned; weight_scale: [n] (NULL = 1); bias: [n] (NULL = 0); y: [rows][n] of dtype.
+ * x_scale given: x is quantised already, [rows][ee_int8_row_bytes(c)], 16-byte aligned, and the workspace is not used.  x_scale NULL: x is [rows][c] of dtype, and the
+ * call quantises it as ee_quantize_rows does into `workspace` (256-byte aligned, at least ee_int8_linear_workspace_bytes(rows, c) bytes, undefined afterwards; calls that may overlap need
+ * one each).  Any integers from -128 to 127 may be given; what lies behind a row's c values is not read.  The sum is exact (32-bit integers, c up to 131071), so a
+ * row's bits depend on nothing else in the call.  For bf16 it is rounded to fp32, multiplied by weight_scale, then by x_scale, the last with bias in one rounding, and rounded to bf16: the
+ * product with weight_scale alone must fit fp32.  For fp32 all of that is fp64, rounded once.  A row or channel whose scale is NaN is NaN throughout.  y and the workspace must not overlap anything else.
+ * Errors: INVALID_ARG, CAPACITY (workspace too small, c above 131071, more than 2^22 rows, n above 2^20), CUDA. */
+ee_status_t ee_int8_linear(int dtype, const void* x, const float* x_scale, int rows, int c, const int8_t* weight, const float* weight_scale, int n, const float* bias,
+                           void* y, void* workspace, size_t workspace_bytes, void* cuda_stream);
+size_t ee_int8_linear_workspace_bytes(int rows, int c);
+
+/* A class (token) of each row of logits, drawn by a given random number, under settings of each row's own.  logits: [rows][n] of dtype; temperature, top_p, min_p: [rows] fp32,
+ * top_k: [rows] (any may be NULL: not asked for); u: [rows], random numbers in [0, 1); tokens: [rows]; probs: [rows][n] fp32; one of tokens and probs may be NULL, u where tokens is.
+ * Classes are ordered by their logits, of equal ones (-0 is 0) the lower index first; a class weighs w = exp((logit - max) / t).  Kept are
+ *   the first top_k in that order (top_k <= 0 or >= n: all);
+ *   of these, those in front of which less than top_p times the weight of them all lies (top_p >= 1 or NaN: all);
+ *   of these, those with w >= min_p (min_p <= 0 or NaN: all);
+ * and the first class always.  A temperature that is not above 0 keeps the first alone.  The token is the first kept class, by index, at which the running sum of weights exceeds
+ * u times their total (where u is not below 1, the last that weighs anything).  probs: w / total of what is kept, else 0, as ee_verify_drafts takes them for p and q.
+ * Weights and sums are fp64.  A logit of -inf is masked: it weighs nothing.  A row with nothing else has the token -1 and probabilities 0; one that holds NaN
+ * or +inf has the token -1 and probabilities NaN.  probs may be logits (fp32); other overlaps are refused.  n up to 614400.  Errors: INVALID_ARG, CAPACITY (n or the grid
+ * too large), CUDA. */
+ee_status_t ee_sample(int dtype, const void* logits, int rows, int n, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
+                      int32_t* tokens, float* probs, void* cuda_stream);
+
 /* Limit, in SM clock cycles, of a block's wait for the others of its cluster in the operators above, on the current device (default about 2 s):
  * what ee_model_set_wait_limit is for a model.  For the calls that follow; a captured one keeps what it was captured with.  Where a wait runs out, a
  * block leaves its part of the outputs as it is.  Errors: INVALID_ARG, CUDA. */

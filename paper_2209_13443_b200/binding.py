@@ -23,7 +23,8 @@ EXPORTS = ["ee_model_create", "ee_model_destroy", "ee_model_query", "ee_stage_ru
            "ee_exit_head_scratch_bytes", "ee_exit_head_static", "ee_gather_survivors", "ee_model_set_graphs", "ee_model_set_branches", "ee_model_set_fused_head", "ee_model_set_proj_fusion", "ee_model_set_gap_fusion", "ee_model_gap_partials", "ee_model_head_launches", "ee_model_head_pools", "ee_model_set_stage_kernel", "ee_model_set_chain", "ee_model_set_timing", "ee_model_get_timing",
            "ee_model_plan", "ee_model_check", "ee_model_set_layer_variant", "ee_model_set_layer_splits", "ee_model_get_layer_config",
            "ee_model_set_wait_limit", "ee_model_selftest_wait", "ee_wait_count", "ee_run_until_exit", "ee_group_norm", "ee_adapted_linear",
-           "ee_adapted_linear_workspace_bytes", "ee_softmax", "ee_verify_drafts", "ee_operators_set_wait_limit", "ee_operators_check", "ee_status_string", "ee_last_cuda_error"]
+           "ee_adapted_linear_workspace_bytes", "ee_softmax", "ee_verify_drafts", "ee_quantize_rows", "ee_int8_row_bytes", "ee_dequantize_rows",
+           "ee_int8_linear", "ee_int8_linear_workspace_bytes", "ee_sample", "ee_operators_set_wait_limit", "ee_operators_check", "ee_status_string", "ee_last_cuda_error"]
 
 
 class EEError(RuntimeError):
@@ -125,6 +126,14 @@ def load_library() -> C.CDLL:
     L.ee_adapted_linear_workspace_bytes.restype = C.c_size_t
     L.ee_softmax.argtypes = [i, vp, i, i, vp, vp, vp]
     L.ee_verify_drafts.argtypes = [vp, vp, vp, vp, vp, vp, i, i, i, vp, vp, vp]
+    L.ee_quantize_rows.argtypes = [i, vp, i, i, vp, vp, vp]
+    L.ee_int8_row_bytes.argtypes = [i]
+    L.ee_int8_row_bytes.restype = C.c_size_t
+    L.ee_dequantize_rows.argtypes = [i, vp, vp, i, i, vp, i, vp, vp]
+    L.ee_int8_linear.argtypes = [i, vp, vp, i, i, vp, vp, i, vp, vp, vp, C.c_size_t, vp]
+    L.ee_int8_linear_workspace_bytes.argtypes = [i, i]
+    L.ee_int8_linear_workspace_bytes.restype = C.c_size_t
+    L.ee_sample.argtypes = [i, vp, i, i, vp, vp, vp, vp, vp, vp, vp, vp]
     L.ee_operators_set_wait_limit.argtypes = [C.c_longlong]
     L.ee_operators_check.argtypes = [vp]
     L.ee_status_string.argtypes = [i]
@@ -452,6 +461,19 @@ def _mem(where: str, t, dtype, count: int, device: int) -> Optional[int]:
     return t.data_ptr()
 
 
+def _workspace(where: str, t: Optional[torch.Tensor], device: int):
+    """(address of the first 256-byte boundary, bytes behind it) of a workspace tensor."""
+    if t is None:
+        return None, 0
+    base = _mem(where, t, t.dtype, 0, device)
+    aligned = (base + 255) // 256 * 256
+    return aligned, max(0, t.numel() * t.element_size() - (aligned - base))
+
+
+def _pitch(c: int) -> int:
+    return (c + 15) // 16 * 16
+
+
 def _dtype(where: str, dtype: str):
     if dtype not in _DTYPES:
         raise EEError(1, where, f"dtype {dtype!r} is neither 'f32' nor 'bf16'")
@@ -477,11 +499,7 @@ def adapted_linear(dtype: str, x, rows: int, c: int, weight, n: int, a, b, rank:
     adapted_linear_workspace_bytes(rows, rank) bytes behind its first 256-byte boundary, one for every call that may be in flight."""
     f, d, f32 = "ee_adapted_linear", torch.cuda.current_device(), torch.float32
     code, td = _dtype(f, dtype)
-    aligned, room = None, 0
-    if workspace is not None:
-        base = _mem(f, workspace, workspace.dtype, 0, d)
-        aligned = (base + 255) // 256 * 256
-        room = max(0, workspace.numel() * workspace.element_size() - (aligned - base))
+    aligned, room = _workspace(f, workspace, d)
     _check(load_library().ee_adapted_linear(code, _mem(f, x, td, rows * c, d), rows, c, _mem(f, weight, td, n * c, d), n, _mem(f, bias, f32, n, d),
                                             _mem(f, a, td, n_adapters * rank * c, d), _mem(f, b, td, n_adapters * n * rank, d), rank, n_adapters,
                                             _mem(f, scale, f32, n_adapters, d), _mem(f, adapter, torch.int32, rows, d), _mem(f, out, td, rows * n, d),
@@ -502,6 +520,56 @@ def verify_drafts(p, q, drafts, u, r, batch: int, k: int, n: int, tokens, n_acce
     _check(load_library().ee_verify_drafts(_mem(f, p, f32, batch * (k + 1) * n, d), _mem(f, q, f32, batch * k * n, d), _mem(f, drafts, i32, batch * k, d),
                                            _mem(f, u, f32, batch * k, d), _mem(f, r, f32, batch, d), _mem(f, n_draft, i32, batch, d), batch, k, n,
                                            _mem(f, tokens, i32, batch * (k + 1), d), _mem(f, n_accepted, i32, batch, d), _stream(stream, d)), f)
+
+
+def int8_row_bytes(c: int) -> int:
+    return int(load_library().ee_int8_row_bytes(c))
+
+
+def quantize_rows(dtype: str, x, rows: int, c: int, q, scale, stream=None):
+    """ee_quantize_rows: rows of x as 8-bit integers (int8 [rows][int8_row_bytes(c)]) and a scale of each row's own."""
+    f, d = "ee_quantize_rows", torch.cuda.current_device()
+    code, td = _dtype(f, dtype)
+    _check(load_library().ee_quantize_rows(code, _mem(f, x, td, rows * c, d), rows, c, _mem(f, q, torch.int8, rows * _pitch(c), d), _mem(f, scale, torch.float32, rows, d),
+                                           _stream(stream, d)), f)
+
+
+def dequantize_rows(dtype: str, q, scale, pool: int, c: int, out, rows: int, index=None, stream=None):
+    """ee_dequantize_rows: out[t] = q[i] * scale[i], i = index[t] (or t), of a pool of quantised rows."""
+    f, d = "ee_dequantize_rows", torch.cuda.current_device()
+    code, td = _dtype(f, dtype)
+    _check(load_library().ee_dequantize_rows(code, _mem(f, q, torch.int8, pool * _pitch(c), d), _mem(f, scale, torch.float32, pool, d), pool, c,
+                                             _mem(f, index, torch.int32, rows, d), rows, _mem(f, out, td, rows * c, d), _stream(stream, d)), f)
+
+
+def int8_linear_workspace_bytes(rows: int, c: int) -> int:
+    return int(load_library().ee_int8_linear_workspace_bytes(rows, c))
+
+
+def int8_linear(dtype: str, x, rows: int, c: int, weight, weight_scale, n: int, out, workspace: Optional[torch.Tensor] = None, x_scale=None, bias=None, stream=None):
+    """ee_int8_linear: out[t][f] = x_scale[t] * weight_scale[f] * (x[t] . weight[f]) + bias[f] in 8-bit integers.  With x_scale, x is int8 [rows][int8_row_bytes(c)]; without,
+    it is of ``dtype`` and quantised by the call into ``workspace``, a device tensor of at least int8_linear_workspace_bytes(rows, c) bytes behind its first 256-byte
+    boundary, one for every call that may be in flight."""
+    f, d, f32 = "ee_int8_linear", torch.cuda.current_device(), torch.float32
+    code, td = _dtype(f, dtype)
+    pitch = _pitch(c)
+    aligned, room = _workspace(f, workspace, d)
+    if x_scale is None:
+        xp, sp = _mem(f, x, td, rows * c, d), None
+    else:
+        xp, sp = _mem(f, x, torch.int8, rows * pitch, d), _mem(f, x_scale, f32, rows, d)
+    _check(load_library().ee_int8_linear(code, xp, sp, rows, c, _mem(f, weight, torch.int8, n * pitch, d), _mem(f, weight_scale, f32, n, d), n, _mem(f, bias, f32, n, d),
+                                         _mem(f, out, td, rows * n, d), aligned, room, _stream(stream, d)), f)
+
+
+def sample(dtype: str, logits, rows: int, n: int, u, tokens, temperature=None, top_k=None, top_p=None, min_p=None, probs=None, stream=None):
+    """ee_sample: a class of each row drawn by u among the top_k, the top_p share of the weight and the classes that weigh at least min_p of the best; and the
+    probabilities that it was drawn from."""
+    f, d, f32, i32 = "ee_sample", torch.cuda.current_device(), torch.float32, torch.int32
+    code, td = _dtype(f, dtype)
+    _check(load_library().ee_sample(code, _mem(f, logits, td, rows * n, d), rows, n, _mem(f, temperature, f32, rows, d), _mem(f, top_k, i32, rows, d),
+                                    _mem(f, top_p, f32, rows, d), _mem(f, min_p, f32, rows, d), _mem(f, u, f32, rows, d), _mem(f, tokens, i32, rows, d),
+                                    _mem(f, probs, f32, rows * n, d), _stream(stream, d)), f)
 
 
 def operators_set_wait_limit(cycles: int):

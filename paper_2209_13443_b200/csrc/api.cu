@@ -24,6 +24,8 @@
 #include "norm.cuh"
 #include "lowrank.cuh"
 #include "draft.cuh"
+#include "quant.cuh"
+#include "sample.cuh"
 
 using namespace ee;
 
@@ -1825,6 +1827,7 @@ namespace {
 struct OperatorContext {   // one per device, filled at its first call
   std::atomic<int> ready{0};
   LrContext lr;
+  I8Context i8;
   int* flag = nullptr;
   std::atomic<long long> wait_cycles{kTcWaitCycles};   // limit of a block's wait for the others of its cluster
 };
@@ -1848,8 +1851,12 @@ ee_status_t operator_context(OperatorContext** out) {
       EE_CUDA(lr_context_init(c.lr));
       EE_CUDA(norm_context_init());
       EE_CUDA(softmax_context_init());
+      EE_CUDA(i8_context_init<bf16>(c.i8));
+      EE_CUDA(i8_context_init<float>(c.i8));
+      EE_CUDA(sample_context_init());
       if (f32_context_init() != EE_OK) return EE_ERR_CUDA;
-      c.lr.encode_tiled = (PFN_encodeTiled)f;
+      c.lr.encode_tiled = c.i8.encode_tiled = (PFN_encodeTiled)f;
+      c.i8.sm_count = c.lr.sm_count;
       c.flag = (int*)flag;
       c.ready.store(1, std::memory_order_release);
     }
@@ -1960,6 +1967,92 @@ ee_status_t ee_verify_drafts(const float* p, const float* q, const int32_t* draf
   const ee_status_t s = operator_context(&ctx);
   if (s != EE_OK) return s;
   EE_CUDA(verify_launch({p, q, drafts, u, r, n_draft, tokens, n_accepted, k, n, 0, 0, ctx->flag, ctx->wait_cycles}, batch, (cudaStream_t)cuda_stream));
+  return EE_OK;
+}
+
+size_t ee_int8_row_bytes(int c) { return c > 0 && c <= kQMaxRow ? (size_t)q_pitch(c) : 0; }
+
+ee_status_t ee_quantize_rows(int dtype, const void* x, int rows, int c, int8_t* q, float* scale, void* cuda_stream) {
+  if ((dtype != EE_F32 && dtype != EE_BF16) || rows < 0 || c < 1) return EE_ERR_INVALID_ARG;
+  if (c > kQMaxRow) return EE_ERR_CAPACITY;
+  if (rows == 0) return EE_OK;
+  const size_t es = esize(dtype), xb = (size_t)rows * c * es, qb = (size_t)rows * q_pitch(c), sb = (size_t)rows * 4;
+  if (!x || !q || !scale || !aligned_to(x, es) || !aligned_to(q, 16) || !aligned_to(scale, 4)) return EE_ERR_INVALID_ARG;
+  if (!apart(x, xb, q, qb) || !apart(x, xb, scale, sb) || !apart(q, qb, scale, sb)) return EE_ERR_INVALID_ARG;
+  OperatorContext* ctx;
+  const ee_status_t s = operator_context(&ctx);
+  if (s != EE_OK) return s;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  EE_CUDA(dtype == EE_BF16 ? quantize_launch<bf16>((const bf16*)x, q, scale, rows, c, st) : quantize_launch<float>((const float*)x, q, scale, rows, c, st));
+  return EE_OK;
+}
+
+ee_status_t ee_dequantize_rows(int dtype, const int8_t* q, const float* scale, int pool, int c, const int32_t* index, int rows, void* y, void* cuda_stream) {
+  if ((dtype != EE_F32 && dtype != EE_BF16) || rows < 0 || pool < 0 || c < 1 || (!index && pool < rows)) return EE_ERR_INVALID_ARG;
+  if (c > kQMaxRow) return EE_ERR_CAPACITY;
+  if (rows == 0 || pool == 0) return EE_OK;
+  const size_t es = esize(dtype), yb = (size_t)rows * c * es;
+  if (!q || !scale || !y || !aligned_to(q, 16) || !aligned_to(scale, 4) || !aligned_to(index, 4) || !aligned_to(y, es)) return EE_ERR_INVALID_ARG;
+  if (!apart(q, (size_t)pool * q_pitch(c), y, yb) || !apart(scale, (size_t)pool * 4, y, yb) || (index && !apart(index, (size_t)rows * 4, y, yb))) return EE_ERR_INVALID_ARG;
+  OperatorContext* ctx;
+  const ee_status_t s = operator_context(&ctx);
+  if (s != EE_OK) return s;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  EE_CUDA(dtype == EE_BF16 ? dequantize_launch<bf16>(q, scale, index, (bf16*)y, rows, pool, c, st) : dequantize_launch<float>(q, scale, index, (float*)y, rows, pool, c, st));
+  return EE_OK;
+}
+
+size_t ee_int8_linear_workspace_bytes(int rows, int c) {
+  return rows > 0 && c > 0 && c <= kQMaxRow ? align_up((size_t)rows * q_pitch(c), 256) + (size_t)rows * 4 : 0;
+}
+
+ee_status_t ee_int8_linear(int dtype, const void* x, const float* x_scale, int rows, int c, const int8_t* weight, const float* weight_scale, int n, const float* bias,
+                           void* y, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if ((dtype != EE_F32 && dtype != EE_BF16) || rows < 0 || c < 1 || n < 1) return EE_ERR_INVALID_ARG;
+  if (c > kQMaxRow || rows > 1 << 22 || n > 1 << 20) return EE_ERR_CAPACITY;
+  if (rows == 0) return EE_OK;
+  const size_t es = esize(dtype), pitch = (size_t)q_pitch(c), xb = x_scale ? (size_t)rows * pitch : (size_t)rows * c * es, wb = (size_t)n * pitch, yb = (size_t)rows * n * es;
+  const size_t need = x_scale ? 0 : ee_int8_linear_workspace_bytes(rows, c), row = (size_t)rows * 4, col = (size_t)n * 4;
+  if (!x || !weight || !y || !aligned_to(x, x_scale ? 16 : es) || !aligned_to(x_scale, 4) || !aligned_to(weight, 16) || !aligned_to(weight_scale, 4) || !aligned_to(bias, 4) ||
+      !aligned_to(y, es))
+    return EE_ERR_INVALID_ARG;
+  if (!x_scale && (!workspace || !aligned_to(workspace, 256))) return EE_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return EE_ERR_CAPACITY;
+  auto clear = [&](const void* p, size_t bytes) { return !p || (apart(p, bytes, y, yb) && (!need || apart(p, bytes, workspace, need))); };
+  if ((need && !apart(workspace, need, y, yb)) || !clear(x, xb) || !clear(x_scale, row) || !clear(weight, wb) || !clear(weight_scale, col) || !clear(bias, col)) return EE_ERR_INVALID_ARG;
+  OperatorContext* ctx;
+  const ee_status_t s = operator_context(&ctx);
+  if (s != EE_OK) return s;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  const int8_t* x8 = x_scale ? (const int8_t*)x : (const int8_t*)workspace;
+  I8Args a = {};
+  a.xs = x_scale ? x_scale : (const float*)((const char*)workspace + align_up((size_t)rows * pitch, 256));
+  a.ws = weight_scale, a.bias = bias, a.y = y, a.rows = rows, a.c = c, a.n = n, a.err_flag = ctx->flag, a.wait_cycles = ctx->wait_cycles;
+  EE_CUDA(dtype == EE_BF16 ? i8_run<bf16>(ctx->i8, x_scale ? nullptr : (const bf16*)x, x8, weight, a, st) : i8_run<float>(ctx->i8, x_scale ? nullptr : (const float*)x, x8, weight, a, st));
+  return EE_OK;
+}
+
+ee_status_t ee_sample(int dtype, const void* logits, int rows, int n, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
+                      int32_t* tokens, float* probs, void* cuda_stream) {
+  if ((dtype != EE_F32 && dtype != EE_BF16) || rows < 0 || n < 1) return EE_ERR_INVALID_ARG;
+  if (n > kSpMost || (long)rows * kSpMaxCluster > 0x7fffffffL) return EE_ERR_CAPACITY;
+  if (rows == 0) return EE_OK;
+  const size_t es = esize(dtype), lb = (size_t)rows * n * es, pb = (size_t)rows * n * 4, row = (size_t)rows * 4;
+  if (!logits || (!tokens && !probs) || (tokens && !u)) return EE_ERR_INVALID_ARG;
+  if (!aligned_to(logits, es) || !aligned_to(temperature, 4) || !aligned_to(top_k, 4) || !aligned_to(top_p, 4) || !aligned_to(min_p, 4) || !aligned_to(u, 4) ||
+      !aligned_to(tokens, 4) || !aligned_to(probs, 4))
+    return EE_ERR_INVALID_ARG;
+  auto clear = [&](const void* p, size_t bytes) { return !p || ((!probs || apart(p, bytes, probs, pb)) && (!tokens || apart(p, bytes, tokens, row))); };
+  if ((probs && tokens && !apart(tokens, row, probs, pb)) || (tokens && !apart(logits, lb, tokens, row)) || !clear(temperature, row) || !clear(top_k, row) || !clear(top_p, row) ||
+      !clear(min_p, row) || !clear(u, row))
+    return EE_ERR_INVALID_ARG;
+  if (probs && !(dtype == EE_F32 && logits == (const void*)probs) && !apart(logits, lb, probs, pb)) return EE_ERR_INVALID_ARG;
+  OperatorContext* ctx;
+  const ee_status_t s = operator_context(&ctx);
+  if (s != EE_OK) return s;
+  const SampleArgs args = {logits, temperature, top_k, top_p, min_p, u, tokens, probs, n, 0};
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  EE_CUDA(dtype == EE_BF16 ? sample_launch<bf16>(args, rows, st) : sample_launch<float>(args, rows, st));
   return EE_OK;
 }
 

@@ -1,0 +1,810 @@
+// Rows in 8 bits, and the projection of such rows.
+//
+// quantise: s = max |x| (1 / 127) of a row, both rounded to fp32, and q = the integer nearest to x / s, of two the even one.  The quotient is meant, not its rounding to
+// fp32: x times 1 / s is off by less than 127 * 2^-22 = 3e-5, so what lies within 1e-4 of the middle of two integers is divided again in fp64 (whose rounding
+// cannot reach the middle: x / s misses it by 2^-26 of itself at least, or not at all).  Bound by memory: a row is read once, kept in the registers of one, four or sixteen
+// warps, whose exchange of the maximum is all they wait for.  Rows too long for that are read twice, from L2 the second time.
+//
+// dequantise: y = q s, rounded once.  Rows in any order.
+//
+// projection: y[t][f] = xs[t] ws[f] sum_k q[t][k] w[f][k] + bias[f], the sum on tcgen05 (kind::i8, 32-bit integers).  A sum of integers is exact, so however
+// K is cut and whatever else is in the batch, a row has the same bits.  The tile is turned, as in lowrank.cuh: filters are the rows of the accumulator, whose scale
+// and bias a thread keeps in registers, rows of the batch its columns; W, which bounds small batches, is read once.
+// Two forms.  Few tiles: a CTA of its own for each, K cut over a cluster whose CTAs send each other their parts as asynchronous stores.  More: CTA pairs
+// (cta_group::2), persistent, 256 filters by 256 rows with two accumulators: each SM of a pair fetches half of either operand, 32 KB for 512 clocks of products, which is
+// what L2 gives (64 bytes a clock); 128 x 256 tiles of a single SM would need 96.
+#pragma once
+#include "common.cuh"
+#include "conv_pair.cuh"
+#include "conv_tc.cuh"
+
+namespace ee {
+
+// Longest row of the projection: 128 * 128 * 131071 < 2^31.
+constexpr int kQMaxRow = 131071;
+__host__ __device__ constexpr int q_pitch(int c) { return (c + 15) / 16 * 16; }   // bytes of a quantised row: TMA wants rows on 16-byte boundaries
+
+// ----------------------------------------------------------------------------- quantise
+
+// |x| as an integer that orders like it; infinities and NaN lie from kQBad on.
+constexpr uint32_t kQBad = 0x7f800000u;
+
+// B bytes of T as floats.
+template <typename T, int B> struct QVec {
+  static constexpr int N = B / (int)sizeof(T);
+  uint32_t w[(B + 3) / 4];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (B == 16) {
+      const uint4 t = *reinterpret_cast<const uint4*>(p);
+      w[0] = t.x, w[1] = t.y, w[2] = t.z, w[3] = t.w;
+    } else if constexpr (B == 8) {
+      const uint2 t = *reinterpret_cast<const uint2*>(p);
+      w[0] = t.x, w[1] = t.y;
+    } else if constexpr (B == 4) {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else {
+      w[0] = (uint32_t)*reinterpret_cast<const unsigned short*>(p);
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < (B + 3) / 4; ++i) w[i] = 0u;
+  }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    return i & 1 ? __uint_as_float(w[i / 2] & 0xffff0000u) : __uint_as_float(w[i / 2] << 16);
+  }
+  __device__ __forceinline__ uint32_t top(uint32_t t) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) t = max(t, __float_as_uint(at(i)) & 0x7fffffffu);
+    return t;
+  }
+};
+
+struct QScale {
+  float s, inv;      // inv 0: everything is 0; s NaN: a row that is not finite
+  bool tiny;         // 1 / s is no finite float
+  __device__ __forceinline__ explicit QScale(uint32_t top) {
+    s = top >= kQBad ? __uint_as_float(0x7fffffffu) : __uint_as_float(top) * (1.f / 127.f);
+    tiny = s < 1e-37f && s > 0.f;
+    inv = s > 0.f && !tiny ? 1.f / s : 0.f;
+  }
+  __device__ __noinline__ int slow(float x) const {
+    const double q = rint((double)x / (double)s);
+    return (int)fmin(fmax(q, -127.0), 127.0);        // s below 2^-126 has fewer bits: x / s may pass 127
+  }
+  // N values as bytes, four a word.
+  template <int N, typename V>
+  __device__ __forceinline__ void bytes(const V& v, uint32_t* out) const {
+    constexpr float kMagic = 12582912.f;             // 1.5 * 2^23: the sum's last place is 1, its low byte the integer
+    float worst = 0.f;
+    uint32_t b[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float t = v.at(i) * inv, r = t + kMagic;
+      worst = fmaxf(worst, fabsf(t - (r - kMagic)));
+      b[i] = __float_as_uint(r);
+    }
+    if (!(inv > 0.f)) {                              // also where x * 0 is NaN
+#pragma unroll
+      for (int i = 0; i < N; ++i) b[i] = 0u;
+      worst = 0.f;
+    }
+    if (worst > 0.4999f || tiny) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float t = v.at(i) * inv;
+        if (tiny || fabsf(t - rintf(t)) > 0.4999f) b[i] = (uint32_t)slow(v.at(i));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < (N + 3) / 4; ++i) {
+      const uint32_t lo = __byte_perm(b[4 * i], N > 4 * i + 1 ? b[4 * i + (N > 1)] : 0u, 0x0040);
+      const uint32_t hi = N > 2 ? __byte_perm(b[N > 2 ? 4 * i + 2 : 0], b[N > 3 ? 4 * i + 3 : 0], 0x0040) : 0u;
+      out[i] = __byte_perm(lo, hi, 0x5410);
+    }
+  }
+};
+
+constexpr int kQKeep = 4;      // accesses of a thread that stay in its registers
+
+// WARPS a row (a CTA has max(4, WARPS) of them); B bytes an access; KEEP: the row is kept in registers, else read again.
+// Nothing that is read here is __restrict__: the kernel starts while the one in front, which may write it, still runs.
+template <typename T, int B, int WARPS, bool KEEP>
+__global__ void __launch_bounds__(WARPS < 4 ? 128 : 32 * WARPS)
+quantize_rows_kernel(const T* x, int8_t* q, float* scale, long rows, int c, int pitch) {
+  constexpr int N = QVec<T, B>::N, kRows = WARPS < 4 ? 4 / WARPS : 1, kStep = 32 * WARPS;
+  __shared__ uint32_t s_top[WARPS];
+  const int tid = threadIdx.x, lane = tid % kStep;      // of the row
+  const long row = (long)blockIdx.x * kRows + tid / kStep;
+  // The next launch may start once the past of the stream is over for this one: it may then read what no launch but this one writes.
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (WARPS == 1 && row >= rows) return;
+  const T* src = x + (size_t)row * c;
+  const int units = c / N;                              // N divides c
+  QVec<T, B> v[kQKeep];
+  uint32_t top = 0u;
+  if constexpr (KEEP) {
+#pragma unroll
+    for (int i = 0; i < kQKeep; ++i) {
+      if (lane + i * kStep < units) v[i].load(src + (size_t)(lane + i * kStep) * N);
+      else v[i].clear();
+    }
+#pragma unroll
+    for (int i = 0; i < kQKeep; ++i) top = v[i].top(top);
+  } else {
+#pragma unroll 4
+    for (int u = lane; u < units; u += kStep) {
+      QVec<T, B> w;
+      w.load(src + (size_t)u * N);
+      top = w.top(top);
+    }
+  }
+  top = __reduce_max_sync(0xffffffffu, top);
+  if constexpr (WARPS > 1) {
+    if ((tid & 31) == 0) s_top[tid >> 5] = top;
+    __syncthreads();
+    top = s_top[tid & (WARPS - 1)];
+    top = __reduce_max_sync(0xffffffffu, top);
+  }
+  const QScale sc(top);
+  if (lane == 0) scale[row] = sc.s;
+  int8_t* dst = q + (size_t)row * pitch;
+  auto put = [&](const QVec<T, B>& w, int u) {
+    uint32_t out[(N + 3) / 4];
+    sc.template bytes<N>(w, out);
+    int8_t* p = dst + (size_t)u * N;
+    if constexpr (N == 8) *reinterpret_cast<uint2*>(p) = make_uint2(out[0], out[1]);
+    else if constexpr (N == 4) *reinterpret_cast<uint32_t*>(p) = out[0];
+    else if constexpr (N == 2) *reinterpret_cast<unsigned short*>(p) = (unsigned short)out[0];
+    else *p = (int8_t)out[0];
+  };
+  if constexpr (KEEP) {
+#pragma unroll
+    for (int i = 0; i < kQKeep; ++i)
+      if (lane + i * kStep < units) put(v[i], lane + i * kStep);
+  } else {
+#pragma unroll 2
+    for (int u = lane; u < units; u += kStep) {
+      QVec<T, B> w;
+      w.load(src + (size_t)u * N);
+      put(w, u);
+    }
+  }
+  for (int i = c + lane; i < pitch; i += kStep) dst[i] = 0;      // up to 15 bytes behind the row
+}
+
+template <typename T, int B, int WARPS, bool KEEP>
+inline cudaError_t quantize_go(const T* x, int8_t* q, float* scale, long rows, int c, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(WARPS < 4 ? (rows + 4 / WARPS - 1) / (4 / WARPS) : rows));
+  cfg.blockDim = dim3(WARPS < 4 ? 128 : 32 * WARPS);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, quantize_rows_kernel<T, B, WARPS, KEEP>, x, q, scale, rows, c, q_pitch(c));
+}
+template <typename T, int B>
+inline cudaError_t quantize_width(const T* x, int8_t* q, float* scale, long rows, int c, cudaStream_t st) {
+  const int units = c / QVec<T, B>::N;
+  if (units <= 32 * kQKeep) return quantize_go<T, B, 1, true>(x, q, scale, rows, c, st);
+  if (units <= 128 * kQKeep) return quantize_go<T, B, 4, true>(x, q, scale, rows, c, st);
+  if (units <= 512 * kQKeep) return quantize_go<T, B, 16, true>(x, q, scale, rows, c, st);
+  return quantize_go<T, B, 16, false>(x, q, scale, rows, c, st);
+}
+// The widest access that rows are whole units of and start on the boundaries of.
+template <typename T>
+inline cudaError_t quantize_launch(const T* x, int8_t* q, float* scale, long rows, int c, cudaStream_t st) {
+  const uintptr_t bits = (uintptr_t)x | (uintptr_t)((size_t)c * sizeof(T));
+  if ((bits & 15) == 0) return quantize_width<T, 16>(x, q, scale, rows, c, st);
+  if ((bits & 7) == 0) return quantize_width<T, 8>(x, q, scale, rows, c, st);
+  if (sizeof(T) == 4 || (bits & 3) == 0) return quantize_width<T, 4>(x, q, scale, rows, c, st);
+  if constexpr (sizeof(T) == 2) return quantize_width<T, 2>(x, q, scale, rows, c, st);
+  return cudaErrorInvalidValue;
+}
+
+// ----------------------------------------------------------------------------- dequantise
+
+// N values an access; 2^lanes threads a row.
+template <typename T, int N>
+__global__ void __launch_bounds__(256)
+dequantize_rows_kernel(const int8_t* q, const float* scale, const int32_t* index, T* y, long rows, int pool, int c, int pitch, int lanes) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const long row = (long)blockIdx.x * (256 >> lanes) + (threadIdx.x >> lanes);
+  if (row >= rows) return;
+  const long from = index ? (long)index[row] : row;
+  if (from < 0 || from >= pool) return;                 // no such row: left as it is
+  const float s = scale[from];
+  const int8_t* src = q + (size_t)from * pitch;
+  T* dst = y + (size_t)row * c;
+  const int units = c / N, step = 1 << lanes;
+#pragma unroll 4
+  for (int u = threadIdx.x & (step - 1); u < units; u += step) {
+    uint32_t w[2] = {0u, 0u};
+    if constexpr (N == 8) {
+      const uint2 t = *reinterpret_cast<const uint2*>(src + (size_t)u * 8);
+      w[0] = t.x, w[1] = t.y;
+    } else if constexpr (N == 4) {
+      w[0] = *reinterpret_cast<const uint32_t*>(src + (size_t)u * 4);
+    } else if constexpr (N == 2) {
+      w[0] = *reinterpret_cast<const unsigned short*>(src + (size_t)u * 2);
+    } else {
+      w[0] = *reinterpret_cast<const unsigned char*>(src + u);
+    }
+    float v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = (float)(int8_t)(w[i / 4] >> (8 * (i & 3))) * s;
+    T* p = dst + (size_t)u * N;
+    if constexpr (sizeof(T) * N == 16) {
+      Vec16<T> o;
+#pragma unroll
+      for (int i = 0; i < N; ++i) o.v[i] = v[i];
+      o.store(p);
+    } else if constexpr (sizeof(T) == 2 && N == 4) {
+      *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    } else if constexpr (sizeof(T) == 2 && N == 2) {
+      *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(v[0], v[1]);
+    } else if constexpr (sizeof(T) == 4 && N == 2) {
+      *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+    } else {
+      Elem<T>::st(p, v[0]);
+    }
+  }
+}
+
+template <typename T, int N>
+inline cudaError_t dequantize_go(const int8_t* q, const float* scale, const int32_t* index, T* y, long rows, int pool, int c, cudaStream_t st) {
+  int lanes = 3;                                        // threads of a row: enough for four accesses each, up to a CTA
+  while (lanes < 8 && c / N > 4 << lanes) ++lanes;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((rows + (256 >> lanes) - 1) / (256 >> lanes)));
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, dequantize_rows_kernel<T, N>, q, scale, index, y, rows, pool, c, q_pitch(c), lanes);
+}
+template <typename T>
+inline cudaError_t dequantize_launch(const int8_t* q, const float* scale, const int32_t* index, T* y, long rows, int pool, int c, cudaStream_t st) {
+  const uintptr_t bits = (uintptr_t)y | (uintptr_t)((size_t)c * sizeof(T));
+  constexpr int E = 16 / (int)sizeof(T);
+  if ((bits & 15) == 0) return dequantize_go<T, E>(q, scale, index, y, rows, pool, c, st);
+  if ((bits & 7) == 0) return dequantize_go<T, E / 2>(q, scale, index, y, rows, pool, c, st);
+  if ((bits & 3) == 0) return dequantize_go<T, E / 4>(q, scale, index, y, rows, pool, c, st);
+  return dequantize_go<T, 1>(q, scale, index, y, rows, pool, c, st);
+}
+
+// ----------------------------------------------------------------------------- projection
+
+struct I8Args {
+  const float* xs;     // [rows]
+  const float* ws;     // [n] or null
+  const float* bias;   // [n] or null
+  void* y;             // [rows][n]
+  int rows, c, n;
+  int early;           // the launch in front writes x and xs, and nothing else that is read here
+  int* err_flag;
+  long long wait_cycles;
+};
+
+// s8 x s8 -> s32, both operands K-major, M = m, N = n.
+__host__ __device__ constexpr uint32_t i8_idesc(int n, int m) { return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
+
+// The four MMAs of a K block of 128 bytes: K = 32 each.
+__device__ __forceinline__ void i8_block(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc, bool accumulate) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(da + 2 * k), "l"(db + 2 * k), "r"(idesc), "r"((uint32_t)(accumulate || k != 0))
+                 : "memory");
+}
+__device__ __forceinline__ void i8_block2(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc, bool accumulate) {   // over a CTA pair
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(da + 2 * k), "l"(db + 2 * k), "r"(idesc), "r"((uint32_t)(accumulate || k != 0))
+                 : "memory");
+}
+
+// Behind a wait that ran out: K blocks `from` and on that may be on their way land before their CTA goes, or another limit passes.
+__device__ __noinline__ void i8_drain(uint32_t full0, int stages, int from, int blocks, int* err_flag) {
+  for (int j = from; j < min(from + stages, blocks); ++j)
+    if (!mbar_wait(full0 + 8u * (j % stages), (uint32_t)(j / stages) & 1u, err_flag)) return;
+}
+
+// A value of y, rounded once: in fp32 for bf16 (three roundings of 2^-24 before one of 2^-8), in fp64 for fp32.
+template <typename T> struct I8Value;
+template <> struct I8Value<bf16> {
+  static __device__ __forceinline__ float of(int acc, float ws, float xs, float bias) { return fmaf((float)acc * ws, xs, bias); }
+};
+template <> struct I8Value<float> {
+  static __device__ __forceinline__ float of(int acc, float ws, float xs, float bias) { return (float)fma((double)acc * (double)ws, (double)xs, (double)bias); }
+};
+
+// Stores of a warp that holds 32 filters of two rows: of bf16, two neighbouring lanes trade, and the even one stores both filters of the even row, the odd one those of the odd.
+template <typename T> struct I8Store {
+  T* y;
+  int rows, n, f, lane;
+  bool pairs, ok;
+  __device__ __forceinline__ I8Store(const I8Args& p, int f_, int lane_)
+      : y((T*)p.y), rows(p.rows), n(p.n), f(f_), lane(lane_), pairs(sizeof(T) == 2 && p.n % 2 == 0 && ((uintptr_t)p.y & 3) == 0), ok(true) {}
+  __device__ __forceinline__ void put2(int t, float v0, float v1) const {       // rows t and t + 1
+    if (sizeof(T) == 2 && pairs) {
+      const float give = lane & 1 ? v0 : v1, keep = lane & 1 ? v1 : v0, got = __shfl_xor_sync(0xffffffffu, give, 1);
+      t += lane & 1;
+      if (ok && f < n && t < rows) *reinterpret_cast<uint32_t*>(y + (size_t)t * n + (f & ~1)) = lane & 1 ? pack_bf16x2(got, keep) : pack_bf16x2(keep, got);
+    } else if (ok && f < n) {
+      if (t < rows) Elem<T>::st(y + (size_t)t * n + f, v0);
+      if (t + 1 < rows) Elem<T>::st(y + (size_t)(t + 1) * n + f, v1);
+    }
+  }
+};
+
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, int* v, std::integral_constant<int, 32>) { tmem_ld32(taddr, reinterpret_cast<float*>(v)); }
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, int* v, std::integral_constant<int, 16>) { tmem_ld16(taddr, reinterpret_cast<float*>(v)); }
+
+constexpr int kI8Threads = 224;   // producer of W, MMA, four epilogue warps, producer of x
+
+template <int TN>
+struct I8Smem {
+  static constexpr int kABytes = 128 * 128, kBBytes = TN * 128, kStage = kABytes + kBBytes;
+  static constexpr int kStages = TN == 128 ? 4 : TN == 64 ? 6 : 8;
+  static constexpr int kPart = TN * 128 * 4;                 // what the cluster's CTAs send
+  static constexpr int kOffPart = kStages * kStage, kOffXs = kOffPart + kPart, kOffBars = kOffXs + TN * 4;
+  static constexpr int kBars = 2 * kStages + 2;
+  static constexpr int kBytes = kOffBars + 8 * kBars + 16 + 1024;
+  static_assert(kBytes <= 227 * 1024, "exceeds the shared memory of an SM");
+};
+
+// tmW: rows of W in boxes of 128, tmX: rows of x in boxes of TN; 128 bytes of K each.  blockIdx: x of filters, y of rows, z: range of K.
+template <typename T, int TN>
+__global__ void __launch_bounds__(kI8Threads)
+int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, I8Args p) {
+  using S = I8Smem<TN>;
+  constexpr int kStages = S::kStages;
+  extern __shared__ uint8_t i8_smem[];
+  const uint32_t raw = smem_u32(i8_smem), base = (raw + 1023u) & ~1023u;
+  uint8_t* gen = i8_smem + (base - raw);
+  float* s_xs = reinterpret_cast<float*>(gen + S::kOffXs);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + S::kOffBars + 8 * S::kBars);
+  const uint32_t bar0 = base + S::kOffBars;
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (kStages + s); };
+  const uint32_t accum_bar = bar0 + 8u * (2 * kStages), part_bar = accum_bar + 8u;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  const int z = (int)blockIdx.z, Z = (int)gridDim.z;
+  const int n0 = (int)blockIdx.x * 128, t0 = (int)blockIdx.y * TN;
+  const int kb_all = (p.c + 127) / 128;
+  const int kb0 = (int)((long)kb_all * z / Z), num_kb = (int)((long)kb_all * (z + 1) / Z) - kb0;   // Z <= kb_all: never empty
+
+  if ((warp == 0 || warp == 6) && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(warp == 0 ? &tmW : &tmX) : "memory");
+  if (tid == 0) {
+    for (int s = 0; s < kStages; ++s) mbar_init(full_bar(s), 2), mbar_init(empty_bar(s), 1);
+    mbar_init(accum_bar, 1), mbar_init(part_bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (Z > 1) mbar_expect_tx(part_bar, (uint32_t)S::kPart);     // TN / Z columns from each of Z CTAs
+  }
+  constexpr uint32_t kCols = TN < 32 ? 32 : TN;
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // The producer of W needs nothing but its barriers, which its own warp set up.
+  if (warp == 0) {
+    __syncwarp();
+    asm volatile("bar.arrive 2, %0;" ::"n"(kI8Threads) : "memory");
+  } else {
+    tc_fence_before();
+    asm volatile("bar.sync 2, %0;" ::"n"(kI8Threads) : "memory");
+    tc_fence_after();
+  }
+  const uint32_t tmem = warp == 0 ? 0u : *tmem_slot;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (Z > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");       // waited for before anything is sent
+  if (!(warp == 0 && p.early)) asm volatile("griddepcontrol.wait;" ::: "memory");
+  bool lost = false;                             // the cluster's parts have not come
+
+  if (warp == 0 || warp == 6) {
+    if (elect_one()) {
+      const CUtensorMap* tm = warp == 0 ? &tmW : &tmX;
+      const uint32_t off = warp == 0 ? 0u : (uint32_t)S::kABytes, bytes = warp == 0 ? S::kABytes : S::kBBytes;
+      const int row = warp == 0 ? n0 : t0;
+      int s = 0;
+      uint32_t ph = 1u;
+      for (int i = 0; i < num_kb; ++i) {
+        if (i >= kStages && !mbar_wait(empty_bar(s), ph, p.err_flag)) break;
+        mbar_expect_tx(full_bar(s), bytes);
+        tma_load_2d(base + (uint32_t)s * S::kStage + off, tm, full_bar(s), (kb0 + i) * 128, row);
+        if (++s == kStages) s = 0, ph ^= 1u;
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (elect_one()) {
+      constexpr uint32_t idesc = i8_idesc(TN, 128);
+      const uint64_t da0 = umma_desc(base), db0 = umma_desc(base + S::kABytes);
+      int s = 0, done = 0;
+      uint32_t ph = 0u;
+      bool ok = true;
+      for (; done < num_kb; ++done) {
+        const int i = done;
+        ok = mbar_wait(full_bar(s), ph, p.err_flag);
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t off = (uint64_t)(s * (S::kStage >> 4));
+        i8_block(tmem, da0 + off, db0 + off, idesc, i != 0);
+        umma_commit(empty_bar(s));
+        if (++s == kStages) s = 0, ph ^= 1u;
+      }
+      if (ok) umma_commit(accum_bar);
+      else i8_drain(full_bar(0), kStages, done, num_kb, p.err_flag);
+    }
+    __syncwarp();
+  } else {
+    const int et = tid - 64, q = warp & 3, row = q * 32 + lane, f = n0 + row;
+    constexpr int CH = TN < 32 ? TN : 32;              // columns read at a time
+    const std::integral_constant<int, CH> ch;
+    const float ws = f < p.n ? (p.ws ? p.ws[f] : 1.f) : 0.f, bias = p.bias && f < p.n ? p.bias[f] : 0.f;
+    if (et < TN) s_xs[et] = t0 + et < p.rows ? p.xs[t0 + et] : 0.f;
+    asm volatile("bar.sync 1, 128;" ::: "memory");
+    I8Store<T> out(p, f, lane);
+    out.ok = __all_sync(0xffffffffu, mbar_wait(accum_bar, 0, p.err_flag));
+    tc_fence_after();
+    const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
+    auto value = [&](int acc, int col) { return I8Value<T>::of(acc, ws, s_xs[col], bias); };
+    if (Z == 1) {
+#pragma unroll 1
+      for (int c = 0; c < TN && t0 + c < p.rows; c += CH) {
+        int v[CH];
+        tmem_ld_cols(lane_base + c, v, ch);
+#pragma unroll
+        for (int i = 0; i < CH; i += 2) out.put2(t0 + c + i, value(v[i], c + i), value(v[i + 1], c + i + 1));
+      }
+    } else {
+      // CTA o of the cluster finishes columns [o * share, + share): everybody sends it its part of them, in runs of four columns (two where a share has no more)
+      const int share = TN / Z, log_share = 31 - __clz(share);
+      asm volatile("barrier.cluster.wait.acquire;" ::: "memory");      // every CTA's barriers are set up
+      const uint32_t recv = base + S::kOffPart;
+#pragma unroll 1
+      for (int c = 0; c < TN; c += CH) {
+        int v[CH];
+        tmem_ld_cols(lane_base + c, v, ch);
+        if (share >= 4) {
+#pragma unroll
+          for (int i = 0; i < CH; i += 4) {
+            const int o = (c + i) >> log_share, at = ((z * share + (c + i) - (o << log_share)) * 128 + row * 4) * 4;
+            asm volatile(
+                "{\n .reg .b32 a, b;\n mapa.shared::cluster.u32 a, %0, %2;\n mapa.shared::cluster.u32 b, %1, %2;\n"
+                " st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [a], {%3, %4, %5, %6}, [b];\n}"
+                ::"r"(recv + (uint32_t)at), "r"(part_bar), "r"(o), "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3])
+                : "memory");
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < CH; i += 2) {
+            const int o = (c + i) >> 1, at = (z * 256 + row * 2) * 4;
+            asm volatile(
+                "{\n .reg .b32 a, b;\n mapa.shared::cluster.u32 a, %0, %2;\n mapa.shared::cluster.u32 b, %1, %2;\n"
+                " st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [a], {%3, %4}, [b];\n}"
+                ::"r"(recv + (uint32_t)at), "r"(part_bar), "r"(o), "r"(v[i]), "r"(v[i + 1])
+                : "memory");
+          }
+        }
+      }
+      lost = !__all_sync(0xffffffffu, mbar_wait_cluster(part_bar, 0, p.err_flag, p.wait_cycles));
+      out.ok = out.ok && !lost;
+      const int* in = reinterpret_cast<const int*>(gen + S::kOffPart);
+#pragma unroll 1
+      for (int i = 0; i < share; i += 4) {
+        int sum[4] = {0, 0, 0, 0};
+        if (share >= 4) {
+#pragma unroll 2
+          for (int k = 0; k < Z; ++k) {
+            const int4 o = *reinterpret_cast<const int4*>(in + (k * share + i) * 128 + row * 4);
+            sum[0] += o.x, sum[1] += o.y, sum[2] += o.z, sum[3] += o.w;
+          }
+        } else {
+#pragma unroll 2
+          for (int k = 0; k < Z; ++k) {
+            const int2 o = *reinterpret_cast<const int2*>(in + k * 256 + row * 2);
+            sum[0] += o.x, sum[1] += o.y;
+          }
+        }
+        const int c = z * share + i;
+        out.put2(t0 + c, value(sum[0], c), value(sum[1], c + 1));
+        if (share >= 4) out.put2(t0 + c + 2, value(sum[2], c + 2), value(sum[3], c + 3));
+      }
+    }
+    tc_fence_before();
+  }
+  if (Z > 1 && !(warp >= 2 && warp < 6)) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");   // the other warps' part in the barrier at the start
+  if (__syncthreads_or(lost)) cluster_drain(part_bar, 0, p.err_flag);      // the status says so, and y stays as it is
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols) : "memory");
+}
+
+// ---- CTA pairs
+
+constexpr int kI8PairEpi = 8, kI8PairThreads = 64 + 32 * kI8PairEpi;
+
+template <int TN>
+struct I8PairSmem {
+  static constexpr int kABytes = 128 * 128, kBBytes = TN / 2 * 128, kStage = kABytes + kBBytes;   // this CTA's filters, its half of the rows of x
+  static constexpr int kStages = TN == 256 ? 6 : 8;
+  static constexpr int kOffXs = kStages * kStage, kOffBars = kOffXs + 2 * TN * 4;
+  static constexpr int kBars = 2 * kStages + 5;
+  static constexpr int kBytes = kOffBars + 8 * kBars + 16 + 1024;
+  static_assert(kBytes <= 227 * 1024, "exceeds the shared memory of an SM");
+};
+
+template <typename T, int TN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8PairThreads, 1)
+int8_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, I8Args p) {
+  using S = I8PairSmem<TN>;
+  constexpr int kStages = S::kStages, HALF = TN / 2;
+  extern __shared__ uint8_t i8_smem[];
+  const uint32_t raw = smem_u32(i8_smem), base = (raw + 1023u) & ~1023u;
+  uint8_t* gen = i8_smem + (base - raw);
+  float* s_xs = reinterpret_cast<float*>(gen + S::kOffXs);         // [2][TN]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + S::kOffBars + 8 * S::kBars);
+  const uint32_t bar0 = base + S::kOffBars;
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };            // the leader's counts both CTAs' loads
+  auto empty_bar = [&](int s) { return bar0 + 8u * (kStages + s); };
+  auto acc_full = [&](int b) { return bar0 + 8u * (2 * kStages + b); };
+  auto acc_empty = [&](int b) { return bar0 + 8u * (2 * kStages + 2 + b); };
+  const uint32_t stop_bar = bar0 + 8u * (2 * kStages + 4);         // behind a wait that ran out: what was issued has ended
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  const uint32_t rank = cluster_rank();                            // 0: leader
+  const int pair = (int)(blockIdx.x >> 1), n_pairs = (int)(gridDim.x >> 1);
+  const int tiles_n = (p.n + 255) / 256, tiles = tiles_n * ((p.rows + TN - 1) / TN), num_kb = (p.c + 127) / 128;
+
+  if (tid == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmW) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmX) : "memory");
+    for (int s = 0; s < kStages; ++s) mbar_init(full_bar(s), 1), mbar_init(empty_bar(s), 1);
+    for (int b = 0; b < 2; ++b) mbar_init(acc_full(b), 1), mbar_init(acc_empty(b), 2 * kI8PairEpi);
+    mbar_init(stop_bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(2 * TN) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  cluster_sync_all();     // barriers and tensor memory of both CTAs are there
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  if (warp == 0) {
+    if (elect_one()) {
+      int s = 0, g = 0;
+      uint32_t ph = 1u;
+      bool ok = true;
+      for (int tile = pair; tile < tiles && ok; tile += n_pairs) {
+        const int n0 = tile % tiles_n * 256 + (int)rank * 128, t0 = tile / tiles_n * TN + (int)rank * HALF;
+        for (int i = 0; i < num_kb; ++i, ++g) {
+          ok = g < kStages || mbar_wait(empty_bar(s), ph, p.err_flag);
+          if (!ok) break;
+          if (rank == 0) mbar_expect_tx(full_bar(s), (uint32_t)(2 * S::kStage));
+          const uint32_t dst = base + (uint32_t)s * S::kStage, bar = map_to_rank(full_bar(s), 0);
+          tma2_load_2d(dst, &tmW, bar, i * 128, n0);
+          tma2_load_2d(dst + S::kABytes, &tmX, bar, i * 128, t0);
+          if (++s == kStages) s = 0, ph ^= 1u;
+        }
+      }
+      // The other CTA's loads count here too, and it waits for this CTA below.
+      if (!ok && rank == 0) i8_drain(full_bar(0), kStages, max(0, g - kStages), g, p.err_flag);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (rank == 0 && elect_one()) {
+      constexpr uint32_t idesc = i8_idesc(TN, 256);
+      const uint64_t da0 = umma_desc(base), db0 = umma_desc(base + S::kABytes);
+      int s = 0, it = 0;
+      uint32_t ph = 0u;
+      bool ok = true;
+      for (int tile = pair; tile < tiles && ok; tile += n_pairs, ++it) {
+        const int b = it & 1;
+        if (it >= 2) ok = mbar_wait(acc_empty(b), (uint32_t)(it / 2 - 1) & 1u, p.err_flag);
+        if (!ok) break;
+        tc_fence_after();
+        for (int i = 0; i < num_kb; ++i) {
+          ok = mbar_wait(full_bar(s), ph, p.err_flag);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t off = (uint64_t)(s * (S::kStage >> 4));
+          i8_block2(tmem + (uint32_t)(b * TN), da0 + off, db0 + off, idesc, i != 0);
+          umma2_commit_both(empty_bar(s));
+          if (++s == kStages) s = 0, ph ^= 1u;
+        }
+        if (ok) umma2_commit_both(acc_full(b));
+      }
+      if (!ok) {
+        umma2_commit_both(stop_bar);
+        mbar_wait(stop_bar, 0, p.err_flag);
+      }
+    }
+    __syncwarp();
+  } else {
+    const int ew = warp - 2, q = warp & 3, h = ew >> 2;
+    const uint32_t drained[2] = {map_to_rank(acc_empty(0), 0), map_to_rank(acc_empty(1), 0)};
+    int it = 0;
+    bool ok = true;
+    for (int tile = pair; tile < tiles; tile += n_pairs, ++it) {    // a warp whose wait ran out stores nothing but meets the others
+      const int b = it & 1, n0 = tile % tiles_n * 256 + (int)rank * 128, t0 = tile / tiles_n * TN;
+      const int f = n0 + q * 32 + lane;
+      const float ws = f < p.n ? (p.ws ? p.ws[f] : 1.f) : 0.f, bias = p.bias && f < p.n ? p.bias[f] : 0.f;
+      // The scales of this tile's rows, in the half of the array that the tile before the last one left.
+      float* xs = s_xs + b * TN;
+      const int et = tid - 64;
+      if (et < TN) xs[et] = t0 + et < p.rows ? p.xs[t0 + et] : 0.f;
+      asm volatile("bar.sync 1, %0;" ::"n"(32 * kI8PairEpi) : "memory");
+      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(acc_full(b), (uint32_t)(it / 2) & 1u, p.err_flag));
+      if (!ok) continue;
+      tc_fence_after();
+      const I8Store<T> out(p, f, lane);
+      const uint32_t acc = tmem + (uint32_t)(b * TN + h * HALF) + ((uint32_t)(q * 32) << 16);
+#pragma unroll 1
+      for (int c = 0; c < HALF; c += 32) {
+        int v[32];
+        tmem_ld32(acc + c, reinterpret_cast<float*>(v));
+        const int col = h * HALF + c;
+        if (c + 32 == HALF) {          // this warp's share is in registers
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(drained[b]);
+        }
+        if (t0 + col >= p.rows) continue;
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+          const float4 x = *reinterpret_cast<const float4*>(xs + col + i);
+          out.put2(t0 + col + i, I8Value<T>::of(v[i], ws, x.x, bias), I8Value<T>::of(v[i + 1], ws, x.y, bias));
+          out.put2(t0 + col + i + 2, I8Value<T>::of(v[i + 2], ws, x.z, bias), I8Value<T>::of(v[i + 3], ws, x.w, bias));
+        }
+      }
+    }
+  }
+  // Both CTAs stay until the other is done with their barriers and tensor memory.
+  tc_fence_before();
+  cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * TN) : "memory");
+  }
+}
+
+// ---- host side
+
+struct I8Context {
+  PFN_encodeTiled encode_tiled = nullptr;
+  int sm_count = 148;
+  int fit[4] = {};   // clusters of 1, 2, 4 and 8 CTAs, one an SM, that run side by side
+};
+
+inline cudaError_t i8_map(const I8Context& c, CUtensorMap* tm, const void* base, long rows, int cols, int box_rows) {
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};      // what lies behind a row's values is not read
+  const cuuint64_t strides[1] = {(cuuint64_t)q_pitch(cols)};
+  const cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+  const cuuint32_t es[2] = {1, 1};
+  return c.encode_tiled(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? cudaSuccess
+             : cudaErrorInvalidValue;
+}
+
+template <typename T>
+inline cudaError_t i8_context_init(I8Context& ctx) {   // once per device and type
+  cudaError_t e = cudaSuccess;
+  auto set = [&](auto kernel, int bytes) {
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  };
+  set(int8_linear_kernel<T, 16>, I8Smem<16>::kBytes);
+  set(int8_linear_kernel<T, 32>, I8Smem<32>::kBytes);
+  set(int8_linear_kernel<T, 64>, I8Smem<64>::kBytes);
+  set(int8_linear_kernel<T, 128>, I8Smem<128>::kBytes);
+  set(int8_linear_pair_kernel<T, 128>, I8PairSmem<128>::kBytes);
+  set(int8_linear_pair_kernel<T, 256>, I8PairSmem<256>::kBytes);
+  for (int i = 0; i < 4 && e == cudaSuccess; ++i) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1u << i;
+    cfg.gridDim = dim3(1, 1, 1u << i);
+    cfg.blockDim = dim3(kI8Threads);
+    cfg.dynamicSmemBytes = I8Smem<64>::kBytes;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&ctx.fit[i], int8_linear_kernel<T, 64>, &cfg);
+  }
+  return e;
+}
+
+struct I8Plan {
+  int tn, splits;    // rows of a tile; CTAs that share its K
+  bool pair;
+};
+
+inline I8Plan i8_plan(int rows, int c, int n, const I8Context& ctx) {
+  I8Plan p;
+  const int kb = cdiv(c, 128);
+  p.tn = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  const long tiles = (long)cdiv(n, 128) * cdiv(rows, p.tn);
+  p.splits = 1;
+  p.pair = tiles > ctx.sm_count && n > 128;
+  if (p.pair) {
+    const int pairs = ctx.sm_count / 2;
+    auto rounds = [&](int tn) { return ((long)cdiv(n, 256) * cdiv(rows, tn) + pairs - 1) / pairs; };
+    p.tn = rows > 128 && rounds(256) * 5 <= rounds(128) * 3 ? 256 : 128;
+    return p;
+  }
+  int i = 0;
+  while (i < 3 && tiles <= ctx.fit[i + 1] && kb >= 2 << i) ++i;
+  p.splits = 1 << i;
+  return p;
+}
+
+template <typename T, int TN>
+inline cudaError_t i8_one(const I8Plan& pl, const CUtensorMap& tmW, const CUtensorMap& tmX, const I8Args& a, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(cdiv(a.n, 128), cdiv(a.rows, TN), pl.splits);
+  cfg.blockDim = dim3(kI8Threads);
+  cfg.dynamicSmemBytes = I8Smem<TN>::kBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = pl.splits;
+  cfg.attrs = attr;
+  cfg.numAttrs = pl.splits > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, int8_linear_kernel<T, TN>, tmW, tmX, a);
+}
+template <typename T, int TN>
+inline cudaError_t i8_pair(const I8Context& ctx, const CUtensorMap& tmW, const CUtensorMap& tmX, const I8Args& a, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * (unsigned)std::min<long>(ctx.sm_count / 2, (long)cdiv(a.n, 256) * cdiv(a.rows, TN)));
+  cfg.blockDim = dim3(kI8PairThreads);
+  cfg.dynamicSmemBytes = I8PairSmem<TN>::kBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, int8_linear_pair_kernel<T, TN>, tmW, tmX, a);
+}
+
+// x8: quantised rows; raw: rows that are quantised into them first, or null.
+template <typename T>
+inline cudaError_t i8_run(const I8Context& ctx, const T* raw, const int8_t* x8, const int8_t* w, I8Args a, cudaStream_t st) {
+  const I8Plan pl = i8_plan(a.rows, a.c, a.n, ctx);
+  CUtensorMap tmW = {}, tmX = {};
+  cudaError_t e = i8_map(ctx, &tmW, w, a.n, a.c, 128);
+  if (e == cudaSuccess) e = i8_map(ctx, &tmX, x8, a.rows, a.c, pl.pair ? pl.tn / 2 : pl.tn);
+  if (e != cudaSuccess) return e;
+  a.early = raw != nullptr;
+  if (raw) {
+    e = quantize_launch<T>(raw, const_cast<int8_t*>(x8), const_cast<float*>(a.xs), a.rows, a.c, st);
+    if (e != cudaSuccess) return e;
+  }
+  if (pl.pair) return pl.tn == 256 ? i8_pair<T, 256>(ctx, tmW, tmX, a, st) : i8_pair<T, 128>(ctx, tmW, tmX, a, st);
+  switch (pl.tn) {
+    case 16: return i8_one<T, 16>(pl, tmW, tmX, a, st);
+    case 32: return i8_one<T, 32>(pl, tmW, tmX, a, st);
+    case 64: return i8_one<T, 64>(pl, tmW, tmX, a, st);
+    default: return i8_one<T, 128>(pl, tmW, tmX, a, st);
+  }
+}
+
+}  // namespace ee
