@@ -5,11 +5,20 @@
 // an index).  The token is the first kept class, by index, at which the running sum of weights exceeds u times their total.
 //
 // Weights and sums are fp64: a row of 10^5 classes has as many borders that u may fall next to, and sums that are off by 10^-7 would take another class on one draw in
-// a hundred.  2^z by the power series of exp on |z - integer| <= 1/2, to 2^-50 of itself.
+// a hundred.  2^z = 2^(k / 256) 2^g with the first factor from a table and |g| <= 1 / 512: the power series of exp up to its fourth term leaves 2^-54 and takes ten fp64 operations
+// with the sum, half of what it takes without a table.
 //
-// A row is kept in the shared memory of a CTA, or of a cluster of them.  Its last member is found digit by digit of the logit's bits: the CTAs count (and weigh) what
-// has the digits found so far by its next one, read each other's counts, and each takes the digit in which the k-th member, or the p-th part of the weight, lies.
+// A row is kept in the shared memory of a CTA, or of a cluster of them, which speak in turns (meet).  The last member is looked for among few:
+//   k: as many groups of lanes as k have a maximum at or above the smallest of those maxima, so the k-th largest lies there too.  Groups are as large as k allows (a warp, four
+//   lanes, a lane): 64 warps of 2000 logits each leave about 250 candidates.  Where they are too many, they are counted in 1024 bins, equally wide in the logit.
+//   p: a class weighs at least (1 - p) / n of the total if it is kept (those behind it would otherwise weigh less than 1 - p), which bounds its logit.  Candidates are weighed in 1024
+//   bins, in the pass that sums the total: a bin is 0.04 octaves wide at most, so a member's share of its bin's largest weight, 17 bits, goes into a 32-bit sum.
+// What lies in the bin of the goal, or everything down to it if that is little, is gathered in a list, ordered by counting, and weighed exactly.
+// Otherwise (thousands of equal logits, k above the list's length, no finite bound) it is found digit by digit of the logit's bits: the CTAs count (and weigh) what
+// has the digits found so far by its next one, read each other's counts, and each takes the digit in which the goal lies.
 #pragma once
+#include <float.h>
+
 #include "common.cuh"
 #include "conv_pair.cuh"
 #include "conv_tc.cuh"
@@ -22,6 +31,8 @@ constexpr int kSpPart = 16384;           // elements of a CTA's part that a clus
 constexpr int kSpMaxCluster = 16, kSpMaxPart = 38400;
 constexpr int kSpBlock = 512;            // elements of a block whose sum is kept
 constexpr int kSpMost = kSpMaxCluster * kSpMaxPart;
+constexpr int kSpBins = 1024, kSpList = 512;
+constexpr int kSpTable = 256;
 
 struct SampleArgs {
   const void* x;           // [rows][n]
@@ -35,27 +46,13 @@ struct SampleArgs {
   int n, per;
 };
 
-// 2^z, z <= 0.  With g = (z - k) ln 2, |g| <= 0.35: the series up to g^12 / 12! leaves 2^-52.
-__device__ __forceinline__ double sp_pow2(double z) {
-  if (!(z > -1080.0)) return 0.0;
-  const double r = z + 6755399441055744.0;            // 1.5 * 2^52: the sum's last place is 1
-  const int k = __double2loint(r);
-  const double g = (z - (r - 6755399441055744.0)) * 0.69314718055994531;
-  double p = 1.0 / 479001600;
-  p = fma(p, g, 1.0 / 39916800);
-  p = fma(p, g, 1.0 / 3628800);
-  p = fma(p, g, 1.0 / 362880);
-  p = fma(p, g, 1.0 / 40320);
-  p = fma(p, g, 1.0 / 5040);
-  p = fma(p, g, 1.0 / 720);
-  p = fma(p, g, 1.0 / 120);
-  p = fma(p, g, 1.0 / 24);
-  p = fma(p, g, 1.0 / 6);
-  p = fma(p, g, 0.5);
-  p = fma(p, g, 1.0);
-  p = fma(p, g, 1.0);
-  if (k < -1000) return __hiloint2double(__double2hiint(p) + ((k + 200) << 20), __double2loint(p)) * 6.223015277861142e-61;   // 2^-200: down to the smallest double
-  return __hiloint2double(__double2hiint(p) + (k << 20), __double2loint(p));
+// 2^(j / 256) by the series of exp up to its 12th term.
+__device__ __forceinline__ double sp_root(int j) {
+  const double g = j * (0.69314718055994531 / kSpTable);
+  double p = 1.0;
+#pragma unroll
+  for (int n = 16; n >= 1; --n) p = fma(p, g * (1.0 / n), 1.0);
+  return p;
 }
 
 // An integer that orders like the float; both zeros are one.
@@ -66,9 +63,29 @@ __device__ __forceinline__ uint32_t sp_key(float l) {
 __device__ __forceinline__ float sp_logit(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 
 struct SpWeight {
+  const double* roots;
   double c, top;
-  __device__ __forceinline__ SpWeight(float heat, float top_) : c(1.4426950408889634 / (double)heat), top((double)top_) {}
-  __device__ __forceinline__ double operator()(float l) const { return l == -INFINITY ? 0.0 : sp_pow2(((double)l - top) * c); }
+  uint32_t far;            // upper half of the difference behind which nothing is left; as bits, that of a negative number grows with its size
+  __device__ __forceinline__ SpWeight(const double* table, float heat, float top_)
+      : roots(table), c(1.4426950408889634 / (double)heat), top((double)top_) {
+    far = (uint32_t)__double2hiint(fmax(-1080.0 / c, -DBL_MAX));
+  }
+  __device__ __forceinline__ double operator()(float l) const {
+    constexpr double kMagic = 26388279066624.0;        // 1.5 * 2^44: the sum's last place is 1 / 256
+    const double d = (double)l - top;
+    if ((uint32_t)__double2hiint(d) > far) return 0.0; // also -inf at any temperature (0 * inf)
+    const double r = fma(d, c, kMagic);
+    const int k = __double2loint(r);
+    const double g = fma(d, c, -(r - kMagic));         // octaves
+    double q = fma(g, 9.6181291076284772e-3, 5.5504108664821580e-2);      // ln(2)^n / n!
+    q = fma(q, g, 0.24022650695910071);
+    q = fma(q, g, 0.69314718055994531);
+    q *= g;
+    const double root = roots[k & (kSpTable - 1)];
+    const int e = k >> 8;
+    const double w = __hiloint2double(__double2hiint(root) + ((e < -1000 ? e + 200 : e) << 20), __double2loint(root));
+    return e < -1000 ? fma(w, q, w) * 6.223015277861142e-61 : fma(w, q, w);     // 2^-200: down to the smallest double
+  }
 };
 
 __device__ __forceinline__ float sp_max(float a, float b) {      // NaN where either is
@@ -103,25 +120,45 @@ struct SpFound {           // the digit, and what lies above it
   int digit;
   int above, in;
 };
+struct SpTop {             // of a CTA: its maximum; the smallest maximum of a lane, of four, of a warp, and how many of them have one
+  float top, low[3];
+  int have[3];
+};
+struct SpWork {
+  union {
+    uint32_t bins[kSpBins];              // members of a bin, or their weight; read by the others
+    unsigned long long all[kSpList];     // the lists of all CTAs; after that
+  };
+  unsigned long long list[kSpList];      // logit << 32 | ~index; read by the others
+  union {
+    struct {
+      unsigned long long sorted[kSpList];
+      double weight[kSpList];
+    };
+    SpHist hist[2];
+  };
+};
 
 template <typename T>
-__global__ void __launch_bounds__(kSpThreads)
+__global__ void __launch_bounds__(kSpThreads, 4)
 sample_kernel(SampleArgs a) {
   extern __shared__ __align__(16) uint8_t sp_smem[];
   __shared__ SpSlot s_slot[2];
-  __shared__ SpHist s_hist[2];
-  __shared__ SpFound s_found;
-  __shared__ double s_warp[kSpWarps], s_block[(kSpMaxPart + kSpBlock - 1) / kSpBlock];
+  __shared__ SpTop s_top, s_tops[kSpWarps];
+  __shared__ SpWork s_work;
+  __shared__ double s_roots[kSpTable];
+  __shared__ double s_warp[kSpWarps], s_block[(kSpMaxPart + kSpBlock - 1) / kSpBlock], s_double;
   __shared__ unsigned long long s_scan_m[kSpWarps];
   __shared__ uint32_t s_scan_c[kSpWarps];
-  __shared__ int s_int;
-  __shared__ float s_tops[kSpWarps];
+  __shared__ SpFound s_found;
+  __shared__ int s_int, s_int2;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   uint32_t rank, cluster;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(cluster));
   const long row = blockIdx.x / cluster;
   const int i0 = min((int)rank * a.per, a.n), cnt = min(a.per, a.n - i0);
+  s_roots[tid] = sp_root(tid);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const T* src = (const T*)a.x + (size_t)row * a.n + i0;
@@ -174,17 +211,56 @@ sample_kernel(SampleArgs a) {
   cp_async_wait<0>();
 #pragma unroll 4
   for (int i = tid; i < words; i += kSpThreads) top = sp_word_max<T>(*reinterpret_cast<const uint4*>(part + head + i * W), top);
+  // The maximum; and of the groups of lanes that have one, the smallest, by the size of the group.
+  float low[3] = {INFINITY, INFINITY, INFINITY};
+  int have[3];
+  {
+    float mine = top;
 #pragma unroll
-  for (int d = 16; d; d >>= 1) top = sp_max(top, __shfl_xor_sync(0xffffffffu, top, d));
-  if (lane == 0) s_tops[warp] = top;
+    for (int g = 0; g < 3; ++g) {          // of a lane, of four, of a warp
+      const bool some = mine > -INFINITY;
+      low[g] = some ? mine : INFINITY;
+      have[g] = __popc(__ballot_sync(0xffffffffu, some)) >> (g == 0 ? 0 : g == 1 ? 2 : 5);
+#pragma unroll
+      for (int d = 16; d; d >>= 1) low[g] = fminf(low[g], __shfl_xor_sync(0xffffffffu, low[g], d));
+      if (g == 0) mine = sp_max(mine, __shfl_xor_sync(0xffffffffu, mine, 1)), mine = sp_max(mine, __shfl_xor_sync(0xffffffffu, mine, 2));
+      if (g == 1) mine = sp_max(mine, __shfl_xor_sync(0xffffffffu, mine, 4)), mine = sp_max(mine, __shfl_xor_sync(0xffffffffu, mine, 8)), mine = sp_max(mine, __shfl_xor_sync(0xffffffffu, mine, 16));
+    }
+    top = mine;
+  }
+  auto join = [&](SpTop& t, int n) {       // over lanes 0 to n - 1
+    if (lane >= n) t = SpTop{-INFINITY, {INFINITY, INFINITY, INFINITY}, {0, 0, 0}};
+#pragma unroll
+    for (int d = 8; d; d >>= 1) {
+      t.top = sp_max(t.top, __shfl_xor_sync(0xffffffffu, t.top, d));
+#pragma unroll
+      for (int g = 0; g < 3; ++g) {
+        t.low[g] = fminf(t.low[g], __shfl_xor_sync(0xffffffffu, t.low[g], d));
+        t.have[g] += __shfl_xor_sync(0xffffffffu, t.have[g], d);
+      }
+    }
+  };
+  if (lane == 0) s_tops[warp] = SpTop{top, {low[0], low[1], low[2]}, {have[0], have[1], have[2]}};
   __syncthreads();
-  top = s_tops[lane & (kSpWarps - 1)];
+  SpTop best = s_tops[lane & (kSpWarps - 1)];
+  join(best, kSpWarps);
+  if (cluster > 1) {
+    if (tid == 0) s_top = best;
+    meet();
+    const uint32_t at = map_to_rank(smem_u32(&s_top), (uint32_t)(lane < (int)cluster ? lane : 0));
+    float v[4];
+    int w[3];
 #pragma unroll
-  for (int d = kSpWarps / 2; d; d >>= 1) top = sp_max(top, __shfl_xor_sync(0xffffffffu, top, d));
-  tell(0.0, 0, top);
-  top = told(lane < (int)cluster ? lane : 0).f;
+    for (int i = 0; i < 4; ++i) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[i]) : "r"(at + 4u * i) : "memory");
 #pragma unroll
-  for (int d = 16; d; d >>= 1) top = sp_max(top, __shfl_xor_sync(0xffffffffu, top, d));
+    for (int i = 0; i < 3; ++i) asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(w[i]) : "r"(at + 16u + 4u * i) : "memory");
+    best = SpTop{v[0], {v[1], v[2], v[3]}, {w[0], w[1], w[2]}};
+    join(best, (int)cluster);
+  }
+  // lanes 16 to 31 have joined nothing
+  top = __shfl_sync(0xffffffffu, best.top, 0);
+#pragma unroll
+  for (int g = 0; g < 3; ++g) best.low[g] = __shfl_sync(0xffffffffu, best.low[g], 0), best.have[g] = __shfl_sync(0xffffffffu, best.have[g], 0);
 
   auto logit = [&](int i) { return Elem<T>::ld(part + i); };
   float* probs = a.probs ? a.probs + (size_t)row * a.n + i0 : nullptr;
@@ -212,7 +288,7 @@ sample_kernel(SampleArgs a) {
     if (probs)
       for (int i = tid; i < cnt; i += kSpThreads) probs[i] = i0 + i == token ? 1.f : 0.f;
   } else {
-    const SpWeight weight(heat, top);
+    const SpWeight weight(s_roots, heat, top);
     // The last member: what is above it by logit, or beside it and not behind it by index, is kept.
     uint32_t last = 0u;
     int last_at = 0x7fffffff;
@@ -229,7 +305,7 @@ sample_kernel(SampleArgs a) {
       int in = 0;
       for (int r = 0; r < kRounds; ++r) {
         const int shift = 24 - 8 * r;
-        SpHist& h = s_hist[r & 1];
+        SpHist& h = s_work.hist[r & 1];
         h.count[tid] = 0u, h.mass[tid] = 0ull;
         __syncthreads();
         for (int i = tid; i < cnt; i += kSpThreads) {
@@ -330,17 +406,306 @@ sample_kernel(SampleArgs a) {
       if (key == last && take >= in) at = last_at;         // of the same logit, what was kept before
       last = key, last_at = at;
     };
-    if (k) select(false, (double)k);
-    if (by_p) {
-      double v = 0.0;
-      for (int i = tid; i < cnt; i += kSpThreads) {
-        const float l = logit(i);
-        if (kept(sp_key(l), i)) v += weight(l);
+
+    // ---- the list: members whose bin lies in [from, to] (bins of width 1 / scale below the maximum; nothing beyond `reach`); with_sums: the sums of blocks of what lies above them.
+    // Returns how many there are, kSpList at most, or -1.
+    const float ftop = top;
+    auto gather = [&](float scale, float reach, int from, int to, bool with_sums) {
+      if (tid == 0) s_int = 0;
+      __syncthreads();
+      for (int b = warp; b < (cnt + kSpBlock - 1) / kSpBlock; b += kSpWarps) {
+        const int end = min((b + 1) * kSpBlock, cnt);
+        double sum = 0.0;
+#pragma unroll 4
+        for (int i = b * kSpBlock + lane; i < end; i += 32) {
+          const float l = logit(i), x = ftop - l, f = x * scale;
+          if (!(x <= reach && f < (float)kSpBins)) continue;
+          const int bin = (int)f;
+          if (bin > to) continue;
+          if (bin >= from) {
+            const int at = atomicAdd(&s_int, 1);
+            if (at < kSpList) s_work.list[at] = (unsigned long long)sp_key(l) << 32 | (uint32_t)~(i0 + i);
+          } else if (with_sums) {
+            sum += weight(l);
+          }
+        }
+        if (with_sums) {
+          sum = warp_total(sum);
+          if (lane == 0) s_block[b] = sum;
+        }
       }
-      tell(cta_sum(v), 0, 0.f);
-      v = 0.0;
-      for (int c = 0; c < (int)cluster; ++c) v += told(c).d;
-      select(true, (double)p * v);
+      __syncthreads();
+      double above = 0.0;
+      if (with_sums)
+        for (int b = 0; b < (cnt + kSpBlock - 1) / kSpBlock; b += 32) above += warp_total(b + lane < (cnt + kSpBlock - 1) / kSpBlock ? s_block[b + lane] : 0.0);
+      tell(above, s_int, 0.f);
+      // everybody copies all lists, in the order of the CTAs
+      const SpSlot o = told(lane < (int)cluster ? lane : 0);
+      const int count = lane < (int)cluster ? min(o.i, kSpList + 1) : 0;
+      int upto = count;
+#pragma unroll
+      for (int d = 1; d < 16; d <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += v;
+      }
+      const int members = __shfl_sync(0xffffffffu, upto, (int)cluster - 1);
+      if (with_sums) {
+        above = 0.0;
+        for (int c = 0; c < (int)cluster; ++c) above += __shfl_sync(0xffffffffu, o.d, c);
+        if (tid == 0) s_double = above;
+      }
+      if (members > kSpList) return -1;
+      for (int i = tid; i - lane < members; i += kSpThreads) {
+        int c = 0, start = 0;
+        for (int r = 0; r < (int)cluster - 1; ++r) {
+          const int v = __shfl_sync(0xffffffffu, upto, r);
+          if (i >= v) c = r + 1, start = v;
+        }
+        if (i < members) {
+          unsigned long long e;
+          asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(e) : "r"(map_to_rank(smem_u32(&s_work.list[i - start]), (uint32_t)c)) : "memory");
+          s_work.all[i] = e;
+        }
+      }
+      __syncthreads();
+      // in order: a member's place is the number of those in front of it
+      for (int i = tid; i < members; i += kSpThreads) {
+        const unsigned long long e = s_work.all[i];
+        int place = 0;
+#pragma unroll 4
+        for (int j = 0; j < members; ++j) place += s_work.all[j] > e;
+        s_work.sorted[place] = e;
+        s_work.weight[place] = weight(sp_logit((uint32_t)(e >> 32)));
+      }
+      __syncthreads();
+      return members;
+    };
+    // Counts or weighs candidates in bins, sums the row (by_weight), and finds the bins in which the goal lies: `goal` in members, or in parts of the sum.
+    // Returns what lies above them, in members (by_weight: at most as many), or -1.
+    double sum_all = 0.0;
+    int from = 0, to = 0, inside = 0;
+    auto look = [&](float scale, float reach, bool by_weight, double goal, double octaves) {
+      for (int i = tid; i < kSpBins; i += kSpThreads) s_work.bins[i] = 0u;
+      if (tid == 0) s_int = kSpBins, s_int2 = -1;
+      __syncthreads();
+      double sum = 0.0;
+      const float fall = -(float)octaves;          // of a bin
+#pragma unroll 4
+      for (int i = tid; i < cnt; i += kSpThreads) {
+        const float l = logit(i), x = ftop - l, f = x * scale;
+        if (by_weight) sum += weight(l);
+        if (!(x <= reach && f < (float)kSpBins)) continue;
+        const int bin = (int)f;
+        uint32_t v = 1u;
+        if (by_weight) {
+          float share;
+          asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(share) : "f"((f - (float)bin) * fall));
+          v = (uint32_t)(share * 131072.f + 0.5f);       // 17 bits: 38400 members of a part stay below 2^33, so parts that long are found digit by digit
+        }
+        atomicAdd(&s_work.bins[bin], v);
+      }
+      if (by_weight) {
+        tell(cta_sum(sum), 0, 0.f);
+        for (int c = 0; c < (int)cluster; ++c) sum_all += told(c).d;
+        goal *= sum_all;
+      } else {
+        meet();
+      }
+      // four bins a thread, over the cluster
+      uint32_t v[4] = {0u, 0u, 0u, 0u};
+      double m[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll 4
+      for (int c = 0; c < (int)cluster; ++c) {
+        uint32_t w[4];
+        asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(map_to_rank(smem_u32(&s_work.bins[4 * tid]), (uint32_t)c)) : "memory");
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (by_weight) m[j] += (double)w[j];
+          else v[j] += w[j];
+        }
+      }
+      if (by_weight) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v[j] = (uint32_t)(m[j] * (1.0 / 131072) * 1.04) + (m[j] > 0.0);          // a bin is 0.04 octaves wide at most: never fewer than there are
+          m[j] *= exp2(-octaves * (4 * tid + j)) * (1.0 / 131072);
+        }
+      }
+      const uint32_t c4 = v[0] + v[1] + v[2] + v[3];
+      const double m4 = m[0] + m[1] + m[2] + m[3];
+      uint32_t cc = c4;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xffffffffu, cc, d);
+        if (lane >= d) cc += o;
+      }
+      double cm = by_weight ? warp_scan(m4, lane) : 0.0;
+      __syncthreads();
+      if (lane == 31) s_scan_c[warp] = cc, s_warp[warp] = cm;
+      __syncthreads();
+      for (int w = 0; w < warp; ++w) cc += s_scan_c[w], cm += s_warp[w];
+      uint32_t before = cc - c4;
+      double before_m = cm - m4;
+      const double slack = by_weight ? 4e-6 * sum_all : 0.0;          // 17 bits a member, and the difference of the two forms of its weight
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int bin = 4 * tid + j;
+        if (v[j] > 0u) {
+          if (by_weight) {
+            if (before_m + m[j] >= goal - slack) atomicMin(&s_int, bin);
+            if (before_m < goal + slack) atomicMax(&s_int2, bin);
+          } else if ((double)before < goal && (double)(before + v[j]) >= goal) {
+            s_int = s_int2 = bin;
+          }
+        }
+        before += v[j], before_m += m[j];
+      }
+      __syncthreads();
+      from = s_int, to = s_int2;
+      __syncthreads();
+      if (to < 0) return -1;
+      from = min(from, to);
+      before = cc - c4;
+      if (tid == 0) s_int2 = 0;
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int bin = 4 * tid + j;
+        if (bin == from) s_int = (int)before;
+        if (bin >= from && bin <= to && v[j]) atomicAdd(&s_int2, (int)v[j]);
+        before += v[j];
+      }
+      __syncthreads();
+      const int above = s_int;
+      inside = s_int2;
+      __syncthreads();
+      return above;
+    };
+
+    bool whole = false;                    // the list holds all that is kept
+    bool summed = false;                   // s_block holds the sums of what is kept
+    int members = -1, cut = 0;
+    bool found_k = !k, found_p = !by_p;
+    double total = 0.0;
+    if (k && k <= kSpList) {
+      const int g = k <= best.have[2] ? 2 : k <= best.have[1] ? 1 : 0;
+      const float reach = ftop - best.low[g], scale = reach > 0.f ? 1023.9f / reach : 0.f;
+      if (k <= best.have[g] && scale < FLT_MAX && reach < FLT_MAX) {
+        if (g == 2 || a.n <= kSpList) members = gather(scale, reach, 0, kSpBins - 1, false);
+        whole = members > 0;
+        if (!whole) {
+          const int above = look(scale, reach, false, (double)k, 0.0);
+          if (above >= 0 && above + inside <= kSpList) {
+            members = gather(scale, reach, 0, to, false);
+            whole = members > 0;
+          } else if (above >= 0 && inside <= kSpList) {
+            members = gather(scale, reach, from, to, false);
+            if (members >= k - above && k > above) {
+              const unsigned long long e = s_work.sorted[k - above - 1];
+              last = (uint32_t)(e >> 32), last_at = (int)~(uint32_t)e;
+              found_k = true;
+            }
+          }
+        }
+      }
+      if (whole) members = min(members, k);
+    } else if (!k && by_p) {
+      // 1 - p is exact; the total is 1 at least
+      const double octaves = (log2((double)a.n) - log2(1.0 - (double)p)) * 1.0001;
+      const float reach = (float)(octaves / weight.c), scale = (float)(kSpBins * weight.c / octaves);
+      if (a.per <= 32767 && reach < FLT_MAX && scale < FLT_MAX && scale > 0.f) {
+        const int above = look(scale, reach, true, (double)p, octaves / kSpBins);
+        const double goal = (double)p * sum_all;
+        if (above >= 0 && above + inside <= kSpList) {
+          members = gather(scale, reach, 0, to, false);
+          whole = members > 0;
+        } else if (above >= 0) {
+          members = gather(scale, reach, from, to, true);
+          if (members > 0) {
+            if (warp == 0) {
+              double before = s_double;
+              int j = 0;
+              for (int i = 0; i < members; i += 32) {
+                const double w = i + lane < members ? s_work.weight[i + lane] : 0.0, cum = before + warp_scan(w, lane);
+                const unsigned in = __ballot_sync(0xffffffffu, i + lane < members && cum - w < goal);
+                j += __popc(in);
+                before = __shfl_sync(0xffffffffu, cum, 31);
+              }
+              if (lane == 0) s_int = max(j, 1);
+            }
+            __syncthreads();
+            cut = s_int;
+            const unsigned long long e = s_work.sorted[cut - 1];
+            last = (uint32_t)(e >> 32), last_at = (int)~(uint32_t)e;
+            found_p = true;
+            summed = !by_m;
+          }
+        }
+      }
+    }
+    if (whole) {
+      // all from the list: what is kept of it, and their total, in order
+      if (warp == 0) {
+        double want = INFINITY;
+        if (by_p) {
+          double sum = 0.0;
+          if (k)
+            for (int i = 0; i < members; i += 32) sum += warp_total(i + lane < members ? s_work.weight[i + lane] : 0.0);
+          else sum = sum_all;
+          want = (double)p * sum;
+        }
+        double before = 0.0;
+        int j = 0;
+        for (int i = 0; i < members; i += 32) {
+          const double w = i + lane < members ? s_work.weight[i + lane] : 0.0, cum = before + warp_scan(w, lane);
+          const bool in = i + lane < members && cum - w < want && !(by_m && w < (double)m);
+          const unsigned b = __ballot_sync(0xffffffffu, in || (i == 0 && lane == 0));
+          const int n = b == 0xffffffffu ? 32 : __ffs(~b) - 1;
+          j += n;
+          before = n > 0 ? __shfl_sync(0xffffffffu, cum, n - 1) : before;
+          if (n < 32) break;
+        }
+        if (lane == 0) s_int = j, s_double = before;
+      }
+      __syncthreads();
+      cut = s_int, total = s_double;
+      const unsigned long long e = s_work.sorted[cut - 1];
+      last = (uint32_t)(e >> 32), last_at = (int)~(uint32_t)e;
+      __syncthreads();
+      if (a.tokens) {
+        // by index: a class that the running sum passes the goal with, the first of them; or the last that weighs anything
+        const double goal = fmax((double)a.u[row] * total, 0.0);
+        if (tid == 0) s_int = 0x7fffffff, s_int2 = -1;
+        __syncthreads();
+        for (int i = tid; i < cut; i += kSpThreads) {
+          const uint32_t at = (uint32_t)s_work.sorted[i];          // the larger, the lower the index
+          const double w = s_work.weight[i];
+          double before = 0.0;
+#pragma unroll 4
+          for (int j = 0; j < cut; ++j)
+            if ((uint32_t)s_work.sorted[j] > at) before += s_work.weight[j];
+          if (w > 0.0) {
+            if (before + w > goal) atomicMin(&s_int, (int)~at);
+            atomicMax(&s_int2, (int)~at);
+          }
+        }
+        __syncthreads();
+        token = s_int != 0x7fffffff ? s_int : s_int2;
+      }
+    } else {
+      if (!found_k) select(false, (double)k);
+      if (!found_p) {
+        double v = 0.0;
+        for (int i = tid; i < cnt; i += kSpThreads) {
+          const float l = logit(i);
+          if (kept(sp_key(l), i)) v += weight(l);
+        }
+        tell(cta_sum(v), 0, 0.f);
+        v = 0.0;
+        for (int c = 0; c < (int)cluster; ++c) v += told(c).d;
+        select(true, (double)p * v);
+      }
     }
     const bool all = !k && !by_p;
     auto mass = [&](int i) {               // what class i adds to the sum
@@ -350,20 +715,33 @@ sample_kernel(SampleArgs a) {
       return by_m && w < (double)m ? 0.0 : w;
     };
     // ---- sums of blocks, the total, and the block in which the running sum passes its goal
+    if (!whole) {
     const int blocks = (cnt + kSpBlock - 1) / kSpBlock;
-    for (int b = warp; b < blocks; b += kSpWarps) {
-      const int end = min((b + 1) * kSpBlock, cnt);
-      double s = 0.0;
+    if (summed) {
+      // those of the list that are kept join their blocks, in order
+      for (int b = tid; b < blocks; b += kSpThreads) {
+        double s = s_block[b];
+        for (int j = 0; j < cut; ++j) {
+          const int at = (int)~(uint32_t)s_work.sorted[j] - i0;
+          if (at >= 0 && at < cnt && at / kSpBlock == b) s += s_work.weight[j];
+        }
+        s_block[b] = s;
+      }
+    } else {
+      for (int b = warp; b < blocks; b += kSpWarps) {
+        const int end = min((b + 1) * kSpBlock, cnt);
+        double s = 0.0;
 #pragma unroll 4
-      for (int i = b * kSpBlock + lane; i < end; i += 32) s += mass(i);
-      s = warp_total(s);
-      if (lane == 0) s_block[b] = s;
+        for (int i = b * kSpBlock + lane; i < end; i += 32) s += mass(i);
+        s = warp_total(s);
+        if (lane == 0) s_block[b] = s;
+      }
     }
     __syncthreads();
     double sum = 0.0;
     for (int b = 0; b < blocks; b += 32) sum += warp_total(b + lane < blocks ? s_block[b + lane] : 0.0);
     tell(sum, 0, 0.f);
-    double before = 0.0, total = 0.0;
+    double before = 0.0;
     int last_one = 0;                      // the last CTA that has any weight
     for (int c = 0; c < (int)cluster; ++c) {
       const double o = told(c).d;
@@ -395,6 +773,7 @@ sample_kernel(SampleArgs a) {
           start = __shfl_sync(0xffffffffu, cum, 31);
         }
       }
+    }
     }
     if (probs) {
       const double scale = 1.0 / total;
