@@ -9,12 +9,12 @@
 // with the sum, half of what it takes without a table.
 //
 // A row is kept in the shared memory of a CTA, or of a cluster of them, which speak in turns (meet).  The last member is looked for among few:
-//   k: as many groups of lanes as k have a maximum at or above the smallest of those maxima, so the k-th largest lies there too.  Groups are as large as k allows (a warp, four
-//   lanes, a lane): 64 warps of 2000 logits each leave about 250 candidates.  Where they are too many, they are counted in 1024 bins, equally wide in the logit.
+//   k: a logit that k of 512 groups of lanes reach with their largest: k-th and better lie at or above it, and little else does (the smallest maximum of 64 warps left 270 candidates
+//   of 128001 for k = 50, this leaves 60).  Where equal logits make too many of them, candidates are counted in 1024 bins, equally wide in the logit.
 //   p: a class weighs at least (1 - p) / n of the total if it is kept (those behind it would otherwise weigh less than 1 - p), which bounds its logit.  Candidates are weighed in 1024
 //   bins, in the pass that sums the total: a bin is 0.04 octaves wide at most, so a member's share of its bin's largest weight, 17 bits, goes into a 32-bit sum.
 // What lies in the bin of the goal, or everything down to it if that is little, is gathered in a list, ordered by counting, and weighed exactly.
-// Otherwise (thousands of equal logits, k above the list's length, no finite bound) it is found digit by digit of the logit's bits: the CTAs count (and weigh) what
+// Otherwise (thousands of equal logits, k above 256, no finite bound) it is found digit by digit of the logit's bits: the CTAs count (and weigh) what
 // has the digits found so far by its next one, read each other's counts, and each takes the digit in which the goal lies.
 #pragma once
 #include <float.h>
@@ -32,7 +32,7 @@ constexpr int kSpMaxCluster = 16, kSpMaxPart = 38400;
 constexpr int kSpBlock = 512;            // elements of a block whose sum is kept
 constexpr int kSpMost = kSpMaxCluster * kSpMaxPart;
 constexpr int kSpBins = 1024, kSpList = 512;
-constexpr int kSpTable = 256;
+constexpr int kSpTable = 16;
 
 struct SampleArgs {
   const void* x;           // [rows][n]
@@ -46,14 +46,21 @@ struct SampleArgs {
   int n, per;
 };
 
-// 2^(j / 256) by the series of exp up to its 12th term.
-__device__ __forceinline__ double sp_root(int j) {
-  const double g = j * (0.69314718055994531 / kSpTable);
-  double p = 1.0;
-#pragma unroll
-  for (int n = 16; n >= 1; --n) p = fma(p, g * (1.0 / n), 1.0);
-  return p;
+// 2^(j / 16) by the series of exp.
+struct SpRoots {
+  double v[kSpTable];
+};
+constexpr SpRoots sp_roots() {
+  SpRoots r{};
+  for (int j = 0; j < kSpTable; ++j) {
+    const double g = j * (0.69314718055994531 / kSpTable);
+    double p = 1.0;
+    for (int n = 20; n >= 1; --n) p = 1.0 + p * g / n;
+    r.v[j] = p;
+  }
+  return r;
 }
+static __device__ const SpRoots g_sp_roots = sp_roots();
 
 // An integer that orders like the float; both zeros are one.
 __device__ __forceinline__ uint32_t sp_key(float l) {
@@ -62,30 +69,46 @@ __device__ __forceinline__ uint32_t sp_key(float l) {
 }
 __device__ __forceinline__ float sp_logit(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 
+// v, or 0: without a branch round what v is made of.
+__device__ __forceinline__ double sp_pick(bool keep, double v) {
+  double r;
+  asm("{\n .reg .pred p;\n setp.ne.u32 p, %2, 0;\n selp.f64 %0, %1, 0d0000000000000000, p;\n}" : "=d"(r) : "d"(v), "r"((int)keep));
+  return r;
+}
+
+// A float as a double, by its bits: the conversion instruction takes 8 clocks a warp of a scheduler, fp64 arithmetic 2.  What is below 2^-126 comes out between 2^-127 and
+// that, in order.
+__device__ __forceinline__ double sp_wide(float l) {
+  const int b = __float_as_int(l);
+  return __hiloint2double(((b >> 3) & (int)0x8fffffff) + 0x38000000, b << 29);
+}
+
+// The weight of a logit.  Below 2^-1000, which no sum of 2^20 of them brings near any u that is not 0, it is 0; whether it would be more is asked for where u is 0 (live).
+// There is neither a branch nor a call in it: with a call for the rare case a row of 128001 took 138 clocks a warp and 32 logits, its elements one after the other.
+// The table has as many entries as 16 lanes read without a conflict: one of 256 took 15 clocks a lookup, and saved two fp64 operations of 2.
 struct SpWeight {
   const double* roots;
   double c, top;
-  uint32_t far;            // upper half of the difference behind which nothing is left; as bits, that of a negative number grows with its size
-  __device__ __forceinline__ SpWeight(const double* table, float heat, float top_)
-      : roots(table), c(1.4426950408889634 / (double)heat), top((double)top_) {
-    far = (uint32_t)__double2hiint(fmax(-1080.0 / c, -DBL_MAX));
+  uint32_t near;           // upper half of the difference from which on the weight is 0; as bits, that of a negative number grows with its size
+  __device__ __forceinline__ SpWeight(const double* table, float heat, float top_) : roots(table), c(1.4426950408889634 / (double)heat), top(sp_wide(top_)) {
+    near = (uint32_t)__double2hiint(fmax(-1000.0 / c, -DBL_MAX));
   }
   __device__ __forceinline__ double operator()(float l) const {
-    constexpr double kMagic = 26388279066624.0;        // 1.5 * 2^44: the sum's last place is 1 / 256
-    const double d = (double)l - top;
-    if ((uint32_t)__double2hiint(d) > far) return 0.0; // also -inf at any temperature (0 * inf)
-    const double r = fma(d, c, kMagic);
+    constexpr double kMagic = 6755399441055744.0 / kSpTable;        // 1.5 * 2^52 / 16: the sum's last place is 1 / 16
+    const double d = sp_wide(l) - top, r = fma(d, c, kMagic);
     const int k = __double2loint(r);
-    const double g = fma(d, c, -(r - kMagic));         // octaves
-    double q = fma(g, 9.6181291076284772e-3, 5.5504108664821580e-2);      // ln(2)^n / n!
+    const double g = fma(d, c, -(r - kMagic));         // octaves, up to 1 / 32
+    double q = fma(g, 1.5403530393381609e-4, 1.3333558146428443e-3);      // ln(2)^n / n!: what is left out is 2^-51
+    q = fma(q, g, 9.6181291076284772e-3);
+    q = fma(q, g, 5.5504108664821580e-2);
     q = fma(q, g, 0.24022650695910071);
     q = fma(q, g, 0.69314718055994531);
     q *= g;
     const double root = roots[k & (kSpTable - 1)];
-    const int e = k >> 8;
-    const double w = __hiloint2double(__double2hiint(root) + ((e < -1000 ? e + 200 : e) << 20), __double2loint(root));
-    return e < -1000 ? fma(w, q, w) * 6.223015277861142e-61 : fma(w, q, w);     // 2^-200: down to the smallest double
+    const double w = __hiloint2double(__double2hiint(root) + ((k & ~(kSpTable - 1)) << (20 - 4)), __double2loint(root));
+    return sp_pick((uint32_t)__double2hiint(d) <= near && l > -INFINITY, fma(w, q, w));
   }
+  __device__ __forceinline__ bool live(float l) const { return l > -INFINITY && (sp_wide(l) - top) * c > -1075.0; }      // half of the smallest double
 };
 
 __device__ __forceinline__ float sp_max(float a, float b) {      // NaN where either is
@@ -110,7 +133,6 @@ __device__ __forceinline__ float sp_word_max(uint4 w, float top) {
 struct SpSlot {            // what a CTA tells the others
   double d;
   int i;
-  float f;
 };
 struct SpHist {            // by digit: members, and their weight in units of 2^-43 (at most 614400 of them, each at most 1)
   uint32_t count[256];
@@ -120,16 +142,18 @@ struct SpFound {           // the digit, and what lies above it
   int digit;
   int above, in;
 };
-struct SpTop {             // of a CTA: its maximum; the smallest maximum of a lane, of four, of a warp, and how many of them have one
-  float top, low[3];
-  int have[3];
+struct SpBorder {          // of a CTA's bins: the first in which the goal may lie and what lies before it, the last and what lies up to its end
+  int from, before, to, end;
 };
-struct SpWork {
+struct alignas(16) SpWork {              // bins are read four at a time
   union {
     uint32_t bins[kSpBins];              // members of a bin, or their weight; read by the others
-    unsigned long long all[kSpList];     // the lists of all CTAs; after that
+    unsigned long long all[2 * kSpList]; // the lists of all CTAs, as many places each; after that
   };
-  unsigned long long list[kSpList];      // logit << 32 | ~index; read by the others
+  union {
+    unsigned long long list[kSpList];    // logit << 32 | ~index; read by the others
+    uint32_t groups[kSpThreads];         // maxima of groups of lanes; read by the others, before that
+  };
   union {
     struct {
       unsigned long long sorted[kSpList];
@@ -142,15 +166,18 @@ struct SpWork {
 template <typename T>
 __global__ void __launch_bounds__(kSpThreads, 4)
 sample_kernel(SampleArgs a) {
+  constexpr int W = 16 / (int)sizeof(T), kBlockWords = kSpBlock / W;
   extern __shared__ __align__(16) uint8_t sp_smem[];
   __shared__ SpSlot s_slot[2];
-  __shared__ SpTop s_top, s_tops[kSpWarps];
-  __shared__ SpWork s_work;
+  __shared__ uint32_t s_top, s_tops[kSpWarps];
+  __shared__ __align__(16) SpWork s_work;
   __shared__ double s_roots[kSpTable];
-  __shared__ double s_warp[kSpWarps], s_block[(kSpMaxPart + kSpBlock - 1) / kSpBlock], s_double;
+  __shared__ double s_warp[kSpWarps], s_block[kSpMaxPart / kSpBlock + 2], s_double;
   __shared__ unsigned long long s_scan_m[kSpWarps];
   __shared__ uint32_t s_scan_c[kSpWarps];
   __shared__ SpFound s_found;
+  __shared__ __align__(16) SpBorder s_border;
+  __shared__ int s_counts[kSpMaxCluster];
   __shared__ int s_int, s_int2;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   uint32_t rank, cluster;
@@ -158,7 +185,7 @@ sample_kernel(SampleArgs a) {
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(cluster));
   const long row = blockIdx.x / cluster;
   const int i0 = min((int)rank * a.per, a.n), cnt = min(a.per, a.n - i0);
-  s_roots[tid] = sp_root(tid);
+  const double root = g_sp_roots.v[tid & (kSpTable - 1)];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const T* src = (const T*)a.x + (size_t)row * a.n + i0;
@@ -170,17 +197,23 @@ sample_kernel(SampleArgs a) {
     if (cluster > 1) asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
     else __syncthreads();
   };
-  auto tell = [&](double d, int i, float f) {            // by thread 0; all threads meet
-    if (tid == 0) s_slot[turn & 1] = SpSlot{d, i, f};
+  auto tell = [&](double d, int i) {                     // by thread 0; all threads meet
+    if (tid == 0) s_slot[turn & 1] = SpSlot{d, i};
     meet();
     ++turn;
   };
   auto told = [&](int c) {                               // what CTA c told last
     SpSlot s;
     const uint32_t at = map_to_rank(smem_u32(&s_slot[(turn - 1) & 1]), (uint32_t)c);
-    asm volatile("ld.shared::cluster.v2.b32 {%0, %1}, [%2];" : "=r"(s.i), "=r"(*reinterpret_cast<int*>(&s.f)) : "r"(at + 8u) : "memory");
+    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(s.i) : "r"(at + 8u) : "memory");
     asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(s.d) : "r"(at) : "memory");
     return s;
+  };
+  auto told_sum = [&]() {                                // over the CTAs, in order
+    const double d = told(lane < (int)cluster ? lane : 0).d;
+    double sum = 0.0;
+    for (int c = 0; c < (int)cluster; ++c) sum += __shfl_sync(0xffffffffu, d, c);
+    return sum;
   };
   auto cta_sum = [&](double v) {                         // of the CTA's threads, in fixed order
     v = warp_total(v);
@@ -193,74 +226,47 @@ sample_kernel(SampleArgs a) {
     return sum;
   };
 
-  // ---- the row, at its own offset within a 16-byte word, and its maximum
-  constexpr int W = 16 / (int)sizeof(T);
-  const int skew = (int)(((uintptr_t)src & 15) / sizeof(T));
+  // ---- the row, at its own offset within a 16-byte word (what else is in its first and its last word is masked), and its maximum
+  const int skew = (int)(((uintptr_t)src & 15) / sizeof(T)), all_words = cnt > 0 ? (skew + cnt + W - 1) / W : 0;
+  const uint4* words = reinterpret_cast<const uint4*>(sp_smem);
   T* part = reinterpret_cast<T*>(sp_smem) + skew;
-  const int head = min(cnt, skew ? W - skew : 0), words = (cnt - head) / W, tail = head + words * W;
+  const int head = min(cnt, skew ? W - skew : 0), whole_words = (cnt - head) / W, tail = head + whole_words * W;
 #pragma unroll 4
-  for (int i = tid; i < words; i += kSpThreads)
+  for (int i = tid; i < whole_words; i += kSpThreads)
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(part + head + i * W)), "l"(src + head + (size_t)i * W) : "memory");
   cp_async_commit();
   float top = -INFINITY;
   if (tid < head) part[tid] = src[tid], top = Elem<T>::ld(part + tid);
   if (tid < cnt - tail) part[tail + tid] = src[tail + tid], top = sp_max(top, Elem<T>::ld(part + tail + tid));
+  if (tid < skew && cnt > 0) Elem<T>::st(part - 1 - tid, -INFINITY);
+  if (tid < all_words * W - skew - cnt) Elem<T>::st(part + cnt + tid, -INFINITY);
   float heat = a.heat ? a.heat[row] : 1.f;
   int k = a.top_k ? a.top_k[row] : 0;
   const float p = a.top_p ? a.top_p[row] : 1.f, m = a.min_p ? a.min_p[row] : 0.f;
+  const float u = a.tokens ? a.u[row] : 0.f;
+  if (tid < kSpTable) s_roots[tid] = root;
   cp_async_wait<0>();
 #pragma unroll 4
-  for (int i = tid; i < words; i += kSpThreads) top = sp_word_max<T>(*reinterpret_cast<const uint4*>(part + head + i * W), top);
-  // The maximum; and of the groups of lanes that have one, the smallest, by the size of the group.
-  float low[3] = {INFINITY, INFINITY, INFINITY};
-  int have[3];
-  {
-    float mine = top;
-#pragma unroll
-    for (int g = 0; g < 3; ++g) {          // of a lane, of four, of a warp
-      const bool some = mine > -INFINITY;
-      low[g] = some ? mine : INFINITY;
-      have[g] = __popc(__ballot_sync(0xffffffffu, some)) >> (g == 0 ? 0 : g == 1 ? 2 : 5);
-#pragma unroll
-      for (int d = 16; d; d >>= 1) low[g] = fminf(low[g], __shfl_xor_sync(0xffffffffu, low[g], d));
-      if (g == 0) mine = sp_max(mine, __shfl_xor_sync(0xffffffffu, mine, 1)), mine = sp_max(mine, __shfl_xor_sync(0xffffffffu, mine, 2));
-      if (g == 1) mine = sp_max(mine, __shfl_xor_sync(0xffffffffu, mine, 4)), mine = sp_max(mine, __shfl_xor_sync(0xffffffffu, mine, 8)), mine = sp_max(mine, __shfl_xor_sync(0xffffffffu, mine, 16));
-    }
-    top = mine;
+  for (int i = tid; i < whole_words; i += kSpThreads) top = sp_word_max<T>(*reinterpret_cast<const uint4*>(part + head + i * W), top);
+  // The maximum, as its key (NaN above everything), and the maxima of groups of lanes (where a row may ask for its k largest): up to 512 over the cluster.
+  uint32_t peak = sp_key(top);
+  const int log_group = cluster <= 2 ? 0 : 30 - __clz(cluster), groups = kSpThreads >> log_group;
+  if (a.top_k) {
+    uint32_t g = peak;
+    for (int d = 1; d < 1 << log_group; d *= 2) g = max(g, __shfl_xor_sync(0xffffffffu, g, d));
+    if ((tid & ((1 << log_group) - 1)) == 0) s_work.groups[tid >> log_group] = g;
   }
-  auto join = [&](SpTop& t, int n) {       // over lanes 0 to n - 1
-    if (lane >= n) t = SpTop{-INFINITY, {INFINITY, INFINITY, INFINITY}, {0, 0, 0}};
-#pragma unroll
-    for (int d = 8; d; d >>= 1) {
-      t.top = sp_max(t.top, __shfl_xor_sync(0xffffffffu, t.top, d));
-#pragma unroll
-      for (int g = 0; g < 3; ++g) {
-        t.low[g] = fminf(t.low[g], __shfl_xor_sync(0xffffffffu, t.low[g], d));
-        t.have[g] += __shfl_xor_sync(0xffffffffu, t.have[g], d);
-      }
-    }
-  };
-  if (lane == 0) s_tops[warp] = SpTop{top, {low[0], low[1], low[2]}, {have[0], have[1], have[2]}};
+  peak = __reduce_max_sync(0xffffffffu, peak);
+  if (lane == 0) s_tops[warp] = peak;
   __syncthreads();
-  SpTop best = s_tops[lane & (kSpWarps - 1)];
-  join(best, kSpWarps);
+  peak = __reduce_max_sync(0xffffffffu, s_tops[lane & (kSpWarps - 1)]);
   if (cluster > 1) {
-    if (tid == 0) s_top = best;
+    if (tid == 0) s_top = peak;
     meet();
-    const uint32_t at = map_to_rank(smem_u32(&s_top), (uint32_t)(lane < (int)cluster ? lane : 0));
-    float v[4];
-    int w[3];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[i]) : "r"(at + 4u * i) : "memory");
-#pragma unroll
-    for (int i = 0; i < 3; ++i) asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(w[i]) : "r"(at + 16u + 4u * i) : "memory");
-    best = SpTop{v[0], {v[1], v[2], v[3]}, {w[0], w[1], w[2]}};
-    join(best, (int)cluster);
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(peak) : "r"(map_to_rank(smem_u32(&s_top), (uint32_t)(lane < (int)cluster ? lane : 0))) : "memory");
+    peak = __reduce_max_sync(0xffffffffu, peak);
   }
-  // lanes 16 to 31 have joined nothing
-  top = __shfl_sync(0xffffffffu, best.top, 0);
-#pragma unroll
-  for (int g = 0; g < 3; ++g) best.low[g] = __shfl_sync(0xffffffffu, best.low[g], 0), best.have[g] = __shfl_sync(0xffffffffu, best.have[g], 0);
+  top = sp_logit(peak);
 
   auto logit = [&](int i) { return Elem<T>::ld(part + i); };
   float* probs = a.probs ? a.probs + (size_t)row * a.n + i0 : nullptr;
@@ -283,16 +289,23 @@ sample_kernel(SampleArgs a) {
     __syncthreads();
     if (lane == 0) atomicMin(&s_int, at);
     __syncthreads();
-    tell(0.0, s_int, 0.f);
+    tell(0.0, s_int);
     token = __reduce_min_sync(0xffffffffu, told(lane < (int)cluster ? lane : 0).i);
     if (probs)
       for (int i = tid; i < cnt; i += kSpThreads) probs[i] = i0 + i == token ? 1.f : 0.f;
   } else {
+    if (heat < 1e-20f && fabsf(top) < 1e-10f) {
+      // So cold that logits below 2^-126 matter, which sp_wide does not tell apart: all of them times 2^64, and the temperature.  What overflows weighs nothing either way.
+      for (int i = tid; i < cnt; i += kSpThreads) Elem<T>::st(part + i, logit(i) * 0x1p64f);
+      heat *= 0x1p64f, top *= 0x1p64f;
+      __syncthreads();
+    }
     const SpWeight weight(s_roots, heat, top);
+    const int blocks = (all_words + kBlockWords - 1) / kBlockWords;
     // The last member: what is above it by logit, or beside it and not behind it by index, is kept.
-    uint32_t last = 0u;
+    float last = -INFINITY;
     int last_at = 0x7fffffff;
-    auto kept = [&](uint32_t key, int i) { return key > last || (key == last && i0 + i <= last_at); };
+    auto kept = [&](float l, int i) { return l > last || (l == last && i0 + i <= last_at); };
 
     // Of what is kept, the new last member: by count (the goal-th), or by weight (the last before which there is less than goal).
     auto select = [&](bool by_weight, double goal) {
@@ -303,6 +316,7 @@ sample_kernel(SampleArgs a) {
       const double unit = 8796093022208.0;                 // 2^43
       const unsigned long long goal_m = (unsigned long long)fmin(ceil(goal * (by_weight ? unit : 1.0)), 1.8e19);
       int in = 0;
+#pragma unroll 1
       for (int r = 0; r < kRounds; ++r) {
         const int shift = 24 - 8 * r;
         SpHist& h = s_work.hist[r & 1];
@@ -311,7 +325,7 @@ sample_kernel(SampleArgs a) {
         for (int i = tid; i < cnt; i += kSpThreads) {
           const float l = logit(i);
           const uint32_t key = sp_key(l);
-          if ((r == 0 || key >> (shift + 8) == prefix) && kept(key, i)) {
+          if ((r == 0 || key >> (shift + 8) == prefix) && kept(l, i)) {
             const int d = key >> shift & 255;
             atomicAdd(&h.count[d], 1u);
             if (by_weight) atomicAdd(&h.mass[d], (unsigned long long)__double2ull_rn(weight(l) * unit));
@@ -354,18 +368,17 @@ sample_kernel(SampleArgs a) {
       // Every one that is left has the same logit: as many of them as the goal asks for, the lower indices first.
       uint32_t key = kRounds == 4 ? prefix : prefix << 16;
       if (kRounds == 2 && !(key & 0x80000000u)) key |= 0xffffu;       // a negative float's bits are turned round
+      const float border = sp_logit(key);
       int take;
       if (by_weight) {
         double v = 0.0;                                    // what lies above, exactly
         for (int i = tid; i < cnt; i += kSpThreads) {
           const float l = logit(i);
-          const uint32_t o = sp_key(l);
-          if (o > key && kept(o, i)) v += weight(l);
+          if (l > border && kept(l, i)) v += weight(l);
         }
-        tell(cta_sum(v), 0, 0.f);
-        v = 0.0;
-        for (int c = 0; c < (int)cluster; ++c) v += told(c).d;
-        const double w = weight(sp_logit(key));
+        tell(cta_sum(v), 0);
+        v = told_sum();
+        const double w = weight(border);
         take = w > 0.0 ? (int)fmin(fmax(ceil((goal - v) / w), 1.0), (double)in) : in;
       } else {
         take = (int)goal - (int)above;
@@ -373,14 +386,14 @@ sample_kernel(SampleArgs a) {
       int at = 0x7fffffff;
       if (take < in) {
         int c = 0;
-        for (int i = tid; i < cnt; i += kSpThreads) c += sp_key(logit(i)) == key && kept(key, i);
+        for (int i = tid; i < cnt; i += kSpThreads) c += logit(i) == border && kept(border, i);
         c = __reduce_add_sync(0xffffffffu, c);
         if (tid == 0) s_int = 0;
         __syncthreads();
         if (lane == 0) atomicAdd(&s_int, c);
         __syncthreads();
         const int have = s_int;
-        tell(0.0, have, 0.f);
+        tell(0.0, have);
         int before = 0;
         for (int c2 = 0; c2 < (int)rank; ++c2) before += told(c2).i;
         // the CTA that has the take-th looks for its index
@@ -389,7 +402,7 @@ sample_kernel(SampleArgs a) {
         if (before < take && take <= before + have && warp == 0) {
           int left = take - before;
           for (int i = lane; i - lane < cnt; i += 32) {
-            const unsigned b = __ballot_sync(0xffffffffu, i < cnt && sp_key(logit(min(i, cnt - 1))) == key && kept(key, i));
+            const unsigned b = __ballot_sync(0xffffffffu, i < cnt && logit(min(i, cnt - 1)) == border && kept(border, i));
             if (__popc(b) >= left) {
               const int j = __fns(b, 0, left);
               if (lane == 0) s_int = i0 + i + j;
@@ -399,34 +412,43 @@ sample_kernel(SampleArgs a) {
           }
         }
         __syncthreads();
-        tell(0.0, s_int, 0.f);
+        tell(0.0, s_int);
         at = 0;
         for (int c2 = 0; c2 < (int)cluster; ++c2) at = max(at, told(c2).i);      // the others say 0
       }
-      if (key == last && take >= in) at = last_at;         // of the same logit, what was kept before
-      last = key, last_at = at;
+      if (border == last && take >= in) at = last_at;      // of the same logit, what was kept before
+      last = border, last_at = at;
     };
 
-    // ---- the list: members whose bin lies in [from, to] (bins of width 1 / scale below the maximum; nothing beyond `reach`); with_sums: the sums of blocks of what lies above them.
-    // Returns how many there are, kSpList at most, or -1.
-    const float ftop = top;
-    auto gather = [&](float scale, float reach, int from, int to, bool with_sums) {
+    // ---- few candidates.  Bins of width 1 / scale in the logit, below the maximum; what lies beyond the last of them is no candidate.
+    float scale = 0.f;
+    double octaves = 0.0;                  // of all bins, for weights
+    // The list: members whose bin lies in [from, to], in order, with their weights; with_sums: the sums of blocks of what lies above them, and in s_double that of the row.
+    // Returns how many there are, or -1: more than the list has room for.
+    auto gather = [&](int from, int to, bool with_sums) {
+      const float f0 = (float)from, f1 = (float)(to + 1);
       if (tid == 0) s_int = 0;
       __syncthreads();
-      for (int b = warp; b < (cnt + kSpBlock - 1) / kSpBlock; b += kSpWarps) {
-        const int end = min((b + 1) * kSpBlock, cnt);
+#pragma unroll 1
+      for (int b = warp; b < blocks; b += kSpWarps) {
         double sum = 0.0;
-#pragma unroll 4
-        for (int i = b * kSpBlock + lane; i < end; i += 32) {
-          const float l = logit(i), x = ftop - l, f = x * scale;
-          if (!(x <= reach && f < (float)kSpBins)) continue;
-          const int bin = (int)f;
-          if (bin > to) continue;
-          if (bin >= from) {
-            const int at = atomicAdd(&s_int, 1);
-            if (at < kSpList) s_work.list[at] = (unsigned long long)sp_key(l) << 32 | (uint32_t)~(i0 + i);
-          } else if (with_sums) {
-            sum += weight(l);
+#pragma unroll 1
+        for (int w = b * kBlockWords + lane; w < min((b + 1) * kBlockWords, all_words); w += 32) {
+          const uint4 word = words[w];
+          if (!((top - sm_word_max<T>(word, -INFINITY)) * scale < f1)) continue;
+          Vec16<T> v;
+          v.unpack(word);
+#pragma unroll
+          for (int e = 0; e < W; ++e) {
+            const float f = (top - v.v[e]) * scale;
+            if (f < f1 && f >= f0) {
+              const int at = atomicAdd(&s_int, 1);
+              if (at < 2 * kSpList / (int)cluster && at < kSpList) s_work.list[at] = (unsigned long long)sp_key(v.v[e]) << 32 | (uint32_t)~(i0 + w * W + e - skew);
+            }
+          }
+          if (with_sums) {
+#pragma unroll
+            for (int e = 0; e < W; ++e) sum += sp_pick((top - v.v[e]) * scale < f0, weight(v.v[e]));
           }
         }
         if (with_sums) {
@@ -437,99 +459,105 @@ sample_kernel(SampleArgs a) {
       __syncthreads();
       double above = 0.0;
       if (with_sums)
-        for (int b = 0; b < (cnt + kSpBlock - 1) / kSpBlock; b += 32) above += warp_total(b + lane < (cnt + kSpBlock - 1) / kSpBlock ? s_block[b + lane] : 0.0);
-      tell(above, s_int, 0.f);
-      // everybody copies all lists, in the order of the CTAs
-      const SpSlot o = told(lane < (int)cluster ? lane : 0);
-      const int count = lane < (int)cluster ? min(o.i, kSpList + 1) : 0;
-      int upto = count;
+        for (int b = 0; b < blocks; b += 32) above += warp_total(b + lane < blocks ? s_block[b + lane] : 0.0);
+      // to everybody, in places of this CTA's own
+      const int room = 2 * kSpList / (int)cluster, mine_here = s_int;
+      for (int i = tid; i < min(mine_here, room) * (int)cluster; i += kSpThreads)
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(map_to_rank(smem_u32(&s_work.all[rank * room + i / (int)cluster]), (uint32_t)i & (cluster - 1))), "l"(s_work.list[i / (int)cluster]) : "memory");
+      if (tid < (int)cluster) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_rank(smem_u32(&s_counts[rank]), (uint32_t)tid)), "r"(mine_here) : "memory");
+      tell(above, 0);
+      if (with_sums) {
+        above = told_sum();
+        if (tid == 0) s_double = above;
+      }
+      int upto = lane < (int)cluster ? min(s_counts[lane], room + 1) : 0;
+      const bool spilt = __any_sync(0xffffffffu, upto > room);
 #pragma unroll
       for (int d = 1; d < 16; d <<= 1) {
         const int v = __shfl_up_sync(0xffffffffu, upto, d);
         if (lane >= d) upto += v;
       }
       const int members = __shfl_sync(0xffffffffu, upto, (int)cluster - 1);
-      if (with_sums) {
-        above = 0.0;
-        for (int c = 0; c < (int)cluster; ++c) above += __shfl_sync(0xffffffffu, o.d, c);
-        if (tid == 0) s_double = above;
-      }
-      if (members > kSpList) return -1;
-      for (int i = tid; i - lane < members; i += kSpThreads) {
-        int c = 0, start = 0;
-        for (int r = 0; r < (int)cluster - 1; ++r) {
-          const int v = __shfl_sync(0xffffffffu, upto, r);
-          if (i >= v) c = r + 1, start = v;
+      if (spilt || members > kSpList) return -1;
+      // in order: a member's place is the number of those in front of it (four lanes a member)
+      for (int i = tid >> 2; i - (lane >> 2) < members; i += kSpThreads / 4) {
+        unsigned long long e = 0ull;
+        int place = 0, start = 0;
+        for (int c = 0; c < (int)cluster; ++c) {
+          const int end = __shfl_sync(0xffffffffu, upto, c);
+          if (i >= start && i < end) e = s_work.all[c * room + i - start];
+          start = end;
         }
-        if (i < members) {
-          unsigned long long e;
-          asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(e) : "r"(map_to_rank(smem_u32(&s_work.list[i - start]), (uint32_t)c)) : "memory");
-          s_work.all[i] = e;
-        }
-      }
-      __syncthreads();
-      // in order: a member's place is the number of those in front of it
-      for (int i = tid; i < members; i += kSpThreads) {
-        const unsigned long long e = s_work.all[i];
-        int place = 0;
+        start = 0;
+        for (int c = 0; c < (int)cluster; ++c) {
+          const int end = __shfl_sync(0xffffffffu, upto, c);
 #pragma unroll 4
-        for (int j = 0; j < members; ++j) place += s_work.all[j] > e;
-        s_work.sorted[place] = e;
-        s_work.weight[place] = weight(sp_logit((uint32_t)(e >> 32)));
+          for (int j = lane & 3; j < end - start; j += 4) place += s_work.all[c * room + j] > e;
+          start = end;
+        }
+        place += __shfl_xor_sync(0xffffffffu, place, 1);
+        place += __shfl_xor_sync(0xffffffffu, place, 2);
+        if (i < members && (lane & 3) == 0) {
+          s_work.sorted[place] = e;
+          s_work.weight[place] = weight(sp_logit((uint32_t)(e >> 32)));
+        }
       }
       __syncthreads();
       return members;
     };
-    // Counts or weighs candidates in bins, sums the row (by_weight), and finds the bins in which the goal lies: `goal` in members, or in parts of the sum.
+    // Counts or weighs candidates in bins, sums the row (by_weight), and finds the bins [from, to] in which the goal lies: `goal` in members, or in parts of the sum.
     // Returns what lies above them, in members (by_weight: at most as many), or -1.
     double sum_all = 0.0;
-    int from = 0, to = 0, inside = 0;
-    auto look = [&](float scale, float reach, bool by_weight, double goal, double octaves) {
+    int from = 0, to = kSpBins - 1, inside = 0;
+    auto look = [&](bool by_weight, double goal) {
       for (int i = tid; i < kSpBins; i += kSpThreads) s_work.bins[i] = 0u;
-      if (tid == 0) s_int = kSpBins, s_int2 = -1;
       __syncthreads();
       double sum = 0.0;
-      const float fall = -(float)octaves;          // of a bin
-#pragma unroll 4
-      for (int i = tid; i < cnt; i += kSpThreads) {
-        const float l = logit(i), x = ftop - l, f = x * scale;
-        if (by_weight) sum += weight(l);
-        if (!(x <= reach && f < (float)kSpBins)) continue;
-        const int bin = (int)f;
-        uint32_t v = 1u;
-        if (by_weight) {
-          float share;
-          asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(share) : "f"((f - (float)bin) * fall));
-          v = (uint32_t)(share * 131072.f + 0.5f);       // 17 bits: 38400 members of a part stay below 2^33, so parts that long are found digit by digit
+      const float fall = -0.69314718f * (float)octaves / kSpBins;          // of a bin
+#pragma unroll 1
+      for (int w = tid; w < all_words; w += kSpThreads) {
+        Vec16<T> v;
+        v.unpack(words[w]);
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          // Conversions by sums with 2^23: the instructions take 8 clocks a warp.
+          const float f = (top - v.v[e]) * scale, down = __fadd_rd(f, 8388608.f);
+          uint32_t member = 1u;
+          if (by_weight) {
+            sum += weight(v.v[e]);
+            const float y = (f - (down - 8388608.f)) * fall;       // exp(y) to y^3 / 6, 4.5e-6 at most
+            member = __float_as_uint(fmaf(fmaf(0.5f * 131072.f, y, 131072.f), y, 131072.f + 8388608.f)) - 0x4b000000u;       // 17 bits; a part has fewer than 2^15 members
+          }
+          if (f < (float)kSpBins) atomicAdd(&s_work.bins[__float_as_uint(down) - 0x4b000000u], member);
         }
-        atomicAdd(&s_work.bins[bin], v);
       }
       if (by_weight) {
-        tell(cta_sum(sum), 0, 0.f);
-        for (int c = 0; c < (int)cluster; ++c) sum_all += told(c).d;
+        tell(cta_sum(sum), 0);
+        sum_all = told_sum();
         goal *= sum_all;
       } else {
         meet();
       }
-      // four bins a thread, over the cluster
+      // This CTA adds up its part of the bins over the cluster (all of them would be 32 KB from other SMs, at 16 bytes a clock).
+      const int share = kSpBins / (int)cluster, each = max(1, share / kSpThreads), bin0 = (int)rank * share + tid * each;
+      const bool has = tid * each < share;
       uint32_t v[4] = {0u, 0u, 0u, 0u};
       double m[4] = {0.0, 0.0, 0.0, 0.0};
-#pragma unroll 4
-      for (int c = 0; c < (int)cluster; ++c) {
-        uint32_t w[4];
-        asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(map_to_rank(smem_u32(&s_work.bins[4 * tid]), (uint32_t)c)) : "memory");
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (by_weight) m[j] += (double)w[j];
-          else v[j] += w[j];
-        }
-      }
-      if (by_weight) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[j] = (uint32_t)(m[j] * (1.0 / 131072) * 1.04) + (m[j] > 0.0);          // a bin is 0.04 octaves wide at most: never fewer than there are
-          m[j] *= exp2(-octaves * (4 * tid + j)) * (1.0 / 131072);
+      for (int j = 0; j < 4; ++j) {
+        if (has && j < each) {
+          double sum_m = 0.0;
+#pragma unroll 8
+          for (int c = 0; c < (int)cluster; ++c) {
+            uint32_t w;
+            asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(w) : "r"(map_to_rank(smem_u32(&s_work.bins[bin0 + j]), (uint32_t)c)) : "memory");
+            if (by_weight) sum_m += __hiloint2double(0x43300000, (int)w) - 4503599627370496.0;       // as a double
+            else v[j] += w;
+          }
+          if (by_weight) {
+            v[j] = (uint32_t)(sum_m * (1.0 / 131072) * 1.04) + (sum_m > 0.0);        // a bin is 0.043 octaves wide at most: never fewer than there are
+            m[j] = sum_m * exp2(octaves * (-1.0 / kSpBins) * (bin0 + j)) * (1.0 / 131072);
+          }
         }
       }
       const uint32_t c4 = v[0] + v[1] + v[2] + v[3];
@@ -544,115 +572,128 @@ sample_kernel(SampleArgs a) {
       __syncthreads();
       if (lane == 31) s_scan_c[warp] = cc, s_warp[warp] = cm;
       __syncthreads();
-      for (int w = 0; w < warp; ++w) cc += s_scan_c[w], cm += s_warp[w];
+      uint32_t sum_c = 0u;
+      double sum_w = 0.0;
+#pragma unroll
+      for (int w = 0; w < kSpWarps; ++w) {
+        if (w == warp) cc += sum_c, cm += sum_w;
+        sum_c += s_scan_c[w], sum_w += s_warp[w];
+      }
+      if (tid == 0) s_border = SpBorder{kSpBins, 0, -1, 0};
+      if (cluster > 1) {                   // what the CTAs in front have
+        tell(sum_w, (int)sum_c);
+        const SpSlot o = told(lane < (int)cluster ? lane : 0);
+        for (int c = 0; c < (int)rank; ++c) cc += (uint32_t)__shfl_sync(0xffffffffu, o.i, c), cm += __shfl_sync(0xffffffffu, o.d, c);
+      } else {
+        __syncthreads();
+      }
       uint32_t before = cc - c4;
       double before_m = cm - m4;
-      const double slack = by_weight ? 4e-6 * sum_all : 0.0;          // 17 bits a member, and the difference of the two forms of its weight
+      const double slack = by_weight ? 1e-5 * sum_all : 0.0;          // 17 bits a member, and the difference of the two forms of its weight
+      int first_bin = kSpBins, last_bin = -1, first_before = 0, last_end = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int bin = 4 * tid + j;
         if (v[j] > 0u) {
-          if (by_weight) {
-            if (before_m + m[j] >= goal - slack) atomicMin(&s_int, bin);
-            if (before_m < goal + slack) atomicMax(&s_int2, bin);
-          } else if ((double)before < goal && (double)(before + v[j]) >= goal) {
-            s_int = s_int2 = bin;
-          }
+          const bool starts = by_weight ? before_m + m[j] >= goal - slack : (double)(before + v[j]) >= goal, ends = by_weight ? before_m < goal + slack : (double)before < goal;
+          if (starts && first_bin == kSpBins) first_bin = bin0 + j, first_before = (int)before;
+          if (ends) last_bin = bin0 + j, last_end = (int)(before + v[j]);
         }
         before += v[j], before_m += m[j];
       }
+      const int wf = __reduce_min_sync(0xffffffffu, first_bin), wl = __reduce_max_sync(0xffffffffu, last_bin);
+      if (lane == 0 && wf < kSpBins) atomicMin(&s_border.from, wf);
+      if (lane == 0 && wl >= 0) atomicMax(&s_border.to, wl);
       __syncthreads();
-      from = s_int, to = s_int2;
-      __syncthreads();
-      if (to < 0) return -1;
-      from = min(from, to);
-      before = cc - c4;
-      if (tid == 0) s_int2 = 0;
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int bin = 4 * tid + j;
-        if (bin == from) s_int = (int)before;
-        if (bin >= from && bin <= to && v[j]) atomicAdd(&s_int2, (int)v[j]);
-        before += v[j];
+      if (first_bin < kSpBins && first_bin == s_border.from) s_border.before = first_before;
+      if (last_bin >= 0 && last_bin == s_border.to) s_border.end = last_end;
+      SpBorder o;
+      meet();
+      {
+        const uint32_t at = map_to_rank(smem_u32(&s_border), (uint32_t)(lane < (int)cluster ? lane : 0));
+        asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(o.from), "=r"(o.before), "=r"(o.to), "=r"(o.end) : "r"(at) : "memory");
       }
-      __syncthreads();
-      const int above = s_int;
-      inside = s_int2;
-      __syncthreads();
+      from = __reduce_min_sync(0xffffffffu, o.from), to = __reduce_max_sync(0xffffffffu, o.to);
+      if (to < 0) return -1;
+      const int has_from = __ffs(__ballot_sync(0xffffffffu, o.from == from)) - 1, has_to = __ffs(__ballot_sync(0xffffffffu, o.to == to)) - 1;
+      const int end = __shfl_sync(0xffffffffu, o.end, has_to);
+      int above = __shfl_sync(0xffffffffu, o.before, has_from);
+      if (from > to) from = to, above = max(0, end - 1);        // the sum of all bins falls short of the goal by its rounding: the last of them (its own members count once)
+      inside = end - above;
       return above;
     };
 
+    bool listed = false, direct = false;   // worth a list; without a look at the bins
+    double goal = 0.0;
+    if (k && k <= kSpThreads) {
+      // A logit that k of the groups' maxima reach, by halving what lies between the smallest and the largest, until no more than a quarter more do.
+      if (warp == 0) {
+        uint32_t v[kSpThreads / 16], low = 0xffffffffu;      // 16 maxima a lane
+        int some = 0;
+#pragma unroll
+        for (int j = 0; j < kSpThreads / 16; ++j) {
+          const int at = j * 32 + lane;
+          v[j] = 0u;
+          if (at < groups * (int)cluster)
+            asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v[j]) : "r"(map_to_rank(smem_u32(&s_work.groups[at & (groups - 1)]), (uint32_t)at / (uint32_t)groups)) : "memory");
+          if (v[j] <= sp_key(-INFINITY)) v[j] = 0u;          // has none
+          else low = min(low, v[j]), ++some;
+        }
+        low = __reduce_min_sync(0xffffffffu, low), some = __reduce_add_sync(0xffffffffu, some);
+        uint32_t high = peak;
+        for (int t = 0; t < 20 && some > k + k / 4 && high - low > 1; ++t) {
+          const uint32_t mid = low + (high - low) / 2;
+          int c = 0;
+#pragma unroll
+          for (int j = 0; j < kSpThreads / 16; ++j) c += v[j] >= mid;
+          c = __reduce_add_sync(0xffffffffu, c);
+          if (c >= k) low = mid, some = c;
+          else high = mid;
+        }
+        if (lane == 0) s_int = some >= k ? (int)low : 0;
+      }
+      __syncthreads();
+      const uint32_t low = (uint32_t)s_int;
+      scale = fminf(1023.9f / (top - sp_logit(low)), FLT_MAX);
+      listed = low != 0u && scale > 0.f;
+      direct = true;
+      goal = (double)k;
+      meet();                              // the maxima have been read: the lists come in their place
+    } else if (!k && by_p) {
+      octaves = (log2((double)a.n) - log2(1.0 - (double)p)) * 1.0001;     // 1 - p is exact; the total is 1 at least
+      scale = (float)(kSpBins * weight.c / octaves);
+      listed = scale > 0.f && scale < FLT_MAX && a.per <= 32767;
+      goal = (double)p;
+    }
     bool whole = false;                    // the list holds all that is kept
     bool summed = false;                   // s_block holds the sums of what is kept
-    int members = -1, cut = 0;
-    bool found_k = !k, found_p = !by_p;
+    int members = -1, above = 0, cut = 0;
     double total = 0.0;
-    if (k && k <= kSpList) {
-      const int g = k <= best.have[2] ? 2 : k <= best.have[1] ? 1 : 0;
-      const float reach = ftop - best.low[g], scale = reach > 0.f ? 1023.9f / reach : 0.f;
-      if (k <= best.have[g] && scale < FLT_MAX && reach < FLT_MAX) {
-        if (g == 2 || a.n <= kSpList) members = gather(scale, reach, 0, kSpBins - 1, false);
-        whole = members > 0;
-        if (!whole) {
-          const int above = look(scale, reach, false, (double)k, 0.0);
-          if (above >= 0 && above + inside <= kSpList) {
-            members = gather(scale, reach, 0, to, false);
-            whole = members > 0;
-          } else if (above >= 0 && inside <= kSpList) {
-            members = gather(scale, reach, from, to, false);
-            if (members >= k - above && k > above) {
-              const unsigned long long e = s_work.sorted[k - above - 1];
-              last = (uint32_t)(e >> 32), last_at = (int)~(uint32_t)e;
-              found_k = true;
-            }
-          }
+    if (listed) {
+#pragma unroll 1
+      for (;;) {
+        bool complete = direct;
+        if (!direct) {
+          above = look(!k, goal);
+          complete = above >= 0 && above + inside <= kSpList;
+          if (above < 0 || (k && inside > kSpList)) break;
         }
-      }
-      if (whole) members = min(members, k);
-    } else if (!k && by_p) {
-      // 1 - p is exact; the total is 1 at least
-      const double octaves = (log2((double)a.n) - log2(1.0 - (double)p)) * 1.0001;
-      const float reach = (float)(octaves / weight.c), scale = (float)(kSpBins * weight.c / octaves);
-      if (a.per <= 32767 && reach < FLT_MAX && scale < FLT_MAX && scale > 0.f) {
-        const int above = look(scale, reach, true, (double)p, octaves / kSpBins);
-        const double goal = (double)p * sum_all;
-        if (above >= 0 && above + inside <= kSpList) {
-          members = gather(scale, reach, 0, to, false);
-          whole = members > 0;
-        } else if (above >= 0) {
-          members = gather(scale, reach, from, to, true);
-          if (members > 0) {
-            if (warp == 0) {
-              double before = s_double;
-              int j = 0;
-              for (int i = 0; i < members; i += 32) {
-                const double w = i + lane < members ? s_work.weight[i + lane] : 0.0, cum = before + warp_scan(w, lane);
-                const unsigned in = __ballot_sync(0xffffffffu, i + lane < members && cum - w < goal);
-                j += __popc(in);
-                before = __shfl_sync(0xffffffffu, cum, 31);
-              }
-              if (lane == 0) s_int = max(j, 1);
-            }
-            __syncthreads();
-            cut = s_int;
-            const unsigned long long e = s_work.sorted[cut - 1];
-            last = (uint32_t)(e >> 32), last_at = (int)~(uint32_t)e;
-            found_p = true;
-            summed = !by_m;
-          }
-        }
+        members = gather(complete ? 0 : from, to, !k && !complete);
+        whole = complete && members > 0;
+        if (!direct || members >= 0) break;
+        direct = false;
       }
     }
     if (whole) {
       // all from the list: what is kept of it, and their total, in order
+      if (k) members = min(members, k);
       if (warp == 0) {
         double want = INFINITY;
         if (by_p) {
-          double sum = 0.0;
-          if (k)
+          double sum = sum_all;
+          if (k) {
+            sum = 0.0;
             for (int i = 0; i < members; i += 32) sum += warp_total(i + lane < members ? s_work.weight[i + lane] : 0.0);
-          else sum = sum_all;
+          }
           want = (double)p * sum;
         }
         double before = 0.0;
@@ -671,11 +712,11 @@ sample_kernel(SampleArgs a) {
       __syncthreads();
       cut = s_int, total = s_double;
       const unsigned long long e = s_work.sorted[cut - 1];
-      last = (uint32_t)(e >> 32), last_at = (int)~(uint32_t)e;
+      last = sp_logit((uint32_t)(e >> 32)), last_at = (int)~(uint32_t)e;
       __syncthreads();
       if (a.tokens) {
-        // by index: a class that the running sum passes the goal with, the first of them; or the last that weighs anything
-        const double goal = fmax((double)a.u[row] * total, 0.0);
+        // by index: the first class with which the running sum passes the goal; or the last that weighs anything
+        goal = fmax((double)u * total, 0.0);
         if (tid == 0) s_int = 0x7fffffff, s_int2 = -1;
         __syncthreads();
         for (int i = tid; i < cut; i += kSpThreads) {
@@ -694,90 +735,161 @@ sample_kernel(SampleArgs a) {
         token = s_int != 0x7fffffff ? s_int : s_int2;
       }
     } else {
-      if (!found_k) select(false, (double)k);
-      if (!found_p) {
-        double v = 0.0;
-        for (int i = tid; i < cnt; i += kSpThreads) {
-          const float l = logit(i);
-          if (kept(sp_key(l), i)) v += weight(l);
+      bool need_k = k != 0, need_p = by_p;
+      if (members > 0 && k) {              // the bin in which the k-th lies
+        const unsigned long long e = s_work.sorted[k - above - 1];
+        last = sp_logit((uint32_t)(e >> 32)), last_at = (int)~(uint32_t)e;
+        need_k = false;
+      } else if (members > 0) {            // the bins in which the p-th part ends
+        if (warp == 0) {
+          double before = s_double;
+          int j = 0;
+          for (int i = 0; i < members; i += 32) {
+            const double w = i + lane < members ? s_work.weight[i + lane] : 0.0, cum = before + warp_scan(w, lane);
+            j += __popc(__ballot_sync(0xffffffffu, i + lane < members && cum - w < goal * sum_all));
+            before = __shfl_sync(0xffffffffu, cum, 31);
+          }
+          if (lane == 0) s_int = max(j, 1);
         }
-        tell(cta_sum(v), 0, 0.f);
-        v = 0.0;
-        for (int c = 0; c < (int)cluster; ++c) v += told(c).d;
-        select(true, (double)p * v);
+        __syncthreads();
+        cut = s_int;
+        const unsigned long long e = s_work.sorted[cut - 1];
+        last = sp_logit((uint32_t)(e >> 32)), last_at = (int)~(uint32_t)e;
+        need_p = false;
+        summed = !by_m;
+      }
+#pragma unroll 1
+      for (int by_weight = 0; by_weight < 2; ++by_weight) {
+        if (!(by_weight ? need_p : need_k)) continue;
+        double v = (double)k;
+        if (by_weight) {
+          v = 0.0;
+          for (int i = tid; i < cnt; i += kSpThreads) {
+            const float l = logit(i);
+            if (kept(l, i)) v += weight(l);
+          }
+          tell(cta_sum(v), 0);
+          v = (double)p * told_sum();
+        }
+        select(by_weight != 0, v);
       }
     }
-    const bool all = !k && !by_p;
-    auto mass = [&](int i) {               // what class i adds to the sum
-      const float l = logit(i);
-      if (!all && !kept(sp_key(l), i)) return 0.0;
+    const double least = by_m ? (double)m : 0.0;
+    const bool all = last == -INFINITY;
+    auto mass = [&](float l, int i) {      // what class i adds to the sum
+      if (!kept(l, i)) return 0.0;
       const double w = weight(l);
-      return by_m && w < (double)m ? 0.0 : w;
+      return sp_pick(w >= least, w);
     };
-    // ---- sums of blocks, the total, and the block in which the running sum passes its goal
     if (!whole) {
-    const int blocks = (cnt + kSpBlock - 1) / kSpBlock;
-    if (summed) {
-      // those of the list that are kept join their blocks, in order
-      for (int b = tid; b < blocks; b += kSpThreads) {
-        double s = s_block[b];
-        for (int j = 0; j < cut; ++j) {
-          const int at = (int)~(uint32_t)s_work.sorted[j] - i0;
-          if (at >= 0 && at < cnt && at / kSpBlock == b) s += s_work.weight[j];
+      // ---- sums of blocks, the total, and the block in which the running sum passes its goal
+      if (summed) {
+        // those of the list that are kept join their blocks, in order
+        for (int b = tid; b < blocks; b += kSpThreads) {
+          double s = s_block[b];
+          for (int j = 0; j < cut; ++j) {
+            const int at = (int)~(uint32_t)s_work.sorted[j] - i0;
+            if (at >= 0 && at < cnt && (at + skew) / kSpBlock == b) s += s_work.weight[j];
+          }
+          s_block[b] = s;
         }
-        s_block[b] = s;
-      }
-    } else {
-      for (int b = warp; b < blocks; b += kSpWarps) {
-        const int end = min((b + 1) * kSpBlock, cnt);
-        double s = 0.0;
-#pragma unroll 4
-        for (int i = b * kSpBlock + lane; i < end; i += 32) s += mass(i);
-        s = warp_total(s);
-        if (lane == 0) s_block[b] = s;
-      }
-    }
-    __syncthreads();
-    double sum = 0.0;
-    for (int b = 0; b < blocks; b += 32) sum += warp_total(b + lane < blocks ? s_block[b + lane] : 0.0);
-    tell(sum, 0, 0.f);
-    double before = 0.0;
-    int last_one = 0;                      // the last CTA that has any weight
-    for (int c = 0; c < (int)cluster; ++c) {
-      const double o = told(c).d;
-      if (c == (int)rank) before = total;
-      if (o > 0.0) last_one = c;
-      total += o;
-    }
-    if (a.tokens) {
-      const double goal = fmax((double)a.u[row] * total, 0.0);
-      mine = sum > 0.0 && before <= goal && (before + sum > goal || last_one == (int)rank);
-      if (mine && warp == 0) {
-        int at = -1;
-        double run = before, start = before;
-        for (int b = 0; b < blocks; b += 32) {
-          const double w = b + lane < blocks ? s_block[b + lane] : 0.0, cum = run + warp_scan(w, lane);
-          const unsigned over = __ballot_sync(0xffffffffu, w > 0.0 && cum > goal), some = __ballot_sync(0xffffffffu, w > 0.0);
-          const int j = over ? __ffs(over) - 1 : 31 - __clz(some);
-          if (some) at = b + j, start = __shfl_sync(0xffffffffu, cum - w, j);
-          if (over) break;
-          run = __shfl_sync(0xffffffffu, cum, 31);
-        }
-        const int end = min((at + 1) * kSpBlock, cnt);
-        bool found = false;
-        for (int i = at * kSpBlock + lane; i - lane < end && !found; i += 32) {
-          const double w = i < end ? mass(i) : 0.0, cum = start + warp_scan(w, lane);
-          const unsigned over = __ballot_sync(0xffffffffu, w > 0.0 && cum > goal), some = __ballot_sync(0xffffffffu, w > 0.0);
-          if (some) token = i0 + i - lane + (over ? __ffs(over) - 1 : 31 - __clz(some));
-          found = over != 0;
-          start = __shfl_sync(0xffffffffu, cum, 31);
+      } else {
+#pragma unroll 1
+        for (int b = warp; b < blocks; b += kSpWarps) {
+          double s = 0.0;
+#pragma unroll 1
+          for (int w = b * kBlockWords + lane; w < min((b + 1) * kBlockWords, all_words); w += 32) {
+            Vec16<T> v;
+            v.unpack(words[w]);
+            if (all && !by_m) {
+#pragma unroll
+              for (int e = 0; e < W; ++e) s += weight(v.v[e]);
+            } else {
+#pragma unroll
+              for (int e = 0; e < W; ++e) {
+                const double g = weight(v.v[e]);
+                s += sp_pick(g >= least && kept(v.v[e], w * W + e - skew), g);
+              }
+            }
+          }
+          s = warp_total(s);
+          if (lane == 0) s_block[b] = s;
         }
       }
+      __syncthreads();
+      double sum = 0.0;
+      for (int b = 0; b < blocks; b += 32) sum += warp_total(b + lane < blocks ? s_block[b + lane] : 0.0);
+      tell(sum, 0);
+      const double o = told(lane < (int)cluster ? lane : 0).d;
+      double before = 0.0;
+      int last_one = 0;                    // the last CTA that has any weight
+      for (int c = 0; c < (int)cluster; ++c) {
+        const double v = __shfl_sync(0xffffffffu, o, c);
+        if (c == (int)rank) before = total;
+        if (v > 0.0) last_one = c;
+        total += v;
+      }
+      if (a.tokens) {
+        goal = fmax((double)u * total, 0.0);
+        mine = sum > 0.0 && before <= goal && (before + sum > goal || last_one == (int)rank);
+        if (mine && warp == 0) {
+          int at = -1;
+          double run = before, start = before;
+          for (int b = 0; b < blocks; b += 32) {
+            const double w = b + lane < blocks ? s_block[b + lane] : 0.0, cum = run + warp_scan(w, lane);
+            const unsigned over = __ballot_sync(0xffffffffu, w > 0.0 && cum > goal), some = __ballot_sync(0xffffffffu, w > 0.0);
+            const int j = over ? __ffs(over) - 1 : 31 - __clz(some);
+            if (some) at = b + j, start = __shfl_sync(0xffffffffu, cum - w, j);
+            if (over) break;
+            run = __shfl_sync(0xffffffffu, cum, 31);
+          }
+          const int end = min((at + 1) * kSpBlock - skew, cnt);
+          bool found = false;
+          for (int i = max(at * kSpBlock - skew, 0) + lane; i - lane < end && !found; i += 32) {
+            const double w = i < end ? mass(logit(i), i) : 0.0, cum = start + warp_scan(w, lane);
+            const unsigned over = __ballot_sync(0xffffffffu, w > 0.0 && cum > goal), some = __ballot_sync(0xffffffffu, w > 0.0);
+            if (some) token = i0 + i - lane + (over ? __ffs(over) - 1 : 31 - __clz(some));
+            found = over != 0;
+            start = __shfl_sync(0xffffffffu, cum, 31);
+          }
+        }
+      }
     }
+    if (a.tokens && !(goal > 0.0)) {       // u is 0: the first that weighs anything, however little
+      int at = 0x7fffffff;
+      for (int i = tid; i < cnt; i += kSpThreads) {
+        const float l = logit(i);
+        if (at == 0x7fffffff && kept(l, i) && weight.live(l) && !(by_m && weight(l) < (double)m)) at = i0 + i;
+      }
+      at = __reduce_min_sync(0xffffffffu, at);
+      __syncthreads();
+      if (tid == 0) s_int = 0x7fffffff;
+      __syncthreads();
+      if (lane == 0) atomicMin(&s_int, at);
+      __syncthreads();
+      tell(0.0, s_int);
+      token = __reduce_min_sync(0xffffffffu, told(lane < (int)cluster ? lane : 0).i);
+      mine = rank == 0;
     }
     if (probs) {
-      const double scale = 1.0 / total;
-      for (int i = tid; i < cnt; i += kSpThreads) probs[i] = (float)(mass(i) * scale);
+      const double part_of = 1.0 / total;
+      if (all) {
+#pragma unroll 4
+        for (int i = tid; i < cnt; i += kSpThreads) {
+          const double g = weight(logit(i));
+          probs[i] = (float)sp_pick(g >= least, g * part_of);
+        }
+      } else if (whole) {                  // few, and most warps have none
+#pragma unroll 4
+        for (int i = tid; i < cnt; i += kSpThreads) probs[i] = (float)(mass(logit(i), i) * part_of);
+      } else {
+#pragma unroll 4
+        for (int i = tid; i < cnt; i += kSpThreads) {
+          const float l = logit(i);
+          const double g = weight(l);
+          probs[i] = (float)sp_pick(g >= least && kept(l, i), g * part_of);
+        }
+      }
     }
   }
   if (a.tokens && mine && tid == 0) a.tokens[row] = token;
@@ -785,7 +897,7 @@ sample_kernel(SampleArgs a) {
 }
 
 template <typename T>
-inline size_t sample_smem(int per) { return align_up((size_t)per * sizeof(T) + 16, 16); }
+inline size_t sample_smem(int per) { return align_up((size_t)per * sizeof(T), 16) + 32; }
 
 inline cudaError_t sample_context_init() {     // once per device
   cudaError_t e = cudaSuccess;
