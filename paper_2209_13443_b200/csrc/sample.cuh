@@ -131,7 +131,7 @@ __device__ __forceinline__ float sp_word_max(uint4 w, float top) {
 }
 
 struct SpSlot {            // what a CTA tells the others
-  double d;
+  double d, e;
   int i;
 };
 struct SpHist {            // by digit: members, and their weight in units of 2^-43 (at most 614400 of them, each at most 1)
@@ -142,8 +142,9 @@ struct SpFound {           // the digit, and what lies above it
   int digit;
   int above, in;
 };
-struct SpBorder {          // of a CTA's bins: the first in which the goal may lie and what lies before it, the last and what lies up to its end
+struct SpBorder {          // of a CTA's bins: the first in which the goal may lie and what lies before it (and its weight), the last and what lies up to its end
   int from, before, to, end;
+  double weight;
 };
 struct alignas(16) SpWork {              // bins are read four at a time
   union {
@@ -172,7 +173,7 @@ sample_kernel(SampleArgs a) {
   __shared__ uint32_t s_top, s_tops[kSpWarps];
   __shared__ __align__(16) SpWork s_work;
   __shared__ double s_roots[kSpTable];
-  __shared__ double s_warp[kSpWarps], s_block[kSpMaxPart / kSpBlock + 2], s_double;
+  __shared__ double s_chunk[kSpList / 32], s_warp[kSpWarps], s_block[kSpMaxPart / kSpBlock + 2], s_double;
   __shared__ unsigned long long s_scan_m[kSpWarps];
   __shared__ uint32_t s_scan_c[kSpWarps];
   __shared__ SpFound s_found;
@@ -197,24 +198,25 @@ sample_kernel(SampleArgs a) {
     if (cluster > 1) asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
     else __syncthreads();
   };
-  auto tell = [&](double d, int i) {                     // by thread 0; all threads meet
-    if (tid == 0) s_slot[turn & 1] = SpSlot{d, i};
+  auto tell = [&](double d, int i, double e = 0.0) {     // by thread 0; all threads meet
+    if (tid == 0) s_slot[turn & 1] = SpSlot{d, e, i};
     meet();
     ++turn;
   };
   auto told = [&](int c) {                               // what CTA c told last
     SpSlot s;
     const uint32_t at = map_to_rank(smem_u32(&s_slot[(turn - 1) & 1]), (uint32_t)c);
-    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(s.i) : "r"(at + 8u) : "memory");
+    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(s.i) : "r"(at + 16u) : "memory");
     asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(s.d) : "r"(at) : "memory");
+    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(s.e) : "r"(at + 8u) : "memory");
     return s;
   };
-  auto told_sum = [&]() {                                // over the CTAs, in order
-    const double d = told(lane < (int)cluster ? lane : 0).d;
+  auto in_order = [&](double d) {                        // the sum over the CTAs, of which each lane has one's
     double sum = 0.0;
     for (int c = 0; c < (int)cluster; ++c) sum += __shfl_sync(0xffffffffu, d, c);
     return sum;
   };
+  auto told_sum = [&]() { return in_order(told(lane < (int)cluster ? lane : 0).d); };
   auto cta_sum = [&](double v) {                         // of the CTA's threads, in fixed order
     v = warp_total(v);
     __syncthreads();
@@ -421,53 +423,90 @@ sample_kernel(SampleArgs a) {
     };
 
     // ---- few candidates.  Bins of width 1 / scale in the logit, below the maximum; what lies beyond the last of them is no candidate.
-    float scale = 0.f;
+    float scale = 0.f, base = 0.f, zoom = 1.f;        // looked at closer, the bins divide what lies from `base` on
     double octaves = 0.0;                  // of all bins, for weights
-    // The list: members whose bin lies in [from, to], in order, with their weights; with_sums: the sums of blocks of what lies above them, and in s_double that of the row.
-    // Returns how many there are, or -1: more than the list has room for.
-    auto gather = [&](int from, int to, bool with_sums) {
+    auto place = [&](float l) { return ((top - l) * scale - base) * zoom; };
+    // The list: members whose bin lies in [from, to], in order, with their weights.  by_weight: and the exact sum of the row in sum_all, of blocks of what lies above them in s_block, and of
+    // the row of those in s_double.  Returns how many members there are, or -1: more than the list has room for.
+    double sum_all = 0.0;
+    auto gather = [&](int from, int to, bool by_weight) {
       const float f0 = (float)from, f1 = (float)(to + 1);
+      const int list_room = min(2 * kSpList / (int)cluster, kSpList);
       if (tid == 0) s_int = 0;
       __syncthreads();
+      double row_sum = 0.0;
+      constexpr int kWords = kBlockWords / 32;         // of a lane and block
 #pragma unroll 1
-      for (int b = warp; b < blocks; b += kSpWarps) {
-        double sum = 0.0;
+      for (int b0 = warp; b0 < blocks; b0 += 4 * kSpWarps) {
+        // Four blocks' members as 64 bits of a lane, put away together: put away one by one, with an atomic each, they took twice the time of everything else here.
+        unsigned long long hits = 0ull;
 #pragma unroll 1
-        for (int w = b * kBlockWords + lane; w < min((b + 1) * kBlockWords, all_words); w += 32) {
-          const uint4 word = words[w];
-          if (!((top - sm_word_max<T>(word, -INFINITY)) * scale < f1)) continue;
-          Vec16<T> v;
-          v.unpack(word);
+        for (int q = 0; q < 4; ++q) {
+          const int b = b0 + q * kSpWarps;
+          if (b >= blocks) break;
+          double sum = 0.0;
+#pragma unroll 1
+          for (int j = 0; j < kWords; ++j) {
+            const int w = b * kBlockWords + j * 32 + lane;
+            if (w >= all_words) break;
+            const uint4 word = words[w];
+            Vec16<T> v;
+            v.unpack(word);
+            unsigned in = 0u;
+            if (by_weight) {
 #pragma unroll
-          for (int e = 0; e < W; ++e) {
-            const float f = (top - v.v[e]) * scale;
-            if (f < f1 && f >= f0) {
-              const int at = atomicAdd(&s_int, 1);
-              if (at < 2 * kSpList / (int)cluster && at < kSpList) s_work.list[at] = (unsigned long long)sp_key(v.v[e]) << 32 | (uint32_t)~(i0 + w * W + e - skew);
+              for (int e = 0; e < W; ++e) {
+                const double g = weight(v.v[e]);
+                const float f = place(v.v[e]);
+                row_sum += g, sum += sp_pick(f < f0, g);
+                if (f >= f0 && f < f1) in |= 1u << e;
+              }
+            } else if (place(sm_word_max<T>(word, -INFINITY)) < f1) {
+#pragma unroll
+              for (int e = 0; e < W; ++e) {
+                const float f = place(v.v[e]);
+                if (f >= f0 && f < f1) in |= 1u << e;
+              }
             }
+            hits |= (unsigned long long)in << ((q * kWords + j) * W);
           }
-          if (with_sums) {
-#pragma unroll
-            for (int e = 0; e < W; ++e) sum += sp_pick((top - v.v[e]) * scale < f0, weight(v.v[e]));
+          if (by_weight) {
+            sum = warp_total(sum);
+            if (lane == 0) s_block[b] = sum;
           }
         }
-        if (with_sums) {
-          sum = warp_total(sum);
-          if (lane == 0) s_block[b] = sum;
+        if (__any_sync(0xffffffffu, hits != 0ull)) {
+          const int count = __popcll(hits);
+          int at = count;
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, at, d);
+            if (lane >= d) at += o;
+          }
+          int first = 0;
+          if (lane == 31) first = atomicAdd(&s_int, at);
+          at += __shfl_sync(0xffffffffu, first, 31) - count;
+          for (; hits; hits &= hits - 1ull, ++at) {
+            const int bit = __ffsll((long long)hits) - 1, seq = bit / W;
+            const int i = ((b0 + seq / kWords * kSpWarps) * kBlockWords + seq % kWords * 32 + lane) * W + bit % W - skew;
+            if (at < list_room) s_work.list[at] = (unsigned long long)sp_key(logit(i)) << 32 | (uint32_t)~(i0 + i);
+          }
         }
       }
+      if (by_weight) row_sum = cta_sum(row_sum);
       __syncthreads();
       double above = 0.0;
-      if (with_sums)
+      if (by_weight)
         for (int b = 0; b < blocks; b += 32) above += warp_total(b + lane < blocks ? s_block[b + lane] : 0.0);
       // to everybody, in places of this CTA's own
       const int room = 2 * kSpList / (int)cluster, mine_here = s_int;
       for (int i = tid; i < min(mine_here, room) * (int)cluster; i += kSpThreads)
         asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(map_to_rank(smem_u32(&s_work.all[rank * room + i / (int)cluster]), (uint32_t)i & (cluster - 1))), "l"(s_work.list[i / (int)cluster]) : "memory");
       if (tid < (int)cluster) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_rank(smem_u32(&s_counts[rank]), (uint32_t)tid)), "r"(mine_here) : "memory");
-      tell(above, 0);
-      if (with_sums) {
-        above = told_sum();
+      tell(above, 0, row_sum);
+      if (by_weight) {
+        const SpSlot o = told(lane < (int)cluster ? lane : 0);
+        above = in_order(o.d), sum_all = in_order(o.e);
         if (tid == 0) s_double = above;
       }
       int upto = lane < (int)cluster ? min(s_counts[lane], room + 1) : 0;
@@ -479,22 +518,21 @@ sample_kernel(SampleArgs a) {
       }
       const int members = __shfl_sync(0xffffffffu, upto, (int)cluster - 1);
       if (spilt || members > kSpList) return -1;
-      // in order: a member's place is the number of those in front of it (four lanes a member)
+      // side by side, then in order: a member's place is the number of those in front of it (four lanes a member)
+      for (int i = tid; i - lane < members; i += kSpThreads) {
+        int from_cta = 0, start = 0;
+        for (int c = 0; c < (int)cluster - 1; ++c) {
+          const int end = __shfl_sync(0xffffffffu, upto, c);
+          if (i >= end) from_cta = c + 1, start = end;
+        }
+        if (i < members) s_work.list[i] = s_work.all[from_cta * room + i - start];
+      }
+      __syncthreads();
       for (int i = tid >> 2; i - (lane >> 2) < members; i += kSpThreads / 4) {
-        unsigned long long e = 0ull;
-        int place = 0, start = 0;
-        for (int c = 0; c < (int)cluster; ++c) {
-          const int end = __shfl_sync(0xffffffffu, upto, c);
-          if (i >= start && i < end) e = s_work.all[c * room + i - start];
-          start = end;
-        }
-        start = 0;
-        for (int c = 0; c < (int)cluster; ++c) {
-          const int end = __shfl_sync(0xffffffffu, upto, c);
+        const unsigned long long e = s_work.list[min(i, members - 1)];
+        int place = 0;
 #pragma unroll 4
-          for (int j = lane & 3; j < end - start; j += 4) place += s_work.all[c * room + j] > e;
-          start = end;
-        }
+        for (int j = lane & 3; j < members; j += 4) place += s_work.list[j] > e;
         place += __shfl_xor_sync(0xffffffffu, place, 1);
         place += __shfl_xor_sync(0xffffffffu, place, 2);
         if (i < members && (lane & 3) == 0) {
@@ -505,15 +543,16 @@ sample_kernel(SampleArgs a) {
       __syncthreads();
       return members;
     };
-    // Counts or weighs candidates in bins, sums the row (by_weight), and finds the bins [from, to] in which the goal lies: `goal` in members, or in parts of the sum.
-    // Returns what lies above them, in members (by_weight: at most as many), or -1.
-    double sum_all = 0.0;
+    // Counts or weighs candidates in bins and finds those, [from, to], in which the goal lies: `goal` in members, or in parts of the sum (both in fp32, and so known to some 10^-5: where
+    // the goal lies nearer than that to a border of bins, both of its sides are taken).  Returns what lies above them, in members (by_weight: at most as many), or -1.
     int from = 0, to = kSpBins - 1, inside = 0;
+    int count0 = 0;                        // what lies above `base`
+    double weight0 = 0.0, border_weight = 0.0, sum_row = 0.0;
     auto look = [&](bool by_weight, double goal) {
       for (int i = tid; i < kSpBins; i += kSpThreads) s_work.bins[i] = 0u;
       __syncthreads();
-      double sum = 0.0;
-      const float fall = -0.69314718f * (float)octaves / kSpBins;          // of a bin
+      float sum = 0.f;
+      const float drop = -(float)octaves / kSpBins, fall = 0.69314718f * drop / zoom;   // of a bin, as powers of 2 and of e
 #pragma unroll 1
       for (int w = tid; w < all_words; w += kSpThreads) {
         Vec16<T> v;
@@ -521,20 +560,22 @@ sample_kernel(SampleArgs a) {
 #pragma unroll
         for (int e = 0; e < W; ++e) {
           // Conversions by sums with 2^23: the instructions take 8 clocks a warp.
-          const float f = (top - v.v[e]) * scale, down = __fadd_rd(f, 8388608.f);
+          const float far = (top - v.v[e]) * scale, f = (far - base) * zoom, down = __fadd_rd(f, 8388608.f);
           uint32_t member = 1u;
           if (by_weight) {
-            sum += weight(v.v[e]);
-            const float y = (f - (down - 8388608.f)) * fall;       // exp(y) to y^3 / 6, 4.5e-6 at most
-            member = __float_as_uint(fmaf(fmaf(0.5f * 131072.f, y, 131072.f), y, 131072.f + 8388608.f)) - 0x4b000000u;       // 17 bits; a part has fewer than 2^15 members
+            float g;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(g) : "f"(far * drop));
+            sum += g;
+            const float y = (f - (down - 8388608.f)) * fall;       // exp(y) to y^4 / 24, 3e-8
+            member = __float_as_uint(fmaf(fmaf(fmaf(131072.f / 6.f, y, 0.5f * 131072.f), y, 131072.f), y, 131072.f + 8388608.f)) - 0x4b000000u;       // 17 bits; a part has fewer than 2^15 members
           }
-          if (f < (float)kSpBins) atomicAdd(&s_work.bins[__float_as_uint(down) - 0x4b000000u], member);
+          if (f >= 0.f && f < (float)kSpBins) atomicAdd(&s_work.bins[__float_as_uint(down) - 0x4b000000u], member);
         }
       }
       if (by_weight) {
-        tell(cta_sum(sum), 0);
-        sum_all = told_sum();
-        goal *= sum_all;
+        tell(cta_sum((double)sum), 0);
+        sum_row = told_sum();                // the same when looked at closer
+        goal *= sum_row;
       } else {
         meet();
       }
@@ -556,7 +597,7 @@ sample_kernel(SampleArgs a) {
           }
           if (by_weight) {
             v[j] = (uint32_t)(sum_m * (1.0 / 131072) * 1.04) + (sum_m > 0.0);        // a bin is 0.043 octaves wide at most: never fewer than there are
-            m[j] = sum_m * exp2(octaves * (-1.0 / kSpBins) * (bin0 + j)) * (1.0 / 131072);
+            m[j] = sum_m * exp2(octaves * (-1.0 / kSpBins) * ((double)base + (bin0 + j) / (double)zoom)) * (1.0 / 131072);
           }
         }
       }
@@ -579,7 +620,7 @@ sample_kernel(SampleArgs a) {
         if (w == warp) cc += sum_c, cm += sum_w;
         sum_c += s_scan_c[w], sum_w += s_warp[w];
       }
-      if (tid == 0) s_border = SpBorder{kSpBins, 0, -1, 0};
+      if (tid == 0) s_border = SpBorder{kSpBins, 0, -1, 0, 0.0};
       if (cluster > 1) {                   // what the CTAs in front have
         tell(sum_w, (int)sum_c);
         const SpSlot o = told(lane < (int)cluster ? lane : 0);
@@ -587,15 +628,17 @@ sample_kernel(SampleArgs a) {
       } else {
         __syncthreads();
       }
-      uint32_t before = cc - c4;
-      double before_m = cm - m4;
-      const double slack = by_weight ? 1e-5 * sum_all : 0.0;          // 17 bits a member, and the difference of the two forms of its weight
+      uint32_t before = (uint32_t)count0 + cc - c4;
+      double before_m = weight0 + cm - m4;
+      // The place of a logit is off by 2^-23 of 1024 bins of 0.043 octaves at most, 3.6e-6 of its weight, in the bins as in the row's sum; a share by half of 2^-17, the power by 2^-22.
+      const double slack = by_weight ? 1.2e-5 * sum_row : 0.0;
       int first_bin = kSpBins, last_bin = -1, first_before = 0, last_end = 0;
+      double first_weight = 0.0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if (v[j] > 0u) {
           const bool starts = by_weight ? before_m + m[j] >= goal - slack : (double)(before + v[j]) >= goal, ends = by_weight ? before_m < goal + slack : (double)before < goal;
-          if (starts && first_bin == kSpBins) first_bin = bin0 + j, first_before = (int)before;
+          if (starts && first_bin == kSpBins) first_bin = bin0 + j, first_before = (int)before, first_weight = before_m;
           if (ends) last_bin = bin0 + j, last_end = (int)(before + v[j]);
         }
         before += v[j], before_m += m[j];
@@ -604,20 +647,22 @@ sample_kernel(SampleArgs a) {
       if (lane == 0 && wf < kSpBins) atomicMin(&s_border.from, wf);
       if (lane == 0 && wl >= 0) atomicMax(&s_border.to, wl);
       __syncthreads();
-      if (first_bin < kSpBins && first_bin == s_border.from) s_border.before = first_before;
+      if (first_bin < kSpBins && first_bin == s_border.from) s_border.before = first_before, s_border.weight = first_weight;
       if (last_bin >= 0 && last_bin == s_border.to) s_border.end = last_end;
       SpBorder o;
       meet();
       {
         const uint32_t at = map_to_rank(smem_u32(&s_border), (uint32_t)(lane < (int)cluster ? lane : 0));
         asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(o.from), "=r"(o.before), "=r"(o.to), "=r"(o.end) : "r"(at) : "memory");
+        asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(o.weight) : "r"(at + 16u) : "memory");
       }
       from = __reduce_min_sync(0xffffffffu, o.from), to = __reduce_max_sync(0xffffffffu, o.to);
       if (to < 0) return -1;
       const int has_from = __ffs(__ballot_sync(0xffffffffu, o.from == from)) - 1, has_to = __ffs(__ballot_sync(0xffffffffu, o.to == to)) - 1;
       const int end = __shfl_sync(0xffffffffu, o.end, has_to);
       int above = __shfl_sync(0xffffffffu, o.before, has_from);
-      if (from > to) from = to, above = max(0, end - 1);        // the sum of all bins falls short of the goal by its rounding: the last of them (its own members count once)
+      border_weight = __shfl_sync(0xffffffffu, o.weight, has_from);
+      if (from > to) return -1;              // the sum of all bins falls short of the goal
       inside = end - above;
       return above;
     };
@@ -627,24 +672,34 @@ sample_kernel(SampleArgs a) {
     if (k && k <= kSpThreads) {
       // A logit that k of the groups' maxima reach, by halving what lies between the smallest and the largest, until no more than a quarter more do.
       if (warp == 0) {
-        uint32_t v[kSpThreads / 16], low = 0xffffffffu;      // 16 maxima a lane
+        uint32_t v[16], low = 0xffffffffu;      // 16 maxima a lane
         int some = 0;
 #pragma unroll
-        for (int j = 0; j < kSpThreads / 16; ++j) {
+        for (int j = 0; j < 16; ++j) {
           const int at = j * 32 + lane;
           v[j] = 0u;
           if (at < groups * (int)cluster)
             asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v[j]) : "r"(map_to_rank(smem_u32(&s_work.groups[at & (groups - 1)]), (uint32_t)at / (uint32_t)groups)) : "memory");
-          if (v[j] <= sp_key(-INFINITY)) v[j] = 0u;          // has none
+        }
+        const bool fold = k <= 64;              // 128 groups are enough
+        if (fold)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] = max(max(v[j], v[j + 4]), max(v[j + 8], v[j + 12]));
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          if (v[j] <= sp_key(-INFINITY) || (fold && j >= 4)) v[j] = 0u;          // has none
           else low = min(low, v[j]), ++some;
         }
         low = __reduce_min_sync(0xffffffffu, low), some = __reduce_add_sync(0xffffffffu, some);
         uint32_t high = peak;
-        for (int t = 0; t < 20 && some > k + k / 4 && high - low > 1; ++t) {
+        for (int t = 0; t < 20 && some > max(k + k / 4, 32) && high - low > 1; ++t) {
           const uint32_t mid = low + (high - low) / 2;
           int c = 0;
 #pragma unroll
-          for (int j = 0; j < kSpThreads / 16; ++j) c += v[j] >= mid;
+          for (int j = 0; j < 4; ++j) c += v[j] >= mid;
+          if (!fold)
+#pragma unroll
+            for (int j = 4; j < 16; ++j) c += v[j] >= mid;
           c = __reduce_add_sync(0xffffffffu, c);
           if (c >= k) low = mid, some = c;
           else high = mid;
@@ -675,59 +730,72 @@ sample_kernel(SampleArgs a) {
         if (!direct) {
           above = look(!k, goal);
           complete = above >= 0 && above + inside <= kSpList;
-          if (above < 0 || (k && inside > kSpList)) break;
+          if (above < 0) break;
+          if (!complete && inside > kSpList) {
+            if (zoom > 1.f) break;           // equal logits, then
+            base = (float)from, zoom = 1023.9f / (float)(to - from + 1);        // `far` - base is exact: what lay in these bins lies in the new ones, and nothing else
+            count0 = above, weight0 = border_weight;
+            continue;
+          }
         }
-        members = gather(complete ? 0 : from, to, !k && !complete);
+        members = gather(complete ? 0 : from, to, !k);
         whole = complete && members > 0;
         if (!direct || members >= 0) break;
         direct = false;
       }
     }
     if (whole) {
-      // all from the list: what is kept of it, and their total, in order
+      // all from the list: what is kept of it, and their total.  Running sums by warps of 32, then over those in front.
       if (k) members = min(members, k);
-      if (warp == 0) {
-        double want = INFINITY;
-        if (by_p) {
-          double sum = sum_all;
-          if (k) {
-            sum = 0.0;
-            for (int i = 0; i < members; i += 32) sum += warp_total(i + lane < members ? s_work.weight[i + lane] : 0.0);
-          }
-          want = (double)p * sum;
+      double w[2], cum[2];
+      static_assert(kSpList == 2 * kSpThreads, "a thread has two members");
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int i = r * kSpThreads + tid;
+        w[r] = i < members ? s_work.weight[i] : 0.0, cum[r] = 0.0;
+        if (i - lane < members) {
+          cum[r] = warp_scan(w[r], lane);
+          if (lane == 31) s_chunk[i >> 5] = cum[r];
         }
-        double before = 0.0;
-        int j = 0;
-        for (int i = 0; i < members; i += 32) {
-          const double w = i + lane < members ? s_work.weight[i + lane] : 0.0, cum = before + warp_scan(w, lane);
-          const bool in = i + lane < members && cum - w < want && !(by_m && w < (double)m);
-          const unsigned b = __ballot_sync(0xffffffffu, in || (i == 0 && lane == 0));
-          const int n = b == 0xffffffffu ? 32 : __ffs(~b) - 1;
-          j += n;
-          before = n > 0 ? __shfl_sync(0xffffffffu, cum, n - 1) : before;
-          if (n < 32) break;
-        }
-        if (lane == 0) s_int = j, s_double = before;
       }
       __syncthreads();
-      cut = s_int, total = s_double;
+      double want = INFINITY, sum = 0.0;
+#pragma unroll
+      for (int c = 0; c < kSpList / 32; ++c) {
+        if (c * 32 < members) {
+          if (c == warp) cum[0] += sum;
+          if (c == warp + kSpWarps) cum[1] += sum;
+          sum += s_chunk[c];
+        }
+      }
+      if (by_p) want = (double)p * (k ? sum : sum_all);
+      cut = 0;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int i = r * kSpThreads + tid;
+        if (r * kSpThreads < members) cut += __syncthreads_count(i < members && ((cum[r] - w[r] < want && !(by_m && w[r] < (double)m)) || i == 0));
+      }
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+        if (r * kSpThreads + tid == cut - 1) s_double = cum[r];
+      if (tid == 0) s_int = 0x7fffffff, s_int2 = -1;
+      __syncthreads();
+      total = s_double;
       const unsigned long long e = s_work.sorted[cut - 1];
       last = sp_logit((uint32_t)(e >> 32)), last_at = (int)~(uint32_t)e;
-      __syncthreads();
       if (a.tokens) {
-        // by index: the first class with which the running sum passes the goal; or the last that weighs anything
+        // by index: the first class with which the running sum passes the goal; or the last that weighs anything (four lanes a member)
         goal = fmax((double)u * total, 0.0);
-        if (tid == 0) s_int = 0x7fffffff, s_int2 = -1;
-        __syncthreads();
-        for (int i = tid; i < cut; i += kSpThreads) {
-          const uint32_t at = (uint32_t)s_work.sorted[i];          // the larger, the lower the index
-          const double w = s_work.weight[i];
+        for (int i = tid >> 2; i - (lane >> 2) < cut; i += kSpThreads / 4) {
+          const uint32_t at = (uint32_t)s_work.sorted[min(i, cut - 1)];          // the larger, the lower the index
+          const double g = s_work.weight[min(i, cut - 1)];
           double before = 0.0;
-#pragma unroll 4
-          for (int j = 0; j < cut; ++j)
-            if ((uint32_t)s_work.sorted[j] > at) before += s_work.weight[j];
-          if (w > 0.0) {
-            if (before + w > goal) atomicMin(&s_int, (int)~at);
+#pragma unroll 2
+          for (int j = lane & 3; j < cut; j += 4) before += sp_pick((uint32_t)s_work.sorted[j] > at, s_work.weight[j]);
+          before += __shfl_xor_sync(0xffffffffu, before, 1);
+          before += __shfl_xor_sync(0xffffffffu, before, 2);
+          if (g > 0.0 && i < cut && (lane & 3) == 0) {
+            if (before + g > goal) atomicMin(&s_int, (int)~at);
             atomicMax(&s_int2, (int)~at);
           }
         }
@@ -785,13 +853,14 @@ sample_kernel(SampleArgs a) {
       // ---- sums of blocks, the total, and the block in which the running sum passes its goal
       if (summed) {
         // those of the list that are kept join their blocks, in order
-        for (int b = tid; b < blocks; b += kSpThreads) {
-          double s = s_block[b];
-          for (int j = 0; j < cut; ++j) {
+        for (int b = warp; b < blocks; b += kSpWarps) {
+          double s = 0.0;
+          for (int j = lane; j < cut; j += 32) {
             const int at = (int)~(uint32_t)s_work.sorted[j] - i0;
-            if (at >= 0 && at < cnt && (at + skew) / kSpBlock == b) s += s_work.weight[j];
+            s += sp_pick(at >= 0 && at < cnt && (at + skew) / kSpBlock == b, s_work.weight[j]);
           }
-          s_block[b] = s;
+          s = warp_total(s);
+          if (lane == 0) s_block[b] += s;
         }
       } else {
 #pragma unroll 1
@@ -872,23 +941,17 @@ sample_kernel(SampleArgs a) {
       mine = rank == 0;
     }
     if (probs) {
-      const double part_of = 1.0 / total;
-      if (all) {
+      // w / total in fp32: the exponent's fraction to 2^-23, the power to two units.  Who weighs at least m is asked in fp64, where the last member does not say it.
+      const float ch = fminf((float)weight.c, FLT_MAX), cl = ch < FLT_MAX ? (float)(weight.c - (double)ch) : 0.f, part_of = (float)(1.0 / total);
+      const bool ask = by_m && !whole;
 #pragma unroll 4
-        for (int i = tid; i < cnt; i += kSpThreads) {
-          const double g = weight(logit(i));
-          probs[i] = (float)sp_pick(g >= least, g * part_of);
-        }
-      } else if (whole) {                  // few, and most warps have none
-#pragma unroll 4
-        for (int i = tid; i < cnt; i += kSpThreads) probs[i] = (float)(mass(logit(i), i) * part_of);
-      } else {
-#pragma unroll 4
-        for (int i = tid; i < cnt; i += kSpThreads) {
-          const float l = logit(i);
-          const double g = weight(l);
-          probs[i] = (float)sp_pick(g >= least && kept(l, i), g * part_of);
-        }
+      for (int i = tid; i < cnt; i += kSpThreads) {
+        const float l = logit(i), d = l - top, r = fmaf(d, ch, 12582912.f), z = r - 12582912.f;
+        float g;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(g) : "f"(fmaf(d, cl, fmaf(d, ch, -z))));
+        g *= part_of * __int_as_float(max(__float_as_int(r) - 0x4b400000 + 127, 0) << 23);
+        const bool in = z >= -126.f && kept(l, i) && (!ask || weight(l) >= least);
+        probs[i] = in ? g : 0.f;
       }
     }
   }
