@@ -31,7 +31,7 @@ constexpr int kSpPart = 16384;           // elements of a CTA's part that a clus
 constexpr int kSpMaxCluster = 16, kSpMaxPart = 38400;
 constexpr int kSpBlock = 512;            // elements of a block whose sum is kept
 constexpr int kSpMost = kSpMaxCluster * kSpMaxPart;
-constexpr int kSpBins = 1024, kSpList = 512;
+constexpr int kSpBins = 2048, kSpList = 512;
 constexpr int kSpTable = 16;
 
 struct SampleArgs {
@@ -142,6 +142,11 @@ struct SpFound {           // the digit, and what lies above it
   int digit;
   int above, in;
 };
+struct SpKept {            // the last member, what is kept of the list, and its weight
+  float last;
+  int last_at;
+  double total;
+};
 struct SpBorder {          // of a CTA's bins: the first in which the goal may lie and what lies before it (and its weight), the last and what lies up to its end
   int from, before, to, end;
   double weight;
@@ -149,10 +154,10 @@ struct SpBorder {          // of a CTA's bins: the first in which the goal may l
 struct alignas(16) SpWork {              // bins are read four at a time
   union {
     uint32_t bins[kSpBins];              // members of a bin, or their weight; read by the others
-    unsigned long long all[2 * kSpList]; // the lists of all CTAs, as many places each; after that
+    unsigned long long all[2 * kSpList]; // the lists of all CTAs, as many places each, written by them into the first CTA's; after that
   };
   union {
-    unsigned long long list[kSpList];    // logit << 32 | ~index; read by the others
+    unsigned long long list[kSpList];    // logit << 32 | ~index
     uint32_t groups[kSpThreads];         // maxima of groups of lanes; read by the others, before that
   };
   union {
@@ -179,6 +184,7 @@ sample_kernel(SampleArgs a) {
   __shared__ SpFound s_found;
   __shared__ __align__(16) SpBorder s_border;
   __shared__ int s_counts[kSpMaxCluster];
+  __shared__ __align__(16) SpKept s_kept;
   __shared__ int s_int, s_int2;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   uint32_t rank, cluster;
@@ -423,14 +429,15 @@ sample_kernel(SampleArgs a) {
     };
 
     // ---- few candidates.  Bins of width 1 / scale in the logit, below the maximum; what lies beyond the last of them is no candidate.
+    const int n_bins = cluster == 1 ? kSpBins / 2 : kSpBins;          // four a thread at most
     float scale = 0.f, base = 0.f, zoom = 1.f;        // looked at closer, the bins divide what lies from `base` on
     double octaves = 0.0;                  // of all bins, for weights
     auto place = [&](float l) { return ((top - l) * scale - base) * zoom; };
-    // The list: members whose bin lies in [from, to], in order, with their weights.  by_weight: and the exact sum of the row in sum_all, of blocks of what lies above them in s_block, and of
+    // The list: members whose place lies in [f0, f1); in the first CTA that of all CTAs, in order, with their weights, in another its own.  by_weight: and the exact sum of the row in sum_all, of blocks of what lies above them in s_block, and of
     // the row of those in s_double.  Returns how many members there are, or -1: more than the list has room for.
     double sum_all = 0.0;
-    auto gather = [&](int from, int to, bool by_weight) {
-      const float f0 = (float)from, f1 = (float)(to + 1);
+    int own = 0;                           // members of this CTA's part
+    auto gather = [&](float f0, float f1, bool by_weight) {
       const int list_room = min(2 * kSpList / (int)cluster, kSpList);
       if (tid == 0) s_int = 0;
       __syncthreads();
@@ -498,11 +505,12 @@ sample_kernel(SampleArgs a) {
       double above = 0.0;
       if (by_weight)
         for (int b = 0; b < blocks; b += 32) above += warp_total(b + lane < blocks ? s_block[b + lane] : 0.0);
-      // to everybody, in places of this CTA's own
-      const int room = 2 * kSpList / (int)cluster, mine_here = s_int;
-      for (int i = tid; i < min(mine_here, room) * (int)cluster; i += kSpThreads)
-        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(map_to_rank(smem_u32(&s_work.all[rank * room + i / (int)cluster]), (uint32_t)i & (cluster - 1))), "l"(s_work.list[i / (int)cluster]) : "memory");
-      if (tid < (int)cluster) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_rank(smem_u32(&s_counts[rank]), (uint32_t)tid)), "r"(mine_here) : "memory");
+      // to the first CTA, in places of this CTA's own
+      const int room = 2 * kSpList / (int)cluster;
+      own = s_int;
+      for (int i = tid; i < min(own, list_room); i += kSpThreads)
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(map_to_rank(smem_u32(&s_work.all[rank * room + i]), 0u)), "l"(s_work.list[i]) : "memory");
+      if (tid < (int)cluster) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_rank(smem_u32(&s_counts[rank]), (uint32_t)tid)), "r"(own) : "memory");
       tell(above, 0, row_sum);
       if (by_weight) {
         const SpSlot o = told(lane < (int)cluster ? lane : 0);
@@ -518,6 +526,7 @@ sample_kernel(SampleArgs a) {
       }
       const int members = __shfl_sync(0xffffffffu, upto, (int)cluster - 1);
       if (spilt || members > kSpList) return -1;
+      if (rank != 0) return members;
       // side by side, then in order: a member's place is the number of those in front of it (four lanes a member)
       for (int i = tid; i - lane < members; i += kSpThreads) {
         int from_cta = 0, start = 0;
@@ -545,14 +554,14 @@ sample_kernel(SampleArgs a) {
     };
     // Counts or weighs candidates in bins and finds those, [from, to], in which the goal lies: `goal` in members, or in parts of the sum (both in fp32, and so known to some 10^-5: where
     // the goal lies nearer than that to a border of bins, both of its sides are taken).  Returns what lies above them, in members (by_weight: at most as many), or -1.
-    int from = 0, to = kSpBins - 1, inside = 0;
+    int from = 0, to = n_bins - 1, inside = 0;
     int count0 = 0;                        // what lies above `base`
     double weight0 = 0.0, border_weight = 0.0, sum_row = 0.0;
     auto look = [&](bool by_weight, double goal) {
-      for (int i = tid; i < kSpBins; i += kSpThreads) s_work.bins[i] = 0u;
+      for (int i = tid; i < n_bins; i += kSpThreads) s_work.bins[i] = 0u;
       __syncthreads();
       float sum = 0.f;
-      const float drop = -(float)octaves / kSpBins, fall = 0.69314718f * drop / zoom;   // of a bin, as powers of 2 and of e
+      const float drop = -(float)octaves / n_bins, fall = 0.69314718f * drop / zoom;   // of a bin, as powers of 2 and of e
 #pragma unroll 1
       for (int w = tid; w < all_words; w += kSpThreads) {
         Vec16<T> v;
@@ -569,7 +578,7 @@ sample_kernel(SampleArgs a) {
             const float y = (f - (down - 8388608.f)) * fall;       // exp(y) to y^4 / 24, 3e-8
             member = __float_as_uint(fmaf(fmaf(fmaf(131072.f / 6.f, y, 0.5f * 131072.f), y, 131072.f), y, 131072.f + 8388608.f)) - 0x4b000000u;       // 17 bits; a part has fewer than 2^15 members
           }
-          if (f >= 0.f && f < (float)kSpBins) atomicAdd(&s_work.bins[__float_as_uint(down) - 0x4b000000u], member);
+          if (f >= 0.f && f < (float)n_bins) atomicAdd(&s_work.bins[__float_as_uint(down) - 0x4b000000u], member);
         }
       }
       if (by_weight) {
@@ -580,7 +589,7 @@ sample_kernel(SampleArgs a) {
         meet();
       }
       // This CTA adds up its part of the bins over the cluster (all of them would be 32 KB from other SMs, at 16 bytes a clock).
-      const int share = kSpBins / (int)cluster, each = max(1, share / kSpThreads), bin0 = (int)rank * share + tid * each;
+      const int share = n_bins / (int)cluster, each = max(1, share / kSpThreads), bin0 = (int)rank * share + tid * each;
       const bool has = tid * each < share;
       uint32_t v[4] = {0u, 0u, 0u, 0u};
       double m[4] = {0.0, 0.0, 0.0, 0.0};
@@ -597,7 +606,7 @@ sample_kernel(SampleArgs a) {
           }
           if (by_weight) {
             v[j] = (uint32_t)(sum_m * (1.0 / 131072) * 1.04) + (sum_m > 0.0);        // a bin is 0.043 octaves wide at most: never fewer than there are
-            m[j] = sum_m * exp2(octaves * (-1.0 / kSpBins) * ((double)base + (bin0 + j) / (double)zoom)) * (1.0 / 131072);
+            m[j] = sum_m * exp2(-octaves / n_bins * ((double)base + (bin0 + j) / (double)zoom)) * (1.0 / 131072);
           }
         }
       }
@@ -708,14 +717,14 @@ sample_kernel(SampleArgs a) {
       }
       __syncthreads();
       const uint32_t low = (uint32_t)s_int;
-      scale = fminf(1023.9f / (top - sp_logit(low)), FLT_MAX);
+      scale = fminf(0.9995f * (float)n_bins / (top - sp_logit(low)), FLT_MAX);
       listed = low != 0u && scale > 0.f;
       direct = true;
       goal = (double)k;
       meet();                              // the maxima have been read: the lists come in their place
     } else if (!k && by_p) {
       octaves = (log2((double)a.n) - log2(1.0 - (double)p)) * 1.0001;     // 1 - p is exact; the total is 1 at least
-      scale = (float)(kSpBins * weight.c / octaves);
+      scale = (float)(n_bins * weight.c / octaves);
       listed = scale > 0.f && scale < FLT_MAX && a.per <= 32767;
       goal = (double)p;
     }
@@ -733,18 +742,18 @@ sample_kernel(SampleArgs a) {
           if (above < 0) break;
           if (!complete && inside > kSpList) {
             if (zoom > 1.f) break;           // equal logits, then
-            base = (float)from, zoom = 1023.9f / (float)(to - from + 1);        // `far` - base is exact: what lay in these bins lies in the new ones, and nothing else
+            base = (float)from, zoom = 0.9995f * (float)n_bins / (float)(to - from + 1);        // `far` - base is exact: what lay in these bins lies in the new ones, and nothing else
             count0 = above, weight0 = border_weight;
             continue;
           }
         }
-        members = gather(complete ? 0 : from, to, !k);
+        members = gather(complete ? -FLT_MAX : (float)from, (float)(to + 1), !k);
         whole = complete && members > 0;
         if (!direct || members >= 0) break;
         direct = false;
       }
     }
-    if (whole) {
+    if (whole && rank == 0) {
       // all from the list: what is kept of it, and their total.  Running sums by warps of 32, then over those in front.
       if (k) members = min(members, k);
       double w[2], cum[2];
@@ -782,7 +791,7 @@ sample_kernel(SampleArgs a) {
       __syncthreads();
       total = s_double;
       const unsigned long long e = s_work.sorted[cut - 1];
-      last = sp_logit((uint32_t)(e >> 32)), last_at = (int)~(uint32_t)e;
+      if (tid == 0) s_kept = SpKept{sp_logit((uint32_t)(e >> 32)), (int)~(uint32_t)e, total};
       if (a.tokens) {
         // by index: the first class with which the running sum passes the goal; or the last that weighs anything (four lanes a member)
         goal = fmax((double)u * total, 0.0);
@@ -802,30 +811,55 @@ sample_kernel(SampleArgs a) {
         __syncthreads();
         token = s_int != 0x7fffffff ? s_int : s_int2;
       }
-    } else {
-      bool need_k = k != 0, need_p = by_p;
-      if (members > 0 && k) {              // the bin in which the k-th lies
-        const unsigned long long e = s_work.sorted[k - above - 1];
-        last = sp_logit((uint32_t)(e >> 32)), last_at = (int)~(uint32_t)e;
-        need_k = false;
-      } else if (members > 0) {            // the bins in which the p-th part ends
-        if (warp == 0) {
-          double before = s_double;
-          int j = 0;
-          for (int i = 0; i < members; i += 32) {
-            const double w = i + lane < members ? s_work.weight[i + lane] : 0.0, cum = before + warp_scan(w, lane);
-            j += __popc(__ballot_sync(0xffffffffu, i + lane < members && cum - w < goal * sum_all));
-            before = __shfl_sync(0xffffffffu, cum, 31);
+    }
+    bool need_k = k != 0, need_p = by_p;
+    if (!whole && members > 0) {
+      if (rank == 0) {
+        if (k) {                             // the bin in which the k-th lies
+          cut = k - above;
+        } else {                             // the bins in which the p-th part ends
+          if (warp == 0) {
+            double before = s_double;
+            int j = 0;
+            for (int i = 0; i < members; i += 32) {
+              const double w = i + lane < members ? s_work.weight[i + lane] : 0.0, cum = before + warp_scan(w, lane);
+              j += __popc(__ballot_sync(0xffffffffu, i + lane < members && cum - w < goal * sum_all));
+              before = __shfl_sync(0xffffffffu, cum, 31);
+            }
+            if (lane == 0) s_int = max(j, 1);
           }
-          if (lane == 0) s_int = max(j, 1);
+          __syncthreads();
+          cut = s_int;
         }
-        __syncthreads();
-        cut = s_int;
         const unsigned long long e = s_work.sorted[cut - 1];
-        last = sp_logit((uint32_t)(e >> 32)), last_at = (int)~(uint32_t)e;
-        need_p = false;
-        summed = !by_m;
+        if (tid == 0) s_kept = SpKept{sp_logit((uint32_t)(e >> 32)), (int)~(uint32_t)e, 0.0};
+      } else if (!k && !by_m) {
+        // This CTA's members, in order, for the sums of its blocks.
+        cut = own;
+        for (int i = tid >> 2; i - (lane >> 2) < own; i += kSpThreads / 4) {
+          const unsigned long long e = s_work.list[min(i, own - 1)];
+          int place = 0;
+#pragma unroll 4
+          for (int j = lane & 3; j < own; j += 4) place += s_work.list[j] > e;
+          place += __shfl_xor_sync(0xffffffffu, place, 1);
+          place += __shfl_xor_sync(0xffffffffu, place, 2);
+          if (i < own && (lane & 3) == 0) {
+            s_work.sorted[place] = e;
+            s_work.weight[place] = weight(sp_logit((uint32_t)(e >> 32)));
+          }
+        }
       }
+      need_k = need_k && !k, need_p = need_p && k;
+      summed = !k && !by_m;
+    }
+    if (members > 0 && !(whole && !probs && u > 0.f)) {      // everybody needs to know
+      meet();
+      const uint32_t at = map_to_rank(smem_u32(&s_kept), 0u);
+      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(last) : "r"(at) : "memory");
+      asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(last_at) : "r"(at + 4u) : "memory");
+      if (whole) asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(total) : "r"(at + 8u) : "memory");
+    }
+    if (!whole) {
 #pragma unroll 1
       for (int by_weight = 0; by_weight < 2; ++by_weight) {
         if (!(by_weight ? need_p : need_k)) continue;
@@ -857,7 +891,7 @@ sample_kernel(SampleArgs a) {
           double s = 0.0;
           for (int j = lane; j < cut; j += 32) {
             const int at = (int)~(uint32_t)s_work.sorted[j] - i0;
-            s += sp_pick(at >= 0 && at < cnt && (at + skew) / kSpBlock == b, s_work.weight[j]);
+            s += sp_pick(at >= 0 && at < cnt && (at + skew) / kSpBlock == b && kept(sp_logit((uint32_t)(s_work.sorted[j] >> 32)), at), s_work.weight[j]);
           }
           s = warp_total(s);
           if (lane == 0) s_block[b] += s;
@@ -924,7 +958,7 @@ sample_kernel(SampleArgs a) {
         }
       }
     }
-    if (a.tokens && !(goal > 0.0)) {       // u is 0: the first that weighs anything, however little
+    if (a.tokens && !(u > 0.f)) {          // u is 0: the first that weighs anything, however little
       int at = 0x7fffffff;
       for (int i = tid; i < cnt; i += kSpThreads) {
         const float l = logit(i);
