@@ -1,8 +1,8 @@
 // Rows in 8 bits, and the projection of such rows.
 //
 // quantise: s = max |x| (1 / 127) of a row, both rounded to fp32, and q = the integer nearest to x / s, of two the even one.  The quotient is meant, not its rounding to
-// fp32: x times 1 / s is off by less than 127 * 2^-22 = 3e-5, so what lies within 1e-4 of the middle of two integers is divided again in fp64 (whose rounding
-// cannot reach the middle: x / s misses it by 2^-26 of itself at least, or not at all).  Bound by memory: a row is read once, kept in the registers of one, four or sixteen
+// fp32: x times 1 / s is off by less than 127 * 2^-23 (1 + 2^-1) = 2.3e-5, so what lies
+// within 3e-5 of the middle of two integers is held against the middle itself: x - (q + 1/2) s in one multiply-add, whose sign is exact.  Bound by memory: a row is read once, kept in the registers of one, four or sixteen
 // warps, whose exchange of the maximum is all they wait for.  Rows too long for that are read twice, from L2 the second time.
 //
 // dequantise: y = q s, rounded once.  Rows in any order.
@@ -26,241 +26,307 @@ __host__ __device__ constexpr int q_pitch(int c) { return (c + 15) / 16 * 16; } 
 
 // ----------------------------------------------------------------------------- quantise
 
-// |x| as an integer that orders like it; infinities and NaN lie from kQBad on.
-constexpr uint32_t kQBad = 0x7f800000u;
+// The larger magnitude, NaN where either is.
+__device__ __forceinline__ float q_max(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
 
-// B bytes of T as floats.
-template <typename T, int B> struct QVec {
-  static constexpr int N = B / (int)sizeof(T);
-  uint32_t w[(B + 3) / 4];
-  __device__ __forceinline__ void load(const T* p) {
-    if constexpr (B == 16) {
-      const uint4 t = *reinterpret_cast<const uint4*>(p);
-      w[0] = t.x, w[1] = t.y, w[2] = t.z, w[3] = t.w;
-    } else if constexpr (B == 8) {
-      const uint2 t = *reinterpret_cast<const uint2*>(p);
-      w[0] = t.x, w[1] = t.y;
-    } else if constexpr (B == 4) {
-      w[0] = *reinterpret_cast<const uint32_t*>(p);
-    } else {
-      w[0] = (uint32_t)*reinterpret_cast<const unsigned short*>(p);
-    }
-  }
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int i = 0; i < (B + 3) / 4; ++i) w[i] = 0u;
-  }
+// 16 bytes of T.
+template <typename T> struct QWord {
+  static constexpr int N = 16 / (int)sizeof(T);
+  uint32_t w[4];
+  __device__ __forceinline__ void set(uint4 t) { w[0] = t.x, w[1] = t.y, w[2] = t.z, w[3] = t.w; }
   __device__ __forceinline__ float at(int i) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
     return i & 1 ? __uint_as_float(w[i / 2] & 0xffff0000u) : __uint_as_float(w[i / 2] << 16);
   }
-  __device__ __forceinline__ uint32_t top(uint32_t t) const {
+  __device__ __forceinline__ float top(float t) const {
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) t = max(t, __float_as_uint(at(i)) & 0x7fffffffu);
-    return t;
+      for (int i = 0; i < N; ++i) t = q_max(t, fabsf(at(i)));
+      return t;
+    } else {                                            // two at a time
+      __nv_bfloat162 m[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(&m[i]) = w[i] & 0x7fff7fffu;
+      m[0] = __hmax2_nan(__hmax2_nan(m[0], m[1]), __hmax2_nan(m[2], m[3]));
+      return q_max(t, q_max(__low2float(m[0]), __high2float(m[0])));
+    }
   }
 };
 
 struct QScale {
   float s, inv;      // inv 0: everything is 0; s NaN: a row that is not finite
   bool tiny;         // 1 / s is no finite float
-  __device__ __forceinline__ explicit QScale(uint32_t top) {
-    s = top >= kQBad ? __uint_as_float(0x7fffffffu) : __uint_as_float(top) * (1.f / 127.f);
+  __device__ __forceinline__ explicit QScale(float top) {
+    s = top < INFINITY ? top * (1.f / 127.f) : __uint_as_float(0x7fffffffu);
     tiny = s < 1e-37f && s > 0.f;
-    inv = s > 0.f && !tiny ? 1.f / s : 0.f;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));       // to 2^-23
+    inv = s > 0.f && !tiny ? inv : 0.f;
   }
-  __device__ __noinline__ int slow(float x) const {
+  static __device__ __noinline__ int slow(float x, float s) {
     const double q = rint((double)x / (double)s);
     return (int)fmin(fmax(q, -127.0), 127.0);        // s below 2^-126 has fewer bits: x / s may pass 127
   }
-  // N values as bytes, four a word.
-  template <int N, typename V>
-  __device__ __forceinline__ void bytes(const V& v, uint32_t* out) const {
+  // A word as bytes, four a register.  By all lanes of a warp.
+  template <typename T>
+  __device__ __forceinline__ void bytes(const QWord<T>& v, uint32_t* out) const {
+    constexpr int N = QWord<T>::N;
     constexpr float kMagic = 12582912.f;             // 1.5 * 2^23: the sum's last place is 1, its low byte the integer
     float worst = 0.f;
     uint32_t b[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float t = v.at(i) * inv, r = t + kMagic;
-      worst = fmaxf(worst, fabsf(t - (r - kMagic)));
+      const float x = v.at(i), r = fmaf(x, inv, kMagic);
       b[i] = __float_as_uint(r);
+      worst = fmaxf(worst, fabsf(fmaf(x, inv, kMagic - r)));     // what is left of x / s
     }
-    if (!(inv > 0.f)) {                              // also where x * 0 is NaN
-#pragma unroll
-      for (int i = 0; i < N; ++i) b[i] = 0u;
-      worst = 0.f;
-    }
-    if (worst > 0.4999f || tiny) {
+    // Rare, and so asked for by whole warps: predicated, these were half of all instructions.
+    if (__any_sync(0xffffffffu, worst > 0.49997f || !(inv > 0.f))) {
+      const bool none = s != s;
+      // x against the middle between the integer and its neighbour: one multiply-add, whose sign is exact (a multiple of 2^-147 at least)
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float t = v.at(i) * inv;
-        if (tiny || fabsf(t - rintf(t)) > 0.4999f) b[i] = (uint32_t)slow(v.at(i));
+        const float x = v.at(i), n = __uint_as_float(b[i]) - kMagic, d = fmaf(x, inv, -n);
+        if (fabsf(d) > 0.49997f) {
+          const float half = n + copysignf(0.5f, d), e = fmaf(-half, s, x);
+          const float q = e == 0.f ? rintf(half) : half + copysignf(0.5f, e);
+          b[i] = __float_as_uint(q + kMagic);
+        }
+        if (none) b[i] = 0u;
+      }
+      if (__any_sync(0xffffffffu, tiny)) {
+#pragma unroll 1
+        for (int i = 0; i < N; ++i) {
+          float x = 0.f;
+#pragma unroll
+          for (int j = 0; j < N; ++j) x = i == j ? v.at(j) : x;
+          const uint32_t q = (uint32_t)slow(x, s);
+#pragma unroll
+          for (int j = 0; j < N; ++j) b[j] = i == j && tiny ? q : b[j];
+        }
       }
     }
 #pragma unroll
-    for (int i = 0; i < (N + 3) / 4; ++i) {
-      const uint32_t lo = __byte_perm(b[4 * i], N > 4 * i + 1 ? b[4 * i + (N > 1)] : 0u, 0x0040);
-      const uint32_t hi = N > 2 ? __byte_perm(b[N > 2 ? 4 * i + 2 : 0], b[N > 3 ? 4 * i + 3 : 0], 0x0040) : 0u;
-      out[i] = __byte_perm(lo, hi, 0x5410);
-    }
+    for (int i = 0; i < N / 4; ++i)
+      out[i] = __byte_perm(__byte_perm(b[4 * i], b[4 * i + 1], 0x0040), __byte_perm(b[4 * i + 2], b[4 * i + 3], 0x0040), 0x5410);
   }
 };
 
-constexpr int kQKeep = 4;      // accesses of a thread that stay in its registers
+constexpr int kQThreads = 256, kQKeep = 4;      // threads of a CTA, words of a lane
 
-// WARPS a row (a CTA has max(4, WARPS) of them); B bytes an access; KEEP: the row is kept in registers, else read again.
+// L lanes a row (8, 16, or a warp) and WARPS such groups of it; KEEP words of a lane stay in its registers (0: the row is read again).
+// SHIFT: rows that do not all start on 16-byte boundaries.  L lanes then take the aligned words that hold the next L - 1 groups of N values, quantise them (what is not of
+// the row counts as 0), and each lane puts its group together from its word's bytes and the next lane's: wide accesses on both sides.
 // Nothing that is read here is __restrict__: the kernel starts while the one in front, which may write it, still runs.
-template <typename T, int B, int WARPS, bool KEEP>
-__global__ void __launch_bounds__(WARPS < 4 ? 128 : 32 * WARPS)
+template <typename T, bool SHIFT, int L, int WARPS, int KEEP>
+__global__ void __launch_bounds__(WARPS > 8 ? 32 * WARPS : kQThreads)
 quantize_rows_kernel(const T* x, int8_t* q, float* scale, long rows, int c, int pitch) {
-  constexpr int N = QVec<T, B>::N, kRows = WARPS < 4 ? 4 / WARPS : 1, kStep = 32 * WARPS;
-  __shared__ uint32_t s_top[WARPS];
-  const int tid = threadIdx.x, lane = tid % kStep;      // of the row
-  const long row = (long)blockIdx.x * kRows + tid / kStep;
+  constexpr int N = QWord<T>::N, kRows = (WARPS > 8 ? 32 * WARPS : kQThreads) / (L * WARPS), kWords = SHIFT ? L - 1 : L, kSteps = WARPS * kWords;
+  typedef typename std::conditional<N == 8, uint2, uint32_t>::type Group;
+  __shared__ uint32_t s_top[WARPS * kRows];
+  const int tid = threadIdx.x, lane = tid % L, warp = tid / L % WARPS;      // of the row
+  const long row = (long)blockIdx.x * kRows + tid / (L * WARPS);
   // The next launch may start once the past of the stream is over for this one: it may then read what no launch but this one writes.
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  if (WARPS == 1 && row >= rows) return;
-  const T* src = x + (size_t)row * c;
-  const int units = c / N;                              // N divides c
-  QVec<T, B> v[kQKeep];
-  uint32_t top = 0u;
-  if constexpr (KEEP) {
-#pragma unroll
-    for (int i = 0; i < kQKeep; ++i) {
-      if (lane + i * kStep < units) v[i].load(src + (size_t)(lane + i * kStep) * N);
-      else v[i].clear();
+  const bool live = row < rows;
+  const T* src = x + (size_t)(live ? row : 0) * c;
+  const int skew = SHIFT ? (int)(((uintptr_t)src & 15) / sizeof(T)) : 0;    // what the first aligned word has in front of the row
+  const int w0 = warp * kWords + lane, groups = live ? pitch / N : 0;
+  const int words = live ? (skew + c + N - 1) / N - w0 : 0;                 // from this lane's first on
+  const uint4* from = reinterpret_cast<const uint4*>(src - skew) + w0;
+  Group* to = reinterpret_cast<Group*>(q + (size_t)row * pitch) + w0;
+  auto load = [&](int k) {                              // word k of this lane's, with zeros in place of what is not of the row
+    QWord<T> v;
+    if (!SHIFT) {
+      v.set(k * kSteps < words ? from[k * kSteps] : make_uint4(0u, 0u, 0u, 0u));
+      return v;
     }
+    const int lo = skew - (w0 + k * kSteps) * N, hi = lo + c;               // its values in [lo, hi) are the row's
+    if (lo <= 0 && hi >= N) {
+      v.set(from[k * kSteps]);
+    } else {
+      v.set(make_uint4(0u, 0u, 0u, 0u));
+      const T* p = reinterpret_cast<const T*>(from + k * kSteps);
 #pragma unroll
-    for (int i = 0; i < kQKeep; ++i) top = v[i].top(top);
+      for (int i = 0; i < N; ++i)
+        if (i >= lo && i < hi && live) {
+          if constexpr (sizeof(T) == 4) v.w[i] = *reinterpret_cast<const uint32_t*>(p + i);
+          else v.w[i / 2] |= (uint32_t)*reinterpret_cast<const unsigned short*>(p + i) << 16 * (i & 1);
+        }
+    }
+    return v;
+  };
+  const int chunks = (pitch / N + kWords - 1) / kWords;                     // of L lanes
+  QWord<T> v[KEEP > 0 ? KEEP : 1];
+  float top = 0.f;
+  if constexpr (KEEP > 0) {
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) v[i] = load(i);
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) top = v[i].top(top);
   } else {
 #pragma unroll 4
-    for (int u = lane; u < units; u += kStep) {
-      QVec<T, B> w;
-      w.load(src + (size_t)u * N);
-      top = w.top(top);
-    }
+    for (int k = 0; warp + k * WARPS < chunks; ++k) top = load(k).top(top);
   }
-  top = __reduce_max_sync(0xffffffffu, top);
-  if constexpr (WARPS > 1) {
-    if ((tid & 31) == 0) s_top[tid >> 5] = top;
-    __syncthreads();
-    top = s_top[tid & (WARPS - 1)];
-    top = __reduce_max_sync(0xffffffffu, top);
-  }
-  const QScale sc(top);
-  if (lane == 0) scale[row] = sc.s;
-  int8_t* dst = q + (size_t)row * pitch;
-  auto put = [&](const QVec<T, B>& w, int u) {
-    uint32_t out[(N + 3) / 4];
-    sc.template bytes<N>(w, out);
-    int8_t* p = dst + (size_t)u * N;
-    if constexpr (N == 8) *reinterpret_cast<uint2*>(p) = make_uint2(out[0], out[1]);
-    else if constexpr (N == 4) *reinterpret_cast<uint32_t*>(p) = out[0];
-    else if constexpr (N == 2) *reinterpret_cast<unsigned short*>(p) = (unsigned short)out[0];
-    else *p = (int8_t)out[0];
-  };
-  if constexpr (KEEP) {
+  // of the lanes, as bits (magnitudes, infinity and NaN order like them)
+  uint32_t bits = __float_as_uint(top);
+  if constexpr (L < 32) {
 #pragma unroll
-    for (int i = 0; i < kQKeep; ++i)
-      if (lane + i * kStep < units) put(v[i], lane + i * kStep);
+    for (int d = L / 2; d; d >>= 1) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, d));
+  } else {
+    bits = __reduce_max_sync(0xffffffffu, bits);
+  }
+  if constexpr (WARPS > 1) {
+    if (lane == 0) s_top[tid / L] = bits;
+    __syncthreads();
+    bits = __reduce_max_sync(0xffffffffu, s_top[tid / (L * WARPS) * WARPS + (lane & (WARPS - 1))]);
+  }
+  const QScale sc(__uint_as_float(bits));
+  if (warp == 0 && lane == 0 && live) scale[row] = sc.s;
+  auto put = [&](const QWord<T>& w, int k) {
+    uint32_t out[N / 4];
+    sc.bytes(w, out);
+    if (SHIFT) {
+      uint32_t next[N / 4];
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) next[i] = __shfl_down_sync(0xffffffffu, out[i], 1, L);
+      if constexpr (N == 8) {
+        const uint32_t a = skew & 4 ? out[1] : out[0], b = skew & 4 ? next[0] : out[1], d = skew & 4 ? next[1] : next[0];
+        out[0] = __funnelshift_r(a, b, 8 * (skew & 3)), out[1] = __funnelshift_r(b, d, 8 * (skew & 3));
+      } else {
+        out[0] = __funnelshift_r(out[0], next[0], 8 * skew);
+      }
+    }
+    if (w0 + k * kSteps < groups && (!SHIFT || lane < L - 1)) {
+      if constexpr (N == 8) to[k * kSteps] = make_uint2(out[0], out[1]);
+      else to[k * kSteps] = out[0];
+    }
+  };
+  if constexpr (KEEP > 0) {
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+      if (i == 0 || warp + i * WARPS < chunks) put(v[i], i);
   } else {
 #pragma unroll 2
-    for (int u = lane; u < units; u += kStep) {
-      QVec<T, B> w;
-      w.load(src + (size_t)u * N);
-      put(w, u);
-    }
+    for (int k = 0; warp + k * WARPS < chunks; ++k) put(load(k), k);
   }
-  for (int i = c + lane; i < pitch; i += kStep) dst[i] = 0;      // up to 15 bytes behind the row
 }
 
-template <typename T, int B, int WARPS, bool KEEP>
+template <typename T, bool SHIFT, int L, int WARPS, int KEEP>
 inline cudaError_t quantize_go(const T* x, int8_t* q, float* scale, long rows, int c, cudaStream_t st) {
+  constexpr int kThreads = WARPS > 8 ? 32 * WARPS : kQThreads, kRows = kThreads / (L * WARPS);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(WARPS < 4 ? (rows + 4 / WARPS - 1) / (4 / WARPS) : rows));
-  cfg.blockDim = dim3(WARPS < 4 ? 128 : 32 * WARPS);
+  cfg.gridDim = dim3((unsigned)((rows + kRows - 1) / kRows));
+  cfg.blockDim = dim3(kThreads);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, quantize_rows_kernel<T, B, WARPS, KEEP>, x, q, scale, rows, c, q_pitch(c));
+  return cudaLaunchKernelEx(&cfg, quantize_rows_kernel<T, SHIFT, L, WARPS, KEEP>, x, q, scale, rows, c, q_pitch(c));
 }
-template <typename T, int B>
-inline cudaError_t quantize_width(const T* x, int8_t* q, float* scale, long rows, int c, cudaStream_t st) {
-  const int units = c / QVec<T, B>::N;
-  if (units <= 32 * kQKeep) return quantize_go<T, B, 1, true>(x, q, scale, rows, c, st);
-  if (units <= 128 * kQKeep) return quantize_go<T, B, 4, true>(x, q, scale, rows, c, st);
-  if (units <= 512 * kQKeep) return quantize_go<T, B, 16, true>(x, q, scale, rows, c, st);
-  return quantize_go<T, B, 16, false>(x, q, scale, rows, c, st);
+// Four words a lane where a row has them: what a row costs besides its words (its maximum, its scale) is shared by as many rows as a warp has.
+template <typename T, bool SHIFT>
+inline cudaError_t quantize_size(const T* x, int8_t* q, float* scale, long rows, int c, cudaStream_t st) {
+  const int groups = q_pitch(c) / QWord<T>::N, less = SHIFT ? 1 : 0;
+  if (groups <= kQKeep * (8 - less)) return quantize_go<T, SHIFT, 8, 1, kQKeep>(x, q, scale, rows, c, st);
+  if (groups <= kQKeep * (16 - less)) return quantize_go<T, SHIFT, 16, 1, kQKeep>(x, q, scale, rows, c, st);
+  const int chunks = cdiv(groups, 32 - less);
+  if (chunks <= kQKeep) return quantize_go<T, SHIFT, 32, 1, kQKeep>(x, q, scale, rows, c, st);
+  if (chunks <= 4 * kQKeep) return quantize_go<T, SHIFT, 32, 4, kQKeep>(x, q, scale, rows, c, st);
+  if (chunks <= 16 * kQKeep) return quantize_go<T, SHIFT, 32, 16, kQKeep>(x, q, scale, rows, c, st);
+  return quantize_go<T, SHIFT, 32, 16, 0>(x, q, scale, rows, c, st);
 }
-// The widest access that rows are whole units of and start on the boundaries of.
 template <typename T>
 inline cudaError_t quantize_launch(const T* x, int8_t* q, float* scale, long rows, int c, cudaStream_t st) {
-  const uintptr_t bits = (uintptr_t)x | (uintptr_t)((size_t)c * sizeof(T));
-  if ((bits & 15) == 0) return quantize_width<T, 16>(x, q, scale, rows, c, st);
-  if ((bits & 7) == 0) return quantize_width<T, 8>(x, q, scale, rows, c, st);
-  if (sizeof(T) == 4 || (bits & 3) == 0) return quantize_width<T, 4>(x, q, scale, rows, c, st);
-  if constexpr (sizeof(T) == 2) return quantize_width<T, 2>(x, q, scale, rows, c, st);
-  return cudaErrorInvalidValue;
+  const bool aligned = (((uintptr_t)x | (uintptr_t)((size_t)c * sizeof(T))) & 15) == 0;
+  return aligned ? quantize_size<T, false>(x, q, scale, rows, c, st) : quantize_size<T, true>(x, q, scale, rows, c, st);
 }
 
 // ----------------------------------------------------------------------------- dequantise
 
-// N values an access; 2^lanes threads a row.
-template <typename T, int N>
+// N values, the bytes in w, times s: 16 bytes of T.
+template <typename T>
+__device__ __forceinline__ Vec16<T> q_values(const uint32_t* w, float s) {
+  Vec16<T> o;
+#pragma unroll
+  for (int i = 0; i < 16 / (int)sizeof(T); ++i) o.v[i] = (float)(int8_t)(w[i / 4] >> (8 * (i & 3))) * s;
+  return o;
+}
+
+// 2^lanes threads a row.  SHIFT: rows of y that do not all start on 16-byte boundaries; L lanes (8, or a warp) then take as many groups of bytes for L - 1 aligned words of y, each
+// put together from a lane's group and the one in front.
+template <typename T, bool SHIFT, int L>
 __global__ void __launch_bounds__(256)
 dequantize_rows_kernel(const int8_t* q, const float* scale, const int32_t* index, T* y, long rows, int pool, int c, int pitch, int lanes) {
+  constexpr int N = 16 / (int)sizeof(T);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const long row = (long)blockIdx.x * (256 >> lanes) + (threadIdx.x >> lanes);
-  if (row >= rows) return;
-  const long from = index ? (long)index[row] : row;
-  if (from < 0 || from >= pool) return;                 // no such row: left as it is
-  const float s = scale[from];
-  const int8_t* src = q + (size_t)from * pitch;
+  const long from = row < rows ? index ? (long)index[row] : row : -1;
+  const bool live = from >= 0 && from < pool;           // else: left as it is
+  if (SHIFT && L < 32 ? __all_sync(0xffffffffu, !live) : !live) return;
+  const float s = live ? scale[from] : 0.f;
+  const int8_t* src = q + (size_t)(live ? from : 0) * pitch;
   T* dst = y + (size_t)row * c;
-  const int units = c / N, step = 1 << lanes;
-#pragma unroll 4
-  for (int u = threadIdx.x & (step - 1); u < units; u += step) {
-    uint32_t w[2] = {0u, 0u};
+  auto group = [&](int g, uint32_t* w) {
     if constexpr (N == 8) {
-      const uint2 t = *reinterpret_cast<const uint2*>(src + (size_t)u * 8);
+      const uint2 t = *reinterpret_cast<const uint2*>(src + (size_t)g * 8);
       w[0] = t.x, w[1] = t.y;
-    } else if constexpr (N == 4) {
-      w[0] = *reinterpret_cast<const uint32_t*>(src + (size_t)u * 4);
-    } else if constexpr (N == 2) {
-      w[0] = *reinterpret_cast<const unsigned short*>(src + (size_t)u * 2);
     } else {
-      w[0] = *reinterpret_cast<const unsigned char*>(src + u);
+      w[0] = *reinterpret_cast<const uint32_t*>(src + (size_t)g * 4);
     }
-    float v[N];
+  };
+  const int lane = threadIdx.x % L, tid = threadIdx.x & ((1 << lanes) - 1);
+  if constexpr (!SHIFT) {
+#pragma unroll 4
+    for (int g = tid; g < c / N; g += 1 << lanes) {
+      uint32_t w[N / 4];
+      group(g, w);
+      q_values<T>(w, s).store(dst + (size_t)g * N);
+    }
+  } else {
+    const int skew = (int)(((uintptr_t)dst & 15) / sizeof(T)), groups = pitch / N, words = (skew + c + N - 1) / N;
+    T* first = dst - skew;
+#pragma unroll 2
+    for (int k = tid / L; k * (L - 1) < (L < 32 ? L - 1 : words); k += (1 << lanes) / L) {      // eight lanes have a row of one round, so that the warp stays together
+      const int g = k * (L - 1) + lane - 1;                  // word g of y: the group in front, then this one
+      uint32_t w[N / 4] = {}, last[N / 4];
+      if (g >= 0 && g < groups) group(g, w);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = (float)(int8_t)(w[i / 4] >> (8 * (i & 3))) * s;
-    T* p = dst + (size_t)u * N;
-    if constexpr (sizeof(T) * N == 16) {
-      Vec16<T> o;
+      for (int i = 0; i < N / 4; ++i) last[i] = __shfl_up_sync(0xffffffffu, w[i], 1, L);
+      if (lane == 0 || g >= words || !live) continue;
+      // the word's first value is number g * N - skew: byte N - skew of the group in front
+      if constexpr (N == 8) {
+        const int b = 8 - skew;                         // 1 to 8
+        uint32_t d[4] = {last[0], last[1], w[0], w[1]};
+        const uint32_t a0 = b >= 8 ? d[2] : b >= 4 ? d[1] : d[0], a1 = b >= 8 ? d[3] : b >= 4 ? d[2] : d[1], a2 = b >= 8 ? 0u : b >= 4 ? d[3] : d[2];
+        w[0] = __funnelshift_r(a0, a1, 8 * (b & 3)), w[1] = __funnelshift_r(a1, a2, 8 * (b & 3));
+      } else if (skew) {
+        w[0] = __funnelshift_r(last[0], w[0], 8 * (4 - skew));
+      }
+      const Vec16<T> o = q_values<T>(w, s);
+      const int lo = max(skew - g * N, 0), hi = min(skew + c - g * N, N);
+      if (lo == 0 && hi == N) {
+        o.store(first + (size_t)g * N);
+      } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i) o.v[i] = v[i];
-      o.store(p);
-    } else if constexpr (sizeof(T) == 2 && N == 4) {
-      *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-    } else if constexpr (sizeof(T) == 2 && N == 2) {
-      *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(v[0], v[1]);
-    } else if constexpr (sizeof(T) == 4 && N == 2) {
-      *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
-    } else {
-      Elem<T>::st(p, v[0]);
+        for (int i = 0; i < N; ++i)
+          if (i >= lo && i < hi) Elem<T>::st(first + (size_t)g * N + i, o.v[i]);
+      }
     }
   }
 }
 
-template <typename T, int N>
+template <typename T, bool SHIFT, int L>
 inline cudaError_t dequantize_go(const int8_t* q, const float* scale, const int32_t* index, T* y, long rows, int pool, int c, cudaStream_t st) {
-  int lanes = 3;                                        // threads of a row: enough for four accesses each, up to a CTA
-  while (lanes < 8 && c / N > 4 << lanes) ++lanes;
+  int lanes = L == 32 ? 5 : 3;                          // threads of a row: enough for four accesses each, up to a CTA
+  while ((!SHIFT || L == 32) && lanes < 8 && c * (int)sizeof(T) / 16 > 4 << lanes) ++lanes;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((rows + (256 >> lanes) - 1) / (256 >> lanes)));
   cfg.blockDim = dim3(256);
@@ -270,16 +336,14 @@ inline cudaError_t dequantize_go(const int8_t* q, const float* scale, const int3
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, dequantize_rows_kernel<T, N>, q, scale, index, y, rows, pool, c, q_pitch(c), lanes);
+  return cudaLaunchKernelEx(&cfg, dequantize_rows_kernel<T, SHIFT, L>, q, scale, index, y, rows, pool, c, q_pitch(c), lanes);
 }
 template <typename T>
 inline cudaError_t dequantize_launch(const int8_t* q, const float* scale, const int32_t* index, T* y, long rows, int pool, int c, cudaStream_t st) {
-  const uintptr_t bits = (uintptr_t)y | (uintptr_t)((size_t)c * sizeof(T));
-  constexpr int E = 16 / (int)sizeof(T);
-  if ((bits & 15) == 0) return dequantize_go<T, E>(q, scale, index, y, rows, pool, c, st);
-  if ((bits & 7) == 0) return dequantize_go<T, E / 2>(q, scale, index, y, rows, pool, c, st);
-  if ((bits & 3) == 0) return dequantize_go<T, E / 4>(q, scale, index, y, rows, pool, c, st);
-  return dequantize_go<T, 1>(q, scale, index, y, rows, pool, c, st);
+  constexpr int E = 16 / (int)sizeof(T);                // a row of c values lies in (c + 2 E - 2) / E aligned words at most
+  const bool aligned = (((uintptr_t)y | (uintptr_t)((size_t)c * sizeof(T))) & 15) == 0;
+  if (aligned) return dequantize_go<T, false, 8>(q, scale, index, y, rows, pool, c, st);
+  return (c + 2 * E - 2) / E <= 7 ? dequantize_go<T, true, 8>(q, scale, index, y, rows, pool, c, st) : dequantize_go<T, true, 32>(q, scale, index, y, rows, pool, c, st);
 }
 
 // ----------------------------------------------------------------------------- projection
