@@ -238,6 +238,7 @@ inline cudaError_t quantize_size(const T* x, int8_t* q, float* scale, long rows,
   if (groups <= kQKeep * (16 - less)) return quantize_go<T, SHIFT, 16, 1, kQKeep>(x, q, scale, rows, c, st);
   const int chunks = cdiv(groups, 32 - less);
   if (chunks <= kQKeep) return quantize_go<T, SHIFT, 32, 1, kQKeep>(x, q, scale, rows, c, st);
+  if (chunks <= 2 * kQKeep) return quantize_go<T, SHIFT, 32, 2, kQKeep>(x, q, scale, rows, c, st);
   if (chunks <= 4 * kQKeep) return quantize_go<T, SHIFT, 32, 4, kQKeep>(x, q, scale, rows, c, st);
   if (chunks <= 16 * kQKeep) return quantize_go<T, SHIFT, 32, 16, kQKeep>(x, q, scale, rows, c, st);
   return quantize_go<T, SHIFT, 32, 16, 0>(x, q, scale, rows, c, st);
@@ -348,8 +349,11 @@ inline cudaError_t dequantize_launch(const int8_t* q, const float* scale, const 
 
 // ----------------------------------------------------------------------------- projection
 
+constexpr int kI8FewRows = 4;   // up to this many rows every CTA quantises for itself
+
 struct I8Args {
   const float* xs;     // [rows]
+  const void* raw;     // [rows][c], few rows that are quantised here
   const float* ws;     // [n] or null
   const float* bias;   // [n] or null
   void* y;             // [rows][n]
@@ -384,14 +388,23 @@ __device__ __noinline__ void i8_drain(uint32_t full0, int stages, int from, int 
     if (!mbar_wait(full0 + 8u * (j % stages), (uint32_t)(j / stages) & 1u, err_flag)) return;
 }
 
-// A value of y, rounded once: in fp32 for bf16 (three roundings of 2^-24 before one of 2^-8), in fp64 for fp32.
+// A value of y, rounded once: in fp32 for bf16 (three roundings of 2^-24 before one of 2^-8), in fp64 for fp32, where integers and scales become doubles by their bits: the
+// instruction for that takes 8 clocks a warp.
 template <typename T> struct I8Value;
 template <> struct I8Value<bf16> {
-  static __device__ __forceinline__ float of(int acc, float ws, float xs, float bias) { return fmaf((float)acc * ws, xs, bias); }
+  float ws, bias;
+  __device__ __forceinline__ I8Value(float ws_, float bias_) : ws(ws_), bias(bias_) {}
+  __device__ __forceinline__ float operator()(int acc, float xs) const { return fmaf((float)acc * ws, xs, bias); }
 };
 template <> struct I8Value<float> {
-  static __device__ __forceinline__ float of(int acc, float ws, float xs, float bias) { return (float)fma((double)acc * (double)ws, (double)xs, (double)bias); }
+  double ws, bias;
+  __device__ __forceinline__ I8Value(float ws_, float bias_) : ws(ws_), bias(bias_) {}
+  __device__ __forceinline__ float operator()(int acc, double xs) const {
+    const double a = __hiloint2double(0x43300000, (int)((unsigned)acc ^ 0x80000000u)) - 4503601774854144.0;      // 2^52 + 2^31
+    return (float)fma(a * ws, xs, bias);
+  }
 };
+template <typename T> using I8Xs = typename std::conditional<sizeof(T) == 4, double, float>::type;    // scales of rows as the epilogue keeps them
 
 // Stores of a warp that holds 32 filters of two rows: of bf16, two neighbouring lanes trade, and the even one stores both filters of the even row, the odd one those of the odd.
 template <typename T> struct I8Store {
@@ -422,14 +435,16 @@ struct I8Smem {
   static constexpr int kABytes = 128 * 128, kBBytes = TN * 128, kStage = kABytes + kBBytes;
   static constexpr int kStages = TN == 128 ? 4 : TN == 64 ? 6 : 8;
   static constexpr int kPart = TN * 128 * 4;                 // what the cluster's CTAs send
-  static constexpr int kOffPart = kStages * kStage, kOffXs = kOffPart + kPart, kOffBars = kOffXs + TN * 4;
+  static constexpr int kOffPart = kStages * kStage, kOffXs = kOffPart + kPart, kOffBars = kOffXs + TN * 8;
   static constexpr int kBars = 2 * kStages + 2;
   static constexpr int kBytes = kOffBars + 8 * kBars + 16 + 1024;
   static_assert(kBytes <= 227 * 1024, "exceeds the shared memory of an SM");
 };
 
 // tmW: rows of W in boxes of 128, tmX: rows of x in boxes of TN; 128 bytes of K each.  blockIdx: x of filters, y of rows, z: range of K.
-template <typename T, int TN>
+// FEW: up to four rows come as they are.  Every CTA finds their scales, for which it reads them whole (8 KB a row of 4096 bf16), and quantises its range of K into the slots, of which
+// there is one for every block: a launch less (1 x 2048 x 1000: 3.4 us in place of 4.7).
+template <typename T, int TN, bool FEW>
 __global__ void __launch_bounds__(kI8Threads)
 int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, I8Args p) {
   using S = I8Smem<TN>;
@@ -437,19 +452,20 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
   extern __shared__ uint8_t i8_smem[];
   const uint32_t raw = smem_u32(i8_smem), base = (raw + 1023u) & ~1023u;
   uint8_t* gen = i8_smem + (base - raw);
-  float* s_xs = reinterpret_cast<float*>(gen + S::kOffXs);
+  I8Xs<T>* s_xs = reinterpret_cast<I8Xs<T>*>(gen + S::kOffXs);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + S::kOffBars + 8 * S::kBars);
   const uint32_t bar0 = base + S::kOffBars;
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (kStages + s); };
   const uint32_t accum_bar = bar0 + 8u * (2 * kStages), part_bar = accum_bar + 8u;
+  __shared__ uint32_t s_top[kI8FewRows][4];
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int z = (int)blockIdx.z, Z = (int)gridDim.z;
   const int n0 = (int)blockIdx.x * 128, t0 = (int)blockIdx.y * TN;
   const int kb_all = (p.c + 127) / 128;
   const int kb0 = (int)((long)kb_all * z / Z), num_kb = (int)((long)kb_all * (z + 1) / Z) - kb0;   // Z <= kb_all: never empty
 
-  if ((warp == 0 || warp == 6) && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(warp == 0 ? &tmW : &tmX) : "memory");
+  if ((warp == 0 || (warp == 6 && !FEW)) && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(warp == 0 ? &tmW : &tmX) : "memory");
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) mbar_init(full_bar(s), 2), mbar_init(empty_bar(s), 1);
     mbar_init(accum_bar, 1), mbar_init(part_bar, 1);
@@ -476,7 +492,7 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
   if (!(warp == 0 && p.early)) asm volatile("griddepcontrol.wait;" ::: "memory");
   bool lost = false;                             // the cluster's parts have not come
 
-  if (warp == 0 || warp == 6) {
+  if (warp == 0 || (warp == 6 && !FEW)) {
     if (elect_one()) {
       const CUtensorMap* tm = warp == 0 ? &tmW : &tmX;
       const uint32_t off = warp == 0 ? 0u : (uint32_t)S::kABytes, bytes = warp == 0 ? S::kABytes : S::kBBytes;
@@ -491,6 +507,7 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
       }
     }
     __syncwarp();
+  } else if (warp == 6) {
   } else if (warp == 1) {
     if (elect_one()) {
       constexpr uint32_t idesc = i8_idesc(TN, 128);
@@ -517,13 +534,61 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     constexpr int CH = TN < 32 ? TN : 32;              // columns read at a time
     const std::integral_constant<int, CH> ch;
     const float ws = f < p.n ? (p.ws ? p.ws[f] : 1.f) : 0.f, bias = p.bias && f < p.n ? p.bias[f] : 0.f;
-    if (et < TN) s_xs[et] = t0 + et < p.rows ? p.xs[t0 + et] : 0.f;
-    asm volatile("bar.sync 1, 128;" ::: "memory");
+    if constexpr (FEW) {
+      constexpr int N = QWord<T>::N;
+      const T* x = (const T*)p.raw;
+      const bool wide = (((uintptr_t)x | (uintptr_t)((size_t)p.c * sizeof(T))) & 15) == 0;
+      auto load = [&](int t, int i) {                    // N values of row t from number i on, 0 behind the last
+        QWord<T> v;
+        const T* src = x + (size_t)t * p.c + i;
+        if (wide) {
+          v.set(i < p.c ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u));
+        } else {
+          v.set(make_uint4(0u, 0u, 0u, 0u));
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (i + e < p.c) {
+              if constexpr (sizeof(T) == 4) v.w[e] = *reinterpret_cast<const uint32_t*>(src + e);
+              else v.w[e / 2] |= (uint32_t)*reinterpret_cast<const unsigned short*>(src + e) << 16 * (e & 1);
+            }
+        }
+        return v;
+      };
+      for (int t = 0; t < p.rows; ++t) {
+        float top = 0.f;
+#pragma unroll 4
+        for (int i = et * N; i < p.c; i += 128 * N) top = load(t, i).top(top);
+        const uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
+        if (lane == 0) s_top[t][warp - 2] = bits;
+      }
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      for (int t = 0; t < p.rows; ++t) {
+        const QScale sc(__uint_as_float(max(max(s_top[t][0], s_top[t][1]), max(s_top[t][2], s_top[t][3]))));
+        if (et == 0) s_xs[t] = sc.s;
+        // behind the last channel W is 0, whatever stands here
+        for (int k = et * N; k - lane * N < num_kb * 128; k += 128 * N) {
+          uint32_t out[N / 4];
+          sc.bytes(load(t, kb0 * 128 + k), out);
+          if (k < num_kb * 128) {
+            uint8_t* dst = gen + (size_t)(k >> 7) * S::kStage + S::kABytes + t * 128 + (((k & 127) >> 4 ^ t & 7) << 4) + (k & 15);
+            if constexpr (N == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(out[0], out[1]);
+            else *reinterpret_cast<uint32_t*>(dst) = out[0];
+          }
+        }
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      if (et < num_kb) mbar_arrive_n(full_bar(et), 1);   // a slot a block
+    } else {
+      if (et < TN) s_xs[et] = t0 + et < p.rows ? p.xs[t0 + et] : 0.f;
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+    }
     I8Store<T> out(p, f, lane);
     out.ok = __all_sync(0xffffffffu, mbar_wait(accum_bar, 0, p.err_flag));
     tc_fence_after();
     const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
-    auto value = [&](int acc, int col) { return I8Value<T>::of(acc, ws, s_xs[col], bias); };
+    const I8Value<T> of(ws, bias);
+    auto value = [&](int acc, int col) { return of(acc, s_xs[col]); };
     if (Z == 1) {
 #pragma unroll 1
       for (int c = 0; c < TN && t0 + c < p.rows; c += CH) {
@@ -602,7 +667,7 @@ template <int TN>
 struct I8PairSmem {
   static constexpr int kABytes = 128 * 128, kBBytes = TN / 2 * 128, kStage = kABytes + kBBytes;   // this CTA's filters, its half of the rows of x
   static constexpr int kStages = TN == 256 ? 6 : 8;
-  static constexpr int kOffXs = kStages * kStage, kOffBars = kOffXs + 2 * TN * 4;
+  static constexpr int kOffXs = kStages * kStage, kOffBars = kOffXs + 2 * TN * 8;
   static constexpr int kBars = 2 * kStages + 5;
   static constexpr int kBytes = kOffBars + 8 * kBars + 16 + 1024;
   static_assert(kBytes <= 227 * 1024, "exceeds the shared memory of an SM");
@@ -616,7 +681,7 @@ int8_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_co
   extern __shared__ uint8_t i8_smem[];
   const uint32_t raw = smem_u32(i8_smem), base = (raw + 1023u) & ~1023u;
   uint8_t* gen = i8_smem + (base - raw);
-  float* s_xs = reinterpret_cast<float*>(gen + S::kOffXs);         // [2][TN]
+  I8Xs<T>* s_xs = reinterpret_cast<I8Xs<T>*>(gen + S::kOffXs);     // [2][TN]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + S::kOffBars + 8 * S::kBars);
   const uint32_t bar0 = base + S::kOffBars;
   auto full_bar = [&](int s) { return bar0 + 8u * s; };            // the leader's counts both CTAs' loads
@@ -708,7 +773,7 @@ int8_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_co
       const int f = n0 + q * 32 + lane;
       const float ws = f < p.n ? (p.ws ? p.ws[f] : 1.f) : 0.f, bias = p.bias && f < p.n ? p.bias[f] : 0.f;
       // The scales of this tile's rows, in the half of the array that the tile before the last one left.
-      float* xs = s_xs + b * TN;
+      I8Xs<T>* xs = s_xs + b * TN;
       const int et = tid - 64;
       if (et < TN) xs[et] = t0 + et < p.rows ? p.xs[t0 + et] : 0.f;
       asm volatile("bar.sync 1, %0;" ::"n"(32 * kI8PairEpi) : "memory");
@@ -716,6 +781,7 @@ int8_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_co
       if (!ok) continue;
       tc_fence_after();
       const I8Store<T> out(p, f, lane);
+      const I8Value<T> of(ws, bias);
       const uint32_t acc = tmem + (uint32_t)(b * TN + h * HALF) + ((uint32_t)(q * 32) << 16);
 #pragma unroll 1
       for (int c = 0; c < HALF; c += 32) {
@@ -730,9 +796,8 @@ int8_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_co
         if (t0 + col >= p.rows) continue;
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
-          const float4 x = *reinterpret_cast<const float4*>(xs + col + i);
-          out.put2(t0 + col + i, I8Value<T>::of(v[i], ws, x.x, bias), I8Value<T>::of(v[i + 1], ws, x.y, bias));
-          out.put2(t0 + col + i + 2, I8Value<T>::of(v[i + 2], ws, x.z, bias), I8Value<T>::of(v[i + 3], ws, x.w, bias));
+          out.put2(t0 + col + i, of(v[i], xs[col + i]), of(v[i + 1], xs[col + i + 1]));
+          out.put2(t0 + col + i + 2, of(v[i + 2], xs[col + i + 2]), of(v[i + 3], xs[col + i + 3]));
         }
       }
     }
@@ -771,10 +836,11 @@ inline cudaError_t i8_context_init(I8Context& ctx) {   // once per device and ty
   auto set = [&](auto kernel, int bytes) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   };
-  set(int8_linear_kernel<T, 16>, I8Smem<16>::kBytes);
-  set(int8_linear_kernel<T, 32>, I8Smem<32>::kBytes);
-  set(int8_linear_kernel<T, 64>, I8Smem<64>::kBytes);
-  set(int8_linear_kernel<T, 128>, I8Smem<128>::kBytes);
+  set(int8_linear_kernel<T, 16, true>, I8Smem<16>::kBytes);
+  set(int8_linear_kernel<T, 16, false>, I8Smem<16>::kBytes);
+  set(int8_linear_kernel<T, 32, false>, I8Smem<32>::kBytes);
+  set(int8_linear_kernel<T, 64, false>, I8Smem<64>::kBytes);
+  set(int8_linear_kernel<T, 128, false>, I8Smem<128>::kBytes);
   set(int8_linear_pair_kernel<T, 128>, I8PairSmem<128>::kBytes);
   set(int8_linear_pair_kernel<T, 256>, I8PairSmem<256>::kBytes);
   for (int i = 0; i < 4 && e == cudaSuccess; ++i) {
@@ -788,7 +854,7 @@ inline cudaError_t i8_context_init(I8Context& ctx) {   // once per device and ty
     cfg.dynamicSmemBytes = I8Smem<64>::kBytes;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    e = cudaOccupancyMaxActiveClusters(&ctx.fit[i], int8_linear_kernel<T, 64>, &cfg);
+    e = cudaOccupancyMaxActiveClusters(&ctx.fit[i], int8_linear_kernel<T, 64, false>, &cfg);
   }
   return e;
 }
@@ -817,7 +883,7 @@ inline I8Plan i8_plan(int rows, int c, int n, const I8Context& ctx) {
   return p;
 }
 
-template <typename T, int TN>
+template <typename T, int TN, bool FEW>
 inline cudaError_t i8_one(const I8Plan& pl, const CUtensorMap& tmW, const CUtensorMap& tmX, const I8Args& a, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(cdiv(a.n, 128), cdiv(a.rows, TN), pl.splits);
@@ -832,7 +898,7 @@ inline cudaError_t i8_one(const I8Plan& pl, const CUtensorMap& tmW, const CUtens
   attr[1].val.clusterDim.z = pl.splits;
   cfg.attrs = attr;
   cfg.numAttrs = pl.splits > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, int8_linear_kernel<T, TN>, tmW, tmX, a);
+  return cudaLaunchKernelEx(&cfg, int8_linear_kernel<T, TN, FEW>, tmW, tmX, a);
 }
 template <typename T, int TN>
 inline cudaError_t i8_pair(const I8Context& ctx, const CUtensorMap& tmW, const CUtensorMap& tmX, const I8Args& a, cudaStream_t st) {
@@ -855,7 +921,12 @@ inline cudaError_t i8_run(const I8Context& ctx, const T* raw, const int8_t* x8, 
   const I8Plan pl = i8_plan(a.rows, a.c, a.n, ctx);
   CUtensorMap tmW = {}, tmX = {};
   cudaError_t e = i8_map(ctx, &tmW, w, a.n, a.c, 128);
-  if (e == cudaSuccess) e = i8_map(ctx, &tmX, x8, a.rows, a.c, pl.pair ? pl.tn / 2 : pl.tn);
+  if (e != cudaSuccess) return e;
+  if (raw && a.rows <= kI8FewRows && !pl.pair && cdiv(cdiv(a.c, 128), pl.splits) <= I8Smem<16>::kStages) {
+    a.raw = raw;
+    return i8_one<T, 16, true>(pl, tmW, tmX, a, st);
+  }
+  e = i8_map(ctx, &tmX, x8, a.rows, a.c, pl.pair ? pl.tn / 2 : pl.tn);
   if (e != cudaSuccess) return e;
   a.early = raw != nullptr;
   if (raw) {
@@ -864,10 +935,10 @@ inline cudaError_t i8_run(const I8Context& ctx, const T* raw, const int8_t* x8, 
   }
   if (pl.pair) return pl.tn == 256 ? i8_pair<T, 256>(ctx, tmW, tmX, a, st) : i8_pair<T, 128>(ctx, tmW, tmX, a, st);
   switch (pl.tn) {
-    case 16: return i8_one<T, 16>(pl, tmW, tmX, a, st);
-    case 32: return i8_one<T, 32>(pl, tmW, tmX, a, st);
-    case 64: return i8_one<T, 64>(pl, tmW, tmX, a, st);
-    default: return i8_one<T, 128>(pl, tmW, tmX, a, st);
+    case 16: return i8_one<T, 16, false>(pl, tmW, tmX, a, st);
+    case 32: return i8_one<T, 32, false>(pl, tmW, tmX, a, st);
+    case 64: return i8_one<T, 64, false>(pl, tmW, tmX, a, st);
+    default: return i8_one<T, 128, false>(pl, tmW, tmX, a, st);
   }
 }
 
