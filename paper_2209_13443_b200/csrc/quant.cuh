@@ -359,6 +359,7 @@ struct I8Args {
   void* y;             // [rows][n]
   int rows, c, n;
   int early;           // the launch in front writes x and xs, and nothing else that is read here
+  int full;            // pairs: tiles in front of those that are halved
   int* err_flag;
   long long wait_cycles;
 };
@@ -428,7 +429,7 @@ template <typename T> struct I8Store {
 __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, int* v, std::integral_constant<int, 32>) { tmem_ld32(taddr, reinterpret_cast<float*>(v)); }
 __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, int* v, std::integral_constant<int, 16>) { tmem_ld16(taddr, reinterpret_cast<float*>(v)); }
 
-constexpr int kI8Threads = 224;   // producer of W, MMA, four epilogue warps, producer of x
+constexpr int kI8Epi = 8, kI8Threads = 32 * (3 + kI8Epi), kI8XWarp = 2 + kI8Epi;   // producer of W, MMA, epilogue warps (two a quarter of the lanes), producer of x
 
 template <int TN>
 struct I8Smem {
@@ -458,14 +459,14 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (kStages + s); };
   const uint32_t accum_bar = bar0 + 8u * (2 * kStages), part_bar = accum_bar + 8u;
-  __shared__ uint32_t s_top[kI8FewRows][4];
+  __shared__ uint32_t s_top[kI8FewRows][kI8Epi];
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int z = (int)blockIdx.z, Z = (int)gridDim.z;
   const int n0 = (int)blockIdx.x * 128, t0 = (int)blockIdx.y * TN;
   const int kb_all = (p.c + 127) / 128;
   const int kb0 = (int)((long)kb_all * z / Z), num_kb = (int)((long)kb_all * (z + 1) / Z) - kb0;   // Z <= kb_all: never empty
 
-  if ((warp == 0 || (warp == 6 && !FEW)) && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(warp == 0 ? &tmW : &tmX) : "memory");
+  if ((warp == 0 || (warp == kI8XWarp && !FEW)) && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(warp == 0 ? &tmW : &tmX) : "memory");
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) mbar_init(full_bar(s), 2), mbar_init(empty_bar(s), 1);
     mbar_init(accum_bar, 1), mbar_init(part_bar, 1);
@@ -492,7 +493,7 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
   if (!(warp == 0 && p.early)) asm volatile("griddepcontrol.wait;" ::: "memory");
   bool lost = false;                             // the cluster's parts have not come
 
-  if (warp == 0 || (warp == 6 && !FEW)) {
+  if (warp == 0 || (warp == kI8XWarp && !FEW)) {
     if (elect_one()) {
       const CUtensorMap* tm = warp == 0 ? &tmW : &tmX;
       const uint32_t off = warp == 0 ? 0u : (uint32_t)S::kABytes, bytes = warp == 0 ? S::kABytes : S::kBBytes;
@@ -507,7 +508,7 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
       }
     }
     __syncwarp();
-  } else if (warp == 6) {
+  } else if (warp == kI8XWarp) {
   } else if (warp == 1) {
     if (elect_one()) {
       constexpr uint32_t idesc = i8_idesc(TN, 128);
@@ -530,8 +531,8 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     }
     __syncwarp();
   } else {
-    const int et = tid - 64, q = warp & 3, row = q * 32 + lane, f = n0 + row;
-    constexpr int CH = TN < 32 ? TN : 32;              // columns read at a time
+    const int et = tid - 64, q = warp & 3, h = (warp - 2) >> 2, row = q * 32 + lane, f = n0 + row;
+    constexpr int kEpi = 32 * kI8Epi, CH = TN < 64 ? 16 : 32;              // threads; columns read at a time
     const std::integral_constant<int, CH> ch;
     const float ws = f < p.n ? (p.ws ? p.ws[f] : 1.f) : 0.f, bias = p.bias && f < p.n ? p.bias[f] : 0.f;
     if constexpr (FEW) {
@@ -557,16 +558,16 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
       for (int t = 0; t < p.rows; ++t) {
         float top = 0.f;
 #pragma unroll 4
-        for (int i = et * N; i < p.c; i += 128 * N) top = load(t, i).top(top);
+        for (int i = et * N; i < p.c; i += kEpi * N) top = load(t, i).top(top);
         const uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
         if (lane == 0) s_top[t][warp - 2] = bits;
       }
-      asm volatile("bar.sync 1, 128;" ::: "memory");
+      asm volatile("bar.sync 1, %0;" ::"n"(kEpi) : "memory");
       for (int t = 0; t < p.rows; ++t) {
-        const QScale sc(__uint_as_float(max(max(s_top[t][0], s_top[t][1]), max(s_top[t][2], s_top[t][3]))));
+        const QScale sc(__uint_as_float(__reduce_max_sync(0xffffffffu, s_top[t][lane & (kI8Epi - 1)])));
         if (et == 0) s_xs[t] = sc.s;
         // behind the last channel W is 0, whatever stands here
-        for (int k = et * N; k - lane * N < num_kb * 128; k += 128 * N) {
+        for (int k = et * N; k - lane * N < num_kb * 128; k += kEpi * N) {
           uint32_t out[N / 4];
           sc.bytes(load(t, kb0 * 128 + k), out);
           if (k < num_kb * 128) {
@@ -577,11 +578,11 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
         }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      asm volatile("bar.sync 1, 128;" ::: "memory");
+      asm volatile("bar.sync 1, %0;" ::"n"(kEpi) : "memory");
       if (et < num_kb) mbar_arrive_n(full_bar(et), 1);   // a slot a block
     } else {
       if (et < TN) s_xs[et] = t0 + et < p.rows ? p.xs[t0 + et] : 0.f;
-      asm volatile("bar.sync 1, 128;" ::: "memory");
+      asm volatile("bar.sync 1, %0;" ::"n"(kEpi) : "memory");
     }
     I8Store<T> out(p, f, lane);
     out.ok = __all_sync(0xffffffffu, mbar_wait(accum_bar, 0, p.err_flag));
@@ -591,7 +592,7 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     auto value = [&](int acc, int col) { return of(acc, s_xs[col]); };
     if (Z == 1) {
 #pragma unroll 1
-      for (int c = 0; c < TN && t0 + c < p.rows; c += CH) {
+      for (int c = h * CH; c < TN && t0 + c < p.rows; c += 2 * CH) {
         int v[CH];
         tmem_ld_cols(lane_base + c, v, ch);
 #pragma unroll
@@ -603,7 +604,7 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
       asm volatile("barrier.cluster.wait.acquire;" ::: "memory");      // every CTA's barriers are set up
       const uint32_t recv = base + S::kOffPart;
 #pragma unroll 1
-      for (int c = 0; c < TN; c += CH) {
+      for (int c = h * CH; c < TN; c += 2 * CH) {
         int v[CH];
         tmem_ld_cols(lane_base + c, v, ch);
         if (share >= 4) {
@@ -632,7 +633,7 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
       out.ok = out.ok && !lost;
       const int* in = reinterpret_cast<const int*>(gen + S::kOffPart);
 #pragma unroll 1
-      for (int i = 0; i < share; i += 4) {
+      for (int i = 4 * h; i < share; i += 8) {
         int sum[4] = {0, 0, 0, 0};
         if (share >= 4) {
 #pragma unroll 2
@@ -654,7 +655,7 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
     }
     tc_fence_before();
   }
-  if (Z > 1 && !(warp >= 2 && warp < 6)) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");   // the other warps' part in the barrier at the start
+  if (Z > 1 && !(warp >= 2 && warp < kI8XWarp)) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");   // the other warps' part in the barrier at the start
   if (__syncthreads_or(lost)) cluster_drain(part_bar, 0, p.err_flag);      // the status says so, and y stays as it is
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols) : "memory");
 }
@@ -675,7 +676,7 @@ struct I8PairSmem {
 
 template <typename T, int TN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kI8PairThreads, 1)
-int8_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, I8Args p) {
+int8_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmH, I8Args p) {
   using S = I8PairSmem<TN>;
   constexpr int kStages = S::kStages, HALF = TN / 2;
   extern __shared__ uint8_t i8_smem[];
@@ -692,11 +693,19 @@ int8_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_co
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const uint32_t rank = cluster_rank();                            // 0: leader
   const int pair = (int)(blockIdx.x >> 1), n_pairs = (int)(gridDim.x >> 1);
-  const int tiles_n = (p.n + 255) / 256, tiles = tiles_n * ((p.rows + TN - 1) / TN), num_kb = (p.c + 127) / 128;
+  const int tiles_n = (p.n + 255) / 256, num_kb = (p.c + 127) / 128;
+  // Whole tiles, then halves (of the rows) of those that are left: 4096 x 4096 are 3.46 tiles a pair, which take 3.5 rounds so in place of four.
+  const int tiles = 2 * tiles_n * ((p.rows + TN - 1) / TN) - p.full;
+  auto place = [&](int i, int& nt, int& t0) {            // returns whether it is a whole one
+    const bool whole = i < p.full;
+    const int tile = whole ? i : p.full + (i - p.full) / 2;
+    nt = tile % tiles_n, t0 = tile / tiles_n * TN + (whole ? 0 : (i - p.full) % 2 * HALF);
+    return whole;
+  };
 
   if (tid == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tmW) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmX) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(p.full ? &tmX : &tmH) : "memory");
     for (int s = 0; s < kStages; ++s) mbar_init(full_bar(s), 1), mbar_init(empty_bar(s), 1);
     for (int b = 0; b < 2; ++b) mbar_init(acc_full(b), 1), mbar_init(acc_empty(b), 2 * kI8PairEpi);
     mbar_init(stop_bar, 1);
@@ -719,14 +728,17 @@ int8_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_co
       uint32_t ph = 1u;
       bool ok = true;
       for (int tile = pair; tile < tiles && ok; tile += n_pairs) {
-        const int n0 = tile % tiles_n * 256 + (int)rank * 128, t0 = tile / tiles_n * TN + (int)rank * HALF;
+        int nt, t0;
+        const bool whole = place(tile, nt, t0);
+        const int n0 = nt * 256 + (int)rank * 128;
+        t0 += (int)rank * (whole ? HALF : HALF / 2);
         for (int i = 0; i < num_kb; ++i, ++g) {
           ok = g < kStages || mbar_wait(empty_bar(s), ph, p.err_flag);
           if (!ok) break;
-          if (rank == 0) mbar_expect_tx(full_bar(s), (uint32_t)(2 * S::kStage));
+          if (rank == 0) mbar_expect_tx(full_bar(s), (uint32_t)(2 * S::kABytes + (whole ? 2 : 1) * S::kBBytes));
           const uint32_t dst = base + (uint32_t)s * S::kStage, bar = map_to_rank(full_bar(s), 0);
           tma2_load_2d(dst, &tmW, bar, i * 128, n0);
-          tma2_load_2d(dst + S::kABytes, &tmX, bar, i * 128, t0);
+          tma2_load_2d(dst + S::kABytes, whole ? &tmX : &tmH, bar, i * 128, t0);
           if (++s == kStages) s = 0, ph ^= 1u;
         }
       }
@@ -736,7 +748,6 @@ int8_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_co
     __syncwarp();
   } else if (warp == 1) {
     if (rank == 0 && elect_one()) {
-      constexpr uint32_t idesc = i8_idesc(TN, 256);
       const uint64_t da0 = umma_desc(base), db0 = umma_desc(base + S::kABytes);
       int s = 0, it = 0;
       uint32_t ph = 0u;
@@ -746,6 +757,8 @@ int8_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_co
         if (it >= 2) ok = mbar_wait(acc_empty(b), (uint32_t)(it / 2 - 1) & 1u, p.err_flag);
         if (!ok) break;
         tc_fence_after();
+        int nt, t0;
+        const uint32_t idesc = place(tile, nt, t0) ? i8_idesc(TN, 256) : i8_idesc(HALF, 256);
         for (int i = 0; i < num_kb; ++i) {
           ok = mbar_wait(full_bar(s), ph, p.err_flag);
           if (!ok) break;
@@ -769,26 +782,28 @@ int8_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_co
     int it = 0;
     bool ok = true;
     for (int tile = pair; tile < tiles; tile += n_pairs, ++it) {    // a warp whose wait ran out stores nothing but meets the others
-      const int b = it & 1, n0 = tile % tiles_n * 256 + (int)rank * 128, t0 = tile / tiles_n * TN;
+      int nt, t0;
+      const int cols = place(tile, nt, t0) ? HALF : HALF / 2;        // of this warp
+      const int b = it & 1, n0 = nt * 256 + (int)rank * 128;
       const int f = n0 + q * 32 + lane;
       const float ws = f < p.n ? (p.ws ? p.ws[f] : 1.f) : 0.f, bias = p.bias && f < p.n ? p.bias[f] : 0.f;
       // The scales of this tile's rows, in the half of the array that the tile before the last one left.
       I8Xs<T>* xs = s_xs + b * TN;
       const int et = tid - 64;
-      if (et < TN) xs[et] = t0 + et < p.rows ? p.xs[t0 + et] : 0.f;
+      if (et < 2 * cols) xs[et] = t0 + et < p.rows ? p.xs[t0 + et] : 0.f;
       asm volatile("bar.sync 1, %0;" ::"n"(32 * kI8PairEpi) : "memory");
       if (ok) ok = __all_sync(0xffffffffu, mbar_wait(acc_full(b), (uint32_t)(it / 2) & 1u, p.err_flag));
       if (!ok) continue;
       tc_fence_after();
       const I8Store<T> out(p, f, lane);
       const I8Value<T> of(ws, bias);
-      const uint32_t acc = tmem + (uint32_t)(b * TN + h * HALF) + ((uint32_t)(q * 32) << 16);
+      const uint32_t acc = tmem + (uint32_t)(b * TN + h * cols) + ((uint32_t)(q * 32) << 16);
 #pragma unroll 1
-      for (int c = 0; c < HALF; c += 32) {
+      for (int c = 0; c < cols; c += 32) {
         int v[32];
         tmem_ld32(acc + c, reinterpret_cast<float*>(v));
-        const int col = h * HALF + c;
-        if (c + 32 == HALF) {          // this warp's share is in registers
+        const int col = h * cols + c;
+        if (c + 32 == cols) {          // this warp's share is in registers
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster(drained[b]);
@@ -864,23 +879,31 @@ struct I8Plan {
   bool pair;
 };
 
+// Measured, us (rows of a tile / CTAs of a cluster, p: pairs): 64 x 4096 x 4096 16/1 7.7, 32/2 6.7, 64/4 7.2, 64/1 7.7; 128 x 4096 x 4096 32/1 8.2, 64/2 9.3, 128/4 11.0, 128/1p 9.8;
+// 256 64/1 10.3, 128/2 14.4, 128/1p 10.3; 512 128/1 14.9, 128/1p 11.8, 256/1p 16.5; 1024 128/1p 17.0, 256/1p 17.5; 4096 49.7 and 47.7; 128 x 1024 x 1024 16/1 3.6, 16/2 4.2, 32/1 4.2, 128/1 6.2.
+// So: tiles of few rows while they fit side by side, since what a tile's epilogue and exchange take grows with its rows, and pairs when tiles of 64 do not fit.
 inline I8Plan i8_plan(int rows, int c, int n, const I8Context& ctx) {
-  I8Plan p;
-  const int kb = cdiv(c, 128);
-  p.tn = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
-  const long tiles = (long)cdiv(n, 128) * cdiv(rows, p.tn);
-  p.splits = 1;
-  p.pair = tiles > ctx.sm_count && n > 128;
-  if (p.pair) {
-    const int pairs = ctx.sm_count / 2;
+  const int kb = cdiv(c, 128), pairs = ctx.sm_count / 2;
+  auto tiles = [&](int tn) { return (long)cdiv(n, 128) * cdiv(rows, tn); };
+  if (rows > 64 && n > 128 && tiles(64) > ctx.sm_count) {
     auto rounds = [&](int tn) { return ((long)cdiv(n, 256) * cdiv(rows, tn) + pairs - 1) / pairs; };
-    p.tn = rows > 128 && rounds(256) * 5 <= rounds(128) * 3 ? 256 : 128;
-    return p;
+    return {rounds(256) * 5 <= rounds(128) * 3 ? 256 : 128, 1, true};
   }
-  int i = 0;
-  while (i < 3 && tiles <= ctx.fit[i + 1] && kb >= 2 << i) ++i;
-  p.splits = 1 << i;
-  return p;
+  // us of a K block, of the epilogue, of the exchange, by the rows of a tile
+  constexpr float kBlock[4] = {0.155f, 0.155f, 0.16f, 0.25f}, kEpilogue[4] = {0.55f, 0.8f, 1.1f, 1.9f}, kExchange[4] = {0.9f, 1.2f, 3.f, 6.f};
+  I8Plan best = {16, 1, false};
+  float least = 1e30f;
+  for (int i = 0; i < 4; ++i) {
+    const int tn = 16 << i;
+    if (i > 0 && rows <= tn / 2) break;
+    for (int s = 0; s < 4 && kb >= 1 << s; ++s) {
+      if (s > 0 && tiles(tn) > ctx.fit[s]) break;
+      const long waves = s > 0 ? 1 : (tiles(tn) + ctx.sm_count - 1) / ctx.sm_count;
+      const float t = (float)waves * ((float)cdiv(kb, 1 << s) * kBlock[i] + kEpilogue[i] + (s > 0 ? kExchange[i] : 0.f) + 1.f);
+      if (t < least) least = t, best = {tn, 1 << s, false};
+    }
+  }
+  return best;
 }
 
 template <typename T, int TN, bool FEW>
@@ -901,9 +924,11 @@ inline cudaError_t i8_one(const I8Plan& pl, const CUtensorMap& tmW, const CUtens
   return cudaLaunchKernelEx(&cfg, int8_linear_kernel<T, TN, FEW>, tmW, tmX, a);
 }
 template <typename T, int TN>
-inline cudaError_t i8_pair(const I8Context& ctx, const CUtensorMap& tmW, const CUtensorMap& tmX, const I8Args& a, cudaStream_t st) {
+inline cudaError_t i8_pair(const I8Context& ctx, const CUtensorMap& tmW, const CUtensorMap& tmX, const CUtensorMap& tmH, I8Args a, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(2 * (unsigned)std::min<long>(ctx.sm_count / 2, (long)cdiv(a.n, 256) * cdiv(a.rows, TN)));
+  const long pairs = ctx.sm_count / 2, tiles = (long)cdiv(a.n, 256) * cdiv(a.rows, TN), over = tiles % pairs;
+  a.full = (int)(2 * over <= pairs ? tiles - over : tiles);
+  cfg.gridDim = dim3(2 * (unsigned)std::min(pairs, 2 * tiles - a.full));
   cfg.blockDim = dim3(kI8PairThreads);
   cfg.dynamicSmemBytes = I8PairSmem<TN>::kBytes;
   cfg.stream = st;
@@ -912,7 +937,7 @@ inline cudaError_t i8_pair(const I8Context& ctx, const CUtensorMap& tmW, const C
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, int8_linear_pair_kernel<T, TN>, tmW, tmX, a);
+  return cudaLaunchKernelEx(&cfg, int8_linear_pair_kernel<T, TN>, tmW, tmX, tmH, a);
 }
 
 // x8: quantised rows; raw: rows that are quantised into them first, or null.
@@ -933,7 +958,12 @@ inline cudaError_t i8_run(const I8Context& ctx, const T* raw, const int8_t* x8, 
     e = quantize_launch<T>(raw, const_cast<int8_t*>(x8), const_cast<float*>(a.xs), a.rows, a.c, st);
     if (e != cudaSuccess) return e;
   }
-  if (pl.pair) return pl.tn == 256 ? i8_pair<T, 256>(ctx, tmW, tmX, a, st) : i8_pair<T, 128>(ctx, tmW, tmX, a, st);
+  if (pl.pair) {
+    CUtensorMap tmH;                     // halves of tiles
+    e = i8_map(ctx, &tmH, x8, a.rows, a.c, pl.tn / 4);
+    if (e != cudaSuccess) return e;
+    return pl.tn == 256 ? i8_pair<T, 256>(ctx, tmW, tmX, tmH, a, st) : i8_pair<T, 128>(ctx, tmW, tmX, tmH, a, st);
+  }
   switch (pl.tn) {
     case 16: return i8_one<T, 16, false>(pl, tmW, tmX, a, st);
     case 32: return i8_one<T, 32, false>(pl, tmW, tmX, a, st);
