@@ -777,43 +777,61 @@ int8_linear_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_co
     }
     __syncwarp();
   } else {
-    const int ew = warp - 2, q = warp & 3, h = ew >> 2;
+    const int ew = warp - 2, q = warp & 3, h = ew >> 2, et = tid - 64;
     const uint32_t drained[2] = {map_to_rank(acc_empty(0), 0), map_to_rank(acc_empty(1), 0)};
+    // A tile's scales and bias are on their way while the tile before it is stored.
+    float ws = 0.f, bias = 0.f, row_scale = 0.f;
+    auto fetch = [&](int tile) {
+      int nt, t0;
+      if (tile >= tiles) return;
+      place(tile, nt, t0);
+      const int f = nt * 256 + (int)rank * 128 + q * 32 + lane;
+      ws = f < p.n ? (p.ws ? p.ws[f] : 1.f) : 0.f, bias = p.bias && f < p.n ? p.bias[f] : 0.f;
+      row_scale = et < TN && t0 + et < p.rows ? p.xs[t0 + et] : 0.f;
+    };
+    fetch(pair);
     int it = 0;
     bool ok = true;
     for (int tile = pair; tile < tiles; tile += n_pairs, ++it) {    // a warp whose wait ran out stores nothing but meets the others
       int nt, t0;
       const int cols = place(tile, nt, t0) ? HALF : HALF / 2;        // of this warp
-      const int b = it & 1, n0 = nt * 256 + (int)rank * 128;
-      const int f = n0 + q * 32 + lane;
-      const float ws = f < p.n ? (p.ws ? p.ws[f] : 1.f) : 0.f, bias = p.bias && f < p.n ? p.bias[f] : 0.f;
+      const int b = it & 1, f = nt * 256 + (int)rank * 128 + q * 32 + lane;
+      const I8Store<T> out(p, f, lane);
+      const I8Value<T> of(ws, bias);
       // The scales of this tile's rows, in the half of the array that the tile before the last one left.
       I8Xs<T>* xs = s_xs + b * TN;
-      const int et = tid - 64;
-      if (et < 2 * cols) xs[et] = t0 + et < p.rows ? p.xs[t0 + et] : 0.f;
+      if (et < TN) xs[et] = row_scale;
       asm volatile("bar.sync 1, %0;" ::"n"(32 * kI8PairEpi) : "memory");
+      fetch(tile + n_pairs);
       if (ok) ok = __all_sync(0xffffffffu, mbar_wait(acc_full(b), (uint32_t)(it / 2) & 1u, p.err_flag));
       if (!ok) continue;
       tc_fence_after();
-      const I8Store<T> out(p, f, lane);
-      const I8Value<T> of(ws, bias);
       const uint32_t acc = tmem + (uint32_t)(b * TN + h * cols) + ((uint32_t)(q * 32) << 16);
+      auto store = [&](const float* v, int col) {
+        if (t0 + col >= p.rows) return;
+#pragma unroll
+        for (int i = 0; i < 32; i += 2)
+          out.put2(t0 + col + i, of(__float_as_int(v[i]), xs[col + i]), of(__float_as_int(v[i + 1]), xs[col + i + 1]));
+      };
 #pragma unroll 1
-      for (int c = 0; c < cols; c += 32) {
-        int v[32];
-        tmem_ld32(acc + c, reinterpret_cast<float*>(v));
+      for (int c = 0; c < cols; c += 64) {
         const int col = h * cols + c;
-        if (c + 32 == cols) {          // this warp's share is in registers
+        float v[32], w[32];
+        if (c + 32 < cols) {
+          tmem_ld32_issue(acc + c, v);
+          tmem_ld32_issue(acc + c + 32, w);
+          tmem_ld_wait(v, w);
+        } else {
+          tmem_ld32(acc + c, v);
+        }
+        if (c + 64 >= cols) {          // this warp's share is in registers
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(drained[b]);
+          // relaxed: nothing but the loads above, which have ended, goes before it; a release waited for the stores too
+          if (lane == 0) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(drained[b]) : "memory");
         }
-        if (t0 + col >= p.rows) continue;
-#pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-          out.put2(t0 + col + i, of(v[i], xs[col + i]), of(v[i + 1], xs[col + i + 1]));
-          out.put2(t0 + col + i + 2, of(v[i + 2], xs[col + i + 2]), of(v[i + 3], xs[col + i + 3]));
-        }
+        store(v, col);
+        if (c + 32 < cols) store(w, col + 32);
       }
     }
   }
