@@ -282,12 +282,18 @@ sample_kernel(SampleArgs a) {
   const bool first = !(heat > 0.f) || k == 1 || p <= 0.f || m > 1.f;   // only the first stays
   if (k < 0 || k >= a.n) k = 0;
   const bool by_p = p < 1.f, by_m = m > 0.f;
+  auto fill = [&](float v) {               // this CTA's part of the probabilities
+    const int skip = min(cnt, (int)(-((uintptr_t)probs >> 2) & 3));
+    float4* mid = reinterpret_cast<float4*>(probs + skip);
+    const int quads = (cnt - skip) / 4;
+    if (tid < skip) probs[tid] = v;
+    for (int i = tid; i < quads; i += kSpThreads) mid[i] = make_float4(v, v, v, v);
+    if (tid < cnt - skip - 4 * quads) probs[skip + 4 * quads + tid] = v;
+  };
   int token = -1;                          // of this CTA: the one that has it stores it
   bool mine = rank == 0;
   if (nothing) {
-    const float v = top == -INFINITY ? 0.f : NAN;
-    if (probs)
-      for (int i = tid; i < cnt; i += kSpThreads) probs[i] = v;
+    if (probs) fill(top == -INFINITY ? 0.f : NAN);
   } else if (first) {
     int at = 0x7fffffff;
     for (int i = tid; i < cnt; i += kSpThreads)
@@ -299,8 +305,11 @@ sample_kernel(SampleArgs a) {
     __syncthreads();
     tell(0.0, s_int);
     token = __reduce_min_sync(0xffffffffu, told(lane < (int)cluster ? lane : 0).i);
-    if (probs)
-      for (int i = tid; i < cnt; i += kSpThreads) probs[i] = i0 + i == token ? 1.f : 0.f;
+    if (probs) {
+      fill(0.f);
+      __syncthreads();
+      if (tid == 0 && token >= i0 && token - i0 < cnt) probs[token - i0] = 1.f;
+    }
   } else {
     if (heat < 1e-20f && fabsf(top) < 1e-10f) {
       // So cold that logits below 2^-126 matter, which sp_wide does not tell apart: all of them times 2^64, and the temperature.  What overflows weighs nothing either way.
@@ -540,7 +549,7 @@ sample_kernel(SampleArgs a) {
       for (int i = tid >> 2; i - (lane >> 2) < members; i += kSpThreads / 4) {
         const unsigned long long e = s_work.list[min(i, members - 1)];
         int place = 0;
-#pragma unroll 4
+#pragma unroll 8
         for (int j = lane & 3; j < members; j += 4) place += s_work.list[j] > e;
         place += __shfl_xor_sync(0xffffffffu, place, 1);
         place += __shfl_xor_sync(0xffffffffu, place, 2);
@@ -799,7 +808,7 @@ sample_kernel(SampleArgs a) {
           const uint32_t at = (uint32_t)s_work.sorted[min(i, cut - 1)];          // the larger, the lower the index
           const double g = s_work.weight[min(i, cut - 1)];
           double before = 0.0;
-#pragma unroll 2
+#pragma unroll 8
           for (int j = lane & 3; j < cut; j += 4) before += sp_pick((uint32_t)s_work.sorted[j] > at, s_work.weight[j]);
           before += __shfl_xor_sync(0xffffffffu, before, 1);
           before += __shfl_xor_sync(0xffffffffu, before, 2);
@@ -977,15 +986,28 @@ sample_kernel(SampleArgs a) {
     if (probs) {
       // w / total in fp32: the exponent's fraction to 2^-23, the power to two units.  Who weighs at least m is asked in fp64, where the last member does not say it.
       const float ch = fminf((float)weight.c, FLT_MAX), cl = ch < FLT_MAX ? (float)(weight.c - (double)ch) : 0.f, part_of = (float)(1.0 / total);
-      const bool ask = by_m && !whole;
-#pragma unroll 4
-      for (int i = tid; i < cnt; i += kSpThreads) {
-        const float l = logit(i), d = l - top, r = fmaf(d, ch, 12582912.f), z = r - 12582912.f;
+      auto prob = [&](float l) {
+        const float d = l - top, r = fmaf(d, ch, 12582912.f), z = r - 12582912.f;
         float g;
         asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(g) : "f"(fmaf(d, cl, fmaf(d, ch, -z))));
         g *= part_of * __int_as_float(max(__float_as_int(r) - 0x4b400000 + 127, 0) << 23);
-        const bool in = z >= -126.f && kept(l, i) && (!ask || weight(l) >= least);
-        probs[i] = in ? g : 0.f;
+        return z >= -126.f ? g : 0.f;
+      };
+      if (whole) {                         // few: zeros, and over them what the list has
+        fill(0.f);
+        __syncthreads();
+        for (int j = tid; j < (rank == 0 ? cut : own); j += kSpThreads) {
+          const unsigned long long e = rank == 0 ? s_work.sorted[j] : s_work.list[j];
+          const float l = sp_logit((uint32_t)(e >> 32));
+          const int i = (int)~(uint32_t)e - i0;
+          if (i >= 0 && i < cnt && kept(l, i)) probs[i] = prob(l);
+        }
+      } else {
+#pragma unroll 4
+        for (int i = tid; i < cnt; i += kSpThreads) {
+          const float l = logit(i);
+          probs[i] = kept(l, i) && (!by_m || weight(l) >= least) ? prob(l) : 0.f;
+        }
       }
     }
   }
