@@ -311,10 +311,11 @@ sample_kernel(SampleArgs a) {
       if (tid == 0 && token >= i0 && token - i0 < cnt) probs[token - i0] = 1.f;
     }
   } else {
-    if (heat < 1e-20f && fabsf(top) < 1e-10f) {
+    const float lift = heat < 1e-20f && fabsf(top) < 1e-10f ? 0x1p64f : 1.f;
+    if (lift > 1.f) {
       // So cold that logits below 2^-126 matter, which sp_wide does not tell apart: all of them times 2^64, and the temperature.  What overflows weighs nothing either way.
-      for (int i = tid; i < cnt; i += kSpThreads) Elem<T>::st(part + i, logit(i) * 0x1p64f);
-      heat *= 0x1p64f, top *= 0x1p64f;
+      for (int i = tid; i < cnt; i += kSpThreads) Elem<T>::st(part + i, logit(i) * lift);
+      heat *= lift, top *= lift;
       __syncthreads();
     }
     const SpWeight weight(s_roots, heat, top);
@@ -441,7 +442,9 @@ sample_kernel(SampleArgs a) {
     const int n_bins = cluster == 1 ? kSpBins / 2 : kSpBins;          // four a thread at most
     float scale = 0.f, base = 0.f, zoom = 1.f;        // looked at closer, the bins divide what lies from `base` on
     double octaves = 0.0;                  // of all bins, for weights
-    auto place = [&](float l) { return ((top - l) * scale - base) * zoom; };
+    // In bins below `base`.  Rounded step by step wherever it is asked: a logit lies in one bin only.
+    auto far_of = [&](float l) { return __fmul_rn(__fsub_rn(top, l), scale); };
+    auto place = [&](float l) { return __fmul_rn(__fsub_rn(far_of(l), base), zoom); };
     // The list: members whose place lies in [f0, f1); in the first CTA that of all CTAs, in order, with their weights, in another its own.  by_weight: and the exact sum of the row in sum_all, of blocks of what lies above them in s_block, and of
     // the row of those in s_double.  Returns how many members there are, or -1: more than the list has room for.
     double sum_all = 0.0;
@@ -578,7 +581,7 @@ sample_kernel(SampleArgs a) {
 #pragma unroll
         for (int e = 0; e < W; ++e) {
           // Conversions by sums with 2^23: the instructions take 8 clocks a warp.
-          const float far = (top - v.v[e]) * scale, f = (far - base) * zoom, down = __fadd_rd(f, 8388608.f);
+          const float far = far_of(v.v[e]), f = place(v.v[e]), down = __fadd_rd(f, 8388608.f);
           uint32_t member = 1u;
           if (by_weight) {
             float g;
@@ -615,7 +618,9 @@ sample_kernel(SampleArgs a) {
           }
           if (by_weight) {
             v[j] = (uint32_t)(sum_m * (1.0 / 131072) * 1.04) + (sum_m > 0.0);        // a bin is 0.043 octaves wide at most: never fewer than there are
-            m[j] = sum_m * exp2(-octaves / n_bins * ((double)base + (bin0 + j) / (double)zoom)) * (1.0 / 131072);
+            float g;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(g) : "f"(drop * (base + (float)(bin0 + j) / zoom)));
+            m[j] = sum_m * (double)g * (1.0 / 131072);
           }
         }
       }
@@ -648,8 +653,9 @@ sample_kernel(SampleArgs a) {
       }
       uint32_t before = (uint32_t)count0 + cc - c4;
       double before_m = weight0 + cm - m4;
-      // The place of a logit is off by 2^-23 of 1024 bins of 0.043 octaves at most, 3.6e-6 of its weight, in the bins as in the row's sum; a share by half of 2^-17, the power by 2^-22.
-      const double slack = by_weight ? 1.2e-5 * sum_row : 0.0;
+      // The place of a logit is off by 2^-23 of 1024 bins of 0.043 octaves at most, 3.6e-6 of its weight, in the bins as in the row's sum; a share by half of 2^-17, the power by 2^-22,
+      // a bin's largest weight by 43 * 2^-23.
+      const double slack = by_weight ? 2e-5 * sum_row : 0.0;
       int first_bin = kSpBins, last_bin = -1, first_before = 0, last_end = 0;
       double first_weight = 0.0;
 #pragma unroll
@@ -726,7 +732,7 @@ sample_kernel(SampleArgs a) {
       }
       __syncthreads();
       const uint32_t low = (uint32_t)s_int;
-      scale = fminf(0.9995f * (float)n_bins / (top - sp_logit(low)), FLT_MAX);
+      scale = fminf(0.9995f * (float)n_bins / (top - sp_logit(low) * lift), FLT_MAX);
       listed = low != 0u && scale > 0.f;
       direct = true;
       goal = (double)k;

@@ -413,6 +413,35 @@ def test_sample_of_logits_of_any_size(dtype, scale):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [700, 20000, 128001])
+def test_sample_of_cold_rows_of_tiny_logits(n, dtype):
+    """Logits and temperatures of about 10^-30 and down to the smallest floats, positive, negative and both."""
+    g = gen(n + 3)
+    rows = 8
+    size = torch.tensor([1e-30, 1e-30, 1e-34, 1e-37, 1e-38, 3e-39, 1e-24, 1e-15], device="cuda").double()[:, None]
+    x = (normal(g, rows, n).double() + torch.tensor([0.0, -9.0, 9.0, 0.0, 0.0, 0.0, 3.0, 0.0], device="cuda").double()[:, None]) * size
+    x = x.float().to(TD[dtype])
+    heat = (size[:, 0] * 0.7).float().clamp(max=9e-21)
+    for case in (dict(), dict(k=i32([1, 2, 30, 64, 65, 100, 200, 256])), dict(p=f32([0.5, 0.9, 0.99, 0.3, 0.7, 0.95, 0.8, 0.6])), dict(k=i32([50] * rows), p=f32([0.9] * rows)), dict(m=f32([0.05] * rows))):
+        sample_check(x, dtype, t=heat, u=uniform(g, rows), **case)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [513, 2048, 16385, 100000])
+def test_sample_of_evenly_spaced_logits(n, dtype):
+    """Differences that are whole multiples of a step, so that logits lie on the borders of whatever equal intervals they are sorted into."""
+    g = gen(n + 4)
+    rows = 10
+    steps = torch.tensor([2.0 ** -10, 2.0 ** -7, 2.0 ** -4, 1e-3, 1 / 3, 0.7, 2.0 ** -12, 0.01, 1.0, 8.0], device="cuda")
+    order = torch.stack([torch.randperm(n, generator=g, device="cuda") for _ in range(rows)]).float()
+    x = (5.0 - order * steps[:, None]).to(TD[dtype])
+    ks = [2, 3, 17, 64, 65, 128, 255, 256, 257, 500]
+    for case in (dict(k=i32(ks)), dict(k=i32(ks[::-1])), dict(p=f32([0.1, 0.5, 0.75, 0.9, 0.99, 0.999, 0.5, 0.9, 0.3, 0.6])), dict(t=steps * 40, p=f32([0.9] * rows)), dict(t=steps * 3000, p=f32([0.8] * rows)),
+                 dict(t=steps * 300, k=i32(ks), p=f32([0.95] * rows))):
+        sample_check(x, dtype, u=uniform(g, rows), **case)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,shift", [(1001, 1), (16001, 3), (33333, 5)])
 def test_sample_off_a_16_byte_boundary(dtype, n, shift):
     g = gen(shift)
