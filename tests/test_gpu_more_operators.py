@@ -583,3 +583,14 @@ def test_the_binding_refuses_what_the_library_cannot_see():
         eb.sample("f32", x, 4, 20, s, torch.empty(4, dtype=torch.int64, device="cuda"))
     with pytest.raises(eb.EEError):
         eb.sample("f16", x, 4, 20, s, torch.empty(4, dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c,n", [(1, 2048, 1000), (3, 4096, 512), (16, 4096, 4096), (40, 4099, 300)])
+def test_int8_linear_whose_exchange_runs_out_of_time(rows, c, n, dtype):
+    from tests.test_gpu_operator_contracts import _late
+
+    x, w, ws, bias = linear_case(rows, c, n, dtype)
+    w8, y = padded(w), torch.empty(rows, n, dtype=TD[dtype], device="cuda")
+    room = torch.empty(eb.int8_linear_workspace_bytes(rows, c) + 256, dtype=torch.uint8, device="cuda")
+    _late(lambda: eb.int8_linear(dtype, x, rows, c, w8, ws, n, y, workspace=room, bias=bias), [y])
