@@ -4,18 +4,23 @@
 // first k, those before which less than p of the k's weight lies, of these the ones that weigh at least m.  So it is told by its last member (a logit and
 // an index).  The token is the first kept class, by index, at which the running sum of weights exceeds u times their total.
 //
-// Weights and sums are fp64: a row of 10^5 classes has as many borders that u may fall next to, and sums that are off by 10^-7 would take another class on one draw in
-// a hundred.  2^z = 2^(k / 256) 2^g with the first factor from a table and |g| <= 1 / 512: the power series of exp up to its fourth term leaves 2^-54 and takes ten fp64 operations
-// with the sum, half of what it takes without a table.
+// Weights and sums that decide are fp64: a row of 10^5 classes has as many borders that u may fall next to, and sums that are off by 10^-7 would take another class on one draw in
+// a hundred.  2^z = 2^(k / 16) 2^g with the first factor from a table and |g| <= 1 / 32: the power series of exp up to its sixth term leaves 2^-51.
 //
 // A row is kept in the shared memory of a CTA, or of a cluster of them, which speak in turns (meet).  The last member is looked for among few:
-//   k: a logit that k of 512 groups of lanes reach with their largest: k-th and better lie at or above it, and little else does (the smallest maximum of 64 warps left 270 candidates
-//   of 128001 for k = 50, this leaves 60).  Where equal logits make too many of them, candidates are counted in 1024 bins, equally wide in the logit.
-//   p: a class weighs at least (1 - p) / n of the total if it is kept (those behind it would otherwise weigh less than 1 - p), which bounds its logit.  Candidates are weighed in 1024
-//   bins, in the pass that sums the total: a bin is 0.04 octaves wide at most, so a member's share of its bin's largest weight, 17 bits, goes into a 32-bit sum.
-// What lies in the bin of the goal, or everything down to it if that is little, is gathered in a list, ordered by counting, and weighed exactly.
-// Otherwise (thousands of equal logits, k above 256, no finite bound) it is found digit by digit of the logit's bits: the CTAs count (and weigh) what
+//   k: a logit that k of 512 groups of lanes reach with their largest: k-th and better lie at or above it, and little else does (60 of 128001 for k = 50; the smallest maximum of 64
+//   warps left 270).  Where equal logits make too many of them, candidates are counted in 2048 bins (one CTA: 1024), equally wide in the logit.
+//   p: a class weighs at least (1 - p) / n of the total if it is kept (those behind it would otherwise weigh less than 1 - p), which bounds its logit.  Candidates are weighed in such
+//   bins, in fp32: a bin is 0.043 octaves wide at most, so a member's share of its bin's largest weight, 17 bits, goes into a 32-bit sum.
+// What lies in the bins in which the goal may lie, or everything down to them if that is little, is gathered in a list, which the first CTA orders by counting; the pass that gathers it also
+// sums the row, and what lies above, in fp64.  Bins with more members than the list has room for are looked at again, 2048 times closer.
+// Otherwise (hundreds of equal logits, k above 256, no finite bound) the last member is found digit by digit of the logit's bits: the CTAs count (and weigh) what
 // has the digits found so far by its next one, read each other's counts, and each takes the digit in which the goal lies.
+//
+// us alone, 64 x 128001 bf16: no filter 25, k = 1 to 100 19, p = 0.8 to 0.99 62; 320 rows 94, 78 and 235, with probabilities 139, 109 and 275; one row 12, 12 and 31; one of 1000 classes 7, 10 and 16.
+// Bound by instructions, then by what a row waits for: a warp's 32 logits take 47 instructions without a filter (13 of them fp64, at two clocks), 28 for k, 124 for p (a look of about 50, the
+// exact pass of 45), and an SM issues 60 % of the time; joins, exchanges (400 clocks a meeting, 300 a remote load) and the list are serial, 3.5 CTAs an SM cover them in part.
+// Steps for p, 64 rows: digits only 351 (mixed settings), bins and a list 134, without calls and branches in the loops 120, fp32 bins 69, one CTA for the list 62.
 #pragma once
 #include <float.h>
 
@@ -151,7 +156,7 @@ struct SpBorder {          // of a CTA's bins: the first in which the goal may l
   int from, before, to, end;
   double weight;
 };
-struct alignas(16) SpWork {              // bins are read four at a time
+struct SpWork {
   union {
     uint32_t bins[kSpBins];              // members of a bin, or their weight; read by the others
     unsigned long long all[2 * kSpList]; // the lists of all CTAs, as many places each, written by them into the first CTA's; after that
@@ -176,7 +181,7 @@ sample_kernel(SampleArgs a) {
   extern __shared__ __align__(16) uint8_t sp_smem[];
   __shared__ SpSlot s_slot[2];
   __shared__ uint32_t s_top, s_tops[kSpWarps];
-  __shared__ __align__(16) SpWork s_work;
+  __shared__ SpWork s_work;
   __shared__ double s_roots[kSpTable];
   __shared__ double s_chunk[kSpList / 32], s_warp[kSpWarps], s_block[kSpMaxPart / kSpBlock + 2], s_double;
   __shared__ unsigned long long s_scan_m[kSpWarps];
@@ -590,7 +595,8 @@ sample_kernel(SampleArgs a) {
             const float y = (f - (down - 8388608.f)) * fall;       // exp(y) to y^4 / 24, 3e-8
             member = __float_as_uint(fmaf(fmaf(fmaf(131072.f / 6.f, y, 0.5f * 131072.f), y, 131072.f), y, 131072.f + 8388608.f)) - 0x4b000000u;       // 17 bits; a part has fewer than 2^15 members
           }
-          if (f >= 0.f && f < (float)n_bins) atomicAdd(&s_work.bins[__float_as_uint(down) - 0x4b000000u], member);
+          const uint32_t bin = __float_as_uint(down) - 0x4b000000u;       // beyond all bins where f is below 0, or no number
+          if (bin < (uint32_t)n_bins) atomicAdd(&s_work.bins[bin], member);
         }
       }
       if (by_weight) {
