@@ -471,7 +471,7 @@ size_t ee_int8_linear_workspace_bytes(int rows, int c);
  *   of these, those in front of which less than top_p times the weight of them all lies (top_p >= 1 or NaN: all);
  *   of these, those with w >= min_p (min_p <= 0 or NaN: all);
  * and the first class always.  A temperature that is not above 0 keeps the first alone.  The token is the first kept class, by index, at which the running sum of weights exceeds
- * u times their total (where u is not below 1, the last that weighs anything; where it is not above 0, the first).  probs: w / total of what is kept, else 0, as ee_verify_drafts
+ * u times their total (where u is 1 or more, the last that weighs anything; where it is not above 0, or NaN, the first).  probs: w / total of what is kept, else 0, as ee_verify_drafts
  * takes them for p and q.  What is kept and which token is drawn goes by weights and sums in fp64 (w below 2^-1075 is 0; with rows off
  * 16-byte boundaries the sums are grouped otherwise); probs are that in fp32, the exponent's argument and the power rounded, and 0 below 2^-126.  A logit of -inf is masked: it weighs nothing.  A row with nothing else has the token -1 and probabilities 0; one that holds NaN
  * or +inf has the token -1 and probabilities NaN.  probs may be logits (fp32); other overlaps are refused.  n up to 614400.  Errors: INVALID_ARG, CAPACITY (n or the grid
