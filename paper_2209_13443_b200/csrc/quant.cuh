@@ -1,9 +1,11 @@
 // Rows in 8 bits, and the projection of such rows.
 //
 // quantise: s = max |x| (1 / 127) of a row, both rounded to fp32, and q = the integer nearest to x / s, of two the even one.  The quotient is meant, not its rounding to
-// fp32: x times 1 / s is off by less than 127 * 2^-23 (1 + 2^-1) = 2.3e-5, so what lies within 3e-5 of the middle of two integers is held against the middle itself: x - (q + 1/2) s in
-// one multiply-add, whose sign is exact.  A row is read once and kept in the registers of 8 lanes to 16 warps, up to four 16-byte words a lane; longer rows are read twice, from L2 the second time.
-// 50176 x 512 bf16: 18 us of 11.8 that its bytes take, 4096 x 4096 14 of 7.7: 110 instructions for eight values of a warp's lanes bound it as much as memory does.  Tried and taken
+// fp32: n, x times 1 / s rounded, is that integer or, within 3e-5 of the middle of two, its neighbour.  e = x - n s is one multiply-add and exact (a multiple of the last place of s, or of x where
+// |x| < s, and not much above s / 2), so |e| against s / 2 says which, and where the middle is hit.  A row is read once and kept in the registers of 8 lanes to 16 warps, up to four
+// 16-byte words a lane; longer rows are read twice, from L2 the second time.
+// 50176 x 512 bf16: 15 us of 11.8 that its bytes take, 4096 x 4096 11.5 of 7.7; 89 instructions for eight values of a warp's lanes.  With the neighbours of a middle told by their distance to it,
+// 3e-5 either way, 117 and 18 us: of values with 8 bits a great many lie that near, and most warps went the rare way.  Tried and taken
 // back: rows copied ahead into shared memory (20 us), persistent CTAs with the next row in registers (19), two multiply-adds an instruction (nothing; the moves to pairs).
 //
 // dequantise: y = q s, rounded once.  Rows in any order.  12544 x 1024 bf16 10 us of 5.9, 50176 x 512 16.5 of 11.8, gathered 0.4 to 2 more.
@@ -67,6 +69,9 @@ struct QScale {
     tiny = s < 1e-37f && s > 0.f;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));       // to 2^-23
     inv = s > 0.f && !tiny ? inv : 0.f;
+    // Values of few bits are often (n + 1/2) max / 127: an inverse on the side of 1 / s on which 127 / max is not puts them where s does.
+    const float below = fmaf(127.f, s, -top), off = fmaf(inv, s, -1.f);
+    if (inv > 0.f && below * off > 0.f) inv = __uint_as_float(__float_as_uint(inv) + (off < 0.f ? 1u : ~0u));
   }
   static __device__ __noinline__ int slow(float x, float s) {
     const double q = rint((double)x / (double)s);
@@ -77,26 +82,23 @@ struct QScale {
   __device__ __forceinline__ void bytes(const QWord<T>& v, uint32_t* out) const {
     constexpr int N = QWord<T>::N;
     constexpr float kMagic = 12582912.f;             // 1.5 * 2^23: the sum's last place is 1, its low byte the integer
-    float worst = 0.f;
+    const float half = 0.5f * s;
+    float worst = 0.f, e[N];
     uint32_t b[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float x = v.at(i), r = fmaf(x, inv, kMagic);
       b[i] = __float_as_uint(r);
-      worst = fmaxf(worst, fabsf(fmaf(x, inv, kMagic - r)));     // what is left of x / s
+      e[i] = fmaf(kMagic - r, s, x);                 // what is left of x
+      worst = fmaxf(worst, fabsf(e[i]));
     }
     // Rare, and so asked for by whole warps: predicated, these were half of all instructions.
-    if (__any_sync(0xffffffffu, worst > 0.49997f || !(inv > 0.f))) {
-      const bool none = s != s;
-      // x against the middle between the integer and its neighbour: one multiply-add, whose sign is exact (a multiple of 2^-147 at least)
+    if (__any_sync(0xffffffffu, worst >= half || !(inv > 0.f))) {
+      const bool none = !(s > 0.f);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float x = v.at(i), n = __uint_as_float(b[i]) - kMagic, d = fmaf(x, inv, -n);
-        if (fabsf(d) > 0.49997f) {
-          const float half = n + copysignf(0.5f, d), e = fmaf(-half, s, x);
-          const float q = e == 0.f ? rintf(half) : half + copysignf(0.5f, e);
-          b[i] = __float_as_uint(q + kMagic);
-        }
+      for (int i = 0; i < N; ++i) {                  // more than half is left, or half of an odd integer's
+        const uint32_t left = (__float_as_uint(e[i]) & 0x7fffffffu) + (b[i] & 1u);
+        if (left > __float_as_uint(half)) b[i] += 1 | (int)__float_as_uint(e[i]) >> 31;
         if (none) b[i] = 0u;
       }
       if (__any_sync(0xffffffffu, tiny)) {
@@ -123,8 +125,9 @@ constexpr int kQThreads = 256, kQKeep = 4;      // threads of a CTA, words of a 
 // SHIFT: rows that do not all start on 16-byte boundaries.  L lanes then take the aligned words that hold the next L - 1 groups of N values, quantise them (what is not of
 // the row counts as 0), and each lane puts its group together from its word's bytes and the next lane's: wide accesses on both sides.
 // Nothing that is read here is __restrict__: the kernel starts while the one in front, which may write it, still runs.
+// CTAs an SM: as many as their words in registers allow (1000 x 20000 fp32, read twice: 26 us with three, 31 with two; 4096 x 4096 bf16 11.5 with four, 12.1 with no number given).
 template <typename T, bool SHIFT, int L, int WARPS, int KEEP>
-__global__ void __launch_bounds__(WARPS > 8 ? 32 * WARPS : kQThreads)
+__global__ void __launch_bounds__(WARPS > 8 ? 32 * WARPS : kQThreads, KEEP == 0 ? 3 : WARPS > 8 ? 2 : sizeof(T) == 4 ? 5 : 4)
 quantize_rows_kernel(const T* x, int8_t* q, float* scale, long rows, int c, int pitch) {
   constexpr int N = QWord<T>::N, kRows = (WARPS > 8 ? 32 * WARPS : kQThreads) / (L * WARPS), kWords = SHIFT ? L - 1 : L, kSteps = WARPS * kWords;
   typedef typename std::conditional<N == 8, uint2, uint32_t>::type Group;

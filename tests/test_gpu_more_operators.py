@@ -108,6 +108,18 @@ def test_the_middle_of_two_integers_goes_to_the_even_one(dtype):
     check_rows(x, *quantised(x, "f32"))
 
 
+def test_every_quotient_of_bf16():
+    """A row for each significand of a maximum, with all values of twelve octaves below it: middles of two integers, and what the rounded scale makes of them."""
+    top = (0x3f80 + torch.arange(128, device="cuda")).to(torch.int16)
+    below = (0x3f80 - 11 * 128 + torch.arange(12 * 128, device="cuda")).to(torch.int16)
+    mag = torch.cat([top[:, None], torch.minimum(below[None].expand(128, -1), top[:, None])], 1)
+    for power in (0, 100, -100):
+        x = torch.cat([mag.view(torch.bfloat16), -mag.view(torch.bfloat16)], 1).mul(2.0 ** power).contiguous()
+        for dtype in ("bf16", "f32"):
+            v = x.to(TD[dtype])
+            check_rows(v, *quantised(v, dtype))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_rows_at_the_ends_of_the_type(dtype):
     big, small = torch.finfo(TD[dtype]).max, 2.0 ** -133
