@@ -139,7 +139,7 @@ struct SpSlot {            // what a CTA tells the others
   double d, e;
   int i;
 };
-struct SpHist {            // by digit: members, and their weight in units of 2^-43 (at most 614400 of them, each at most 1)
+struct SpHist {            // by digit: members, and their weight in whole units
   uint32_t count[256];
   unsigned long long mass[256];
 };
@@ -330,14 +330,16 @@ sample_kernel(SampleArgs a) {
     int last_at = 0x7fffffff;
     auto kept = [&](float l, int i) { return l > last || (l == last && i0 + i <= last_at); };
 
-    // Of what is kept, the new last member: by count (the goal-th), or by weight (the last before which there is less than goal).
-    auto select = [&](bool by_weight, double goal) {
+    // Of what is kept, the new last member: by count (the goal-th), or by weight (the last before which there is less than goal; all of it weighs `sum`).
+    // Weights are added as whole numbers, in any order.  Their unit is the power of 2 between 2^-62 and 2^-63 of the sum: n of them are off by n 2^-63 of it at most, 2^-43.7, where chains of fp64
+    // additions could be by n 2^-53.  (In units of 2^-43 a top_p of 1 - 2^-24 over 262144 classes ended in another class in one row of four.)
+    auto select = [&](bool by_weight, double goal, double sum) {
       constexpr int kRounds = sizeof(T) == 2 ? 2 : 4;      // a bf16's bits end after two digits
       uint32_t prefix = 0u;
       uint32_t above = 0u;
       unsigned long long above_m = 0ull;
-      const double unit = 8796093022208.0;                 // 2^43
-      const unsigned long long goal_m = (unsigned long long)fmin(ceil(goal * (by_weight ? unit : 1.0)), 1.8e19);
+      const double units = __hiloint2double((int)((2u * 1023u + 62u << 20) - ((unsigned)__double2hiint(sum) & 0x7ff00000u)), 0);      // of 1: 2^62 over the power of 2 in the sum, which is 1 at least
+      const unsigned long long goal_m = (unsigned long long)ceil(goal * (by_weight ? units : 1.0));       // below 2^63
       int in = 0;
 #pragma unroll 1
       for (int r = 0; r < kRounds; ++r) {
@@ -351,7 +353,7 @@ sample_kernel(SampleArgs a) {
           if ((r == 0 || key >> (shift + 8) == prefix) && kept(l, i)) {
             const int d = key >> shift & 255;
             atomicAdd(&h.count[d], 1u);
-            if (by_weight) atomicAdd(&h.mass[d], (unsigned long long)__double2ull_rn(weight(l) * unit));
+            if (by_weight) atomicAdd(&h.mass[d], (unsigned long long)__double2ull_rn(weight(l) * units));
           }
         }
         meet();
@@ -884,17 +886,16 @@ sample_kernel(SampleArgs a) {
 #pragma unroll 1
       for (int by_weight = 0; by_weight < 2; ++by_weight) {
         if (!(by_weight ? need_p : need_k)) continue;
-        double v = (double)k;
+        double v = 0.0;
         if (by_weight) {
-          v = 0.0;
           for (int i = tid; i < cnt; i += kSpThreads) {
             const float l = logit(i);
             if (kept(l, i)) v += weight(l);
           }
           tell(cta_sum(v), 0);
-          v = (double)p * told_sum();
+          v = told_sum();
         }
-        select(by_weight != 0, v);
+        select(by_weight != 0, by_weight ? (double)p * v : (double)k, v);
       }
     }
     const double least = by_m ? (double)m : 0.0;

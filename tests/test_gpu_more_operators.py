@@ -369,6 +369,33 @@ def test_sample_of_the_longest_rows(n, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,spread", [(262144, 4.0), (614400, 3.0), (614400, 4.0)])
+def test_sample_of_a_nucleus_that_leaves_out_next_to_nothing(n, spread, dtype):
+    """top_p one step below 1: what stays outside is 2^-24 of the total, in classes that weigh down to 10^-13 of it.  Weights are off by 2^-47 of theirs (|z| <= 44 octaves in 53 bits, the
+    polynomial), sums in fp64 by chains of 180 additions, 2^-45; whole numbers in which the search counts, half a unit of up to 2^-62 of the total for each of n classes:
+    2^-43.7.  So the last class that is kept has less than p (1 + 2^-42) of the total in front of it, and p (1 - 2^-42) at least with it."""
+    g = gen(n + int(spread))
+    rows = 12
+    x = (spread * normal(g, rows, n)).to(TD[dtype])
+    k = torch.tensor([0, 5000, 0, n // 2] * 3, dtype=torch.int32, device="cuda")
+    p, u = 1 - 2.0 ** -24, uniform(g, rows)
+    tokens, out = sample_run(x, dtype, k=k, p=f32([p] * rows), u=u)
+    host, got = x.float().cpu().numpy().astype(np.longdouble), out.cpu().numpy()
+    for i in range(rows):
+        order = np.argsort(-host[i], kind="stable")[:int(k[i]) or n]
+        w = np.exp(host[i][order] - host[i][order[0]])
+        c = np.concatenate([[np.longdouble(0)], np.cumsum(w)])
+        count = int((got[i] > 0).sum())
+        assert (got[i][order[:count]] > 0).all()               # the first of the order
+        goal, off = p * c[-1], np.longdouble(2.0 ** -42)
+        assert c[count - 1] < goal * (1 + off) and c[count] >= goal * (1 - off), (i, count, int((c[:-1] < goal).sum()))
+        q = np.zeros(n, np.longdouble)
+        q[order[:count]] = w[:count]
+        cum = np.cumsum(q)
+        assert int(tokens[i]) == int(np.nonzero(cum > np.longdouble(float(u[i])) * cum[-1])[0][0])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n", [5, 700, 20000, 128001])
 def test_sample_settings_at_their_ends(n, dtype):
     g = gen(n + 1)
