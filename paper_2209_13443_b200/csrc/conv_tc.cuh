@@ -126,6 +126,18 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, int* er
   }
   return true;
 }
+// The same within a limit of the caller's, which counts from a look that does not suspend the thread.  try_wait may do so for longer than a short limit, which is kept by further such looks.
+__device__ __forceinline__ bool mbar_wait_within(uint32_t bar, uint32_t parity, int* err_flag, long long limit) {
+  if (mbar_test_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  do {
+    if (clock64() - t0 > limit) {
+      atomicExch(err_flag, (int)EE_ERR_TIMEOUT);
+      return false;
+    }
+  } while (!(limit < 1000000 ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)));
+  return true;
+}
 // Bounded wait for what other CTAs of the cluster send into this one's shared memory (st.async, counted by the barrier): acquire at the scope of the
 // cluster, the one at which st.async releases (without a qualifier the waits are of the CTA's).  A look that does not suspend the thread comes first,
 // so the limit counts from there.

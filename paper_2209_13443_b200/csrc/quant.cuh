@@ -354,6 +354,7 @@ inline cudaError_t dequantize_launch(const int8_t* q, const float* scale, const 
 
 // ----------------------------------------------------------------------------- projection
 
+constexpr int kI8None = (int)0x80000000;   // no sum of products: those end at 128 * 128 * 131071
 constexpr int kI8FewRows = 4;   // up to this many rows every CTA quantises for itself
 
 struct I8Args {
@@ -590,7 +591,8 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
       asm volatile("bar.sync 1, %0;" ::"n"(kEpi) : "memory");
     }
     I8Store<T> out(p, f, lane);
-    out.ok = __all_sync(0xffffffffu, mbar_wait(accum_bar, 0, p.err_flag));
+    const bool own = __all_sync(0xffffffffu, mbar_wait_within(accum_bar, 0, p.err_flag, Z > 1 ? p.wait_cycles : kTcWaitCycles));
+    out.ok = own;
     tc_fence_after();
     const uint32_t lane_base = tmem + ((uint32_t)(q * 32) << 16);
     const I8Value<T> of(ws, bias);
@@ -611,7 +613,12 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
 #pragma unroll 1
       for (int c = h * CH; c < TN; c += 2 * CH) {
         int v[CH];
-        tmem_ld_cols(lane_base + c, v, ch);
+        if (own) {
+          tmem_ld_cols(lane_base + c, v, ch);
+        } else {                  // nobody waits for bytes that are never sent, nor takes these for a part
+#pragma unroll
+          for (int i = 0; i < CH; ++i) v[i] = kI8None;
+        }
         if (share >= 4) {
 #pragma unroll
           for (int i = 0; i < CH; i += 4) {
@@ -635,28 +642,31 @@ int8_linear_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constan
         }
       }
       lost = !__all_sync(0xffffffffu, mbar_wait_cluster(part_bar, 0, p.err_flag, p.wait_cycles));
-      out.ok = out.ok && !lost;
+      out.ok = own && !lost;
       const int* in = reinterpret_cast<const int*>(gen + S::kOffPart);
 #pragma unroll 1
       for (int i = 4 * h; i < share; i += 8) {
-        int sum[4] = {0, 0, 0, 0};
+        uint32_t sum[4] = {0u, 0u, 0u, 0u};
+        int least = 0;
         if (share >= 4) {
 #pragma unroll 2
           for (int k = 0; k < Z; ++k) {
             const int4 o = *reinterpret_cast<const int4*>(in + (k * share + i) * 128 + row * 4);
-            sum[0] += o.x, sum[1] += o.y, sum[2] += o.z, sum[3] += o.w;
+            sum[0] += o.x, sum[1] += o.y, sum[2] += o.z, sum[3] += o.w, least = min(least, o.x);      // a warp sends a run of columns whole
           }
         } else {
 #pragma unroll 2
           for (int k = 0; k < Z; ++k) {
             const int2 o = *reinterpret_cast<const int2*>(in + k * 256 + row * 2);
-            sum[0] += o.x, sum[1] += o.y;
+            sum[0] += o.x, sum[1] += o.y, least = min(least, o.x);
           }
         }
+        out.ok = __all_sync(0xffffffffu, out.ok && least != kI8None);
         const int c = z * share + i;
-        out.put2(t0 + c, value(sum[0], c), value(sum[1], c + 1));
-        if (share >= 4) out.put2(t0 + c + 2, value(sum[2], c + 2), value(sum[3], c + 3));
+        out.put2(t0 + c, value((int)sum[0], c), value((int)sum[1], c + 1));
+        if (share >= 4) out.put2(t0 + c + 2, value((int)sum[2], c + 2), value((int)sum[3], c + 3));
       }
+      if (!own) mbar_wait(accum_bar, 0, p.err_flag);      // the tensor memory is not given back under a product
     }
     tc_fence_before();
   }

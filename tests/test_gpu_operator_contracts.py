@@ -274,6 +274,38 @@ def _late(call, outs):
     assert all(torch.equal(o, w) for o, w in zip(outs, want))
 
 
+def _whatever_the_limit(call, outs):
+    """`call` under limits from far too short to long enough, a tenth apart.  Between them the own products of some blocks come in time and those of others do not: whoever lacks a part of its sums leaves
+    its outputs (77) as they are."""
+    for o in outs:
+        o.fill_(77)
+    call()
+    eb.operators_check()
+    want, late = [o.clone() for o in outs], 0
+    try:
+        for step in range(62):
+            eb.operators_set_wait_limit(int(100 * 1.1 ** step))
+            for _ in range(6):
+                for o in outs:
+                    o.fill_(77)
+                call()
+                try:
+                    eb.operators_check()
+                except eb.EEError as e:
+                    assert e.status == 7                               # EE_ERR_TIMEOUT
+                    late += 1
+                for o, w in zip(outs, want):
+                    assert bool(((o == w) | (o == 77)).all())
+    finally:
+        eb.operators_set_wait_limit(4_000_000_000)
+    assert late
+    for o in outs:
+        o.fill_(77)
+    call()
+    eb.operators_check()
+    assert all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("shape", [(2, 3136, 64, 8), (1, 30000, 520, 40), (3, 957, 96, 32)], ids=str)
 def test_group_norm_whose_exchange_runs_out_of_time(shape, dtype):
@@ -327,3 +359,14 @@ def test_a_models_group_norms_go_by_its_limit():
     m.check()
     assert torch.equal(y, want)
     m.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c,n", [(1, 2048, 1000), (3, 8192, 512), (16, 4096, 2048), (40, 8199, 300), (128, 2048, 256)])
+def test_int8_linear_in_which_some_products_are_late(rows, c, n, dtype):
+    g = gen(rows + c)
+    x = normal(g, rows, c).to(TD[dtype])
+    w = torch.zeros(n, eb.int8_row_bytes(c), dtype=torch.int8, device="cuda")
+    w[:, :c] = torch.randint(-127, 128, (n, c), generator=g, device="cuda")
+    y, room = torch.empty(rows, n, dtype=TD[dtype], device="cuda"), torch.empty(eb.int8_linear_workspace_bytes(rows, c) + 256, dtype=torch.uint8, device="cuda")
+    _whatever_the_limit(lambda: eb.int8_linear(dtype, x, rows, c, w, None, n, y, workspace=room), [y])
