@@ -37,6 +37,7 @@ constexpr int kLrParts = 2;            // bf16 parts of h
 constexpr int kLrMaxRank = 128;
 constexpr float kLrBf16Max = 3.3895313892515355e38f;   // the largest bf16
 constexpr int kLrShrinkTN = 64;        // rows of a tile of the first launch
+constexpr uint32_t kLrNone = 0xffffffffu;   // a NaN that no sum is: what arithmetic makes of NaN is 0x7fffffff
 constexpr long kLrSimtWork = 24L << 20;  // products of the first launch up to which CUDA cores take it: every row of x reads its adapter from L2
 constexpr int kLrCopyWarps = 8, kLrFillWarps = 8;
 template <bool COPY, bool SHRINK> constexpr int kLrThreads = 192 + 32 * (COPY ? kLrCopyWarps : 1) + (SHRINK ? 0 : 32 * kLrFillWarps);
@@ -543,7 +544,11 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
         const int* s_ad = s_ad0 + (it & (kAcc - 1)) * TN;
         const int* s_slot = s_slot0 + (it & (kAcc - 1)) * TN;
         const int acc = it & (kAcc - 1);
-        ok = __all_sync(0xffffffffu, mbar_wait(accum_bar(acc), (uint32_t)(it / kAcc) & 1u, p.err_flag) && mbar_wait(filled_bar(it & 1), (uint32_t)(it >> 1) & 1u, p.err_flag)) && ok;
+        auto come = [&](uint32_t bar, uint32_t parity) {
+          if constexpr (kPersist) return mbar_wait(bar, parity, p.err_flag);
+          else return mbar_wait_within(bar, parity, p.err_flag, Z > 1 ? p.wait_cycles : kTcWaitCycles);
+        };
+        ok = __all_sync(0xffffffffu, come(accum_bar(acc), (uint32_t)(it / kAcc) & 1u) && come(filled_bar(it & 1), (uint32_t)(it >> 1) & 1u)) && ok;
         tc_fence_after();
         const uint32_t lane_base = tmem + (uint32_t)(acc * TN) + ((uint32_t)(q * 32) << 16);
         const int f = n0 + row;
@@ -590,7 +595,12 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
 #pragma unroll 1
           for (int c = 0; c < TN; c += CH) {
             float v[CH];
-            columns_of(c, v);
+            if (ok) {
+              columns_of(c, v);
+            } else {                // nobody waits for bytes that are never sent, nor takes these for a part
+#pragma unroll
+              for (int i = 0; i < CH; ++i) v[i] = __uint_as_float(kLrNone);
+            }
             if (share >= 4) {
 #pragma unroll
               for (int i = 0; i < CH; i += 4) {
@@ -613,6 +623,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
               }
             }
           }
+          const bool own = ok;
           lost = !__all_sync(0xffffffffu, mbar_wait_cluster(part_bar, 0, p.err_flag, p.wait_cycles));
           ok = ok && !lost;
           const float* in = reinterpret_cast<const float*>(gen + S::kOffPart);
@@ -620,19 +631,21 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
 #pragma unroll 1
           for (int i = 0; i < share; i += run) {
             float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            uint32_t most = 0u;
             if (run == 4) {
 #pragma unroll 2
               for (int k = 0; k < Z; ++k) {
                 const float4 o = *reinterpret_cast<const float4*>(in + (k * share + i) * 128 + row * 4);
-                sum[0] += o.x, sum[1] += o.y, sum[2] += o.z, sum[3] += o.w;
+                sum[0] += o.x, sum[1] += o.y, sum[2] += o.z, sum[3] += o.w, most = max(most, __float_as_uint(o.x));      // a warp sends a run of columns whole
               }
             } else {
 #pragma unroll 2
               for (int k = 0; k < Z; ++k) {
                 const float2 o = *reinterpret_cast<const float2*>(in + k * 256 + row * 2);
-                sum[0] += o.x, sum[1] += o.y;
+                sum[0] += o.x, sum[1] += o.y, most = max(most, __float_as_uint(o.x));
               }
             }
+            ok = __all_sync(0xffffffffu, ok && most != kLrNone);
             const int t = t0 + z * share + i;
             if (pairs) {
               store2(t, sum[0] + bias, sum[1] + bias);
@@ -643,6 +656,7 @@ lowrank_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
                 if (j < run && ok && f < p.n && t + j < p.rows) p.y[(size_t)(t + j) * p.n + f] = __float2bfloat16_rn(sum[j] + bias);
             }
           }
+          if (!own) mbar_wait(accum_bar(acc), 0, p.err_flag);      // the tensor memory is not given back under a product
         }
       }
     }

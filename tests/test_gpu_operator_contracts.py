@@ -370,3 +370,28 @@ def test_int8_linear_in_which_some_products_are_late(rows, c, n, dtype):
     w[:, :c] = torch.randint(-127, 128, (n, c), generator=g, device="cuda")
     y, room = torch.empty(rows, n, dtype=TD[dtype], device="cuda"), torch.empty(eb.int8_linear_workspace_bytes(rows, c) + 256, dtype=torch.uint8, device="cuda")
     _whatever_the_limit(lambda: eb.int8_linear(dtype, x, rows, c, w, None, n, y, workspace=room), [y])
+
+
+@pytest.mark.parametrize("shape", [(1, 2048, 1000, 8, 16), (16, 8192, 512, 16, 32), (64, 4096, 512, 16, 32), (40, 1001, 300, 3, 4), (256, 4096, 256, 64, 9)], ids=str)
+def test_adapted_linear_in_which_some_products_are_late(shape):
+    rows, c, n, rank, m = shape
+    x, w, bias, a, b, scale, which = linear_operands(3, *shape, "bf16")
+    y, ws = torch.empty((rows, n), dtype=torch.bfloat16, device="cuda"), torch.empty(eb.adapted_linear_workspace_bytes(rows, rank) + 256, dtype=torch.uint8, device="cuda")
+    _whatever_the_limit(lambda: eb.adapted_linear("bf16", x, rows, c, w, n, a, b, rank, m, which, y, ws, bias=bias, scale=scale), [y])
+
+
+def test_adapted_linear_of_nan_in_every_bit():
+    """Sums of products with NaN of any bits are NaN, in a tile whose K a cluster shares."""
+    rows, c, n, rank, m = shape = (20, 4096, 300, 4, 3)
+    x, w, bias, a, b, scale, which = linear_operands(4, *shape, "bf16")
+    bits = torch.tensor([-1, 0x7fff, 0x7fc0, -64, 0x7f81, -127], dtype=torch.int16, device="cuda")      # 0xffff, 0x7fff, 0x7fc0, 0xffc0, 0x7f81, 0xff81
+    for i in range(6):
+        x[2 * i, 700 * i] = bits[i:i + 1].view(torch.bfloat16)[0]
+    w[7, 5], w[9, 4000] = bits[:1].view(torch.bfloat16)[0], bits[3:4].view(torch.bfloat16)[0]
+    y, ws = torch.full((rows, n), 77, dtype=torch.bfloat16, device="cuda"), torch.empty(eb.adapted_linear_workspace_bytes(rows, rank) + 256, dtype=torch.uint8, device="cuda")
+    eb.adapted_linear("bf16", x, rows, c, w, n, a, b, rank, m, which, y, ws, bias=bias, scale=scale)
+    eb.operators_check()
+    bad = torch.zeros(rows, n, dtype=torch.bool, device="cuda")
+    bad[[0, 2, 4, 6, 8, 10]] = True
+    bad[:, [7, 9]] = True
+    assert torch.equal(y.isnan(), bad) and not bool((y == 77).any())
