@@ -395,6 +395,23 @@ def test_sample_of_a_nucleus_that_leaves_out_next_to_nothing(n, spread, dtype):
         assert int(tokens[i]) == int(np.nonzero(cum > np.longdouble(float(u[i])) * cum[-1])[0][0])
 
 
+@pytest.mark.parametrize("n", [16384, 32768, 262080])
+def test_sample_of_weights_that_sums_in_fp32_lose(n):
+    """One class of weight 1 for each thread (of a part's words, every 256th is a thread's), and a tail of which each weighs less than half a unit in the last place of that: added to it in fp32 they are lost,
+    and the nucleus ends among them, at a quarter, a half and three quarters of what they weigh."""
+    g = gen(n)
+    per = n // max(1, min(8, n // 16384))
+    place = torch.arange(n, device="cuda") % per
+    tail = -np.log(2.0) * (24.01 + 0.6 * uniform(g, 3, n))
+    x = torch.where((place < 1024) & (place % 4 == 0), torch.zeros_like(tail), tail)
+    w = torch.exp(x.double())
+    out = 1 - (w * (x == 0)).sum(1) / w.sum(1)
+    p = (1 - out * torch.tensor([0.75, 0.5, 0.25], device="cuda")).float()
+    assert bool((p < 1).all()) and bool((out > 1e-6).all())
+    for u in (uniform(g, 3), f32([1 - 2.0 ** -24] * 3)):
+        sample_check(x, "f32", p=p, u=u)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n", [5, 700, 20000, 128001])
 def test_sample_settings_at_their_ends(n, dtype):
