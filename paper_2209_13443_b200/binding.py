@@ -573,7 +573,8 @@ def sample(dtype: str, logits, rows: int, n: int, u, tokens, temperature=None, t
 
 
 def operators_set_wait_limit(cycles: int):
-    """ee_operators_set_wait_limit: how long, in SM clock cycles, a block of an operator's kernel waits for the others of its cluster."""
+    """ee_operators_set_wait_limit: how long, in SM clock cycles, a block of an operator's kernel waits for the others of its cluster, and
+    in the projections for its own part of the sums that they share."""
     _check(load_library().ee_operators_set_wait_limit(int(cycles)), "ee_operators_set_wait_limit")
 
 

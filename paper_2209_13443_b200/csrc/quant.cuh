@@ -4,18 +4,22 @@
 // fp32: n, x times 1 / s rounded, is that integer or, within 3e-5 of the middle of two, its neighbour.  e = x - n s is one multiply-add and exact (a multiple of the last place of s, or of x where
 // |x| < s, and not much above s / 2), so |e| against s / 2 says which, and where the middle is hit.  A row is read once and kept in the registers of 8 lanes to 16 warps, up to four
 // 16-byte words a lane; longer rows are read twice, from L2 the second time.
-// 50176 x 512 bf16: 15 us of 11.8 that its bytes take, 4096 x 4096 11.5 of 7.7; 89 instructions for eight values of a warp's lanes.  With the neighbours of a middle told by their distance to it,
+// 50176 x 512 bf16: 15 us of 11.8 that its bytes take, 4096 x 4096 11.5 of 7.7; fp32 20.6 of 19.6 and 25 of 12.8 (rows above 2048 take a CTA of 512 threads, two an SM: a warp waits 6.6 of the 16
+// clocks between two issues for its loads); 89 instructions for eight values of a warp's lanes.  With the neighbours of a middle told by their distance to it,
 // 3e-5 either way, 117 and 18 us: of values with 8 bits a great many lie that near, and most warps went the rare way.  Tried and taken
 // back: rows copied ahead into shared memory (20 us), persistent CTAs with the next row in registers (19), two multiply-adds an instruction (nothing; the moves to pairs).
 //
-// dequantise: y = q s, rounded once.  Rows in any order.  12544 x 1024 bf16 10 us of 5.9, 50176 x 512 16.5 of 11.8, gathered 0.4 to 2 more.
+// dequantise: y = q s, rounded once.  Rows in any order.  12544 x 1024 bf16 10 us of 5.9, 50176 x 512 16.5 of 11.8, fp32 14.4 of 9.8 and 27 of 19.6, gathered 0.4 to 4 more.  Bound by its loads' latency: a
+// warp waits for them 26 of the 35 clocks between two issues (index, then scale and bytes; nothing of the next row is on its way).
 //
 // projection: y[t][f] = xs[t] ws[f] sum_k q[t][k] w[f][k] + bias[f], the sum on tcgen05 (kind::i8, 32-bit integers).  A sum of integers is exact, so however
 // K is cut and whatever else is in the batch, a row has the same bits.  The tile is turned, as in lowrank.cuh: filters are the rows of the accumulator, whose scale
 // and bias a thread keeps in registers, rows of the batch its columns; W, which bounds small batches, is read once.
 // Two forms.  Few tiles: a CTA of its own for each, K cut over a cluster whose CTAs send each other their parts as asynchronous stores.  More: CTA pairs
 // (cta_group::2), persistent, 256 filters by 256 rows with two accumulators: each SM of a pair fetches half of either operand, 32 KB for 512 clocks of products, which is
-// what L2 gives (64 bytes a clock); 128 x 256 tiles of a single SM would need 96.  4096 x 4096 x 4096: 45.5 us (3.0 POP/s, 0.90 of twice the bf16 rate); from bf16 rows 55, from and to fp32 91.
+// what L2 gives (64 bytes a clock); 128 x 256 tiles of a single SM would need 96.  4096 x 4096 x 4096: 45.5 us (3.0 POP/s, 0.90 of twice the bf16 rate); from bf16 rows 55.  To fp32
+// 60 to 65: the epilogue, 7 us a tile (K = 128: 25 us, bf16 16), waits for the fp64 units and the way back from fp64 (4.4 of 13 clocks between two issues), and the last one lies under no product; from
+// fp32 rows 90 to 96.
 // 64 x 4096 x 4096: 6.7 us, of which its 17 MB take 2.7: the set-up and the first bytes 2, the exchange 1.5, the epilogue 1.
 #pragma once
 #include "common.cuh"

@@ -14,12 +14,17 @@
 //   bins, in fp32: a bin is 0.043 octaves wide at most, so a member's share of its bin's largest weight, 17 bits, goes into a 32-bit sum.
 // What lies in the bins in which the goal may lie, or everything down to them if that is little, is gathered in a list, which the first CTA orders by counting; the pass that gathers it also
 // sums the row, and what lies above, in fp64.  Bins with more members than the list has room for are looked at again, 2048 times closer.
-// Otherwise (hundreds of equal logits, k above 256, no finite bound) the last member is found digit by digit of the logit's bits: the CTAs count (and weigh) what
-// has the digits found so far by its next one, read each other's counts, and each takes the digit in which the goal lies.
+// Otherwise the last member is found digit by digit of the logit's bits: the CTAs count (and weigh) what has the digits found so far by its next one, read each other's counts, and each takes the
+// digit in which the goal lies.  That is so for k above 256, for p behind such a k or with no finite bound, for CTAs' parts above 32767 (p and 262137 to 307200 classes, or more than 524272; 17-bit
+// shares would pass 32 bits), where more than the list's 512 places hold have the logit at the border, and where a CTA has more members than its share of the list's room (128 of eight, when few rows
+// of a vocabulary ordered by frequency have most of the weight).  The last two happen to ordinary bf16 rows: the further their logits lie from 0 the more of them are equal.
 //
-// us alone, 64 x 128001 bf16: no filter 25, k = 1 to 100 19, p = 0.8 to 0.99 62; 320 rows 94, 78 and 235, with probabilities 139, 109 and 275; one row 12, 12 and 31; one of 1000 classes 7, 10 and 16.
+// us alone, 64 x 128001 bf16: no filter 25, k = 1 to 100 19, p = 0.8 to 0.99 62; 320 rows 94, 78 and 235, with probabilities 139, 109 and 275; one row 12, 12 and 31; one of 1000 classes 7, 10 and 16;
+// the best alone (t = 0) 11, one of 1000 classes 3.  These are N(0, 3).  p on 64 rows by digits: N(4, 2) 850, N(8, 2) and N(-8, 1) 630, logits that fall with the index 990, 262144 classes 1060, 614400 2860; 128001
+// in fp32, where few are equal, 78 to 96, 262144 1950; k = 1000 102, with p behind it 229 (k = 5000); k = 200 39, 84 where the logits fall with the index.
 // Bound by instructions, then by what a row waits for: a warp's 32 logits take 47 instructions without a filter (13 of them fp64, at two clocks), 28 for k, 124 for p (a look of about 50, the
 // exact pass of 45), and an SM issues 60 % of the time; joins, exchanges (400 clocks a meeting, 300 a remote load) and the list are serial, 3.5 CTAs an SM cover them in part.
+// 64 registers let four CTAs share an SM, and put some 110 bytes of a thread in local memory.
 // Steps for p, 64 rows: digits only 351 (mixed settings), bins and a list 134, without calls and branches in the loops 120, fp32 bins 69, one CTA for the list 62.
 #pragma once
 #include <float.h>
