@@ -771,8 +771,9 @@ sample_kernel(SampleArgs a) {
           complete = above >= 0 && above + inside <= kSpList;
           if (above < 0) break;
           if (!complete && inside > kSpList) {
-            if (zoom > 1.f) break;           // equal logits, then
-            base = (float)from, zoom = 0.9995f * (float)n_bins / (float)(to - from + 1);        // `far` - base is exact: what lay in these bins lies in the new ones, and nothing else
+            const float closer = 0.9995f * (float)n_bins / (float)(to - from + 1);
+            if (zoom > 1.f || !(closer > 1.f)) break;           // equal logits, then; or the goal may lie in any bin (a class with all but some 10^-5 of the weight, and p beyond it): no closer look to take
+            base = (float)from, zoom = closer;        // `far` - base is exact: what lay in these bins lies in the new ones, and nothing else
             count0 = above, weight0 = border_weight;
             continue;
           }

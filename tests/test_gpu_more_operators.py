@@ -395,6 +395,19 @@ def test_sample_of_a_nucleus_that_leaves_out_next_to_nothing(n, spread, dtype):
         assert int(tokens[i]) == int(np.nonzero(cum > np.longdouble(float(u[i])) * cum[-1])[0][0])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [16000, 32768, 128001])
+def test_sample_of_a_nucleus_that_may_end_in_any_bin(n, dtype):
+    """One class has all of the weight but 10^-5, and top_p asks for some of the rest, which lies at the far end of what a kept class may be away from the best: (1 - p) / n of the total."""
+    g = gen(n)
+    p = 1 - np.array([1e-5, 2e-5, 5e-6, 1e-5])
+    far = np.log(n / (1 - p.astype(np.float32)).astype(np.float64))
+    x = torch.tensor(-far, device="cuda")[:, None] + torch.tensor([0.8, 0.8, 0.8, 6.0], device="cuda").double()[:, None] * uniform(g, 4, n).double()
+    x[torch.arange(4), torch.tensor([0, n // 2, n - 1, 7])] = 0.0
+    for off in (0.0, 5.0):
+        sample_check((x + off).float().to(TD[dtype]), dtype, p=f32(p.tolist()), u=uniform(g, 4))
+
+
 @pytest.mark.parametrize("n", [16384, 32768, 262080])
 def test_sample_of_weights_that_sums_in_fp32_lose(n):
     """One class of weight 1 for each thread (of a part's words, every 256th is a thread's), and a tail of which each weighs less than half a unit in the last place of that: added to it in fp32 they are lost,
