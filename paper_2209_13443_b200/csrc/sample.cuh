@@ -16,8 +16,8 @@
 // sums the row, and what lies above, in fp64.  Bins with more members than the list has room for are looked at again, 2048 times closer.
 // Otherwise the last member is found digit by digit of the logit's bits: the CTAs count (and weigh) what has the digits found so far by its next one, read each other's counts, and each takes the
 // digit in which the goal lies.  That is so for k above 256, for p behind such a k or with no finite bound, for CTAs' parts above 32767 (p and 262137 to 307200 classes, or more than 524272; 17-bit
-// shares would pass 32 bits), where more than the list's 512 places hold have the logit at the border, and where a CTA has more members than its share of the list's room (128 of eight, when few rows
-// of a vocabulary ordered by frequency have most of the weight).  The last two happen to ordinary bf16 rows: the further their logits lie from 0 the more of them are equal.
+// shares would pass 32 bits), where more than the list's 512 places hold have the logit at the border, where p leaves out less than some 10^-5 and the goal may lie in too many bins, and where a CTA has more members than its share of the list's room (128 of eight, when few rows
+// of a vocabulary ordered by frequency have most of the weight).  Equal logits happen to ordinary bf16 rows: the further they lie from 0 the more of them there are.
 //
 // us alone, 64 x 128001 bf16: no filter 25, k = 1 to 100 19, p = 0.8 to 0.99 62; 320 rows 94, 78 and 235, with probabilities 139, 109 and 275; one row 12, 12 and 31; one of 1000 classes 7, 10 and 16;
 // the best alone (t = 0) 11, one of 1000 classes 3.  These are N(0, 3).  p on 64 rows by digits: N(4, 2) 850, N(8, 2) and N(-8, 1) 630, logits that fall with the index 990, 262144 classes 1060, 614400 2860; 128001
