@@ -479,10 +479,10 @@ size_t ee_int8_linear_workspace_bytes(int rows, int c);
 ee_status_t ee_sample(int dtype, const void* logits, int rows, int n, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
                       int32_t* tokens, float* probs, void* cuda_stream);
 
-/* Limit, in SM clock cycles, of a block's wait for the others of its cluster in the operators above, and of its wait for its own part of a sum that they share in
- * ee_int8_linear and ee_adapted_linear,
- * on the current device (default about 2 s): what ee_model_set_wait_limit is for a model.  For the calls that follow; a captured one keeps what it was captured with.  Where a wait runs out, a
- * block leaves its part of the outputs as it is.  Errors: INVALID_ARG, CUDA. */
+/* Limit, in SM clock cycles, of a block's wait for the others of its cluster in the operators above, and, in ee_int8_linear and ee_adapted_linear, of its wait for
+ * its own part of a sum that they share, on the current device (default about 2 s): what ee_model_set_wait_limit is for a model.  For the calls that follow; a
+ * captured one keeps what it was captured with.  Where a wait runs out, a block leaves its part of the outputs as it is, and so does one that lacks another's part.
+ * Errors: INVALID_ARG, CUDA. */
 ee_status_t ee_operators_set_wait_limit(long long cycles);
 
 /* Synchronises the stream and reports what ee_model_check reports, for the operators above on the current device:
